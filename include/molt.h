@@ -224,6 +224,62 @@ int molt_paged_attention(const void* q, const void* k_cache, const void* v_cache
                          molt_stream_t stream);
 
 /* ------------------------------------------------------------------------------
+ * 4-bit KV cache: keys and values held in MXFP4 (OCP microscaling), 17 D / 16 bytes per key
+ * and kv head in place of the 4 D of a bf16 cache. A token's head vector is D / 32 groups of
+ * 32 dims, each 32 e2m1 codes (sign, 2 exponent bits, 1 mantissa bit: 0, 0.5, 1, 1.5, 2, 3,
+ * 4, 6; code 8 + c is -c) and one e8m0 scale byte s that stands for 2^(s - 127).
+ *  - Writing: a group with largest magnitude a takes the power of two 2^e with
+ *    a / 2^e in [3.5, 7), e kept in -125 .. 125 (s = e + 127; a zero group's codes are 0);
+ *    codes are x / 2^e to the nearest, ties to the even code, saturating at 6, so no element
+ *    is off by more than 2^e. A group with an infinity or NaN gets s = 255.
+ *  - Reading: code * 2^(s - 127), exact in bf16; NaN for s = 255.
+ * Layout, blocks of 16 tokens as in the other caches, two uint8 tensors
+ * [num_blocks, n_kv_heads, 17 D / 2] that start at multiples of 16 bytes:
+ *    K: codes [16 tokens][D / 2], then scales [16 tokens][D / 32]
+ *    V: codes [4][D / 8][4 tokens][4 bytes] (token 4 a + c, dims 8 i .. 8 i + 7), then
+ *       scales [4][D / 32][4 tokens]
+ * with dim 2 i of a token in the low nibble of its byte i.
+ *
+ * molt_kvq_write -- rows into the cache. Row b n + j (j < n; j < lens[b] if lens is given)
+ * goes to position context_lens[b] + j of sequence b; its other slots, and the slots of rows
+ * j >= lens[b], stay as they were. A row whose position is negative or past the table, or
+ * whose block id is outside [0, num_blocks), is not written. Rows that share a slot (a block
+ * in two tables) leave one of them there, code by code.
+ *   k, v      rows of n_kv_heads x D elements of dtype (F32 or BF16), k_stride and v_stride
+ *             elements apart (>= n_kv_heads * D: slices of fused projection rows will do)
+ *   lens      [B] i32 or NULL (all n rows count)
+ *
+ * molt_kvq_read -- positions out of the cache: out_k, out_v [B n, n_kv_heads, D] of dtype
+ * get position starts[b] + j in row b n + j; rows j >= lens[b] and rows without a place (as
+ * above) are zeros.
+ *
+ * molt_paged_attention_kvq -- molt_paged_attention over this cache, with q, out and the
+ * arithmetic in dtype: every key and value is taken as the value it stands for. Any number
+ * 1 + k of query positions. Rows see positions 0 .. context_lens[b] + j of the table; blocks
+ * whose id is outside [0, num_blocks) are not seen, and a row that sees no key
+ * (context_lens[b] + j < 0: a sequence that sits a step out) is zeros. Slots that a row does
+ * not see may hold anything.
+ * Supported, all three: D in {64, 128}; Hq % Hkv == 0, Hq/Hkv any. Errors: INVALID_ARG for NULL
+ * required pointers, sizes < 1, caches that are not 16-byte aligned; WORKSPACE.
+ * ---------------------------------------------------------------------------- */
+int molt_kvq_write(const void* k, const void* v, long long k_stride, long long v_stride,
+                   void* k_cache, void* v_cache, const int32_t* block_tables,
+                   const int32_t* context_lens, const int32_t* lens, int B, int n, int n_kv_heads,
+                   int head_dim, int max_blocks_per_seq, int num_blocks, molt_dtype dtype,
+                   molt_stream_t stream);
+int molt_kvq_read(const void* k_cache, const void* v_cache, const int32_t* block_tables,
+                  const int32_t* starts, const int32_t* lens, int B, int n, int n_kv_heads,
+                  int head_dim, int max_blocks_per_seq, int num_blocks, molt_dtype dtype,
+                  void* out_k, void* out_v, molt_stream_t stream);
+size_t molt_paged_attention_kvq_workspace_size(int B, int k, int n_q_heads, int n_kv_heads,
+                                               int head_dim, int max_blocks_per_seq);
+int molt_paged_attention_kvq(const void* q, const void* k_cache, const void* v_cache,
+                             const int32_t* block_tables, const int32_t* context_lens, int B,
+                             int k, int n_q_heads, int n_kv_heads, int head_dim,
+                             int max_blocks_per_seq, int num_blocks, molt_dtype dtype, void* out,
+                             void* workspace, size_t workspace_bytes, molt_stream_t stream);
+
+/* ------------------------------------------------------------------------------
  * molt_dense_gemm -- the dense projection of the verify step's decoder (QKV, O, router,
  * LM head): C[M, N] (f32, row-major) = A[M, K] * B[N, K]^T, or C += A * B^T with
  * accumulate != 0 (the O projection adds into the residual stream). A and B in `dtype`

@@ -63,6 +63,13 @@ _SIGS = {
     "molt_paged_attention_workspace_size": (c_size, [c_int] * 6),
     "molt_paged_attention": (c_int, [c_vp, c_vp, c_vp, c_vp, c_vp, c_int, c_int, c_int, c_int,
                                      c_int, c_int, c_int, c_vp, c_vp, c_size, c_vp]),
+    "molt_kvq_write": (c_int, [c_vp, c_vp, ctypes.c_longlong, ctypes.c_longlong, c_vp, c_vp, c_vp, c_vp,
+                               c_vp, c_int, c_int, c_int, c_int, c_int, c_int, c_int, c_vp]),
+    "molt_kvq_read": (c_int, [c_vp, c_vp, c_vp, c_vp, c_vp, c_int, c_int, c_int, c_int, c_int, c_int,
+                              c_int, c_vp, c_vp, c_vp]),
+    "molt_paged_attention_kvq_workspace_size": (c_size, [c_int] * 6),
+    "molt_paged_attention_kvq": (c_int, [c_vp, c_vp, c_vp, c_vp, c_vp, c_int, c_int, c_int, c_int,
+                                         c_int, c_int, c_int, c_int, c_vp, c_vp, c_size, c_vp]),
     "molt_decoder_workspace_size": (c_size, [ctypes.POINTER(MoltModel), c_int, c_int, c_int]),
     "molt_decoder_forward": (c_int, [ctypes.POINTER(MoltModel), ctypes.POINTER(MoltKV), c_int,
                                      c_int, c_vp, c_vp, c_vp, c_size, c_vp]),
@@ -337,6 +344,96 @@ def paged_attention(q, k_cache, v_cache, block_tables, context_lens, k, workspac
 
     _call("molt_paged_attention", call, lib.molt_paged_attention_workspace_size(B, k, Hq, Hkv, D, maxb),
           q.device, workspace)
+    return out
+
+
+# ------------------------------------------------------------------ 4-bit KV cache
+
+def kvq_cache(num_blocks, n_kv_heads, head_dim, device="cuda"):
+    """Empty (k_cache, v_cache) of the 4-bit format (molt.h): uint8 [num_blocks, n_kv_heads, 17 D / 2]."""
+    shape = (num_blocks, n_kv_heads, 17 * head_dim // 2)
+    return (torch.zeros(shape, dtype=torch.uint8, device=device),
+            torch.zeros(shape, dtype=torch.uint8, device=device))
+
+
+def _kvq_caches(k_cache, v_cache, block_tables, starts):
+    """Checks of a pair of caches and the tables; returns (B, num_blocks, n_kv_heads, head_dim, max_blocks)."""
+    _dev(k_cache, torch.uint8, name="k_cache")
+    if k_cache.dim() != 3 or k_cache.shape[2] * 2 % 17:
+        raise MoltError(f"k_cache has shape {tuple(k_cache.shape)}, expected [num_blocks, n_kv_heads, 17 * head_dim / 2]")
+    nb, Hkv, rec = k_cache.shape
+    _dev(v_cache, torch.uint8, (nb, Hkv, rec), "v_cache")
+    B = starts.shape[0]
+    _dev(starts, torch.int32, (B,), "context_lens")
+    _dev(block_tables, torch.int32, name="block_tables")
+    if block_tables.dim() != 2 or block_tables.shape[0] != B:
+        raise MoltError(f"block_tables has shape {tuple(block_tables.shape)}, expected ({B}, max_blocks)")
+    return B, nb, Hkv, rec * 2 // 17, block_tables.shape[1]
+
+
+def _rows_stride(t, dtype, shape, name):
+    """Row stride (elements) of rows [T, Hkv, D] whose heads are contiguous, e.g. a slice of fused QKV rows."""
+    if not t.is_cuda:
+        raise MoltError(f"{name} must be a GPU tensor")
+    if t.dtype != dtype:
+        raise MoltError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if tuple(t.shape) != shape:
+        raise MoltError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
+    T, H, D = shape
+    if t.stride(2) != 1 or (H > 1 and t.stride(1) != D) or (T > 1 and t.stride(0) < H * D):
+        raise MoltError(f"{name} must have contiguous heads in rows that do not overlap, strides are {t.stride()}")
+    return t.stride(0) if T > 1 else H * D
+
+
+def kvq_write(k, v, k_cache, v_cache, block_tables, context_lens, n, lens=None):
+    """Writes rows k, v [B*n, Hkv, D] (f32|bf16; row-strided views will do) into the 4-bit cache at
+    positions context_lens[b] + j, j < n (j < lens[b] if given)."""
+    lib = load()
+    B, nb, Hkv, D, maxb = _kvq_caches(k_cache, v_cache, block_tables, context_lens)
+    if k.dtype not in (torch.float32, torch.bfloat16):
+        raise MoltError(f"k has dtype {k.dtype}, expected float32 or bfloat16")
+    ks = _rows_stride(k, k.dtype, (B * n, Hkv, D), "k")
+    vs = _rows_stride(v, k.dtype, (B * n, Hkv, D), "v")
+    _dev(lens, torch.int32, (B,), "lens")
+    _check(lib.molt_kvq_write(_ptr(k), _ptr(v), ks, vs, _ptr(k_cache), _ptr(v_cache), _ptr(block_tables),
+                              _ptr(context_lens), _ptr(lens), B, n, Hkv, D, maxb, nb, DTYPE_CODE[k.dtype],
+                              _stream()), "molt_kvq_write")
+
+
+def kvq_read(k_cache, v_cache, block_tables, starts, n, lens=None, dtype=torch.bfloat16):
+    """Positions starts[b] + j, j < n, of the 4-bit cache as (k, v) [B*n, Hkv, D] of dtype (bf16|f32); rows
+    j >= lens[b], and rows without a place in the table, are zeros."""
+    lib = load()
+    B, nb, Hkv, D, maxb = _kvq_caches(k_cache, v_cache, block_tables, starts)
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise MoltError(f"dtype is {dtype}, expected float32 or bfloat16")
+    _dev(lens, torch.int32, (B,), "lens")
+    k = torch.empty(B * n, Hkv, D, dtype=dtype, device=k_cache.device)
+    v = torch.empty(B * n, Hkv, D, dtype=dtype, device=k_cache.device)
+    _check(lib.molt_kvq_read(_ptr(k_cache), _ptr(v_cache), _ptr(block_tables), _ptr(starts), _ptr(lens), B, n,
+                             Hkv, D, maxb, nb, DTYPE_CODE[dtype], _ptr(k), _ptr(v), _stream()), "molt_kvq_read")
+    return k, v
+
+
+def paged_attention_kvq_workspace_size(B, k, n_q_heads, n_kv_heads, head_dim, max_blocks):
+    return load().molt_paged_attention_kvq_workspace_size(B, k, n_q_heads, n_kv_heads, head_dim, max_blocks)
+
+
+def paged_attention_kvq(q, k_cache, v_cache, block_tables, context_lens, k, workspace=None):
+    """paged_attention over a 4-bit cache: q [B*(1+k), Hq, D] (f32|bf16); returns [T, Hq*D] of q's dtype."""
+    lib = load()
+    B, nb, Hkv, D, maxb = _kvq_caches(k_cache, v_cache, block_tables, context_lens)
+    if q.dtype not in (torch.float32, torch.bfloat16):
+        raise MoltError(f"q has dtype {q.dtype}, expected float32 or bfloat16")
+    if q.dim() != 3:
+        raise MoltError(f"q has shape {tuple(q.shape)}, expected [B*(1+k), Hq, D]")
+    Hq = q.shape[1]
+    _dev(q, None, (B * (k + 1), Hq, D), "q")
+    out = torch.empty(q.shape[0], Hq * D, dtype=q.dtype, device=q.device)
+    ws, nbytes = _workspace(lib.molt_paged_attention_kvq_workspace_size(B, k, Hq, Hkv, D, maxb), q.device, workspace)
+    _check(lib.molt_paged_attention_kvq(_ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(block_tables),
+                                        _ptr(context_lens), B, k, Hq, Hkv, D, maxb, nb, DTYPE_CODE[q.dtype],
+                                        _ptr(out), _ptr(ws), nbytes, _stream()), "molt_paged_attention_kvq")
     return out
 
 

@@ -512,6 +512,78 @@ int molt_paged_attention(const void* q, const void* k_cache, const void* v_cache
   return hip_status(e, "molt_paged_attention");
 }
 
+// ------------------------------------------------------------------ 4-bit KV cache
+
+static int kvq_rows_ok(const void* k_cache, const void* v_cache, const int32_t* block_tables, const int32_t* start,
+                       int B, int n, int Hkv, int D, int max_blocks, int num_blocks, molt_dtype dt) {
+  REQUIRE(B >= 1, "B = %d must be >= 1", B);
+  REQUIRE(n >= 1, "n = %d must be >= 1", n);
+  REQUIRE(act_ok(dt), "dtype must be F32 or BF16");
+  REQUIRE(D == 64 || D == 128, "head_dim = %d must be 64 or 128", D);
+  REQUIRE(Hkv >= 1, "n_kv_heads = %d must be >= 1", Hkv);
+  REQUIRE(max_blocks >= 1, "max_blocks_per_seq = %d must be >= 1", max_blocks);
+  REQUIRE(num_blocks >= 1, "num_blocks = %d must be >= 1", num_blocks);
+  REQUIRE(double(B) * n * Hkv * D < 6.0e10, "B * n * n_kv_heads * head_dim too large");
+  REQUIRE(k_cache && v_cache && block_tables && start, "a required pointer is NULL");
+  REQUIRE((reinterpret_cast<uintptr_t>(k_cache) | reinterpret_cast<uintptr_t>(v_cache)) % 16 == 0,
+          "the caches must start at a multiple of 16 bytes");
+  return MOLT_OK;
+}
+
+int molt_kvq_write(const void* k, const void* v, long long k_stride, long long v_stride, void* k_cache, void* v_cache,
+                   const int32_t* block_tables, const int32_t* context_lens, const int32_t* lens, int B, int n,
+                   int Hkv, int D, int max_blocks, int num_blocks, molt_dtype dtype, molt_stream_t stream) {
+  if (int r = kvq_rows_ok(k_cache, v_cache, block_tables, context_lens, B, n, Hkv, D, max_blocks, num_blocks, dtype))
+    return r;
+  REQUIRE(k && v, "a required pointer is NULL");
+  REQUIRE(k_stride >= (long long)Hkv * D && v_stride >= (long long)Hkv * D,
+          "row strides %lld and %lld must be at least n_kv_heads * head_dim = %lld", k_stride, v_stride,
+          (long long)Hkv * D);
+  const molt::KvqRows p{context_lens, lens, block_tables, B, n, Hkv, max_blocks, num_blocks,
+                        static_cast<uint8_t*>(k_cache), static_cast<uint8_t*>(v_cache)};
+  return hip_status(molt::launch_kvq_write(p, k, k_stride, v, v_stride, D, dtype, reinterpret_cast<hipStream_t>(stream)),
+                    "molt_kvq_write");
+}
+
+int molt_kvq_read(const void* k_cache, const void* v_cache, const int32_t* block_tables, const int32_t* starts,
+                  const int32_t* lens, int B, int n, int Hkv, int D, int max_blocks, int num_blocks,
+                  molt_dtype dtype, void* out_k, void* out_v, molt_stream_t stream) {
+  if (int r = kvq_rows_ok(k_cache, v_cache, block_tables, starts, B, n, Hkv, D, max_blocks, num_blocks, dtype)) return r;
+  REQUIRE(out_k && out_v, "a required pointer is NULL");
+  const molt::KvqRows p{starts, lens, block_tables, B, n, Hkv, max_blocks, num_blocks,
+                        static_cast<uint8_t*>(const_cast<void*>(k_cache)),
+                        static_cast<uint8_t*>(const_cast<void*>(v_cache))};
+  return hip_status(molt::launch_kvq_read(p, out_k, out_v, D, dtype, reinterpret_cast<hipStream_t>(stream)),
+                    "molt_kvq_read");
+}
+
+size_t molt_paged_attention_kvq_workspace_size(int B, int k, int Hq, int Hkv, int D, int max_blocks) {
+  if (B < 1 || k < 0 || Hkv < 1 || Hq < Hkv || Hq % Hkv != 0 || D < 1 || max_blocks < 1) return 0;
+  return molt::kvq_attention_ws_bytes(B, k + 1, Hq, Hkv, D, max_blocks);
+}
+
+int molt_paged_attention_kvq(const void* q, const void* k_cache, const void* v_cache, const int32_t* block_tables,
+                             const int32_t* context_lens, int B, int k, int Hq, int Hkv, int D, int max_blocks,
+                             int num_blocks, molt_dtype dtype, void* out, void* workspace, size_t workspace_bytes,
+                             molt_stream_t stream) {
+  REQUIRE(k >= 0 && k < 0x7fffffff, "k = %d must be >= 0", k);
+  if (int r = kvq_rows_ok(k_cache, v_cache, block_tables, context_lens, B, k + 1, Hkv, D, max_blocks, num_blocks, dtype))
+    return r;
+  REQUIRE(Hq >= Hkv && Hq % Hkv == 0, "n_q_heads %d must be a multiple of n_kv_heads %d", Hq, Hkv);
+  REQUIRE(double(B) * (k + 1) * Hq < 1.0e9, "B * (1+k) * n_q_heads too large");
+  REQUIRE(max_blocks <= (1 << 26), "max_blocks_per_seq = %d must be <= 2^26", max_blocks);
+  REQUIRE(q && out, "a required pointer is NULL");
+  if (int r = check_ws(workspace, workspace_bytes, molt::kvq_attention_ws_bytes(B, k + 1, Hq, Hkv, D, max_blocks)))
+    return r;
+  hipError_t e;
+  {
+    ProfScope ps(MOLT_PROF_ATTENTION, reinterpret_cast<hipStream_t>(stream));
+    e = molt::launch_kvq_attention(q, k_cache, v_cache, block_tables, context_lens, B, k + 1, Hq, Hkv, D, max_blocks,
+                                   num_blocks, dtype, out, false, workspace, reinterpret_cast<hipStream_t>(stream));
+  }
+  return hip_status(e, "molt_paged_attention_kvq");
+}
+
 // ------------------------------------------------------------------ decoder / verify step
 
 namespace {

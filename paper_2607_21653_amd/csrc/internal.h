@@ -160,4 +160,23 @@ hipError_t launch_paged_attention(const void* q, const void* kc, const void* vc,
                                   int max_blocks, molt_dtype dt, void* out, bool out_tiled,
                                   void* ws, bool fine, hipStream_t s);
 
+// ------------------------------------------------------------- 4-bit KV cache
+// Rows b n + j of a call: position start[b] + j of sequence b, those with j < lens[b] (lens may be null)
+struct KvqRows {
+  const int32_t* start; const int32_t* lens; const int32_t* bt;
+  int B, n, Hkv, max_blocks, num_blocks;
+  uint8_t* kc; uint8_t* vc;
+};
+// k, v: rows of Hkv heads x D elements, k_stride and v_stride elements apart
+hipError_t launch_kvq_write(const KvqRows& p, const void* k, long k_stride, const void* v, long v_stride, int D,
+                            molt_dtype dt, hipStream_t s);
+// k, v [B n, Hkv, D]; zeros where a row has no place in the cache
+hipError_t launch_kvq_read(const KvqRows& p, void* k, void* v, int D, molt_dtype dt, hipStream_t s);
+size_t kvq_attention_ws_bytes(int B, int n, int Hq, int Hkv, int D, int max_blocks);
+// n query positions per sequence; out as in launch_paged_attention
+hipError_t launch_kvq_attention(const void* q, const void* kc, const void* vc, const int32_t* bt,
+                                const int32_t* ctx, int B, int n, int Hq, int Hkv, int D, int max_blocks,
+                                int num_blocks, molt_dtype dt, void* out, bool out_tiled, void* ws,
+                                hipStream_t s);
+
 }  // namespace molt
