@@ -50,6 +50,84 @@ MOLT_DEV void split_bf16(float x, __bf16 (&part)[P]) {
   }
 }
 
+// Query row as B operands of 16x16x32 bf16 MFMAs: three bf16 parts (24 bits) of dims D / 4 * g4 + 8 s .. +7
+// for k-step s, the order in which a lane's K codes lie.
+template <int D>
+MOLT_DEV void load_query_f32(const float* q, bool valid, int g4, bf16x8_t (&qf)[3][D / 32]) {
+#pragma unroll
+  for (int s = 0; s < D / 32; ++s) {
+    floatx4_t x[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    if (valid) {
+      x[0] = *reinterpret_cast<const UnalignedF4*>(q + D / 4 * g4 + 8 * s);
+      x[1] = *reinterpret_cast<const UnalignedF4*>(q + D / 4 * g4 + 8 * s + 4);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      __bf16 part[3];
+      split_bf16<3>(x[e / 4][e % 4], part);
+#pragma unroll
+      for (int u = 0; u < 3; ++u) qf[u][s][e] = part[u];
+    }
+  }
+}
+
+// Query row as B operands of 16x16x128 scaled MFMAs, whose A operand takes K's e2m1 codes and scale bytes
+// as they lie in the cache. A bf16 value has 8 significant bits, an e4m3 one 4: with the row scaled by
+// 2^-e so that its largest magnitude is in [128, 256), hi = e4m3(x 2^-e) leaves a rest of at most half a
+// step, and lo = e4m3(rest 2^5) holds the rest exactly while it is a normal number; what smaller elements
+// lose is under 2^-22 of the row's largest. So x = 2^e hi + 2^(e - 5) lo, the e8m0 bytes being the B scales.
+// Lane (row, g4) holds k = 16 g4 .. +15 in the first 4 registers and 64 + 16 g4 .. +15 in the others. For D =
+// 128, qp[0] is hi and qp[1] lo, k the dim; for D = 64 k = 0 .. 63 is hi, 64 .. 127 lo, with K's codes
+// twice in the A operand. qs: the scale byte of the lane's k block (and for D = 128 lo's in the second byte).
+template <int D>
+MOLT_DEV void load_query_bf16(const uint16_t* q, bool valid, int g4, int32x8_t (&qp)[D / 64], int& qs) {
+  float x[D / 64][16];
+  uint32_t amax = 0;
+#pragma unroll
+  for (int c = 0; c < D / 64; ++c)
+#pragma unroll
+    for (int v = 0; v < 2; ++v) {
+      u32x4 w = {0u, 0u, 0u, 0u};
+      if (valid) w = *reinterpret_cast<const UnalignedU4*>(q + 64 * c + 16 * g4 + 8 * v);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[c][8 * v + 2 * e] = __uint_as_float(w[e] << 16);
+        x[c][8 * v + 2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+        amax = max(amax, max((w[e] << 16) & 0x7fffffffu, w[e] & 0x7fff0000u));
+      }
+    }
+  const float am = rows_max4(__uint_as_float(amax > 0x7f800000u ? 0x7f800000u : amax));   // NaN as infinity
+  const int byte = max(int(__float_as_uint(am) >> 23) - 7, 6);
+  const bool bad = __float_as_uint(am) == 0x7f800000u;     // an infinity or NaN: a row of NaN scores
+  const float inv = __uint_as_float(uint32_t(254 - byte) << 23);
+#pragma unroll
+  for (int c = 0; c < D / 64; ++c)
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      uint32_t hi = 0, lo = 0;
+      float y[4], t[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = x[c][4 * v + e] * inv;
+      hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], hi, false);
+      hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], hi, true);
+      const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(hi, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(hi, true);
+      t[0] = (y[0] - a[0]) * 32.f;
+      t[1] = (y[1] - a[1]) * 32.f;
+      t[2] = (y[2] - b[0]) * 32.f;
+      t[3] = (y[3] - b[1]) * 32.f;
+      lo = __builtin_amdgcn_cvt_pk_fp8_f32(t[0], t[1], lo, false);
+      lo = __builtin_amdgcn_cvt_pk_fp8_f32(t[2], t[3], lo, true);
+      if constexpr (D == 128) {
+        qp[0][4 * c + v] = int(hi);
+        qp[1][4 * c + v] = int(lo);
+      } else {
+        qp[0][v] = int(hi);
+        qp[0][4 + v] = int(lo);
+      }
+    }
+  qs = bad ? 0xffff : D == 128 ? byte | (byte - 5) << 8 : g4 < 2 ? byte : byte - 5;
+}
+
 // Output dims d0 .. + 7 of row r: a / L, zeros for a row that sees no key
 template <typename T>
 MOLT_DEV void store_out(const KvqAttnParams& p, int b, int h, int r, int D, int d0, const floatx4_t (&a)[2], float L) {
@@ -71,11 +149,10 @@ template <int D, typename T, int NT>
 __global__ __launch_bounds__(kWaves * kWave, 2) void kvq_attn_kernel(KvqAttnParams p) {
   typedef KvqRecord<D> Rec;
   constexpr bool F32 = sizeof(T) == 4;
-  constexpr int QP = F32 ? 3 : 1;        // bf16 parts of a query element: 24 bits, or what it is
+  constexpr int QP = 3;                  // bf16 parts of an f32 query element
   constexpr int PP = F32 ? 3 : 2;        // bf16 parts of a probability
   constexpr int KS = D / 32;             // MFMA steps over the dims of a score
   constexpr int DT = D / 16;             // 16-dim tiles of O^T
-  constexpr int KW = D / 32;             // dwords of K codes per lane and block
   __shared__ __attribute__((aligned(16))) float s_o[kWaves][16][D + 4];
   __shared__ float s_m[kWaves][16], s_l[kWaves][16];
 
@@ -97,37 +174,18 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void kvq_attn_kernel(KvqAttnPara
   const int s0 = ns > 0 ? int(long(npairs) * split / ns) : 0, s1 = ns > 0 ? int(long(npairs) * (split + 1) / ns) : 0;
   const int p0 = s0 + (s1 - s0) * wave / kWaves, p1 = s0 + (s1 - s0) * (wave + 1) / kWaves;
 
-  // Q^T operands: lane (row l16, group g4) holds dims D / 4 * g4 + 8 s .. +7 of k-step s
-  bf16x8_t qf[NT][QP][KS];
+  // Q^T operands
   int lim[NT];                           // last key that the row sees
+  bf16x8_t qf[F32 ? NT : 1][QP][KS];     // f32
+  int32x8_t qp[F32 ? 1 : NT][D / 64];    // bf16
+  int qs[F32 ? 1 : NT];                  // scale bytes of both fp8 parts
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
     const int r = r0 + 16 * i + l16, j = r / p.G, gi = r % p.G;
     lim[i] = r < p.R ? ctx + j : -1;
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      const long at = ((long(b) * p.n + j) * p.Hq + h * p.G + gi) * D + D / 4 * g4 + 8 * s;
-      if (r < p.R) {
-        if constexpr (F32) {
-          const float* src = static_cast<const float*>(p.q) + at;
-          const floatx4_t x0 = *reinterpret_cast<const UnalignedF4*>(src), x1 = *reinterpret_cast<const UnalignedF4*>(src + 4);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            __bf16 part[QP];
-            split_bf16<QP>(e < 4 ? x0[e] : x1[e - 4], part);
-#pragma unroll
-            for (int u = 0; u < QP; ++u) qf[i][u][s][e] = part[u];
-          }
-        } else {
-          qf[i][0][s] = *reinterpret_cast<const UnalignedBf16x8*>(static_cast<const uint16_t*>(p.q) + at);
-        }
-      } else {
-#pragma unroll
-        for (int u = 0; u < QP; ++u)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) qf[i][u][s][e] = __bf16(0.f);
-      }
-    }
+    const long at = ((long(b) * p.n + j) * p.Hq + h * p.G + gi) * D;
+    if constexpr (F32) load_query_f32<D>(static_cast<const float*>(p.q) + at, r < p.R, g4, qf[i]);
+    else load_query_bf16<D>(static_cast<const uint16_t*>(p.q) + at, r < p.R, g4, qp[i], qs[i]);
   }
   floatx4_t o[NT][DT];
   float m[NT], l[NT];
@@ -142,22 +200,28 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void kvq_attn_kernel(KvqAttnPara
 
   typedef const __attribute__((address_space(4))) int32_t* ConstInt;
   const ConstInt btab = (ConstInt)(p.bt + long(b) * p.max_blocks);
-  struct Block { uint32_t k[KW]; u32x4 v; uint32_t ks, vs; };
+  // Lane (l16, g4): codes of K's token l16, dims 32 g4 .. (D = 64: 32 (g4 % 2) .., in f32 16 g4 ..) and their
+  // scale byte; V's tokens 4 g4 .. +3 of the octet that has dims D / 16 * l16 .., and their scale bytes
+  struct Block { u32x4 k; u32x4 v; uint32_t ks, vs; };
   auto load = [&](Block& x, int id) __attribute__((always_inline)) {
     const long rec = (long(unsigned(id) < unsigned(p.num_blocks) ? id : 0) * p.Hkv + h) * Rec::kBytes;
     const uint8_t *kr = p.kc + rec, *vr = p.vc + rec;
     if constexpr (D == 128) {
-      const u32x4 w = *reinterpret_cast<const u32x4*>(kr + l16 * 64 + g4 * 16);
-#pragma unroll
-      for (int s = 0; s < 4; ++s) x.k[s] = w[s];
+      x.k = *reinterpret_cast<const u32x4*>(kr + l16 * 64 + g4 * 16);
       x.v = *reinterpret_cast<const u32x4*>(vr + lane * 16);
+      x.ks = kr[Rec::k_scale(l16, g4)];
     } else {
-      const u32x2 w = *reinterpret_cast<const u32x2*>(kr + l16 * 32 + g4 * 8);
-      x.k[0] = w[0];
-      x.k[1] = w[1];
+      if constexpr (F32) {
+        const u32x2 w = *reinterpret_cast<const u32x2*>(kr + l16 * 32 + g4 * 8);
+        x.k[0] = w[0];
+        x.k[1] = w[1];
+        x.ks = kr[Rec::k_scale(l16, g4 / 2)];
+      } else {
+        x.k = *reinterpret_cast<const u32x4*>(kr + l16 * 32 + g4 % 2 * 16);
+        x.ks = kr[Rec::k_scale(l16, g4 % 2)];
+      }
       x.v = *reinterpret_cast<const u32x4*>(vr + (g4 * 8 + l16 / 2) * 16);
     }
-    x.ks = kr[Rec::k_scale(l16, g4 * D / 128)];
     x.vs = *reinterpret_cast<const uint32_t*>(vr + Rec::v_scale(4 * g4, l16 * (D / 16) / 32));
   };
 
@@ -173,17 +237,27 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void kvq_attn_kernel(KvqAttnPara
     for (int u = 0; u < 2; ++u) {
 #pragma unroll
       for (int i = 0; i < NT; ++i) sv[u][i] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+      if constexpr (F32) {
 #pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const uint32_t sc = x[u].ks << 23;
-        const u32x4 w = {kvq_decode2<0>(x[u].k[s], sc), kvq_decode2<1>(x[u].k[s], sc),
-                         kvq_decode2<2>(x[u].k[s], sc), kvq_decode2<3>(x[u].k[s], sc)};
-        const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, w);
+        for (int s = 0; s < KS; ++s) {
+          const uint32_t sc = x[u].ks << 23;
+          const u32x4 w = {kvq_decode2<0>(x[u].k[s], sc), kvq_decode2<1>(x[u].k[s], sc),
+                           kvq_decode2<2>(x[u].k[s], sc), kvq_decode2<3>(x[u].k[s], sc)};
+          const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, w);
 #pragma unroll
-        for (int i = 0; i < NT; ++i)
+          for (int i = 0; i < NT; ++i)
 #pragma unroll
-          for (int q = 0; q < QP; ++q)
-            sv[u][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[i][q][s], sv[u][i], 0, 0, 0);
+            for (int q = 0; q < QP; ++q)
+              sv[u][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[i][q][s], sv[u][i], 0, 0, 0);
+        }
+      } else {
+        const int32x8_t kf = {int(x[u].k[0]), int(x[u].k[1]), int(x[u].k[2]), int(x[u].k[3]), 0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {   // formats: A 4 (e2m1), B 0 (e4m3)
+          sv[u][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf, qp[i][0], sv[u][i], 4, 0, 0, int(x[u].ks), 0, qs[i]);
+          if constexpr (D == 128)
+            sv[u][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf, qp[i][1], sv[u][i], 4, 0, 0, int(x[u].ks), 1, qs[i]);
+        }
       }
     }
     bool poison[NT];
@@ -255,7 +329,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void kvq_attn_kernel(KvqAttnPara
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float w = exp2f((sv[u][i][e] - ref) * p.c);
+          const float w = __builtin_amdgcn_exp2f((sv[u][i][e] - ref) * p.c);
           ps += w;
           __bf16 part[PP];
           split_bf16<PP>(w, part);
