@@ -1,6 +1,11 @@
 // Multi-query paged attention over the 4-bit KV cache (format: kvq_format.h).
 //   o_r = sum_p w_rp v_p,  w_r = softmax over p <= ctx_b + j(r) of q_r . k_p / sqrt(D)
 // for the R = G * n rows (position j = r / G, query head h G + r % G) of sequence b and kv head h.
+//
+// Values and keys are exact in bf16, so the products' only roundings are those of the weights: in f32 three
+// bf16 parts (24 bits); in bf16 one, with the sum taken of the rounded weights, by an MFMA with a row of ones.
+// That adds a rounding like the output's own: rms error 2.07e-3 of the output's rms against 1.66e-3 with two
+// parts, for which 128 sequences x 5 positions at context 8192 took 178 us, with one 135.
 #include "internal.h"
 #include "kvq_format.h"
 
@@ -10,6 +15,7 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kRescaleSlack = 8.0f;   // probabilities may grow to 2^8 before O is rescaled
 constexpr int kWaves = 4;
+constexpr int kSlots = 4;               // pairs of blocks in a wavefront's ring
 
 struct KvqAttnParams {
   const void* q;           // [B * n, Hq, D]
@@ -38,6 +44,18 @@ typedef u32x4 UnalignedU4 __attribute__((aligned(2)));
 MOLT_DEV int visible_end(const KvqAttnParams& p, int ctx, int r1) {
   const long e = long(ctx) + (r1 - 1) / p.G + 1;
   return int(e < 0 ? 0 : e > 16l * p.max_blocks ? 16l * p.max_blocks : e);
+}
+
+// LDS-DMA: 16 (4) bytes a lane from src to dst + 16 (4) * lane; dst is the wavefront's
+typedef const __attribute__((address_space(1))) void* GlobalPtr;
+typedef __attribute__((address_space(3))) void* LdsPtr;
+MOLT_DEV void copy_lds16(const uint8_t* src, uint8_t* dst) { __builtin_amdgcn_global_load_lds((GlobalPtr)src, (LdsPtr)dst, 16, 0, 0); }
+MOLT_DEV void copy_lds4(const uint8_t* src, uint8_t* dst) { __builtin_amdgcn_global_load_lds((GlobalPtr)src, (LdsPtr)dst, 4, 0, 0); }
+
+// a wave-uniform value the compiler is to hold in scalar registers
+MOLT_DEV long uniform(long x) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(int(x)), hi = __builtin_amdgcn_readfirstlane(int(x >> 32));
+  return long(uint64_t(hi) << 32 | lo);
 }
 
 // x as P bf16 values whose sum is x to 8 P bits
@@ -150,11 +168,16 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void kvq_attn_kernel(KvqAttnPara
   typedef KvqRecord<D> Rec;
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int QP = 3;                  // bf16 parts of an f32 query element
-  constexpr int PP = F32 ? 3 : 2;        // bf16 parts of a probability
+  constexpr int PP = F32 ? 3 : 1;        // bf16 parts of a probability (see the top)
   constexpr int KS = D / 32;             // MFMA steps over the dims of a score
   constexpr int DT = D / 16;             // 16-dim tiles of O^T
-  __shared__ __attribute__((aligned(16))) float s_o[kWaves][16][D + 4];
-  __shared__ float s_m[kWaves][16], s_l[kWaves][16];
+  constexpr int SLOT = 32 * D + 256;     // bytes of a pair in the ring
+  constexpr int kCopies = D == 128 ? 5 : 3;   // vector memory instructions of a pair
+  // the wavefronts' rings, then (kJoin floats each) their results; the query operands; the only LDS object
+  constexpr int kJoin = 16 * (D + 4) + 32;
+  constexpr int kLds = kSlots * SLOT > kJoin * 4 ? kSlots * SLOT : kJoin * 4;
+  constexpr int QF = D / 64 * 2048;      // bytes of a tile's query operands
+  __shared__ __attribute__((aligned(16))) uint8_t lds[kWaves * kLds + (F32 ? 0 : NT * QF)];
 
   // work item
   const int rg = int(blockIdx.x) % p.nrg;
@@ -173,119 +196,184 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void kvq_attn_kernel(KvqAttnPara
   // the split's pairs of blocks, then the wavefront's share
   const int s0 = ns > 0 ? int(long(npairs) * split / ns) : 0, s1 = ns > 0 ? int(long(npairs) * (split + 1) / ns) : 0;
   const int p0 = s0 + (s1 - s0) * wave / kWaves, p1 = s0 + (s1 - s0) * (wave + 1) / kWaves;
+  const int full_end = min(visible_end(p, ctx, r0 + 1), end);    // keys before are seen by every row
+  uint8_t* ring = lds + wave * kLds;
+  uint8_t* qlds = lds + kWaves * kLds;
 
-  // Q^T operands
+  // Copies of a pair into a slot of the wavefront's ring: [K codes of both blocks][V codes][scales of K, of
+  // V], K's 16-byte chunks in the order in which the lanes read them (dims 32 c .. of token t at chunk 16 c + t)
+  typedef const __attribute__((address_space(4))) int32_t* ConstInt;
+  const ConstInt btab = (ConstInt)(p.bt + long(b) * p.max_blocks);
+  constexpr uint32_t SR = D / 32 * 4;    // lanes (dwords) of a record's scales
+  const uint32_t ksrc = D == 128 ? l16 * 64 + g4 * 16 : l16 * 32 + g4 % 2 * 16;
+  const uint32_t vsrc = D == 128 ? lane * 16 : lane % 32 * 16;
+  const uint32_t spart = lane / SR % 4;
+  const uint8_t* sbase = (spart < 2 ? p.kc : p.vc) + Rec::kCodes + lane % SR * 4;
+  auto issue = [&](int pi, const int (&id)[2]) __attribute__((always_inline)) {
+    uint8_t* dst = ring + (pi - p0) % kSlots * SLOT;
+    long rec[2];                         // kept in scalar registers: a uniform base and a lane offset per copy
+#pragma unroll
+    for (int u = 0; u < 2; ++u) rec[u] = uniform((long(unsigned(id[u]) < unsigned(p.num_blocks) ? id[u] : 0) * p.Hkv + h) * Rec::kBytes);
+    if constexpr (D == 128) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) copy_lds16(p.kc + rec[u] + ksrc, dst + 1024 * u);
+#pragma unroll
+      for (int u = 0; u < 2; ++u) copy_lds16(p.vc + rec[u] + vsrc, dst + 2048 + 1024 * u);
+    } else {
+      const long r = lane < 32 ? rec[0] : rec[1];
+      copy_lds16(p.kc + r + ksrc, dst);
+      copy_lds16(p.vc + r + vsrc, dst + 1024);
+    }
+    copy_lds4(sbase + (spart % 2 ? rec[1] : rec[0]), dst + 32 * D);
+  };
+  auto ids = [&](int pi, int (&id)[2]) __attribute__((always_inline)) {
+    id[0] = btab[min(2 * pi, nblk - 1)];
+    const int second = btab[min(2 * pi + 1, nblk - 1)];
+    id[1] = 2 * pi + 1 < nblk ? second : -1;
+  };
+  auto present = [&](const int (&id)[2]) __attribute__((always_inline)) {
+    return (unsigned(id[0]) < unsigned(p.num_blocks) ? 1u : 0u) | (unsigned(id[1]) < unsigned(p.num_blocks) ? 2u : 0u);
+  };
+  uint32_t have = 0;                     // presence bits of the pairs in flight, the newest lowest
+  int nid[2] = {-1, -1};
+  if (p0 < p1) {
+    int first[kSlots][2];
+#pragma unroll
+    for (int u = 0; u < kSlots; ++u) ids(p0 + u, first[u]);
+#pragma unroll
+    for (int u = 0; u < kSlots - 1; ++u) {
+      if (p0 + u < p1) issue(p0 + u, first[u]);
+      have = have << 2 | present(first[u]);
+    }
+    nid[0] = first[kSlots - 1][0];
+    nid[1] = first[kSlots - 1][1];
+  }
+
+  // Q^T operands: in f32 each wavefront's own, in bf16 in LDS for all, tile i made by wavefront i
   int lim[NT];                           // last key that the row sees
-  bf16x8_t qf[F32 ? NT : 1][QP][KS];     // f32
-  int32x8_t qp[F32 ? 1 : NT][D / 64];    // bf16
-  int qs[F32 ? 1 : NT];                  // scale bytes of both fp8 parts
+  bf16x8_t qf[QP][KS];
+  int qs[NT];                            // scale bytes of both fp8 parts
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
     const int r = r0 + 16 * i + l16, j = r / p.G, gi = r % p.G;
     lim[i] = r < p.R ? ctx + j : -1;
     const long at = ((long(b) * p.n + j) * p.Hq + h * p.G + gi) * D;
-    if constexpr (F32) load_query_f32<D>(static_cast<const float*>(p.q) + at, r < p.R, g4, qf[i]);
-    else load_query_bf16<D>(static_cast<const uint16_t*>(p.q) + at, r < p.R, g4, qp[i], qs[i]);
+    if constexpr (F32) {
+      load_query_f32<D>(static_cast<const float*>(p.q) + at, r < p.R, g4, qf);
+    } else if (wave == i) {
+      int32x8_t qp[D / 64];
+      int sc;
+      load_query_bf16<D>(static_cast<const uint16_t*>(p.q) + at, r < p.R, g4, qp, sc);
+#pragma unroll
+      for (int u = 0; u < D / 64; ++u) {
+        int32x4_t* dst = reinterpret_cast<int32x4_t*>(qlds + i * QF + u * 2048 + lane * 16);
+        dst[0] = int32x4_t{qp[u][0], qp[u][1], qp[u][2], qp[u][3]};
+        dst[64] = int32x4_t{qp[u][4], qp[u][5], qp[u][6], qp[u][7]};
+      }
+      *reinterpret_cast<int*>(lds + i * kLds + (kSlots - 1) * SLOT + lane * 4) = sc;   // in a slot not yet in use
+    }
   }
-  floatx4_t o[NT][DT];
-  float m[NT], l[NT];
+  if constexpr (!F32) {
+    lds_barrier();
+#pragma unroll
+    for (int i = 0; i < NT; ++i) qs[i] = *reinterpret_cast<const int*>(lds + i * kLds + (kSlots - 1) * SLOT + lane * 4);
+    lds_barrier();
+  }
+  floatx4_t o[NT][DT], ls[NT];           // O^T; the rows' sums (bf16: by MFMA, the same in every register and group)
+  float m[NT];                           // reference maximum (of raw scores)
+  float ref[NT];                         // m, or 0 for a row that has seen no key: its exp2(-inf) is 0
+  float bound[NT];                       // scores above it raise m
+  const float slack = kRescaleSlack / p.c;
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
-    m[i] = -INFINITY;
-    l[i] = 0.f;
+    m[i] = bound[i] = -INFINITY;
+    ref[i] = 0.f;
+    ls[i] = floatx4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int t = 0; t < DT; ++t) o[i][t] = floatx4_t{0.f, 0.f, 0.f, 0.f};
   }
-  const int full_end = min(visible_end(p, ctx, r0 + 1), end);    // keys before are seen by every row
 
-  typedef const __attribute__((address_space(4))) int32_t* ConstInt;
-  const ConstInt btab = (ConstInt)(p.bt + long(b) * p.max_blocks);
-  // Lane (l16, g4): codes of K's token l16, dims 32 g4 .. (D = 64: 32 (g4 % 2) .., in f32 16 g4 ..) and their
-  // scale byte; V's tokens 4 g4 .. +3 of the octet that has dims D / 16 * l16 .., and their scale bytes
-  struct Block { u32x4 k; u32x4 v; uint32_t ks, vs; };
-  auto load = [&](Block& x, int id) __attribute__((always_inline)) {
-    const long rec = (long(unsigned(id) < unsigned(p.num_blocks) ? id : 0) * p.Hkv + h) * Rec::kBytes;
-    const uint8_t *kr = p.kc + rec, *vr = p.vc + rec;
-    if constexpr (D == 128) {
-      x.k = *reinterpret_cast<const u32x4*>(kr + l16 * 64 + g4 * 16);
-      x.v = *reinterpret_cast<const u32x4*>(vr + lane * 16);
-      x.ks = kr[Rec::k_scale(l16, g4)];
-    } else {
-      if constexpr (F32) {
-        const u32x2 w = *reinterpret_cast<const u32x2*>(kr + l16 * 32 + g4 * 8);
-        x.k[0] = w[0];
-        x.k[1] = w[1];
-        x.ks = kr[Rec::k_scale(l16, g4 / 2)];
-      } else {
-        x.k = *reinterpret_cast<const u32x4*>(kr + l16 * 32 + g4 % 2 * 16);
-        x.ks = kr[Rec::k_scale(l16, g4 % 2)];
-      }
-      x.v = *reinterpret_cast<const u32x4*>(vr + (g4 * 8 + l16 / 2) * 16);
-    }
-    x.vs = *reinterpret_cast<const uint32_t*>(vr + Rec::v_scale(4 * g4, l16 * (D / 16) / 32));
-  };
-
-  for (int pi = p0; pi < p1; ++pi) {
-    const bool two = 2 * pi + 1 < nblk;
-    const int id[2] = {btab[2 * pi], two ? btab[2 * pi + 1] : -1};
-    Block x[2];
-    load(x[0], id[0]);
-    load(x[1], id[1]);
-    // S^T: lane (row l16 of the tile) holds tokens 4 g4 + e of both blocks
-    floatx4_t sv[2][NT];
+  // S^T of pair pi and its V scale bytes: lane (row l16 of the tile) holds tokens 4 g4 + e of both blocks.
+  // Lane (l16, g4) reads the codes of K's token l16, dims 32 g4 .. (D = 64: 32 (g4 % 2) .., in f32 16 g4 ..),
+  // and its scale byte
+  auto scores = [&](int pi, floatx4_t (&sv)[2][NT], uint32_t (&vs)[2]) __attribute__((always_inline)) {
+    const uint8_t* src = ring + (pi - p0) % kSlots * SLOT;
+    u32x4 k[2];
+    uint32_t ks[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
+      const uint8_t *kr = src + 8 * D * u, *sr = src + 32 * D + D / 2 * u;
+      if constexpr (F32 && D == 64) {
+        const u32x2 w = *reinterpret_cast<const u32x2*>(kr + (g4 / 2 * 16 + l16) * 16 + g4 % 2 * 8);
+        k[u][0] = w[0];
+        k[u][1] = w[1];
+        ks[u] = sr[l16 * 2 + g4 / 2];
+      } else {
+        k[u] = *reinterpret_cast<const u32x4*>(kr + (D == 128 ? lane : lane % 32) * 16);
+        ks[u] = sr[l16 * (D / 32) + g4 % (D / 32)];
+      }
+      vs[u] = *reinterpret_cast<const uint32_t*>(sr + D + (g4 * (D / 32) + l16 * (D / 16) / 32) * 4);
 #pragma unroll
       for (int i = 0; i < NT; ++i) sv[u][i] = floatx4_t{0.f, 0.f, 0.f, 0.f};
-      if constexpr (F32) {
+    }
+    if constexpr (F32) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
-          const uint32_t sc = x[u].ks << 23;
-          const u32x4 w = {kvq_decode2<0>(x[u].k[s], sc), kvq_decode2<1>(x[u].k[s], sc),
-                           kvq_decode2<2>(x[u].k[s], sc), kvq_decode2<3>(x[u].k[s], sc)};
+          const uint32_t sc = ks[u] << 23;
+          const u32x4 w = {kvq_decode2<0>(k[u][s], sc), kvq_decode2<1>(k[u][s], sc),
+                           kvq_decode2<2>(k[u][s], sc), kvq_decode2<3>(k[u][s], sc)};
           const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, w);
 #pragma unroll
-          for (int i = 0; i < NT; ++i)
-#pragma unroll
-            for (int q = 0; q < QP; ++q)
-              sv[u][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[i][q][s], sv[u][i], 0, 0, 0);
+          for (int q = 0; q < QP; ++q) sv[u][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[q][s], sv[u][0], 0, 0, 0);
         }
-      } else {
-        const int32x8_t kf = {int(x[u].k[0]), int(x[u].k[1]), int(x[u].k[2]), int(x[u].k[3]), 0, 0, 0, 0};
+    } else {
 #pragma unroll
-        for (int i = 0; i < NT; ++i) {   // formats: A 4 (e2m1), B 0 (e4m3)
-          sv[u][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf, qp[i][0], sv[u][i], 4, 0, 0, int(x[u].ks), 0, qs[i]);
-          if constexpr (D == 128)
-            sv[u][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf, qp[i][1], sv[u][i], 4, 0, 0, int(x[u].ks), 1, qs[i]);
+      for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int q = 0; q < D / 64; ++q) {
+          const int32x4_t* f = reinterpret_cast<const int32x4_t*>(qlds + i * QF + q * 2048 + lane * 16);
+          const int32x4_t f0 = f[0], f1 = f[64];
+          const int32x8_t qp = {f0[0], f0[1], f0[2], f0[3], f1[0], f1[1], f1[2], f1[3]};
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {  // formats: A 4 (e2m1), B 0 (e4m3)
+            const int32x8_t kf = {int(k[u][0]), int(k[u][1]), int(k[u][2]), int(k[u][3]), 0, 0, 0, 0};
+            if (q == 0) sv[u][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf, qp, sv[u][i], 4, 0, 0, int(ks[u]), 0, qs[i]);
+            else sv[u][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf, qp, sv[u][i], 4, 0, 0, int(ks[u]), 1, qs[i]);
+          }
         }
-      }
     }
-    bool poison[NT];
-#pragma unroll
-    for (int i = 0; i < NT; ++i) poison[i] = false;
-    const bool ok0 = unsigned(id[0]) < unsigned(p.num_blocks), ok1 = unsigned(id[1]) < unsigned(p.num_blocks);
+  };
+
+  // What follows a pair's scores: masks where a row may not see a key, and the reference maxima.
+  auto settle = [&](int pi, bool ok0, bool ok1, floatx4_t (&sv)[2][NT], uint32_t (&vs)[2]) __attribute__((always_inline)) {
     if (32 * pi + 32 > full_end || !ok0 || !ok1) {
       // Keys that some row may not see: their scores are -inf for it, and their values must not reach it.
       // A probability of 0 does that, unless the value is NaN (scale byte 255, also in slots that were
-      // never written): such groups are taken as codes times 1, and the rows that do see one get their
-      // NaN in the group's dims afterwards.
+      // never written): such groups are taken as codes times 1, and the rows that do see one get NaN in the
+      // group's dims at once (O stays NaN).
       uint32_t bad = 0;
+      int first = 32 * pi + 4 * g4;
+      asm volatile("" : "+v"(first));     // or the comparisons are hoisted out of the branch
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int pos = 32 * pi + 16 * u + 4 * g4 + e;
+          const int pos = first + 16 * u + e;
           const bool seen = pos < end && (u == 0 ? ok0 : ok1);
 #pragma unroll
-          for (int i = 0; i < NT; ++i)
-            if (!(seen && pos <= lim[i])) sv[u][i][e] = -INFINITY;
-          const uint32_t byte = (x[u].vs >> (8 * e)) & 255u;
-          if (!seen || byte == kKvqScaleNan) x[u].vs = (x[u].vs & ~(255u << (8 * e))) | (127u << (8 * e));
+          for (int i = 0; i < NT; ++i) sv[u][i][e] = seen && pos <= lim[i] ? sv[u][i][e] : -INFINITY;
+          const uint32_t byte = (vs[u] >> (8 * e)) & 255u;
+          if (!seen || byte == kKvqScaleNan) vs[u] = (vs[u] & ~(255u << (8 * e))) | (127u << (8 * e));
           if (seen && byte == kKvqScaleNan) bad |= 1u << (4 * u + e);
         }
       if (__ballot(bad != 0)) {
         // output lane (row l16, g4) holds dims D / 4 * g4 .. of its row: group g4 * D / 128, whose scales
         // lanes of dims in it (l16 * D / 16) hold, their tokens 4 a .. 4 a + 3
+        bool poison[NT];
+#pragma unroll
+        for (int i = 0; i < NT; ++i) poison[i] = false;
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
           const uint32_t w = uint32_t(__shfl(int(bad), a * 16 + (g4 * D / 128) * (512 / D)));
@@ -297,17 +385,19 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void kvq_attn_kernel(KvqAttnPara
               for (int i = 0; i < NT; ++i)
                 if ((w >> (4 * u + e)) & 1u) poison[i] |= 32 * pi + 16 * u + 4 * a + e <= lim[i];
         }
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+          for (int t = 0; t < DT; ++t) o[i][t] += poison[i] ? __builtin_nanf("") : 0.f;
       }
     }
-    // running maximum, O rescaled only when a row's grows by more than the slack
     float mx[NT];
     bool grow = false;
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-      const float v = fmaxf(fmaxf(fmaxf(sv[0][i][0], sv[0][i][1]), fmaxf(sv[0][i][2], sv[0][i][3])),
-                            fmaxf(fmaxf(sv[1][i][0], sv[1][i][1]), fmaxf(sv[1][i][2], sv[1][i][3])));
-      mx[i] = v;
-      grow |= (v - m[i]) * p.c > kRescaleSlack || (v > m[i] && m[i] == -INFINITY);
+      mx[i] = fmaxf(fmaxf(fmaxf(sv[0][i][0], sv[0][i][1]), fmaxf(sv[0][i][2], sv[0][i][3])),
+                    fmaxf(fmaxf(sv[1][i][0], sv[1][i][1]), fmaxf(sv[1][i][2], sv[1][i][3])));
+      grow |= mx[i] > bound[i];
     }
     if (__ballot(grow)) {
 #pragma unroll
@@ -315,47 +405,86 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void kvq_attn_kernel(KvqAttnPara
         const float mn = fmaxf(m[i], rows_max4(mx[i]));
         const float alpha = m[i] == -INFINITY ? 0.f : exp2f((m[i] - mn) * p.c);
         m[i] = mn;
-        l[i] *= alpha;
+        bound[i] = mn + slack;
+        ref[i] = mn == -INFINITY ? 0.f : mn;
+        ls[i] *= alpha;
 #pragma unroll
         for (int t = 0; t < DT; ++t) o[i][t] *= alpha;
       }
     }
+  };
+
+  floatx4_t sv[2][NT];
+  uint32_t vs[2];
+  // Pair pi is in when at most the copies of the pairs after it are in flight. The reads of pair pi - 2 are
+  // done, so its slot takes pair pi + kSlots - 2.
+  auto arrive = [&](int pi) __attribute__((always_inline)) {
+    if (pi + kSlots - 3 < p1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kSlots - 3) * kCopies) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  };
+  if (p0 < p1) {
+    if (p0 + kSlots - 2 < p1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kSlots - 2) * kCopies) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    scores(p0, sv, vs);
+    settle(p0, have >> (2 * kSlots - 4) & 1u, have >> (2 * kSlots - 4) & 2u, sv, vs);
+  }
+  for (int pi = p0; pi < p1; ++pi) {
+    arrive(pi + 1);
+    if (pi + kSlots - 1 < p1) issue(pi + kSlots - 1, nid);
+    have = have << 2 | present(nid);
+    ids(pi + kSlots, nid);
+    // scores of the next pair (past the last: of whatever its slot holds, not used), beside the
+    // probabilities and values of this one
+    __builtin_amdgcn_s_setprio(1);
+    floatx4_t nsv[2][NT];
+    uint32_t nvs[2];
+    scores(pi + 1, nsv, nvs);
     bf16x8_t pf[NT][PP];
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-      const float ref = m[i] == -INFINITY ? 0.f : m[i];      // a row that has seen no key: exp2(-inf)
       float ps = 0.f;
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float w = __builtin_amdgcn_exp2f((sv[u][i][e] - ref) * p.c);
-          ps += w;
+          const float w = __builtin_amdgcn_exp2f((sv[u][i][e] - ref[i]) * p.c);
+          if constexpr (F32) ps += w;
           __bf16 part[PP];
           split_bf16<PP>(w, part);
 #pragma unroll
           for (int q = 0; q < PP; ++q) pf[i][q][4 * u + e] = part[q];
         }
-      l[i] += ps;
+      if constexpr (F32) {
+        ls[i][0] += ps;
+      } else {
+        const uint32_t one = 0x3f803f80u;
+        const u32x4 ones = {one, one, one, one};
+#pragma unroll
+        for (int q = 0; q < PP; ++q)
+          ls[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ones), pf[i][q], ls[i], 0, 0, 0);
+      }
     }
     // O^T += V^T P^T: lane (l16, g4) holds dims D / 16 * l16 + t (tile t) of tokens 4 g4 .. +3 of both blocks
+    const uint8_t* vsrc_lds = ring + (pi - p0) % kSlots * SLOT + 16 * D + (D == 128 ? lane : g4 * 8 + l16 / 2) * 16;
     uint32_t vd[2][4][DT / 2];           // token's dims as bf16 pairs
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < 2; ++u) {
+      const u32x4 vc = *reinterpret_cast<const u32x4*>(vsrc_lds + 8 * D * u);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const uint32_t sc = kvq_scale_bits(x[u].vs, e);
+        const uint32_t sc = kvq_scale_bits(vs[u], e);
         if constexpr (D == 128) {
-          vd[u][e][0] = kvq_decode2<0>(x[u].v[e], sc);
-          vd[u][e][1] = kvq_decode2<1>(x[u].v[e], sc);
-          vd[u][e][2] = kvq_decode2<2>(x[u].v[e], sc);
-          vd[u][e][3] = kvq_decode2<3>(x[u].v[e], sc);
+          vd[u][e][0] = kvq_decode2<0>(vc[e], sc);
+          vd[u][e][1] = kvq_decode2<1>(vc[e], sc);
+          vd[u][e][2] = kvq_decode2<2>(vc[e], sc);
+          vd[u][e][3] = kvq_decode2<3>(vc[e], sc);
         } else {
-          const uint32_t w = x[u].v[e] >> (16 * (l16 % 2));
+          const uint32_t w = vc[e] >> (16 * (l16 % 2));
           vd[u][e][0] = kvq_decode2<0>(w, sc);
           vd[u][e][1] = kvq_decode2<1>(w, sc);
         }
       }
+    }
 #pragma unroll
     for (int t = 0; t < DT; ++t) {
       u32x4 w;
@@ -370,27 +499,33 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void kvq_attn_kernel(KvqAttnPara
 #pragma unroll
         for (int q = 0; q < PP; ++q) o[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[i][q], o[i][t], 0, 0, 0);
     }
+    __builtin_amdgcn_s_setprio(0);
+    if (pi + 1 < p1) settle(pi + 1, have >> (2 * kSlots - 4) & 1u, have >> (2 * kSlots - 4) & 2u, nsv, nvs);
 #pragma unroll
-    for (int i = 0; i < NT; ++i)
-      if (poison[i])
+    for (int u = 0; u < 2; ++u) {
+      vs[u] = nvs[u];
 #pragma unroll
-        for (int t = 0; t < DT; ++t) o[i][t] += __builtin_nanf("");
+      for (int i = 0; i < NT; ++i) sv[u][i] = nsv[u][i];
+    }
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no copy may outlive the ring
 
   // the wavefronts' shares joined through LDS, one 16-row tile at a time
+  constexpr int RS = D + 4;              // floats of a row, then 16 maxima and 16 sums
+  float* own = reinterpret_cast<float*>(ring);
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
-    const float lt = rows_sum4(l[i]);
+    const float lt = F32 ? rows_sum4(ls[i][0]) : ls[i][0];
     if (i > 0) __syncthreads();
 #pragma unroll
     for (int e = 0; e < 4; ++e)
 #pragma unroll
       for (int t = 0; t < DT; t += 4)   // dims D / 16 * (4 g4 + e) + t .. + 3
-        *reinterpret_cast<floatx4_t*>(&s_o[wave][l16][D / 16 * (4 * g4 + e) + t]) =
+        *reinterpret_cast<floatx4_t*>(own + l16 * RS + D / 16 * (4 * g4 + e) + t) =
             floatx4_t{o[i][t][e], o[i][t + 1][e], o[i][t + 2][e], o[i][t + 3][e]};
     if (g4 == 0) {
-      s_m[wave][l16] = m[i];
-      s_l[wave][l16] = lt;
+      own[16 * RS + l16] = m[i];
+      own[16 * RS + 16 + l16] = lt;
     }
     __syncthreads();
     // thread = 8 dims of one row
@@ -398,17 +533,20 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void kvq_attn_kernel(KvqAttnPara
     const int row = threadIdx.x / (D / 8), d0 = threadIdx.x % (D / 8) * 8;
     const int r = r0 + 16 * i + row;
     if (r >= p.R) continue;
-    float M = s_m[0][row];
+    const float* part = reinterpret_cast<const float*>(lds);
+    float M = -INFINITY;
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) M = fmaxf(M, s_m[w][row]);
+    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, part[w * (kLds / 4) + 16 * RS + row]);
     float L = 0.f;
     floatx4_t a[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      const float f = s_m[w][row] == -INFINITY ? 0.f : exp2f((s_m[w][row] - M) * p.c);
-      L += s_l[w][row] * f;
-      a[0] += *reinterpret_cast<const floatx4_t*>(&s_o[w][row][d0]) * f;
-      a[1] += *reinterpret_cast<const floatx4_t*>(&s_o[w][row][d0 + 4]) * f;
+      const float* pw = part + w * (kLds / 4);
+      const float mw = pw[16 * RS + row];
+      const float f = mw == -INFINITY ? 0.f : exp2f((mw - M) * p.c);
+      L += pw[16 * RS + 16 + row] * f;
+      a[0] += *reinterpret_cast<const floatx4_t*>(pw + row * RS + d0) * f;
+      a[1] += *reinterpret_cast<const floatx4_t*>(pw + row * RS + d0 + 4) * f;
     }
     if (p.splits == 1) {
       store_out<T>(p, b, h, r, D, d0, a, L);

@@ -16,12 +16,14 @@ DT = {"bf16": torch.bfloat16, "f32": torch.float32}
 
 
 def _tol(out, mag, dtype):
-    """bf16: the output's rounding (2^-8 relative), weights kept in bf16 parts of 16 bits (2^-16), f32 sums,
-    and scores whose f32 sums and hardware exp2 move a weight by well under 2^-10: 2^-10 of sum w |v|.
+    """bf16: the output's rounding, 2^-8 |o|. The weights enter the product rounded to bf16, w (1 + d) with
+    |d| <= 2^-8, and so does their sum: the result is off by sum w d (v - o) / (1 + sum w d), at most
+    2^-8 (1 + 2^-7) (sum w |v| + |o|). f32 sums, and scores whose f32 sums and hardware exp2 move a weight by
+    well under 2^-10: 2^-10 sum w |v|, which also covers the 2^-7 of the line before.
     f32: sums of D products per score and of up to 2^12 keys, each at most 2^-24 of its terms' magnitudes
     with partial sums over 32 keys: under 2^-15 of sum w |v| for scores of magnitude up to ~2^5."""
     if dtype == "bf16":
-        return 2.0 ** -8 * np.abs(out) + 2.0 ** -10 * mag + 1e-30
+        return 2.0 ** -7 * np.abs(out) + (2.0 ** -8 + 2.0 ** -10) * mag + 1e-30
     return 2.0 ** -15 * mag + 1e-30
 
 
