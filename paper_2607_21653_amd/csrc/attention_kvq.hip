@@ -6,6 +6,8 @@
 // bf16 parts (24 bits); in bf16 one, with the sum taken of the rounded weights, by an MFMA with a row of ones.
 // That adds a rounding like the output's own: rms error 2.07e-3 of the output's rms against 1.66e-3 with two
 // parts, for which 128 sequences x 5 positions at context 8192 took 178 us, with one 135.
+#include <algorithm>
+
 #include "internal.h"
 #include "kvq_format.h"
 
@@ -24,12 +26,15 @@ struct KvqAttnParams {
   const int32_t* bt;       // [B, max_blocks]
   const int32_t* ctx;      // [B]
   void* out;               // [B * n, Hq * D], row-major or tiled
-  float* part_o;           // [B, Hkv, S, R, D]
-  float* part_ml;          // [B, Hkv, S, R, 2]
+  float* part_o;           // [nrg, Hkv, slots, group, D] partial outputs of split ranges
+  float* part_ml;          // [nrg, Hkv, slots, group, 2] their maxima and sums
+  int32_t* split;          // [nrg, B, 2] first slot and slots of a sequence
   int B, n, Hq, Hkv, max_blocks, num_blocks;
   int G, R;                // query heads per kv head, rows of a (b, h)
   int nrg, group;          // row groups of a (b, h) and rows of one (16 NT)
-  int splits, bps;         // splits of the longest table, blocks of one
+  int slots;               // workgroups of a (row group, kv head); B: one per sequence, nothing is cut
+  int resident;            // workgroups that the chip holds
+  int spread;              // a slot's heads run on one XCD
   float c;                 // log2(e) / sqrt(D)
   int out_tiled;
 };
@@ -39,6 +44,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef bf16x8_t UnalignedBf16x8 __attribute__((aligned(2)));
 typedef floatx4_t UnalignedF4 __attribute__((aligned(4)));
 typedef u32x4 UnalignedU4 __attribute__((aligned(2)));
+typedef u32x2 UnalignedU2 __attribute__((aligned(2)));
 
 // Keys 0 .. end - 1 are those that rows [r0, r1) of sequence b may see (the last row the most).
 MOLT_DEV int visible_end(const KvqAttnParams& p, int ctx, int r1) {
@@ -46,11 +52,20 @@ MOLT_DEV int visible_end(const KvqAttnParams& p, int ctx, int r1) {
   return int(e < 0 ? 0 : e > 16l * p.max_blocks ? 16l * p.max_blocks : e);
 }
 
-// LDS-DMA: 16 (4) bytes a lane from src to dst + 16 (4) * lane; dst is the wavefront's
+// LDS-DMA: 16 (4) bytes a lane from src to dst + 16 (4) * lane; dst is the wavefront's. ONCE: nontemporal, for keys
+// that one workgroup reads
 typedef const __attribute__((address_space(1))) void* GlobalPtr;
 typedef __attribute__((address_space(3))) void* LdsPtr;
-MOLT_DEV void copy_lds16(const uint8_t* src, uint8_t* dst) { __builtin_amdgcn_global_load_lds((GlobalPtr)src, (LdsPtr)dst, 16, 0, 0); }
-MOLT_DEV void copy_lds4(const uint8_t* src, uint8_t* dst) { __builtin_amdgcn_global_load_lds((GlobalPtr)src, (LdsPtr)dst, 4, 0, 0); }
+template <bool ONCE>
+MOLT_DEV void copy_lds16(const uint8_t* src, uint8_t* dst) {
+  if constexpr (ONCE) __builtin_amdgcn_global_load_lds((GlobalPtr)src, (LdsPtr)dst, 16, 0, 2);
+  else __builtin_amdgcn_global_load_lds((GlobalPtr)src, (LdsPtr)dst, 16, 0, 0);
+}
+template <bool ONCE>
+MOLT_DEV void copy_lds4(const uint8_t* src, uint8_t* dst) {
+  if constexpr (ONCE) __builtin_amdgcn_global_load_lds((GlobalPtr)src, (LdsPtr)dst, 4, 0, 2);
+  else __builtin_amdgcn_global_load_lds((GlobalPtr)src, (LdsPtr)dst, 4, 0, 0);
+}
 
 // a wave-uniform value the compiler is to hold in scalar registers
 MOLT_DEV long uniform(long x) {
@@ -98,15 +113,14 @@ MOLT_DEV void load_query_f32(const float* q, bool valid, int g4, bf16x8_t (&qf)[
 // 128, qp[0] is hi and qp[1] lo, k the dim; for D = 64 k = 0 .. 63 is hi, 64 .. 127 lo, with K's codes
 // twice in the A operand. qs: the scale byte of the lane's k block (and for D = 128 lo's in the second byte).
 template <int D>
-MOLT_DEV void load_query_bf16(const uint16_t* q, bool valid, int g4, int32x8_t (&qp)[D / 64], int& qs) {
+MOLT_DEV void split_query_bf16(const u32x4 (&raw)[D / 64][2], int g4, int32x8_t (&qp)[D / 64], int& qs) {
   float x[D / 64][16];
   uint32_t amax = 0;
 #pragma unroll
   for (int c = 0; c < D / 64; ++c)
 #pragma unroll
     for (int v = 0; v < 2; ++v) {
-      u32x4 w = {0u, 0u, 0u, 0u};
-      if (valid) w = *reinterpret_cast<const UnalignedU4*>(q + 64 * c + 16 * g4 + 8 * v);
+      const u32x4 w = raw[c][v];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         x[c][8 * v + 2 * e] = __uint_as_float(w[e] << 16);
@@ -146,24 +160,95 @@ MOLT_DEV void load_query_bf16(const uint16_t* q, bool valid, int g4, int32x8_t (
   qs = bad ? 0xffff : D == 128 ? byte | (byte - 5) << 8 : g4 < 2 ? byte : byte - 5;
 }
 
-// Output dims d0 .. + 7 of row r: a / L, zeros for a row that sees no key
+// Output dims d0 .. + 3 of row r: a / L, zeros for a row that sees no key
 template <typename T>
-MOLT_DEV void store_out(const KvqAttnParams& p, int b, int h, int r, int D, int d0, const floatx4_t (&a)[2], float L) {
+MOLT_DEV void store_out4(const KvqAttnParams& p, int b, int h, int r, int D, int d0, const floatx4_t& a, float L) {
   const float inv = L == 0.f ? 0.f : 1.f / L;
   const long t = long(b) * p.n + r / p.G, c = (h * p.G + r % p.G) * D + d0, cols = long(p.Hq) * D;
-  T* out = static_cast<T*>(p.out);
-  if constexpr (sizeof(T) == 4) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      *reinterpret_cast<UnalignedF4*>(out + (p.out_tiled ? tiled_index(t, c + 4 * i, cols, 4) : t * cols + c + 4 * i)) = a[i] * inv;
-  } else {
-    *reinterpret_cast<UnalignedU4*>(out + (p.out_tiled ? tiled_index(t, c, cols, 2) : t * cols + c)) =
-        u32x4{f32x2_to_bf16(a[0][0] * inv, a[0][1] * inv), f32x2_to_bf16(a[0][2] * inv, a[0][3] * inv),
-              f32x2_to_bf16(a[1][0] * inv, a[1][1] * inv), f32x2_to_bf16(a[1][2] * inv, a[1][3] * inv)};
-  }
+  T* out = static_cast<T*>(p.out) + (p.out_tiled ? tiled_index(t, c, cols, sizeof(T)) : t * cols + c);
+  if constexpr (sizeof(T) == 4)
+    *reinterpret_cast<UnalignedF4*>(out) = a * inv;
+  else
+    *reinterpret_cast<UnalignedU2*>(out) = u32x2{f32x2_to_bf16(a[0] * inv, a[1] * inv), f32x2_to_bf16(a[2] * inv, a[3] * inv)};
 }
 
-template <int D, typename T, int NT>
+// The work of slot `slot` of a row group (whose rows end before r1): part `part` of `parts` of sequence b, whose
+// slots start at `first`; b < 0: none.
+struct Share { int b, part, parts, first; };
+
+// Few sequences, or sequences of uneven lengths, are cut into parts of about c pairs of blocks: max(1, ceil(T / c))
+// of a sequence of T pairs. The lengths are known on the device only, so every workgroup works out c and its own
+// place (a microsecond). Lane j weighs one of 64 values of c, from no cut at all down, by the time it would take, in
+// pairs of blocks: the longest part, or all parts and what each costs besides (its start and its join of
+// wavefronts, kPartCost) over the workgroups that are resident, half a part more where they do not all fit at
+// once, and the joining launch (kJoinCost) if anything is cut. Of equal ones the longest c wins.
+constexpr int kMaxCut = 256, kMinPairs = 4;
+constexpr float kJoinCost = 30.f;
+MOLT_DEV float cut(float pairs, float inv_c) { return fmaxf(1.f, ceilf(pairs * inv_c)); }
+
+template <int NT>
+MOLT_DEV Share find_share(const KvqAttnParams& p, int r1, int slot, float* lds) {
+  constexpr int kPer = kMaxCut / kWave;
+  constexpr float kPartCost = 48.f / NT;
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  float pairs[kPer];                     // of sequences lane, lane + 64, .. (in every wavefront)
+  float sum = 0.f, most = 0.f;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int b = lane + kWave * i;
+    pairs[i] = b < p.B ? float((visible_end(p, p.ctx[b], r1) + 31) / 32) : -1.f;
+    sum += fmaxf(pairs[i], 0.f);
+    most = fmaxf(most, pairs[i]);
+  }
+  sum = wave_sum_dpp(sum);
+  most = fmaxf(wave_max_dpp(most), float(kMinPairs));
+  const float least = fminf(fmaxf(sum / float(p.slots), float(kMinPairs)), most);
+  // (hardware approximations: the same in every workgroup)
+  const float c = lane == 0 ? most : most * __builtin_amdgcn_exp2f(__builtin_amdgcn_logf(least / most) * (float(lane) / 63.f));
+  const float inv = __builtin_amdgcn_rcpf(c);
+  float n = 0.f;                         // parts with the lane's c; each wavefront counts 16 of 64 sequences
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    if (kWave * i >= p.B) break;
+#pragma unroll
+    for (int j = 0; j < kWave / kWaves; ++j) {      // (past the last sequence: no part)
+      const float t = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(pairs[i]), wave * (kWave / kWaves) + j));
+      n += t < 0.f ? 0.f : cut(t, inv);
+    }
+  }
+  lds[wave * kWave + lane] = n;
+  __syncthreads();
+  n = lds[lane] + lds[kWave + lane] + lds[2 * kWave + lane] + lds[3 * kWave + lane];
+  __syncthreads();
+  const float res = float(p.resident) / (float(p.Hkv) * float(p.nrg));
+  float cost = fmaxf(c + kPartCost, (sum + n * kPartCost) / res + (n > res ? 0.5f * c : 0.f));
+  if (n > float(p.B)) cost += kJoinCost;
+  if (n > float(p.slots)) cost = INFINITY;
+  const float best = -wave_max_dpp(-cost);
+  const int pick = __ffsll((unsigned long long)__ballot(cost == best)) - 1;
+  const float inv_c = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(inv), pick));
+  // the sequence that has the slot
+  int before = 0;
+  Share w{-1, 0, 1, 0};
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    if (kWave * i >= p.B || w.b >= 0) break;
+    const int parts = lane + kWave * i < p.B ? int(cut(pairs[i], inv_c)) : 0;
+    const int upto = before + wave_scan_dpp(parts);
+    const unsigned long long has = __ballot(slot < upto);
+    if (has) {
+      const int l = __ffsll(has) - 1;
+      w.b = kWave * i + l;
+      w.parts = __builtin_amdgcn_readlane(parts, l);
+      w.first = __builtin_amdgcn_readlane(upto, l) - w.parts;
+      w.part = slot - w.first;
+    }
+    before = __builtin_amdgcn_readlane(upto, 63);
+  }
+  return w;
+}
+
+template <int D, typename T, int NT, bool ONCE>
 __global__ __launch_bounds__(kWaves * kWave, 2) void kvq_attn_kernel(KvqAttnParams p) {
   typedef KvqRecord<D> Rec;
   constexpr bool F32 = sizeof(T) == 4;
@@ -179,22 +264,46 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void kvq_attn_kernel(KvqAttnPara
   constexpr int QF = D / 64 * 2048;      // bytes of a tile's query operands
   __shared__ __attribute__((aligned(16))) uint8_t lds[kWaves * kLds + (F32 ? 0 : NT * QF)];
 
-  // work item
-  const int rg = int(blockIdx.x) % p.nrg;
-  const int unit = int(blockIdx.x) / p.nrg;
-  const int split = unit % p.splits;
-  const int bh = unit / p.splits;
-  const int b = bh / p.Hkv, h = bh % p.Hkv;
+  // Work item. Consecutive workgroups run on consecutive XCDs: the row groups of a slot and head, which read the same
+  // keys, are 8 apart, and with many slots (spread) a slot's heads too, whose records share lines (read requests of 128
+  // sequences x 4 heads at context 8192: 1.02 times the records' bytes, 1.07 with heads on neighbouring XCDs).
+  const int bi = int(blockIdx.x), rg = bi / 8 % p.nrg, hi = bi / (8 * p.nrg), lo = bi % 8;
+  const int h = p.spread ? hi % p.Hkv : (hi * 8 + lo) % p.Hkv;
+  const int slot = p.spread ? hi / p.Hkv * 8 + lo : (hi * 8 + lo) / p.Hkv;
+  if (slot >= p.slots) return;
   const int r0 = rg * 16 * NT, r1 = min(r0 + 16 * NT, p.R);
+  Share w{slot, 0, 1, slot};
+  if (p.slots > p.B) {
+    w = find_share<NT>(p, r1, slot, reinterpret_cast<float*>(lds));
+    if (w.b < 0) return;
+    if (h == 0 && w.part == 0 && threadIdx.x == 0) {
+      p.split[2 * (long(rg) * p.B + w.b)] = w.first;
+      p.split[2 * (long(rg) * p.B + w.b) + 1] = w.parts;
+    }
+  }
+  const int b = w.b;
+  const int lane = threadIdx.x % kWave, l16 = lane % 16, g4 = lane / 16;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  // The query rows are loaded first: behind the copies of keys and values they would wait for those. Wavefront i
+  // makes the operands of tile i.
+  const int qtile = F32 ? 0 : min(wave, NT - 1), qr = min(r0 + 16 * qtile + l16, p.R - 1);
+  const long qrow = ((long(b) * p.n + qr / p.G) * p.Hq + h * p.G + qr % p.G) * D;
+  u32x4 raw[D / 64][2];
+  if constexpr (!F32) {
+    const uint16_t* src = static_cast<const uint16_t*>(p.q) + qrow + 16 * g4;
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c)
+#pragma unroll
+      for (int v = 0; v < 2; ++v) raw[c][v] = *reinterpret_cast<const UnalignedU4*>(src + 64 * c + 8 * v);
+  }
   const int ctx = p.ctx[b];
   const int end = visible_end(p, ctx, r1);
   const int nblk = (end + 15) / 16, npairs = (nblk + 1) / 2;
-  const int ns = (nblk + p.bps - 1) / p.bps;
-  if (split >= max(ns, 1)) return;
-  const int lane = threadIdx.x % kWave, l16 = lane % 16, g4 = lane / 16;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  // the split's pairs of blocks, then the wavefront's share
-  const int s0 = ns > 0 ? int(long(npairs) * split / ns) : 0, s1 = ns > 0 ? int(long(npairs) * (split + 1) / ns) : 0;
+  int lim[NT];                           // last key that a row sees (past the last row: as the last)
+#pragma unroll
+  for (int i = 0; i < NT; ++i) lim[i] = ctx + min(r0 + 16 * i + l16, p.R - 1) / p.G;
+  // the share's pairs of blocks, then the wavefront's
+  const int s0 = int(long(npairs) * w.part / w.parts), s1 = int(long(npairs) * (w.part + 1) / w.parts);
   const int p0 = s0 + (s1 - s0) * wave / kWaves, p1 = s0 + (s1 - s0) * (wave + 1) / kWaves;
   const int full_end = min(visible_end(p, ctx, r0 + 1), end);    // keys before are seen by every row
   uint8_t* ring = lds + wave * kLds;
@@ -216,15 +325,15 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void kvq_attn_kernel(KvqAttnPara
     for (int u = 0; u < 2; ++u) rec[u] = uniform((long(unsigned(id[u]) < unsigned(p.num_blocks) ? id[u] : 0) * p.Hkv + h) * Rec::kBytes);
     if constexpr (D == 128) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u) copy_lds16(p.kc + rec[u] + ksrc, dst + 1024 * u);
+      for (int u = 0; u < 2; ++u) copy_lds16<ONCE>(p.kc + rec[u] + ksrc, dst + 1024 * u);
 #pragma unroll
-      for (int u = 0; u < 2; ++u) copy_lds16(p.vc + rec[u] + vsrc, dst + 2048 + 1024 * u);
+      for (int u = 0; u < 2; ++u) copy_lds16<ONCE>(p.vc + rec[u] + vsrc, dst + 2048 + 1024 * u);
     } else {
       const long r = lane < 32 ? rec[0] : rec[1];
-      copy_lds16(p.kc + r + ksrc, dst);
-      copy_lds16(p.vc + r + vsrc, dst + 1024);
+      copy_lds16<ONCE>(p.kc + r + ksrc, dst);
+      copy_lds16<ONCE>(p.vc + r + vsrc, dst + 1024);
     }
-    copy_lds4(sbase + (spart % 2 ? rec[1] : rec[0]), dst + 32 * D);
+    copy_lds4<ONCE>(sbase + (spart % 2 ? rec[1] : rec[0]), dst + 32 * D);
   };
   auto ids = [&](int pi, int (&id)[2]) __attribute__((always_inline)) {
     id[0] = btab[min(2 * pi, nblk - 1)];
@@ -249,29 +358,22 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void kvq_attn_kernel(KvqAttnPara
     nid[1] = first[kSlots - 1][1];
   }
 
-  // Q^T operands: in f32 each wavefront's own, in bf16 in LDS for all, tile i made by wavefront i
-  int lim[NT];                           // last key that the row sees
+  // the query operands: in f32 each wavefront's own, in bf16 in LDS for all
   bf16x8_t qf[QP][KS];
   int qs[NT];                            // scale bytes of both fp8 parts
+  if constexpr (F32) {
+    load_query_f32<D>(static_cast<const float*>(p.q) + qrow, r0 + l16 < p.R, g4, qf);
+  } else if (wave < NT) {
+    int32x8_t qp[D / 64];
+    int sc;
+    split_query_bf16<D>(raw, g4, qp, sc);
 #pragma unroll
-  for (int i = 0; i < NT; ++i) {
-    const int r = r0 + 16 * i + l16, j = r / p.G, gi = r % p.G;
-    lim[i] = r < p.R ? ctx + j : -1;
-    const long at = ((long(b) * p.n + j) * p.Hq + h * p.G + gi) * D;
-    if constexpr (F32) {
-      load_query_f32<D>(static_cast<const float*>(p.q) + at, r < p.R, g4, qf);
-    } else if (wave == i) {
-      int32x8_t qp[D / 64];
-      int sc;
-      load_query_bf16<D>(static_cast<const uint16_t*>(p.q) + at, r < p.R, g4, qp, sc);
-#pragma unroll
-      for (int u = 0; u < D / 64; ++u) {
-        int32x4_t* dst = reinterpret_cast<int32x4_t*>(qlds + i * QF + u * 2048 + lane * 16);
-        dst[0] = int32x4_t{qp[u][0], qp[u][1], qp[u][2], qp[u][3]};
-        dst[64] = int32x4_t{qp[u][4], qp[u][5], qp[u][6], qp[u][7]};
-      }
-      *reinterpret_cast<int*>(lds + i * kLds + (kSlots - 1) * SLOT + lane * 4) = sc;   // in a slot not yet in use
+    for (int u = 0; u < D / 64; ++u) {
+      int32x4_t* dst = reinterpret_cast<int32x4_t*>(qlds + wave * QF + u * 2048 + lane * 16);
+      dst[0] = int32x4_t{qp[u][0], qp[u][1], qp[u][2], qp[u][3]};
+      dst[64] = int32x4_t{qp[u][4], qp[u][5], qp[u][6], qp[u][7]};
     }
+    *reinterpret_cast<int*>(ring + (kSlots - 1) * SLOT + lane * 4) = sc;   // in a slot not yet in use
   }
   if constexpr (!F32) {
     lds_barrier();
@@ -370,20 +472,16 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void kvq_attn_kernel(KvqAttnPara
         }
       if (__ballot(bad != 0)) {
         // output lane (row l16, g4) holds dims D / 4 * g4 .. of its row: group g4 * D / 128, whose scales
-        // lanes of dims in it (l16 * D / 16) hold, their tokens 4 a .. 4 a + 3
+        // lanes of dims in it (l16 * D / 16) hold
         bool poison[NT];
 #pragma unroll
         for (int i = 0; i < NT; ++i) poison[i] = false;
+#pragma unroll 1
+        for (int t = 0; t < 32; ++t) {   // the pair's tokens
+          const uint32_t w = uint32_t(__shfl(int(bad), t % 16 / 4 * 16 + (g4 * D / 128) * (512 / D)));
+          const bool nan = w >> (t / 16 * 4 + t % 4) & 1u;
 #pragma unroll
-        for (int a = 0; a < 4; ++a) {
-          const uint32_t w = uint32_t(__shfl(int(bad), a * 16 + (g4 * D / 128) * (512 / D)));
-#pragma unroll
-          for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-              for (int i = 0; i < NT; ++i)
-                if ((w >> (4 * u + e)) & 1u) poison[i] |= 32 * pi + 16 * u + 4 * a + e <= lim[i];
+          for (int i = 0; i < NT; ++i) poison[i] |= nan && 32 * pi + t <= lim[i];
         }
 #pragma unroll
         for (int i = 0; i < NT; ++i)
@@ -548,10 +646,11 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void kvq_attn_kernel(KvqAttnPara
       a[0] += *reinterpret_cast<const floatx4_t*>(pw + row * RS + d0) * f;
       a[1] += *reinterpret_cast<const floatx4_t*>(pw + row * RS + d0 + 4) * f;
     }
-    if (p.splits == 1) {
-      store_out<T>(p, b, h, r, D, d0, a, L);
+    if (w.parts == 1) {
+      store_out4<T>(p, b, h, r, D, d0, a[0], L);
+      store_out4<T>(p, b, h, r, D, d0 + 4, a[1], L);
     } else {
-      const long pr = (long(bh) * p.splits + split) * p.R + r;
+      const long pr = ((long(rg) * p.Hkv + h) * p.slots + slot) * p.group + 16 * i + row;
       *reinterpret_cast<floatx4_t*>(p.part_o + pr * D + d0) = a[0];
       *reinterpret_cast<floatx4_t*>(p.part_o + pr * D + d0 + 4) = a[1];
       if (d0 == 0) {
@@ -562,54 +661,74 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void kvq_attn_kernel(KvqAttnPara
   }
 }
 
-// log-sum-exp join of the splits: thread = 8 dims of one row
+// log-sum-exp join of a sequence's slots: thread = 4 dims of one row, kU slots' loads in flight together
 template <int D, typename T>
 __global__ __launch_bounds__(256) void kvq_merge_kernel(KvqAttnParams p) {
   const long i = long(blockIdx.x) * 256 + threadIdx.x;
-  const int d0 = int(i % (D / 8)) * 8;
-  const long row = i / (D / 8);
+  const int d0 = int(i % (D / 4)) * 4;
+  const long row = i / (D / 4);
   const int bh = int(row / p.R), r = int(row % p.R);
-  const int b = bh / p.Hkv, h = bh % p.Hkv;
+  const int b = bh / p.Hkv, h = bh % p.Hkv, rg = r / p.group;
   if (b >= p.B) return;
-  const int end = visible_end(p, p.ctx[b], min((r / p.group + 1) * p.group, p.R));
-  const int ns = max(((end + 15) / 16 + p.bps - 1) / p.bps, 1);
-  const long pr0 = long(bh) * p.splits * p.R + r;
-  float M = -INFINITY;
-  for (int s = 0; s < ns; ++s) M = fmaxf(M, p.part_ml[2 * (pr0 + long(s) * p.R)]);
-  float L = 0.f;
-  floatx4_t a[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-  for (int s = 0; s < ns; ++s) {
-    const long pr = pr0 + long(s) * p.R;
-    const float ms = p.part_ml[2 * pr];
-    const float f = ms == -INFINITY ? 0.f : exp2f((ms - M) * p.c);
-    L += p.part_ml[2 * pr + 1] * f;
-    a[0] += *reinterpret_cast<const floatx4_t*>(p.part_o + pr * D + d0) * f;
-    a[1] += *reinterpret_cast<const floatx4_t*>(p.part_o + pr * D + d0 + 4) * f;
+  const int2 sp = *reinterpret_cast<const int2*>(p.split + 2 * (long(rg) * p.B + b));
+  if (sp.y == 1) return;
+  const long pr0 = ((long(rg) * p.Hkv + h) * p.slots + sp.x) * p.group + r % p.group;
+  constexpr int kU = 8;
+  float M = -INFINITY, L = 0.f;
+  floatx4_t a = {0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < sp.y; s0 += kU) {
+    float2 ml[kU];
+    floatx4_t o[kU];
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {       // past the last: its own again, not added
+      const long pr = pr0 + long(min(s0 + u, sp.y - 1)) * p.group;
+      ml[u] = *reinterpret_cast<const float2*>(p.part_ml + 2 * pr);
+      o[u] = *reinterpret_cast<const floatx4_t*>(p.part_o + pr * D + d0);
+    }
+    float mn = M;
+#pragma unroll
+    for (int u = 0; u < kU; ++u) mn = fmaxf(mn, ml[u].x);
+    const float f0 = M == -INFINITY ? 0.f : exp2f((M - mn) * p.c);
+    M = mn;
+    L *= f0;
+    a *= f0;
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      if (s0 + u >= sp.y) break;
+      const float f = ml[u].x == -INFINITY ? 0.f : exp2f((ml[u].x - M) * p.c);
+      L += ml[u].y * f;
+      a += o[u] * f;
+    }
   }
-  store_out<T>(p, b, h, r, D, d0, a, L);
+  store_out4<T>(p, b, h, r, D, d0, a, L);
 }
 
 constexpr int kMaxTiles = 3;             // 16-row tiles of a wavefront (bf16; one in f32)
 
-// Row groups of as few 16-row tiles as cover the R rows, and the splits of the key range: enough that
-// the workgroups fill the chip (512 are resident), at least 8 blocks each.
-void kvq_plan(KvqAttnParams& p, bool f32) {
+// Row groups of as few 16-row tiles as cover the R rows. Slots: one per sequence where that gives as many workgroups
+// as are resident (a cut for uneven lengths would cost 8% of even ones: the work of finding it, workgroups without a
+// part, the joining launch), or the tables are short (kMinCutBlocks), else room for as many parts as are resident.
+constexpr int kMinCutBlocks = 48;
+void kvq_plan(KvqAttnParams& p, int D, bool f32) {
   p.G = p.Hq / p.Hkv;
   p.R = p.G * p.n;
   const int tiles = (p.R + 15) / 16, most = f32 ? 1 : kMaxTiles;
   p.nrg = (tiles + most - 1) / most;
-  p.group = 16 * ((tiles + p.nrg - 1) / p.nrg);
-  const long units = long(p.B) * p.Hkv * p.nrg;
-  long s = units >= 512 ? 1 : (1024 + units - 1) / units;
-  const long cap = (p.max_blocks + 7) / 8;
-  if (s > cap) s = cap;
-  p.bps = int((p.max_blocks + s - 1) / s + 1) / 2 * 2;
-  p.splits = (p.max_blocks + p.bps - 1) / p.bps;
+  const int nt = (tiles + p.nrg - 1) / p.nrg;
+  p.group = 16 * nt;
+  p.resident = 256 * (D == 128 || nt == 3 ? 2 : f32 || nt == 2 ? 3 : 4);   // by LDS and registers
+  const long per = long(p.Hkv) * p.nrg, pairs = (p.max_blocks + 1) / 2;
+  const long slots = std::min(p.resident / per, p.B * ((pairs + kMinPairs - 1) / kMinPairs));
+  p.slots = slots > p.B && p.B <= kMaxCut && p.max_blocks >= kMinCutBlocks ? int(slots) : p.B;
+  p.spread = p.slots >= 64;
 }
 
 template <int D, typename T, int NT>
 void launch_nt(const KvqAttnParams& p, hipStream_t s) {
-  kvq_attn_kernel<D, T, NT><<<unsigned(long(p.B) * p.Hkv * p.splits * p.nrg), kWaves * kWave, 0, s>>>(p);
+  const long units = p.spread ? (long(p.slots) + 7) / 8 * 8 * p.Hkv : (long(p.slots) * p.Hkv + 7) / 8 * 8;
+  const unsigned grid = unsigned(units * p.nrg);
+  if (p.nrg == 1) kvq_attn_kernel<D, T, NT, true><<<grid, kWaves * kWave, 0, s>>>(p);
+  else kvq_attn_kernel<D, T, NT, false><<<grid, kWaves * kWave, 0, s>>>(p);
 }
 
 template <int D, typename T>
@@ -621,29 +740,34 @@ void launch_dt(const KvqAttnParams& p, hipStream_t s) {
     else if (p.group == 32) launch_nt<D, T, 2>(p, s);
     else launch_nt<D, T, 3>(p, s);
   }
-  if (p.splits > 1) {
-    const long threads = long(p.B) * p.Hkv * p.R * (D / 8);
+  if (p.slots > p.B) {
+    const long threads = long(p.B) * p.Hkv * p.R * (D / 4);
     kvq_merge_kernel<D, T><<<unsigned((threads + 255) / 256), 256, 0, s>>>(p);
   }
 }
 
 void carve_parts(Carver& c, KvqAttnParams& p, int D) {
-  if (p.splits <= 1) return;
-  const long rows = long(p.B) * p.Hkv * p.splits * p.R;
+  if (p.slots <= p.B) return;
+  const long rows = long(p.nrg) * p.Hkv * p.slots * p.group;
   p.part_o = c.take<float>(rows * D);
   p.part_ml = c.take<float>(rows * 2);
+  p.split = c.take<int32_t>(2l * p.nrg * p.B);
 }
 
 }  // namespace
 
-// f32 calls have more row groups, so never more splits: one size serves both types
+// (of the type that needs more)
 size_t kvq_attention_ws_bytes(int B, int n, int Hq, int Hkv, int D, int max_blocks) {
-  KvqAttnParams p{};
-  p.B = B; p.n = n; p.Hq = Hq; p.Hkv = Hkv; p.max_blocks = max_blocks;
-  kvq_plan(p, false);
-  Carver c(nullptr, 0);
-  carve_parts(c, p, D);
-  return c.used ? c.used + 256 : 0;
+  size_t most = 0;
+  for (int f32 = 0; f32 < 2; ++f32) {
+    KvqAttnParams p{};
+    p.B = B; p.n = n; p.Hq = Hq; p.Hkv = Hkv; p.max_blocks = max_blocks;
+    kvq_plan(p, D, f32 != 0);
+    Carver c(nullptr, 0);
+    carve_parts(c, p, D);
+    if (c.used && c.used + 256 > most) most = c.used + 256;
+  }
+  return most;
 }
 
 hipError_t launch_kvq_attention(const void* q, const void* kc, const void* vc, const int32_t* bt,
@@ -658,7 +782,7 @@ hipError_t launch_kvq_attention(const void* q, const void* kc, const void* vc, c
   p.B = B; p.n = n; p.Hq = Hq; p.Hkv = Hkv; p.max_blocks = max_blocks; p.num_blocks = num_blocks;
   p.c = kLog2e / sqrtf(float(D));
   p.out_tiled = out_tiled;
-  kvq_plan(p, dt == MOLT_F32);
+  kvq_plan(p, D, dt == MOLT_F32);
   Carver c(ws, 0);
   carve_parts(c, p, D);
   if (dt == MOLT_F32) {
