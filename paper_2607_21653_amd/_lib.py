@@ -158,6 +158,11 @@ def _stream():
     return torch.cuda.current_stream().cuda_stream
 
 
+def _raw_stream(device):
+    """The current stream of a device (by index), without a torch.cuda.Stream object around it (2.6 us)."""
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
 def _workspace(nbytes, device, ws=None):
     if nbytes == 0:
         return None, 0
@@ -357,61 +362,77 @@ def kvq_cache(num_blocks, n_kv_heads, head_dim, device="cuda"):
 
 
 def _kvq_caches(k_cache, v_cache, block_tables, starts):
-    """Checks of a pair of caches and the tables; returns (B, num_blocks, n_kv_heads, head_dim, max_blocks)."""
-    _dev(k_cache, torch.uint8, name="k_cache")
-    if k_cache.dim() != 3 or k_cache.shape[2] * 2 % 17:
-        raise MoltError(f"k_cache has shape {tuple(k_cache.shape)}, expected [num_blocks, n_kv_heads, 17 * head_dim / 2]")
-    nb, Hkv, rec = k_cache.shape
-    _dev(v_cache, torch.uint8, (nb, Hkv, rec), "v_cache")
-    B = starts.shape[0]
-    _dev(starts, torch.int32, (B,), "context_lens")
-    _dev(block_tables, torch.int32, name="block_tables")
-    if block_tables.dim() != 2 or block_tables.shape[0] != B:
-        raise MoltError(f"block_tables has shape {tuple(block_tables.shape)}, expected ({B}, max_blocks)")
-    return B, nb, Hkv, rec * 2 // 17, block_tables.shape[1]
+    """Checks of a pair of caches and the tables; returns (device index, B, num_blocks, n_kv_heads, head_dim,
+    max_blocks)."""
+    dev = k_cache.get_device()
+    shape, table = k_cache.shape, block_tables.shape
+    if not (dev >= 0 and len(shape) == 3 and shape[2] * 2 % 17 == 0 and len(table) == 2 and starts.shape == table[:1]
+            and v_cache.shape == shape and k_cache.dtype is v_cache.dtype is torch.uint8
+            and block_tables.dtype is starts.dtype is torch.int32
+            and v_cache.get_device() == block_tables.get_device() == starts.get_device() == dev
+            and k_cache.is_contiguous() and v_cache.is_contiguous() and block_tables.is_contiguous()
+            and starts.is_contiguous()):
+        _dev(k_cache, torch.uint8, name="k_cache")
+        if len(shape) != 3 or shape[2] * 2 % 17:
+            raise MoltError(f"k_cache has shape {tuple(shape)}, expected [num_blocks, n_kv_heads, 17 * head_dim / 2]")
+        _dev(v_cache, torch.uint8, shape, "v_cache")
+        _dev(starts, torch.int32, (starts.numel(),), "context_lens")
+        _dev(block_tables, torch.int32, name="block_tables")
+        if len(table) != 2 or table[0] != starts.shape[0]:
+            raise MoltError(f"block_tables has shape {tuple(table)}, expected ({starts.shape[0]}, max_blocks)")
+        raise MoltError("k_cache, v_cache, block_tables and context_lens must be on one device")
+    if dev != torch.cuda.current_device():
+        raise MoltError(f"the caches are on device {dev}, the current device is {torch.cuda.current_device()}")
+    return dev, table[0], shape[0], shape[1], shape[2] * 2 // 17, table[1]
 
 
-def _rows_stride(t, dtype, shape, name):
-    """Row stride (elements) of rows [T, Hkv, D] whose heads are contiguous, e.g. a slice of fused QKV rows."""
-    if not t.is_cuda:
-        raise MoltError(f"{name} must be a GPU tensor")
-    if t.dtype != dtype:
+def _same_device(t, dev, name):
+    if t is not None and t.get_device() != dev:
+        raise MoltError(f"{name} must be a GPU tensor on device {dev}, the caches', is on {t.device}")
+
+
+def _rows_stride(t, dtype, T, H, D, name):
+    """Row stride (elements) of rows [T, H, D] whose heads are contiguous, e.g. a slice of fused QKV rows."""
+    if t.dtype is not dtype:
         raise MoltError(f"{name} has dtype {t.dtype}, expected {dtype}")
-    if tuple(t.shape) != shape:
-        raise MoltError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
-    T, H, D = shape
-    if t.stride(2) != 1 or (H > 1 and t.stride(1) != D) or (T > 1 and t.stride(0) < H * D):
+    if t.shape != (T, H, D):
+        raise MoltError(f"{name} has shape {tuple(t.shape)}, expected {(T, H, D)}")
+    row, head, dim = t.stride()
+    if dim != 1 or (H > 1 and head != D) or (T > 1 and row < H * D):
         raise MoltError(f"{name} must have contiguous heads in rows that do not overlap, strides are {t.stride()}")
-    return t.stride(0) if T > 1 else H * D
+    return row if T > 1 else H * D
 
 
 def kvq_write(k, v, k_cache, v_cache, block_tables, context_lens, n, lens=None):
     """Writes rows k, v [B*n, Hkv, D] (f32|bf16; row-strided views will do) into the 4-bit cache at
     positions context_lens[b] + j, j < n (j < lens[b] if given)."""
     lib = load()
-    B, nb, Hkv, D, maxb = _kvq_caches(k_cache, v_cache, block_tables, context_lens)
-    if k.dtype not in (torch.float32, torch.bfloat16):
-        raise MoltError(f"k has dtype {k.dtype}, expected float32 or bfloat16")
-    ks = _rows_stride(k, k.dtype, (B * n, Hkv, D), "k")
-    vs = _rows_stride(v, k.dtype, (B * n, Hkv, D), "v")
+    dev, B, nb, Hkv, D, maxb = _kvq_caches(k_cache, v_cache, block_tables, context_lens)
+    dt = k.dtype
+    if dt is not torch.bfloat16 and dt is not torch.float32:
+        raise MoltError(f"k has dtype {dt}, expected float32 or bfloat16")
+    ks, vs = _rows_stride(k, dt, B * n, Hkv, D, "k"), _rows_stride(v, dt, B * n, Hkv, D, "v")
     _dev(lens, torch.int32, (B,), "lens")
+    for t, name in ((k, "k"), (v, "v"), (lens, "lens")):
+        _same_device(t, dev, name)
     _check(lib.molt_kvq_write(_ptr(k), _ptr(v), ks, vs, _ptr(k_cache), _ptr(v_cache), _ptr(block_tables),
-                              _ptr(context_lens), _ptr(lens), B, n, Hkv, D, maxb, nb, DTYPE_CODE[k.dtype],
-                              _stream()), "molt_kvq_write")
+                              _ptr(context_lens), _ptr(lens), B, n, Hkv, D, maxb, nb, DTYPE_CODE[dt],
+                              _raw_stream(dev)), "molt_kvq_write")
 
 
 def kvq_read(k_cache, v_cache, block_tables, starts, n, lens=None, dtype=torch.bfloat16):
     """Positions starts[b] + j, j < n, of the 4-bit cache as (k, v) [B*n, Hkv, D] of dtype (bf16|f32); rows
     j >= lens[b], and rows without a place in the table, are zeros."""
     lib = load()
-    B, nb, Hkv, D, maxb = _kvq_caches(k_cache, v_cache, block_tables, starts)
-    if dtype not in (torch.float32, torch.bfloat16):
+    dev, B, nb, Hkv, D, maxb = _kvq_caches(k_cache, v_cache, block_tables, starts)
+    if dtype is not torch.bfloat16 and dtype is not torch.float32:
         raise MoltError(f"dtype is {dtype}, expected float32 or bfloat16")
     _dev(lens, torch.int32, (B,), "lens")
+    _same_device(lens, dev, "lens")
     k = torch.empty(B * n, Hkv, D, dtype=dtype, device=k_cache.device)
     v = torch.empty(B * n, Hkv, D, dtype=dtype, device=k_cache.device)
     _check(lib.molt_kvq_read(_ptr(k_cache), _ptr(v_cache), _ptr(block_tables), _ptr(starts), _ptr(lens), B, n,
-                             Hkv, D, maxb, nb, DTYPE_CODE[dtype], _ptr(k), _ptr(v), _stream()), "molt_kvq_read")
+                             Hkv, D, maxb, nb, DTYPE_CODE[dtype], _ptr(k), _ptr(v), _raw_stream(dev)), "molt_kvq_read")
     return k, v
 
 
@@ -422,18 +443,29 @@ def paged_attention_kvq_workspace_size(B, k, n_q_heads, n_kv_heads, head_dim, ma
 def paged_attention_kvq(q, k_cache, v_cache, block_tables, context_lens, k, workspace=None):
     """paged_attention over a 4-bit cache: q [B*(1+k), Hq, D] (f32|bf16); returns [T, Hq*D] of q's dtype."""
     lib = load()
-    B, nb, Hkv, D, maxb = _kvq_caches(k_cache, v_cache, block_tables, context_lens)
-    if q.dtype not in (torch.float32, torch.bfloat16):
-        raise MoltError(f"q has dtype {q.dtype}, expected float32 or bfloat16")
+    dev, B, nb, Hkv, D, maxb = _kvq_caches(k_cache, v_cache, block_tables, context_lens)
+    dt = q.dtype
+    if dt is not torch.bfloat16 and dt is not torch.float32:
+        raise MoltError(f"q has dtype {dt}, expected float32 or bfloat16")
     if q.dim() != 3:
         raise MoltError(f"q has shape {tuple(q.shape)}, expected [B*(1+k), Hq, D]")
     Hq = q.shape[1]
     _dev(q, None, (B * (k + 1), Hq, D), "q")
-    out = torch.empty(q.shape[0], Hq * D, dtype=q.dtype, device=q.device)
-    ws, nbytes = _workspace(lib.molt_paged_attention_kvq_workspace_size(B, k, Hq, Hkv, D, maxb), q.device, workspace)
-    _check(lib.molt_paged_attention_kvq(_ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(block_tables),
-                                        _ptr(context_lens), B, k, Hq, Hkv, D, maxb, nb, DTYPE_CODE[q.dtype],
-                                        _ptr(out), _ptr(ws), nbytes, _stream()), "molt_paged_attention_kvq")
+    _same_device(q, dev, "q")
+    _same_device(workspace, dev, "workspace")
+    out = torch.empty(q.shape[0], Hq * D, dtype=dt, device=q.device)
+
+    def call(ws, have):
+        return lib.molt_paged_attention_kvq(_ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(block_tables),
+                                            _ptr(context_lens), B, k, Hq, Hkv, D, maxb, nb, DTYPE_CODE[dt],
+                                            _ptr(out), _ptr(ws), have, _raw_stream(dev))
+
+    status = MOLT_ERR_WORKSPACE
+    if workspace is not None:
+        status = call(workspace, workspace.numel() * workspace.element_size())
+    if status == MOLT_ERR_WORKSPACE:     # none, or one that is too small
+        status = call(*_workspace(lib.molt_paged_attention_kvq_workspace_size(B, k, Hq, Hkv, D, maxb), q.device))
+    _check(status, "molt_paged_attention_kvq")
     return out
 
 
