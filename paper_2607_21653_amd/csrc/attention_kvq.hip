@@ -248,39 +248,28 @@ MOLT_DEV Share find_share(const KvqAttnParams& p, int r1, int slot, float* lds) 
   return w;
 }
 
-template <int D, typename T, int NT, bool ONCE>
-__global__ __launch_bounds__(kWaves * kWave, 2) void kvq_attn_kernel(KvqAttnParams p) {
+// bytes of LDS: the wavefronts' rings of kSlots pairs, later their results; the query operands (bf16)
+template <int D, typename T, int NT, int W>
+struct Lds {
+  static constexpr int kPair = 32 * D + 256;                  // bytes of a pair in the ring
+  static constexpr int kJoin = (16 * (D + 4) + 32) * 4;       // a wavefront's results of one tile
+  static constexpr int kWaveBytes = kSlots * kPair > kJoin ? kSlots * kPair : kJoin;
+  static constexpr int kQuery = sizeof(T) == 4 ? 0 : D / 64 * 2048;   // a tile's query operands
+  static constexpr int kBytes = W * kWaveBytes + NT * kQuery;
+};
+
+// Rows [r0, r0 + 16 NT) of kv head h over the keys of share w, by W wavefronts.
+template <int D, typename T, int NT, bool ONCE, int W>
+MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h, int slot, const Share& w) {
   typedef KvqRecord<D> Rec;
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int QP = 3;                  // bf16 parts of an f32 query element
   constexpr int PP = F32 ? 3 : 1;        // bf16 parts of a probability (see the top)
   constexpr int KS = D / 32;             // MFMA steps over the dims of a score
   constexpr int DT = D / 16;             // 16-dim tiles of O^T
-  constexpr int SLOT = 32 * D + 256;     // bytes of a pair in the ring
+  constexpr int SLOT = Lds<D, T, NT, W>::kPair, kLds = Lds<D, T, NT, W>::kWaveBytes, QF = Lds<D, T, NT, W>::kQuery;
   constexpr int kCopies = D == 128 ? 5 : 3;   // vector memory instructions of a pair
-  // the wavefronts' rings, then (kJoin floats each) their results; the query operands; the only LDS object
-  constexpr int kJoin = 16 * (D + 4) + 32;
-  constexpr int kLds = kSlots * SLOT > kJoin * 4 ? kSlots * SLOT : kJoin * 4;
-  constexpr int QF = D / 64 * 2048;      // bytes of a tile's query operands
-  __shared__ __attribute__((aligned(16))) uint8_t lds[kWaves * kLds + (F32 ? 0 : NT * QF)];
-
-  // Work item. Consecutive workgroups run on consecutive XCDs: the row groups of a slot and head, which read the same
-  // keys, are 8 apart, and with many slots (spread) a slot's heads too, whose records share lines (read requests of 128
-  // sequences x 4 heads at context 8192: 1.02 times the records' bytes, 1.07 with heads on neighbouring XCDs).
-  const int bi = int(blockIdx.x), rg = bi / 8 % p.nrg, hi = bi / (8 * p.nrg), lo = bi % 8;
-  const int h = p.spread ? hi % p.Hkv : (hi * 8 + lo) % p.Hkv;
-  const int slot = p.spread ? hi / p.Hkv * 8 + lo : (hi * 8 + lo) / p.Hkv;
-  if (slot >= p.slots) return;
-  const int r0 = rg * 16 * NT, r1 = min(r0 + 16 * NT, p.R);
-  Share w{slot, 0, 1, slot};
-  if (p.slots > p.B) {
-    w = find_share<NT>(p, r1, slot, reinterpret_cast<float*>(lds));
-    if (w.b < 0) return;
-    if (h == 0 && w.part == 0 && threadIdx.x == 0) {
-      p.split[2 * (long(rg) * p.B + w.b)] = w.first;
-      p.split[2 * (long(rg) * p.B + w.b) + 1] = w.parts;
-    }
-  }
+  const int r1 = min(r0 + 16 * NT, p.R);
   const int b = w.b;
   const int lane = threadIdx.x % kWave, l16 = lane % 16, g4 = lane / 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -304,10 +293,10 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void kvq_attn_kernel(KvqAttnPara
   for (int i = 0; i < NT; ++i) lim[i] = ctx + min(r0 + 16 * i + l16, p.R - 1) / p.G;
   // the share's pairs of blocks, then the wavefront's
   const int s0 = int(long(npairs) * w.part / w.parts), s1 = int(long(npairs) * (w.part + 1) / w.parts);
-  const int p0 = s0 + (s1 - s0) * wave / kWaves, p1 = s0 + (s1 - s0) * (wave + 1) / kWaves;
+  const int p0 = s0 + (s1 - s0) * wave / W, p1 = s0 + (s1 - s0) * (wave + 1) / W;
   const int full_end = min(visible_end(p, ctx, r0 + 1), end);    // keys before are seen by every row
   uint8_t* ring = lds + wave * kLds;
-  uint8_t* qlds = lds + kWaves * kLds;
+  uint8_t* qlds = lds + W * kLds;
 
   // Copies of a pair into a slot of the wavefront's ring: [K codes of both blocks][V codes][scales of K, of
   // V], K's 16-byte chunks in the order in which the lanes read them (dims 32 c .. of token t at chunk 16 c + t)
@@ -634,11 +623,11 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void kvq_attn_kernel(KvqAttnPara
     const float* part = reinterpret_cast<const float*>(lds);
     float M = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, part[w * (kLds / 4) + 16 * RS + row]);
+    for (int w = 0; w < W; ++w) M = fmaxf(M, part[w * (kLds / 4) + 16 * RS + row]);
     float L = 0.f;
     floatx4_t a[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < W; ++w) {
       const float* pw = part + w * (kLds / 4);
       const float mw = pw[16 * RS + row];
       const float f = mw == -INFINITY ? 0.f : exp2f((mw - M) * p.c);
@@ -661,6 +650,31 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void kvq_attn_kernel(KvqAttnPara
   }
 }
 
+template <int D, typename T, int NT, bool ONCE, int W>
+__global__ __launch_bounds__(W * kWave, 2) void kvq_attn_kernel(KvqAttnParams p) {
+  __shared__ __attribute__((aligned(16))) uint8_t lds[Lds<D, T, NT, W>::kBytes];   // the only LDS object
+  // Work item. Consecutive workgroups run on consecutive XCDs: the row groups of a slot and head, which read the same
+  // keys, are 8 apart, and with many slots (spread) a slot's heads too, whose records share lines (read requests of 128
+  // sequences x 4 heads at context 8192: 1.02 times the records' bytes, 1.07 with heads on neighbouring XCDs).
+  const int bi = int(blockIdx.x), rg = bi / 8 % p.nrg, hi = bi / (8 * p.nrg), lo = bi % 8;
+  const int h = p.spread ? hi % p.Hkv : (hi * 8 + lo) % p.Hkv;
+  const int slot = p.spread ? hi / p.Hkv * 8 + lo : (hi * 8 + lo) / p.Hkv;
+  if (slot >= p.slots) return;
+  const int r0 = rg * 16 * NT, r1 = min(r0 + 16 * NT, p.R);
+  Share w{slot, 0, 1, slot};
+  if (W == kWaves && p.slots > p.B) {
+    w = find_share<NT>(p, r1, slot, reinterpret_cast<float*>(lds));
+    if (w.b < 0) return;
+    if (h == 0 && w.part == 0 && threadIdx.x == 0) {
+      p.split[2 * (long(rg) * p.B + w.b)] = w.first;
+      p.split[2 * (long(rg) * p.B + w.b) + 1] = w.parts;
+    }
+  }
+  // the last of several row groups may have a tile less
+  if (NT == 3 && !ONCE && r1 - r0 <= 32) attend<D, T, 2, ONCE, W>(p, lds, rg, r0, h, slot, w);
+  else attend<D, T, NT, ONCE, W>(p, lds, rg, r0, h, slot, w);
+}
+
 // log-sum-exp join of a sequence's slots: thread = 4 dims of one row, kU slots' loads in flight together
 template <int D, typename T>
 __global__ __launch_bounds__(256) void kvq_merge_kernel(KvqAttnParams p) {
@@ -673,7 +687,7 @@ __global__ __launch_bounds__(256) void kvq_merge_kernel(KvqAttnParams p) {
   const int2 sp = *reinterpret_cast<const int2*>(p.split + 2 * (long(rg) * p.B + b));
   if (sp.y == 1) return;
   const long pr0 = ((long(rg) * p.Hkv + h) * p.slots + sp.x) * p.group + r % p.group;
-  constexpr int kU = 8;
+  constexpr int kU = 16;
   float M = -INFINITY, L = 0.f;
   floatx4_t a = {0.f, 0.f, 0.f, 0.f};
   for (int s0 = 0; s0 < sp.y; s0 += kU) {
@@ -694,10 +708,11 @@ __global__ __launch_bounds__(256) void kvq_merge_kernel(KvqAttnParams p) {
     a *= f0;
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
-      if (s0 + u >= sp.y) break;
-      const float f = ml[u].x == -INFINITY ? 0.f : exp2f((ml[u].x - M) * p.c);
-      L += ml[u].y * f;
-      a += o[u] * f;
+      const bool live = s0 + u < sp.y && ml[u].x != -INFINITY;
+      const float f = exp2f((ml[u].x - M) * p.c);
+      L += live ? ml[u].y * f : 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) a[e] += live ? o[u][e] * f : 0.f;
     }
   }
   store_out4<T>(p, b, h, r, D, d0, a, L);
@@ -709,6 +724,8 @@ constexpr int kMaxTiles = 3;             // 16-row tiles of a wavefront (bf16; o
 // as are resident (a cut for uneven lengths would cost 8% of even ones: the work of finding it, workgroups without a
 // part, the joining launch), or the tables are short (kMinCutBlocks), else room for as many parts as are resident.
 constexpr int kMinCutBlocks = 48;
+// Uncut calls of up to kFew workgroups, a compute unit for each, take kMoreWaves wavefronts in each.
+constexpr int kFew = 256, kMoreWaves = 8;
 void kvq_plan(KvqAttnParams& p, int D, bool f32) {
   p.G = p.Hq / p.Hkv;
   p.R = p.G * p.n;
@@ -727,8 +744,9 @@ template <int D, typename T, int NT>
 void launch_nt(const KvqAttnParams& p, hipStream_t s) {
   const long units = p.spread ? (long(p.slots) + 7) / 8 * 8 * p.Hkv : (long(p.slots) * p.Hkv + 7) / 8 * 8;
   const unsigned grid = unsigned(units * p.nrg);
-  if (p.nrg == 1) kvq_attn_kernel<D, T, NT, true><<<grid, kWaves * kWave, 0, s>>>(p);
-  else kvq_attn_kernel<D, T, NT, false><<<grid, kWaves * kWave, 0, s>>>(p);
+  if (p.nrg > 1) kvq_attn_kernel<D, T, NT, false, kWaves><<<grid, kWaves * kWave, 0, s>>>(p);
+  else if (p.slots > p.B || units > kFew) kvq_attn_kernel<D, T, NT, true, kWaves><<<grid, kWaves * kWave, 0, s>>>(p);
+  else kvq_attn_kernel<D, T, NT, true, kMoreWaves><<<grid, kMoreWaves * kWave, 0, s>>>(p);
 }
 
 template <int D, typename T>
