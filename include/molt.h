@@ -330,8 +330,17 @@ typedef struct molt_kv {
   const int32_t* context_lens; /* [B] tokens already cached                               */
   int max_blocks_per_seq;
   int num_blocks;
-  int block_size; /* must be 16 */
+  int block_size; /* 16; or 16 | MOLT_KV_MX, where the caches are 4-bit ones (molt_kvq_write's layout) */
 } molt_kv;
+
+/* Calls on a model take 4-bit caches too: every layer's keys (after RoPE) and values, rounded to the
+ * model's dtype as for the other caches, are quantised as molt_kvq_write does and attended over as by
+ * molt_paged_attention_kvq. They need molt_kvq_workspace_extra(m, B, k, max_blocks_per_seq) bytes of
+ * workspace besides the call's own *_workspace_size (k + 1: positions per sequence, of prefill n);
+ * molt_mtp_draft, whose head runs windows and single rows, that of k = window - 1 and that of k = 0,
+ * both of its layer's model. The extra is 0 for bad arguments. */
+#define MOLT_KV_MX 0x100
+size_t molt_kvq_workspace_extra(const molt_model* m, int B, int k, int max_blocks_per_seq);
 
 /* ------------------------------------------------------------------------------
  * molt_decoder_forward -- all n_layers decoder layers of the verify step on a

@@ -15,6 +15,7 @@ LIB_PATH = os.path.join(HERE, "libmolt.so")
 
 MOLT_F32, MOLT_BF16, MOLT_FP8_E4M3 = 0, 1, 2
 MOLT_ERR_WORKSPACE = -3
+MOLT_KV_MX = 0x100                # MOLT_KV_MX of include/molt.h
 NOALLOC_SCRATCH_BYTES = 8 << 20   # MOLT_NOALLOC_SCRATCH_BYTES of include/molt.h
 DTYPE_CODE = {torch.float32: MOLT_F32, torch.bfloat16: MOLT_BF16, torch.uint8: MOLT_FP8_E4M3}
 NAME_CODE = {"f32": MOLT_F32, "bf16": MOLT_BF16, "fp8": MOLT_FP8_E4M3}
@@ -70,6 +71,7 @@ _SIGS = {
     "molt_paged_attention_kvq_workspace_size": (c_size, [c_int] * 6),
     "molt_paged_attention_kvq": (c_int, [c_vp, c_vp, c_vp, c_vp, c_vp, c_int, c_int, c_int, c_int,
                                          c_int, c_int, c_int, c_int, c_vp, c_vp, c_size, c_vp]),
+    "molt_kvq_workspace_extra": (c_size, [ctypes.POINTER(MoltModel), c_int, c_int, c_int]),
     "molt_decoder_workspace_size": (c_size, [ctypes.POINTER(MoltModel), c_int, c_int, c_int]),
     "molt_decoder_forward": (c_int, [ctypes.POINTER(MoltModel), ctypes.POINTER(MoltKV), c_int,
                                      c_int, c_vp, c_vp, c_vp, c_size, c_vp]),
@@ -520,7 +522,8 @@ class Model:
 
 
 class KVCache:
-    """Per-layer paged caches plus the block tables and context lengths (all on the GPU)."""
+    """Per-layer paged caches plus the block tables and context lengths (all on the GPU). Caches of
+    kvq_cache (uint8) are 4-bit ones: the calls on a model quantise into them and attend over them."""
 
     def __init__(self, k_caches, v_caches, block_tables, context_lens):
         self.k_caches, self.v_caches = k_caches, v_caches
@@ -534,8 +537,27 @@ class KVCache:
         s.context_lens = context_lens.data_ptr()
         s.max_blocks_per_seq = block_tables.shape[1]
         s.num_blocks = k_caches[0].shape[0]
-        s.block_size = 16
+        self.mx = k_caches[0].dtype is torch.uint8
+        if any((t.dtype is torch.uint8) != self.mx for t in [*k_caches, *v_caches]):
+            raise MoltError("the caches of all layers must be 4-bit ones, or none")
+        s.block_size = 16 | MOLT_KV_MX if self.mx else 16
         self.struct = s
+
+    def check(self, model):
+        """4-bit caches have the model's heads."""
+        m = model.struct
+        want = (self.struct.num_blocks, m.n_kv_heads, 17 * m.head_dim // 2)
+        if self.mx and any(tuple(t.shape) != want for t in [*self.k_caches, *self.v_caches]):
+            raise MoltError(f"a 4-bit cache has shape {[tuple(t.shape) for t in [*self.k_caches, *self.v_caches]]}, "
+                            f"expected {want}")
+
+    def extra(self, model, B, *ks):
+        """Workspace bytes that 4-bit caches add to a call of B sequences of 1 + k positions, for each k of ks."""
+        if not self.mx:
+            return 0
+        self.check(model)
+        return sum(load().molt_kvq_workspace_extra(ctypes.byref(model.struct), B, k, self.struct.max_blocks_per_seq)
+                   for k in ks)
 
 
 def decoder_workspace_size(model, B, k, max_blocks):
@@ -555,8 +577,8 @@ def decoder_forward(model, kv, B, k, x, want_routes=False, workspace=None):
         return lib.molt_decoder_forward(ctypes.byref(model.struct), ctypes.byref(kv.struct), B, k, _ptr(x),
                                         _ptr(routes), ws, nb, _stream())
 
-    _call("molt_decoder_forward", call, decoder_workspace_size(model, B, k, kv.struct.max_blocks_per_seq),
-          x.device, workspace)
+    _call("molt_decoder_forward", call, decoder_workspace_size(model, B, k, kv.struct.max_blocks_per_seq)
+          + kv.extra(model, B, k), x.device, workspace)
     return routes
 
 
@@ -594,8 +616,8 @@ def verify_step(model, kv, tokens, uniforms, draft_probs=None, want_logits=True,
                                     _ptr(out["tokens"]), _ptr(out["n_accepted"]), _ptr(out["logprobs"]),
                                     _ptr(out.get("routes")), _ptr(out.get("hidden")), ws, nb, _stream())
 
-    _call("molt_verify_step", call, verify_step_workspace_size(model, B, k, kv.struct.max_blocks_per_seq),
-          dev, workspace)
+    _call("molt_verify_step", call, verify_step_workspace_size(model, B, k, kv.struct.max_blocks_per_seq)
+          + kv.extra(model, B, k), dev, workspace)
     return out
 
 
@@ -623,8 +645,8 @@ def prefill(model, kv, tokens, lens, want_hidden=False, want_routes=False, works
                                 _ptr(out["logits"]), _ptr(out.get("hidden")), _ptr(out.get("routes")),
                                 ws, nb, _stream())
 
-    _call("molt_prefill", call, prefill_workspace_size(model, B, n, kv.struct.max_blocks_per_seq),
-          dev, workspace)
+    _call("molt_prefill", call, prefill_workspace_size(model, B, n, kv.struct.max_blocks_per_seq)
+          + kv.extra(model, B, n - 1), dev, workspace)
     return out
 
 
@@ -707,8 +729,8 @@ def score_tokens(model, kv, tokens, targets, replay_routes=None, want_logits=Fal
                                      _ptr(targets), _ptr(replay_routes), _ptr(out["logprobs"]),
                                      _ptr(out.get("logits")), _ptr(out.get("routes")), ws, nb, _stream())
 
-    _call("molt_score_tokens", call, score_tokens_workspace_size(model, B, k, kv.struct.max_blocks_per_seq),
-          dev, workspace)
+    _call("molt_score_tokens", call, score_tokens_workspace_size(model, B, k, kv.struct.max_blocks_per_seq)
+          + kv.extra(model, B, k), dev, workspace)
     return out
 
 
@@ -764,8 +786,8 @@ def mtp_draft(target, mtp, kv, hidden, tokens, n_accepted, next_tokens, uniforms
                                          _ptr(None if greedy else uniforms), _ptr(out["drafts"]),
                                          _ptr(out["draft_probs"]), ws, nb, _stream())
 
-    _call("molt_mtp_draft", call, mtp_draft_workspace_size(target, mtp, B, k, kv.struct.max_blocks_per_seq, W),
-          dev, workspace)
+    _call("molt_mtp_draft", call, mtp_draft_workspace_size(target, mtp, B, k, kv.struct.max_blocks_per_seq, W)
+          + kv.extra(mtp.layer, B, W - 1, 0), dev, workspace)
     return out
 
 

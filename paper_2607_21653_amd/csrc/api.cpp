@@ -614,10 +614,14 @@ int model_ok(const molt_model* m, const molt_kv* kv, int B, int k, bool need_hea
     REQUIRE(m->embed && m->lm_head && m->final_norm, "embed, final_norm and lm_head are required");
   }
   REQUIRE(kv != nullptr, "kv is NULL");
-  REQUIRE(kv->block_size == 16, "block_size = %d must be 16", kv->block_size);
+  REQUIRE((kv->block_size & ~MOLT_KV_MX) == 16, "block_size = %d must be 16 (or 16 | MOLT_KV_MX)", kv->block_size);
   REQUIRE(kv->k_cache && kv->v_cache && kv->block_tables && kv->context_lens, "a kv pointer is NULL");
   for (int l = 0; l < m->n_layers; ++l)
     REQUIRE(kv->k_cache[l] && kv->v_cache[l], "layer %d: cache pointer is NULL", l);
+  if (kv->block_size & MOLT_KV_MX)
+    for (int l = 0; l < m->n_layers; ++l)
+      REQUIRE((reinterpret_cast<uintptr_t>(kv->k_cache[l]) | reinterpret_cast<uintptr_t>(kv->v_cache[l])) % 16 == 0,
+              "layer %d: 4-bit caches must start at a multiple of 16 bytes", l);
   REQUIRE(kv->num_blocks >= 1, "num_blocks = %d must be >= 1", kv->num_blocks);
   return attn_shape_ok(B, k, m->n_q_heads, m->n_kv_heads, m->head_dim, kv->max_blocks_per_seq,
                        m->dtype);
@@ -631,9 +635,11 @@ struct DecWs {
   void* rope;                     // RoPE cos/sin of the step's positions, [T, D/2] f64 pairs
   int32_t* kv_slot;               // KV-cache slot of each token of the step (or -1)
   bool fine;                      // attn_ws holds the finer attention splits
+  void* kvq_ws;                   // workspace of the attention over 4-bit caches
 };
 
-DecWs carve_dec(molt::Carver& c, const molt_model* m, int B, int k, int max_blocks, bool fine) {
+// with `mx` also what 4-bit caches need besides
+DecWs carve_dec(molt::Carver& c, const molt_model* m, int B, int k, int max_blocks, bool fine, bool mx) {
   DecWs w{};
   w.fine = fine;
   const long T = long(B) * (k + 1);
@@ -659,8 +665,14 @@ DecWs carve_dec(molt::Carver& c, const molt_model* m, int B, int k, int max_bloc
   w.part = c.take<float>(w.part_elems);
   w.rope = c.take<double>(T * D);
   w.kv_slot = c.take<int32_t>(T);
+  if (mx) {
+    if (!w.qkv && m->dtype == MOLT_BF16 && D == 128) w.qkv = c.take<float>(T * (Hq + 2 * Hkv) * D);
+    w.kvq_ws = c.take<uint8_t>(molt::kvq_attention_ws_bytes(B, k + 1, Hq, Hkv, D, max_blocks));
+  }
   return w;
 }
+
+bool is_mx(const molt_kv* kv) { return (kv->block_size & MOLT_KV_MX) != 0; }
 
 // All layers on the residual stream x. With final_g, the last layer's MoE combine is fused
 // with the final RMSNorm, whose tiled output goes to final_y. With replay ([L, T, K] expert
@@ -678,8 +690,18 @@ hipError_t run_decoder(const DecWs& w, const molt_model* m, const molt_kv* kv, i
                              kv->max_blocks_per_seq, kv->num_blocks, w.kv_slot};
   RUN(molt::launch_residual_norm(x, nullptr, 0, nullptr, nullptr, 0, m->attn_norm[0], T, d,
                                  m->rms_eps, m->dtype, w.y, s, nullptr, nullptr, nullptr, &rope));
+  const bool mx = is_mx(kv);
   for (int l = 0; l < L; ++l) {
-    if (m->dtype == MOLT_BF16 && D == 128) {
+    if (mx) {
+      {
+        ProfScope ps(MOLT_PROF_PROJECTIONS, s);
+        RUN(molt::launch_gemm(w.y, m->w_qkv[l], w.qkv, T, (Hq + 2 * Hkv) * D, d, m->dtype, false,
+                              w.part, w.part_elems, s));
+      }
+      RUN(molt::launch_rope_kvq_write(w.qkv, B, k, Hq, Hkv, D, w.rope, kv->context_lens,
+                                      kv->block_tables, kv->max_blocks_per_seq, kv->num_blocks,
+                                      m->dtype, w.q, kv->k_cache[l], kv->v_cache[l], s));
+    } else if (m->dtype == MOLT_BF16 && D == 128) {
       // one 128-column tile per head: RoPE and the KV-cache write in the GEMM epilogue
       ProfScope ps(MOLT_PROF_PROJECTIONS, s);
       RUN(molt::launch_qkv_rope(w.y, m->w_qkv[l], T, d, Hq, Hkv, w.rope, w.kv_slot, w.q,
@@ -696,9 +718,14 @@ hipError_t run_decoder(const DecWs& w, const molt_model* m, const molt_kv* kv, i
     }
     {
       ProfScope ps(MOLT_PROF_ATTENTION, s);
-      RUN(molt::launch_paged_attention(w.q, kv->k_cache[l], kv->v_cache[l], kv->block_tables,
-                                       kv->context_lens, B, k, Hq, Hkv, D, kv->max_blocks_per_seq,
-                                       m->dtype, w.attn, true, w.attn_ws, w.fine, s));
+      if (mx)
+        RUN(molt::launch_kvq_attention(w.q, kv->k_cache[l], kv->v_cache[l], kv->block_tables,
+                                       kv->context_lens, B, k + 1, Hq, Hkv, D, kv->max_blocks_per_seq,
+                                       kv->num_blocks, m->dtype, w.attn, true, w.kvq_ws, s));
+      else
+        RUN(molt::launch_paged_attention(w.q, kv->k_cache[l], kv->v_cache[l], kv->block_tables,
+                                         kv->context_lens, B, k, Hq, Hkv, D, kv->max_blocks_per_seq,
+                                         m->dtype, w.attn, true, w.attn_ws, w.fine, s));
     }
     int np = 1;   // O projection: accumulate into x, or leave split-K partials
     {
@@ -732,7 +759,16 @@ hipError_t run_decoder(const DecWs& w, const molt_model* m, const molt_kv* kv, i
 
 size_t molt_decoder_workspace_size(const molt_model* m, int B, int k, int max_blocks) {
   if (!m || B < 1 || k < 0 || max_blocks < 1 || !pair_ok(m->dtype, m->expert_dtype)) return 0;
-  return carved_bytes(carve_dec, m, B, k, max_blocks, true);
+  return carved_bytes(carve_dec, m, B, k, max_blocks, true, false);
+}
+
+size_t molt_kvq_workspace_extra(const molt_model* m, int B, int k, int max_blocks) {
+  if (!m || B < 1 || k < 0 || max_blocks < 1 || m->n_kv_heads < 1 || m->n_q_heads < m->n_kv_heads ||
+      m->n_q_heads % m->n_kv_heads != 0 || !pair_ok(m->dtype, m->expert_dtype))
+    return 0;
+  // 256 bytes for each of the two aligned pieces
+  return carved_bytes(carve_dec, m, B, k, max_blocks, true, true) -
+         carved_bytes(carve_dec, m, B, k, max_blocks, true, false) + 512;
 }
 
 int molt_decoder_forward(const molt_model* m, const molt_kv* kv, int B, int k, float* x,
@@ -740,11 +776,11 @@ int molt_decoder_forward(const molt_model* m, const molt_kv* kv, int B, int k, f
                          molt_stream_t stream) {
   if (int r = model_ok(m, kv, B, k, false)) return r;
   REQUIRE(x, "x is NULL");
-  auto need = [&](bool f) { return carved_bytes(carve_dec, m, B, k, kv->max_blocks_per_seq, f); };
+  auto need = [&](bool f) { return carved_bytes(carve_dec, m, B, k, kv->max_blocks_per_seq, f, is_mx(kv)); };
   bool fine = false;
   if (int r = check_attn_ws(workspace, workspace_bytes, need, fine)) return r;
   molt::Carver c(workspace, workspace_bytes);
-  DecWs w = carve_dec(c, m, B, k, kv->max_blocks_per_seq, fine);
+  DecWs w = carve_dec(c, m, B, k, kv->max_blocks_per_seq, fine, is_mx(kv));
   return hip_status(run_decoder(w, m, kv, B, k, x, out_routes, nullptr, nullptr,
                                 reinterpret_cast<hipStream_t>(stream)),
                     "molt_decoder_forward");
@@ -752,14 +788,14 @@ int molt_decoder_forward(const molt_model* m, const molt_kv* kv, int B, int k, f
 
 namespace {
 struct StepWs { float* x; void* yf; float* logits; void* samp; DecWs dec; };
-StepWs carve_step(molt::Carver& c, const molt_model* m, int B, int k, int max_blocks, bool fine) {
+StepWs carve_step(molt::Carver& c, const molt_model* m, int B, int k, int max_blocks, bool fine, bool mx) {
   StepWs w{};
   const long T = long(B) * (k + 1);
   w.x = c.take<float>(T * m->d_model);
   w.yf = c.take<uint8_t>(pad32(T) * m->d_model * dt_size(m->dtype));
   w.logits = c.take<float>(T * long(m->vocab));
   w.samp = c.take<uint8_t>(molt::sampler_ws_bytes(B, k, m->vocab));
-  w.dec = carve_dec(c, m, B, k, max_blocks, fine);
+  w.dec = carve_dec(c, m, B, k, max_blocks, fine, mx);
   return w;
 }
 }  // namespace
@@ -767,7 +803,7 @@ StepWs carve_step(molt::Carver& c, const molt_model* m, int B, int k, int max_bl
 size_t molt_verify_step_workspace_size(const molt_model* m, int B, int k, int max_blocks) {
   if (!m || B < 1 || k < 0 || max_blocks < 1 || m->vocab < 1 || !pair_ok(m->dtype, m->expert_dtype))
     return 0;
-  return carved_bytes(carve_step, m, B, k, max_blocks, true);
+  return carved_bytes(carve_step, m, B, k, max_blocks, true, false);
 }
 
 int molt_verify_step(const molt_model* m, const molt_kv* kv, int B, int k, const int32_t* tokens,
@@ -778,12 +814,12 @@ int molt_verify_step(const molt_model* m, const molt_kv* kv, int B, int k, const
   if (int r = model_ok(m, kv, B, k, true)) return r;
   if (int r = spec_accept_shape_ok(B, k, m->vocab)) return r;
   REQUIRE(tokens && uniforms && out_tokens && out_num_accepted, "a required pointer is NULL");
-  auto need = [&](bool f) { return carved_bytes(carve_step, m, B, k, kv->max_blocks_per_seq, f); };
+  auto need = [&](bool f) { return carved_bytes(carve_step, m, B, k, kv->max_blocks_per_seq, f, is_mx(kv)); };
   bool fine = false;
   if (int r = check_attn_ws(workspace, workspace_bytes, need, fine)) return r;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   molt::Carver c(workspace, workspace_bytes);
-  StepWs w = carve_step(c, m, B, k, kv->max_blocks_per_seq, fine);
+  StepWs w = carve_step(c, m, B, k, kv->max_blocks_per_seq, fine, is_mx(kv));
   float* logits = out_logits ? out_logits : w.logits;
   float* x = out_hidden ? out_hidden : w.x;   // the residual stream
   const int T = B * (k + 1);
@@ -807,7 +843,7 @@ int molt_verify_step(const molt_model* m, const molt_kv* kv, int B, int k, const
 
 namespace {
 struct PrefillWs { float* x; void* yf; float* hsel; void* ysel; DecWs dec; };
-PrefillWs carve_prefill(molt::Carver& c, const molt_model* m, int B, int n, int max_blocks, bool fine) {
+PrefillWs carve_prefill(molt::Carver& c, const molt_model* m, int B, int n, int max_blocks, bool fine, bool mx) {
   PrefillWs w{};
   const long T = long(B) * n;
   const size_t es = dt_size(m->dtype);
@@ -815,7 +851,7 @@ PrefillWs carve_prefill(molt::Carver& c, const molt_model* m, int B, int n, int 
   w.yf = c.take<uint8_t>(pad32(T) * m->d_model * es);
   w.hsel = c.take<float>(long(B) * m->d_model);
   w.ysel = c.take<uint8_t>(pad32(B) * m->d_model * es);
-  w.dec = carve_dec(c, m, B, n - 1, max_blocks, fine);
+  w.dec = carve_dec(c, m, B, n - 1, max_blocks, fine, mx);
   return w;
 }
 }  // namespace
@@ -823,7 +859,7 @@ PrefillWs carve_prefill(molt::Carver& c, const molt_model* m, int B, int n, int 
 size_t molt_prefill_workspace_size(const molt_model* m, int B, int n, int max_blocks) {
   if (!m || B < 1 || n < 1 || max_blocks < 1 || m->vocab < 1 || !pair_ok(m->dtype, m->expert_dtype))
     return 0;
-  return carved_bytes(carve_prefill, m, B, n, max_blocks, true);
+  return carved_bytes(carve_prefill, m, B, n, max_blocks, true, false);
 }
 
 int molt_prefill(const molt_model* m, const molt_kv* kv, int B, int n, const int32_t* tokens,
@@ -832,12 +868,12 @@ int molt_prefill(const molt_model* m, const molt_kv* kv, int B, int n, const int
   REQUIRE(n >= 1, "n = %d must be >= 1", n);
   if (int r = model_ok(m, kv, B, n - 1, true)) return r;
   REQUIRE(tokens && lens && out_logits, "a required pointer is NULL");
-  auto need = [&](bool f) { return carved_bytes(carve_prefill, m, B, n, kv->max_blocks_per_seq, f); };
+  auto need = [&](bool f) { return carved_bytes(carve_prefill, m, B, n, kv->max_blocks_per_seq, f, is_mx(kv)); };
   bool fine = false;
   if (int r = check_attn_ws(workspace, workspace_bytes, need, fine)) return r;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   molt::Carver c(workspace, workspace_bytes);
-  PrefillWs w = carve_prefill(c, m, B, n, kv->max_blocks_per_seq, fine);
+  PrefillWs w = carve_prefill(c, m, B, n, kv->max_blocks_per_seq, fine, is_mx(kv));
   float* x = out_hidden ? out_hidden : w.x;
   const int T = B * n;
   hipError_t e = molt::launch_embed(m->embed, tokens, T, m->d_model, m->vocab, m->dtype, x, s);
@@ -856,14 +892,14 @@ int molt_prefill(const molt_model* m, const molt_kv* kv, int B, int n, const int
 
 namespace {
 struct ScoreWs { float* x; void* yf; float* logits; void* lp; DecWs dec; };
-ScoreWs carve_score(molt::Carver& c, const molt_model* m, int B, int k, int max_blocks, bool fine) {
+ScoreWs carve_score(molt::Carver& c, const molt_model* m, int B, int k, int max_blocks, bool fine, bool mx) {
   ScoreWs w{};
   const long T = long(B) * (k + 1);
   w.x = c.take<float>(T * m->d_model);
   w.yf = c.take<uint8_t>(pad32(T) * m->d_model * dt_size(m->dtype));
   w.logits = c.take<float>(T * long(m->vocab));
   w.lp = c.take<uint8_t>(molt::token_logprob_ws_bytes(T, m->vocab));
-  w.dec = carve_dec(c, m, B, k, max_blocks, fine);
+  w.dec = carve_dec(c, m, B, k, max_blocks, fine, mx);
   return w;
 }
 }  // namespace
@@ -871,7 +907,7 @@ ScoreWs carve_score(molt::Carver& c, const molt_model* m, int B, int k, int max_
 size_t molt_score_tokens_workspace_size(const molt_model* m, int B, int k, int max_blocks) {
   if (!m || B < 1 || k < 0 || max_blocks < 1 || m->vocab < 1 || !pair_ok(m->dtype, m->expert_dtype))
     return 0;
-  return carved_bytes(carve_score, m, B, k, max_blocks, true);
+  return carved_bytes(carve_score, m, B, k, max_blocks, true, false);
 }
 
 int molt_score_tokens(const molt_model* m, const molt_kv* kv, int B, int k, const int32_t* tokens,
@@ -881,12 +917,12 @@ int molt_score_tokens(const molt_model* m, const molt_kv* kv, int B, int k, cons
   if (int r = model_ok(m, kv, B, k, true)) return r;
   if (int r = spec_accept_shape_ok(B, k, m->vocab)) return r;
   REQUIRE(tokens && targets && out_logprobs, "a required pointer is NULL");
-  auto need = [&](bool f) { return carved_bytes(carve_score, m, B, k, kv->max_blocks_per_seq, f); };
+  auto need = [&](bool f) { return carved_bytes(carve_score, m, B, k, kv->max_blocks_per_seq, f, is_mx(kv)); };
   bool fine = false;
   if (int r = check_attn_ws(workspace, workspace_bytes, need, fine)) return r;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   molt::Carver c(workspace, workspace_bytes);
-  ScoreWs w = carve_score(c, m, B, k, kv->max_blocks_per_seq, fine);
+  ScoreWs w = carve_score(c, m, B, k, kv->max_blocks_per_seq, fine, is_mx(kv));
   float* logits = out_logits ? out_logits : w.logits;
   const int T = B * (k + 1);
   hipError_t e = molt::launch_embed(m->embed, tokens, T, m->d_model, m->vocab, m->dtype, w.x, s);
@@ -916,7 +952,7 @@ struct MtpWs {
 };
 
 MtpWs carve_mtp(molt::Carver& c, const molt_model* t, const molt_model* L, int B, int W,
-                int max_blocks, bool fine) {
+                int max_blocks, bool fine, bool mx) {
   MtpWs w{};
   const long T = long(B) * W;
   const int d = t->d_model;
@@ -934,8 +970,8 @@ MtpWs carve_mtp(molt::Carver& c, const molt_model* t, const molt_model* L, int B
   w.ysel = c.take<uint8_t>(pad32(B) * d * es);
   w.logits = c.take<float>(long(B) * t->vocab);
   w.draw = c.take<uint8_t>(molt::draft_draw_ws_bytes(B, t->vocab));
-  w.cat = carve_dec(c, L, B, W - 1, max_blocks, fine);
-  w.one = carve_dec(c, L, B, 0, max_blocks, fine);
+  w.cat = carve_dec(c, L, B, W - 1, max_blocks, fine, mx);
+  w.one = carve_dec(c, L, B, 0, max_blocks, fine, mx);
   return w;
 }
 
@@ -965,7 +1001,7 @@ size_t molt_mtp_draft_window_workspace_size(const molt_model* target, const molt
   if (!target || !mtp || !mtp->layer || B < 1 || window < 1 || k < 1 || max_blocks < 1 ||
       target->vocab < 1 || !pair_ok(mtp->layer->dtype, mtp->layer->expert_dtype))
     return 0;
-  return carved_bytes(carve_mtp, target, mtp->layer, B, window, max_blocks, true);
+  return carved_bytes(carve_mtp, target, mtp->layer, B, window, max_blocks, true, false);
 }
 
 size_t molt_mtp_draft_workspace_size(const molt_model* target, const molt_mtp* mtp, int B, int k,
@@ -983,13 +1019,13 @@ int molt_mtp_draft_window(const molt_model* target, const molt_mtp* mtp, const m
   REQUIRE(hidden && tokens && n_accepted && next_tokens && out_drafts, "a required pointer is NULL");
   REQUIRE(out_draft_probs == nullptr || uniforms, "sampled drafts (out_draft_probs) need uniforms");
   auto need = [&](bool f) {
-    return carved_bytes(carve_mtp, target, mtp->layer, B, W, mtp_kv->max_blocks_per_seq, f);
+    return carved_bytes(carve_mtp, target, mtp->layer, B, W, mtp_kv->max_blocks_per_seq, f, is_mx(mtp_kv));
   };
   bool fine = false;
   if (int r = check_attn_ws(workspace, workspace_bytes, need, fine)) return r;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   molt::Carver c(workspace, workspace_bytes);
-  MtpWs w = carve_mtp(c, target, mtp->layer, B, W, mtp_kv->max_blocks_per_seq, fine);
+  MtpWs w = carve_mtp(c, target, mtp->layer, B, W, mtp_kv->max_blocks_per_seq, fine, is_mx(mtp_kv));
   const molt_model* L = mtp->layer;
   const int d = target->d_model, V = target->vocab, T = B * W;
   const molt_dtype dt = target->dtype;

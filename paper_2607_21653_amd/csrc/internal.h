@@ -170,6 +170,10 @@ struct KvqRows {
 // k, v: rows of Hkv heads x D elements, k_stride and v_stride elements apart
 hipError_t launch_kvq_write(const KvqRows& p, const void* k, long k_stride, const void* v, long v_stride, int D,
                             molt_dtype dt, hipStream_t s);
+// launch_rope_kv_write into 4-bit caches: q as there; the keys and values that it would store, quantised
+hipError_t launch_rope_kvq_write(const float* qkv, int B, int k, int Hq, int Hkv, int D, const void* table,
+                                 const int32_t* ctx, const int32_t* bt, int max_blocks, int num_blocks,
+                                 molt_dtype dt, void* q_out, void* k_cache, void* v_cache, hipStream_t s);
 // k, v [B n, Hkv, D]; zeros where a row has no place in the cache
 hipError_t launch_kvq_read(const KvqRows& p, void* k, void* v, int D, molt_dtype dt, hipStream_t s);
 size_t kvq_attention_ws_bytes(int B, int n, int Hq, int Hkv, int D, int max_blocks);

@@ -206,6 +206,57 @@ __global__ __launch_bounds__(kThreads) void kvq_read_kernel(KvqRows p, int nblk,
   }
 }
 
+// The decoder's rows: workgroup = token t of the QKV projection's f32 rows, rotated in f64 with the step's table as for
+// the other caches. q -> q_out; thread = octet of a key (both halves of its pairs read, its own rotated) or value
+// head, rounded to the model's type, then quantised: the bytes that kvq_write makes of those rows.
+MOLT_DEV void store_q(uint16_t* p, float x) { *p = f32_to_bf16(x); }
+MOLT_DEV void store_q(float* p, float x) { *p = x; }
+template <int D, typename T>
+__global__ __launch_bounds__(kThreads) void rope_kvq_kernel(const float* __restrict__ qkv, int k, int Hq, int Hkv,
+                                                            const double2* __restrict__ table,
+                                                            const int32_t* __restrict__ ctx,
+                                                            const int32_t* __restrict__ bt, int max_blocks,
+                                                            int num_blocks, T* __restrict__ q_out,
+                                                            uint8_t* __restrict__ kc, uint8_t* __restrict__ vc) {
+  typedef KvqRecord<D> Rec;
+  constexpr int half = D / 2, O = D / 8;
+  const int t = blockIdx.x, b = t / (k + 1);
+  const double2* cs = table + long(t) * half;
+  const float* row = qkv + long(t) * (Hq + 2 * Hkv) * D;
+  for (int w = threadIdx.x; w < Hq * half; w += kThreads) {
+    const int h = w / half, i = w % half;
+    const double a = row[h * D + i], c = row[h * D + i + half];
+    const double2 r = cs[i];
+    store_q(q_out + (long(t) * Hq + h) * D + i, float(a * r.x - c * r.y));
+    store_q(q_out + (long(t) * Hq + h) * D + i + half, float(c * r.x + a * r.y));
+  }
+  const long pos = long(ctx[b]) + t % (k + 1);
+  if (pos < 0 || pos >= 16l * max_blocks) return;
+  const int blk = bt[long(b) * max_blocks + pos / 16], slot = int(pos % 16);
+  if (blk < 0 || blk >= num_blocks) return;
+  for (int w = threadIdx.x; w < 2 * Hkv * O; w += kThreads) {
+    const bool value = w >= Hkv * O;
+    const int h = w / O % Hkv, oct = w % O;
+    const float* src = row + long(Hq + (value ? Hkv : 0) + h) * D;
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int d = oct * 8 + e;
+      float v = src[d];
+      if (!value) {
+        const double other = src[d < half ? d + half : d - half];
+        const double2 r = cs[d % half];
+        v = float(d < half ? v * r.x - other * r.y : v * r.x + other * r.y);
+      }
+      x[e] = sizeof(T) == 2 ? round_to_bf16(v) : v;
+    }
+    const uint32_t s = kvq_scale(group_max(magnitude(x)));
+    uint8_t* rec = (value ? vc : kc) + (long(blk) * Hkv + h) * Rec::kBytes;
+    *reinterpret_cast<uint32_t*>(rec + (value ? Rec::v_code(slot, oct) : Rec::k_code(slot, oct))) = kvq_encode8(x, s);
+    if (oct % 4 == 0) rec[value ? Rec::v_scale(slot, oct / 4) : Rec::k_scale(slot, oct / 4)] = uint8_t(s);
+  }
+}
+
 // blocks that n consecutive positions may touch, and workgroups of a call
 int blocks_of(int n) { return int((long(n) + 30) / 16); }
 unsigned grid_of(const KvqRows& p, int D) {
@@ -238,6 +289,24 @@ hipError_t launch_kvq_read(const KvqRows& p, void* k, void* v, int D, molt_dtype
   } else {
     auto *a = static_cast<uint16_t*>(k), *b = static_cast<uint16_t*>(v);
     if (D == 128) go(kvq_read_kernel<128, uint16_t>, a, b); else go(kvq_read_kernel<64, uint16_t>, a, b);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_rope_kvq_write(const float* qkv, int B, int k, int Hq, int Hkv, int D, const void* table,
+                                 const int32_t* ctx, const int32_t* bt, int max_blocks, int num_blocks,
+                                 molt_dtype dt, void* q_out, void* k_cache, void* v_cache, hipStream_t s) {
+  auto go = [&](auto kernel, auto* q) {
+    kernel<<<B * (k + 1), kThreads, 0, s>>>(qkv, k, Hq, Hkv, static_cast<const double2*>(table), ctx, bt, max_blocks,
+                                            num_blocks, q, static_cast<uint8_t*>(k_cache),
+                                            static_cast<uint8_t*>(v_cache));
+  };
+  if (dt == MOLT_F32) {
+    auto* q = static_cast<float*>(q_out);
+    if (D == 128) go(rope_kvq_kernel<128, float>, q); else go(rope_kvq_kernel<64, float>, q);
+  } else {
+    auto* q = static_cast<uint16_t*>(q_out);
+    if (D == 128) go(rope_kvq_kernel<128, uint16_t>, q); else go(rope_kvq_kernel<64, uint16_t>, q);
   }
   return hipGetLastError();
 }
