@@ -523,7 +523,9 @@ static int kvq_rows_ok(const void* k_cache, const void* v_cache, const int32_t* 
   REQUIRE(Hkv >= 1, "n_kv_heads = %d must be >= 1", Hkv);
   REQUIRE(max_blocks >= 1, "max_blocks_per_seq = %d must be >= 1", max_blocks);
   REQUIRE(num_blocks >= 1, "num_blocks = %d must be >= 1", num_blocks);
-  REQUIRE(double(B) * n * Hkv * D < 6.0e10, "B * n * n_kv_heads * head_dim too large");
+  // a launch holds 2^32 threads; a wavefront takes 16 positions of 128 dims
+  REQUIRE(double(B) * ((double(n) + 30) / 16) * ((double(Hkv) * D + 127) / 128) < 6.0e7,
+          "B * n * n_kv_heads * head_dim too large");
   REQUIRE(k_cache && v_cache && block_tables && start, "a required pointer is NULL");
   REQUIRE((reinterpret_cast<uintptr_t>(k_cache) | reinterpret_cast<uintptr_t>(v_cache)) % 16 == 0,
           "the caches must start at a multiple of 16 bytes");
@@ -536,6 +538,7 @@ int molt_kvq_write(const void* k, const void* v, long long k_stride, long long v
   if (int r = kvq_rows_ok(k_cache, v_cache, block_tables, context_lens, B, n, Hkv, D, max_blocks, num_blocks, dtype))
     return r;
   REQUIRE(k && v, "a required pointer is NULL");
+  REQUIRE(k_cache != v_cache, "k_cache and v_cache are the same");
   REQUIRE(k_stride >= (long long)Hkv * D && v_stride >= (long long)Hkv * D,
           "row strides %lld and %lld must be at least n_kv_heads * head_dim = %lld", k_stride, v_stride,
           (long long)Hkv * D);
@@ -570,7 +573,9 @@ int molt_paged_attention_kvq(const void* q, const void* k_cache, const void* v_c
   if (int r = kvq_rows_ok(k_cache, v_cache, block_tables, context_lens, B, k + 1, Hkv, D, max_blocks, num_blocks, dtype))
     return r;
   REQUIRE(Hq >= Hkv && Hq % Hkv == 0, "n_q_heads %d must be a multiple of n_kv_heads %d", Hq, Hkv);
-  REQUIRE(double(B) * (k + 1) * Hq < 1.0e9, "B * (1+k) * n_q_heads too large");
+  // workgroups: row groups of 16 (f32) or 48 rows of a kv head
+  REQUIRE(double(B) * Hkv * (double(Hq / Hkv) * (k + 1) / (dtype == MOLT_F32 ? 16 : 48) + 1) < 1.6e7,
+          "B * (1+k) * n_q_heads too large");
   REQUIRE(max_blocks <= (1 << 26), "max_blocks_per_seq = %d must be <= 2^26", max_blocks);
   REQUIRE(q && out, "a required pointer is NULL");
   if (int r = check_ws(workspace, workspace_bytes, molt::kvq_attention_ws_bytes(B, k + 1, Hq, Hkv, D, max_blocks)))

@@ -290,7 +290,7 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
   const int nblk = (end + 15) / 16, npairs = (nblk + 1) / 2;
   int lim[NT];                           // last key that a row sees (past the last row: as the last)
 #pragma unroll
-  for (int i = 0; i < NT; ++i) lim[i] = ctx + min(r0 + 16 * i + l16, p.R - 1) / p.G;
+  for (int i = 0; i < NT; ++i) lim[i] = visible_end(p, ctx, min(r0 + 16 * i + l16, p.R - 1) + 1) - 1;
   // the share's pairs of blocks, then the wavefront's
   const int s0 = int(long(npairs) * w.part / w.parts), s1 = int(long(npairs) * (w.part + 1) / w.parts);
   const int p0 = s0 + (s1 - s0) * wave / W, p1 = s0 + (s1 - s0) * (wave + 1) / W;

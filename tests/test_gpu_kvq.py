@@ -163,6 +163,25 @@ def test_rows_without_a_place(molt_lib):
         assert (out.reshape(B, n, -1)[0, :3] == 0).all() and (out.reshape(B, n, -1)[3] == 0).all()
 
 
+def test_context_past_the_table(molt_lib):
+    """Contexts past the table's end, up to the largest: the rows see the whole table."""
+    rng = np.random.default_rng(10)
+    B, k, Hq, Hkv, D, maxb = 3, 2, 4, 2, 128, 4
+    kc, vc, tables = _caches(molt_lib, rng, B, maxb, Hkv, D)
+    _fill(rng, kc, vc, tables, [64] * B, D)
+    ctx = np.array([63, 5000, 2 ** 31 - 1], np.int32)
+    for dtype in ("bf16", "f32"):
+        q, q64 = _rows(rng, B * (k + 1), Hq, D, dtype)
+        out = molt_lib.paged_attention_kvq(q.cuda(), _t(kc), _t(vc), _t(tables), _t(ctx), k).double().cpu().numpy()
+        want, mag = (x.reshape(out.shape) for x in kvq.attention(q64, kc, vc, tables, np.minimum(ctx, 63), k))
+        assert (np.abs(out - want) <= _tol(want, mag, dtype)).all()
+    rows = _rows(rng, B * 2, Hkv, D, "f32")[0].cuda()
+    gk, gv = _t(kc), _t(vc)
+    molt_lib.kvq_write(rows, rows, gk, gv, _t(tables), _t(ctx), 2)     # row 0 of the first sequence only
+    kvq.write_rows(rows.double().cpu().numpy(), rows.double().cpu().numpy(), kc, vc, tables, ctx.astype(np.int64), 2)
+    assert np.array_equal(host(gk), kc) and np.array_equal(host(gv), vc)
+
+
 CASES = [
     # B, k, Hq, Hkv, D, lo, hi
     (1, 0, 1, 1, 128, 0, 0),            # one key
@@ -178,6 +197,9 @@ CASES = [
     (1, 256, 8, 2, 64, 100, 100),       # a window of 257 positions
     (1, 15, 8, 8, 128, 2500, 2500),     # 16 positions of one head
     (33, 1, 2, 1, 64, 0, 129),
+    (300, 0, 2, 1, 64, 0, 20),          # more sequences than a cut looks at
+    (2, 7, 16, 1, 128, 1000, 2600),     # 128 rows, three row groups with a smaller last, cut
+    (5, 2, 4, 4, 128, 0, 1900),         # uneven lengths, cut
 ]
 
 
