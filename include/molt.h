@@ -231,8 +231,11 @@ int molt_paged_attention(const void* q, const void* k_cache, const void* v_cache
  *  - Writing: a group with largest magnitude a takes the power of two 2^e with
  *    a / 2^e in [3.5, 7), e kept in -125 .. 125 (s = e + 127; a zero group's codes are 0);
  *    codes are x / 2^e to the nearest, ties to the even code, saturating at 6, so no element
- *    is off by more than 2^e. A group with an infinity or NaN gets s = 255.
- *  - Reading: code * 2^(s - 127), exact in bf16; NaN for s = 255.
+ *    is off by more than 2^e (but those past 7 * 2^125). A group with an infinity or NaN gets
+ *    s = 255.
+ *  - Reading: code * 2^(s - 127), exact in bf16; NaN for s = 255. A record of zero bytes
+ *    reads as zeros; what other bytes that writing never makes (s = 0, 1, 253, 254) stand for
+ *    is not defined.
  * Layout, blocks of 16 tokens as in the other caches, two uint8 tensors
  * [num_blocks, n_kv_heads, 17 D / 2] that start at multiples of 16 bytes:
  *    K: codes [16 tokens][D / 2], then scales [16 tokens][D / 32]

@@ -431,6 +431,8 @@ def kvq_read(k_cache, v_cache, block_tables, starts, n, lens=None, dtype=torch.b
         raise MoltError(f"dtype is {dtype}, expected float32 or bfloat16")
     _dev(lens, torch.int32, (B,), "lens")
     _same_device(lens, dev, "lens")
+    if n < 1:
+        raise MoltError(f"n = {n} must be >= 1")
     k = torch.empty(B * n, Hkv, D, dtype=dtype, device=k_cache.device)
     v = torch.empty(B * n, Hkv, D, dtype=dtype, device=k_cache.device)
     _check(lib.molt_kvq_read(_ptr(k_cache), _ptr(v_cache), _ptr(block_tables), _ptr(starts), _ptr(lens), B, n,
@@ -455,6 +457,8 @@ def paged_attention_kvq(q, k_cache, v_cache, block_tables, context_lens, k, work
     _dev(q, None, (B * (k + 1), Hq, D), "q")
     _same_device(q, dev, "q")
     _same_device(workspace, dev, "workspace")
+    if workspace is not None and not workspace.is_contiguous():
+        raise MoltError("workspace must be contiguous")
     out = torch.empty(q.shape[0], Hq * D, dtype=dt, device=q.device)
 
     def call(ws, have):

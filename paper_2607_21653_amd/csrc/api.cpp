@@ -574,7 +574,7 @@ int molt_paged_attention_kvq(const void* q, const void* k_cache, const void* v_c
     return r;
   REQUIRE(Hq >= Hkv && Hq % Hkv == 0, "n_q_heads %d must be a multiple of n_kv_heads %d", Hq, Hkv);
   // workgroups: row groups of 16 (f32) or 48 rows of a kv head
-  REQUIRE(double(B) * Hkv * (double(Hq / Hkv) * (k + 1) / (dtype == MOLT_F32 ? 16 : 48) + 1) < 1.6e7,
+  REQUIRE(double(B) * Hkv * (double(Hq / Hkv) * (k + 1) / (dtype == MOLT_F32 ? 16 : 48) + 1) < 1.4e7,
           "B * (1+k) * n_q_heads too large");
   REQUIRE(max_blocks <= (1 << 26), "max_blocks_per_seq = %d must be <= 2^26", max_blocks);
   REQUIRE(q && out, "a required pointer is NULL");

@@ -205,7 +205,8 @@ MOLT_DEV Share find_share(const KvqAttnParams& p, int r1, int slot, float* lds) 
   const float least = fminf(fmaxf(sum / float(p.slots), float(kMinPairs)), most);
   // (hardware approximations: the same in every workgroup)
   const float c = lane == 0 ? most : most * __builtin_amdgcn_exp2f(__builtin_amdgcn_logf(least / most) * (float(lane) / 63.f));
-  const float inv = __builtin_amdgcn_rcpf(c);
+  // (and a little less than 1 / c: T pairs with c = T are one part)
+  const float inv = __builtin_amdgcn_rcpf(c) * (1.f - 0x1p-20f);
   float n = 0.f;                         // parts with the lane's c; each wavefront counts 16 of 64 sequences
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
@@ -704,12 +705,14 @@ __global__ __launch_bounds__(256) void kvq_merge_kernel(KvqAttnParams p) {
     for (int u = 0; u < kU; ++u) mn = fmaxf(mn, ml[u].x);
     const float f0 = M == -INFINITY ? 0.f : exp2f((M - mn) * p.c);
     M = mn;
+    // a part without a maximum has seen no key, or NaN only: its factor is 0, its sum 0 or NaN
+    const float ref = M == -INFINITY ? 0.f : M;
     L *= f0;
     a *= f0;
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
-      const bool live = s0 + u < sp.y && ml[u].x != -INFINITY;
-      const float f = exp2f((ml[u].x - M) * p.c);
+      const bool live = s0 + u < sp.y;
+      const float f = exp2f((ml[u].x - ref) * p.c);
       L += live ? ml[u].y * f : 0.f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) a[e] += live ? o[u][e] * f : 0.f;

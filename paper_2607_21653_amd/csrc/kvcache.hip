@@ -102,7 +102,7 @@ __global__ __launch_bounds__(kThreads) void kvq_write_kernel(KvqRows p, int nblk
   const Place w = find_place<D>(p, nblk);
   if (!w.any || w.id < 0) return;
   const Tile<D> t{int(threadIdx.x % kWave)};
-  const int hi = p.lens ? min(w.hi, p.lens[w.b] - w.first) : w.hi;
+  const int hi = p.lens ? min(w.hi, min(max(p.lens[w.b], 0), p.n) - w.first) : w.hi;
   const long row0 = long(w.b) * p.n + w.first;
   const long rec = (long(w.id) * p.Hkv + w.h0) * Rec::kBytes;
   const int oct = t.oct();
@@ -167,7 +167,7 @@ __global__ __launch_bounds__(kThreads) void kvq_read_kernel(KvqRows p, int nblk,
   if (!w.any) return;
   const Tile<D> t{int(threadIdx.x % kWave)};
   // rows from `hi` on and rows of a block without a place are zeros: nothing is read for them
-  const int hi = w.id < 0 ? 0 : p.lens ? min(w.hi, p.lens[w.b] - w.first) : w.hi;
+  const int hi = w.id < 0 ? 0 : p.lens ? min(w.hi, min(max(p.lens[w.b], 0), p.n) - w.first) : w.hi;
   const long row0 = long(w.b) * p.n + w.first;
   const long rec = (long(max(w.id, 0)) * p.Hkv + w.h0) * Rec::kBytes;
   const int oct = t.oct();

@@ -291,6 +291,121 @@ def test_infinite_query(molt_lib):
     assert torch.equal(out[keep], base[keep])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_nan_query_of_a_cut_sequence(molt_lib, dtype):
+    """A row of NaN scores has no maximum in any part of its keys: the parts joined are NaN, not zeros."""
+    rng = np.random.default_rng(31)
+    kc, vc, tables = _caches(molt_lib, rng, 1, 60, 1, 128)
+    _fill(rng, kc, vc, tables, [902], 128)
+    args = (_t(kc), _t(vc), _t(tables), _t(np.array([900], np.int32)), 1)
+    assert molt_lib.paged_attention_kvq_workspace_size(1, 1, 3, 1, 128, 60) > 0
+    q, _ = _rows(rng, 2, 3, 128, dtype)
+    base = molt_lib.paged_attention_kvq(q.cuda(), *args).view(2, 3, 128)
+    q[0, 1, 3] = float("nan")
+    q[1, 2, 77] = float("inf")
+    out = molt_lib.paged_attention_kvq(q.cuda(), *args).view(2, 3, 128)
+    bad = torch.zeros(2, 3, dtype=torch.bool)
+    bad[0, 1] = bad[1, 2] = True
+    assert torch.isnan(out[0, 1]).all() and torch.isnan(out[1, 2]).all()
+    assert torch.equal(out[~bad], base[~bad])
+
+
+@pytest.mark.parametrize("pairs", [24, 47, 1535])
+def test_equal_lengths_with_few_spare_slots(molt_lib, pairs):
+    """200 sequences of one length (and table, and query), which the workgroups that fit cannot all cut in
+    two: none is lost. 1535: the hardware reciprocal is above 1 / 1535."""
+    rng = np.random.default_rng(33)
+    B, Hq, Hkv, D = 200, 2, 2, 128
+    n, maxb = 32 * pairs, 2 * pairs + 10
+    gk, gv = molt_lib.kvq_cache(maxb, Hkv, D)
+    table = _t(rng.permutation(maxb).astype(np.int32)[None])
+    rows = [torch.from_numpy(rng.standard_normal((n, Hkv, D), np.float32)).cuda() for _ in range(2)]
+    start = torch.zeros(1, dtype=torch.int32, device="cuda")
+    molt_lib.kvq_write(*rows, gk, gv, table, start, n)
+    k, v = (x.double().cpu().numpy() for x in molt_lib.kvq_read(gk, gv, table, start, n, dtype=torch.float32))
+    q, q64 = _rows(rng, 1, Hq, D, "bf16")
+    out = molt_lib.paged_attention_kvq(q.cuda().repeat(B, 1, 1), gk, gv, table.repeat(B, 1), start.repeat(B) + n - 1, 0)
+    assert torch.equal(out, out[:1].expand_as(out))
+    score = np.einsum("hd,nhd->hn", q64[0], k) / np.sqrt(D)
+    w = np.exp(score - score.max(axis=1, keepdims=True))
+    w /= w.sum(axis=1, keepdims=True)
+    want, mag = (np.einsum("hn,nhd->hd", w, x).reshape(1, -1) for x in (v, np.abs(v)))
+    assert (np.abs(out[:1].double().cpu().numpy() - want) <= _tol(want, mag, "bf16")).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_padded_batch_of_cut_sequences(molt_lib, dtype):
+    """Sequences that sit the step out (no row sees a key) beside one long enough to be cut; a workspace of
+    just the size asked for, from an odd address, the bytes around it as they were; a smaller one."""
+    rng = np.random.default_rng(35)
+    B, k, Hq, Hkv, D, maxb = 4, 4, 8, 2, 64, 130
+    ctx = np.array([-(k + 1), 2000, -2 ** 31, -2], np.int32)
+    kc, vc, tables = _caches(molt_lib, rng, B, maxb, Hkv, D)
+    _fill(rng, kc, vc, tables, [0, 2000 + k + 1, 0, k - 1], D)
+    q, q64 = _rows(rng, B * (k + 1), Hq, D, dtype)
+    args = (q.cuda(), _t(kc), _t(vc), _t(tables), _t(ctx), k)
+    size = molt_lib.paged_attention_kvq_workspace_size(B, k, Hq, Hkv, D, maxb)
+    assert size > 0
+    buf = torch.full((size + 512,), 0xAB, dtype=torch.uint8, device="cuda")
+    got = molt_lib.paged_attention_kvq(*args, workspace=buf[255:255 + size])
+    assert (buf[:255] == 0xAB).all() and (buf[255 + size:] == 0xAB).all()
+    assert torch.equal(got, molt_lib.paged_attention_kvq(*args))
+    assert torch.equal(got, molt_lib.paged_attention_kvq(*args, workspace=buf[:16]))
+    out = got.double().cpu().numpy()
+    want, mag = (x.reshape(out.shape) for x in kvq.attention(q64, kc, vc, tables, ctx.astype(np.int64), k))
+    assert (np.abs(out - want) <= _tol(want, mag, dtype)).all()
+    assert (out.reshape(B, k + 1, -1)[[0, 2]] == 0).all()
+
+
+def test_lens_of_any_value(molt_lib):
+    """Negative lens count as 0, lens above n as n, in blocks that begin before, with and behind row 0."""
+    rng = np.random.default_rng(37)
+    B, n, Hkv, D = 6, 40, 2, 128
+    ctx = np.array([0, 7, 7, 7, 16, 3], np.int32)
+    lens = np.array([-2 ** 31, -2 ** 31, 2 ** 31 - 1, 41, -1, 2 ** 31 - 1], np.int32)
+    kc, vc, tables = _caches(molt_lib, rng, B, 4, Hkv, D)
+    k, v = (_rows(rng, B * n, Hkv, D, "bf16")[0] for _ in range(2))
+    gk, gv, gt, gc = _t(kc), _t(vc), _t(tables), _t(ctx)
+    molt_lib.kvq_write(k.cuda(), v.cuda(), gk, gv, gt, gc, n, lens=_t(lens))
+    kvq.write_rows(k.double().numpy(), v.double().numpy(), kc, vc, tables, ctx, n, lens)
+    assert np.array_equal(host(gk), kc) and np.array_equal(host(gv), vc)
+    got = molt_lib.kvq_read(gk, gv, gt, gc, n, lens=_t(lens))
+    for g, w in zip(got, kvq.read_rows(kc, vc, tables, ctx, n, D, lens)):
+        assert np.array_equal(g.double().cpu().numpy(), w, equal_nan=True)
+
+
+def test_zeroed_cache(molt_lib):
+    """Slots of kvq_cache that were never written are zeros to the calls that see them."""
+    for D in (64, 128):
+        kc, vc = molt_lib.kvq_cache(60, 2, D)
+        tables = torch.arange(60, dtype=torch.int32, device="cuda").view(1, 60)
+        ctx = torch.tensor([900], dtype=torch.int32, device="cuda")
+        assert all((t == 0).all() for t in molt_lib.kvq_read(kc, vc, tables, ctx * 0, 900))
+        for dt in DT.values():
+            assert (molt_lib.paged_attention_kvq(torch.ones(2, 4, D, dtype=dt, device="cuda"), kc, vc, tables, ctx, 1) == 0).all()
+
+
+def test_two_streams_at_once(molt_lib):
+    """Calls of other sizes on two streams beside each other, each with a workspace of its own."""
+    rng = np.random.default_rng(39)
+    runs = []
+    for B, k, Hq, Hkv, D, L in ((2, 1, 16, 2, 128, 2000), (3, 3, 8, 4, 64, 1500)):
+        kc, vc, tables = _caches(molt_lib, rng, B, 130, Hkv, D)
+        ctx = np.full(B, L, np.int32)
+        _fill(rng, kc, vc, tables, [L + k + 1] * B, D)
+        args = (_rows(rng, B * (k + 1), Hq, D, "bf16")[0].cuda(), _t(kc), _t(vc), _t(tables), _t(ctx), k)
+        runs.append((args, molt_lib.paged_attention_kvq(*args), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    outs = [[], []]
+    for _ in range(5):
+        for i, (args, _, stream) in enumerate(runs):
+            with torch.cuda.stream(stream):
+                outs[i].append(molt_lib.paged_attention_kvq(*args))
+    torch.cuda.synchronize()
+    for (_, want, _), got in zip(runs, outs):
+        assert all(torch.equal(want, g) for g in got)
+
+
 def test_unaligned_rows_of_queries(molt_lib):
     rng = np.random.default_rng(23)
     for dtype in ("bf16", "f32"):
@@ -447,5 +562,9 @@ def test_refusals(molt_lib):
     refused("dtype", lambda: A(q=q.half()))
     refused("multiple", lambda: A(q=q[:, :3].contiguous()))
     refused("shape", lambda: A(k=3))
+    flat_ws = torch.empty(1, dtype=torch.uint8, device="cuda")
+    refused("workspace", lambda: A(workspace=flat_ws.expand(1 << 20)))
+    refused("workspace", lambda: A(workspace=flat_ws.cpu()))
+    refused("n = -1", lambda: R(n=-1))
     refused("k = -1", lambda: A(q=q[:0], k=-1))
     refused("contiguous", lambda: A(q=q.transpose(0, 1).contiguous().transpose(0, 1)))
