@@ -676,49 +676,69 @@ __global__ __launch_bounds__(W * kWave, 2) void kvq_attn_kernel(KvqAttnParams p)
   else attend<D, T, NT, ONCE, W>(p, lds, rg, r0, h, slot, w);
 }
 
-// log-sum-exp join of a sequence's slots: thread = 4 dims of one row, kU slots' loads in flight together
-template <int D, typename T>
+// log-sum-exp join of a sequence's slots, thread = 4 dims of one row. P = 1: a thread takes all slots; else P groups of
+// threads every P-th, a row a workgroup, and then their sums through LDS.
+template <int D, typename T, int P>
 __global__ __launch_bounds__(256) void kvq_merge_kernel(KvqAttnParams p) {
-  const long i = long(blockIdx.x) * 256 + threadIdx.x;
-  const int d0 = int(i % (D / 4)) * 4;
-  const long row = i / (D / 4);
-  const int bh = int(row / p.R), r = int(row % p.R);
+  constexpr int O = D / 4, kU = 4;
+  static_assert(P == 1 || P * O == 256, "a row or 256 / O rows a workgroup");
+  const int d = threadIdx.x % O, g = P == 1 ? 0 : threadIdx.x / O;
+  const int row = P == 1 ? int(blockIdx.x) * (256 / O) + int(threadIdx.x) / O : int(blockIdx.x);
+  const int bh = row / p.R, r = row % p.R;
   const int b = bh / p.Hkv, h = bh % p.Hkv, rg = r / p.group;
   if (b >= p.B) return;
   const int2 sp = *reinterpret_cast<const int2*>(p.split + 2 * (long(rg) * p.B + b));
   if (sp.y == 1) return;
   const long pr0 = ((long(rg) * p.Hkv + h) * p.slots + sp.x) * p.group + r % p.group;
-  constexpr int kU = 16;
   float M = -INFINITY, L = 0.f;
   floatx4_t a = {0.f, 0.f, 0.f, 0.f};
-  for (int s0 = 0; s0 < sp.y; s0 += kU) {
+  for (int s0 = g; s0 < sp.y; s0 += kU * P) {
     float2 ml[kU];
     floatx4_t o[kU];
 #pragma unroll
     for (int u = 0; u < kU; ++u) {       // past the last: its own again, not added
-      const long pr = pr0 + long(min(s0 + u, sp.y - 1)) * p.group;
+      const long pr = pr0 + long(min(s0 + u * P, sp.y - 1)) * p.group;
       ml[u] = *reinterpret_cast<const float2*>(p.part_ml + 2 * pr);
-      o[u] = *reinterpret_cast<const floatx4_t*>(p.part_o + pr * D + d0);
+      o[u] = *reinterpret_cast<const floatx4_t*>(p.part_o + pr * D + 4 * d);
     }
     float mn = M;
 #pragma unroll
     for (int u = 0; u < kU; ++u) mn = fmaxf(mn, ml[u].x);
-    const float f0 = M == -INFINITY ? 0.f : exp2f((M - mn) * p.c);
+    // what has no maximum has seen no key, or NaN only: its factor is 0, its sum 0 or NaN
+    const float ref = mn == -INFINITY ? 0.f : mn;
+    const float f0 = exp2f((M - ref) * p.c);
     M = mn;
-    // a part without a maximum has seen no key, or NaN only: its factor is 0, its sum 0 or NaN
-    const float ref = M == -INFINITY ? 0.f : M;
     L *= f0;
     a *= f0;
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
-      const bool live = s0 + u < sp.y;
+      const bool live = s0 + u * P < sp.y;
       const float f = exp2f((ml[u].x - ref) * p.c);
       L += live ? ml[u].y * f : 0.f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) a[e] += live ? o[u][e] * f : 0.f;
     }
   }
-  store_out4<T>(p, b, h, r, D, d0, a, L);
+  if constexpr (P > 1) {
+    __shared__ floatx4_t sum[256];
+    __shared__ float2 stat[P];           // maximum and sum of the weights
+    sum[threadIdx.x] = a;
+    if (d == 0) stat[g] = make_float2(M, L);
+    __syncthreads();
+    if (g != 0) return;
+#pragma unroll
+    for (int u = 1; u < P; ++u) M = fmaxf(M, stat[u].x);
+    const float ref = M == -INFINITY ? 0.f : M;
+    L = 0.f;
+    a = floatx4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < P; ++u) {
+      const float f = exp2f((stat[u].x - ref) * p.c);
+      L += stat[u].y * f;
+      a += sum[u * O + d] * f;
+    }
+  }
+  store_out4<T>(p, b, h, r, D, 4 * d, a, L);
 }
 
 constexpr int kMaxTiles = 3;             // 16-row tiles of a wavefront (bf16; one in f32)
@@ -761,10 +781,12 @@ void launch_dt(const KvqAttnParams& p, hipStream_t s) {
     else if (p.group == 32) launch_nt<D, T, 2>(p, s);
     else launch_nt<D, T, 3>(p, s);
   }
-  if (p.slots > p.B) {
-    const long threads = long(p.B) * p.Hkv * p.R * (D / 4);
-    kvq_merge_kernel<D, T><<<unsigned((threads + 255) / 256), 256, 0, s>>>(p);
-  }
+  // (room for more than 8 slots a sequence: a row a workgroup; 1 sequence of 65536 keys x 4 kv heads: 4.7 us, by one
+  // thread for all slots 16; 16 sequences with 8 slots each, 640 rows a head: 6.4 us, by one thread 4.7)
+  const unsigned rows = unsigned(p.B * p.Hkv * p.R);
+  constexpr int kRows = 1024 / D;        // of a workgroup
+  if (p.slots > 8l * p.B) kvq_merge_kernel<D, T, kRows><<<rows, 256, 0, s>>>(p);
+  else if (p.slots > p.B) kvq_merge_kernel<D, T, 1><<<(rows + kRows - 1) / kRows, 256, 0, s>>>(p);
 }
 
 void carve_parts(Carver& c, KvqAttnParams& p, int D) {
