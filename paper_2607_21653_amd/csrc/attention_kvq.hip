@@ -7,6 +7,7 @@
 // That adds a rounding like the output's own: rms error 2.07e-3 of the output's rms against 1.66e-3 with two
 // parts, for which 128 sequences x 5 positions at context 8192 took 178 us, with one 135.
 #include <algorithm>
+#include <cmath>
 
 #include "internal.h"
 #include "kvq_format.h"
@@ -35,6 +36,7 @@ struct KvqAttnParams {
   int slots;               // workgroups of a (row group, kv head); B: one per sequence, nothing is cut
   int resident;            // workgroups that the chip holds
   int spread;              // a slot's heads run on one XCD
+  int waves;               // wavefronts of a workgroup
   float c;                 // log2(e) / sqrt(D)
   int out_tiled;
 };
@@ -160,16 +162,24 @@ MOLT_DEV void split_query_bf16(const u32x4 (&raw)[D / 64][2], int g4, int32x8_t 
   qs = bad ? 0xffff : D == 128 ? byte | (byte - 5) << 8 : g4 < 2 ? byte : byte - 5;
 }
 
-// Output dims d0 .. + 3 of row r: a / L, zeros for a row that sees no key
+// 4 output dims from column c of output row t on
 template <typename T>
-MOLT_DEV void store_out4(const KvqAttnParams& p, int b, int h, int r, int D, int d0, const floatx4_t& a, float L) {
-  const float inv = L == 0.f ? 0.f : 1.f / L;
-  const long t = long(b) * p.n + r / p.G, c = (h * p.G + r % p.G) * D + d0, cols = long(p.Hq) * D;
+MOLT_DEV void store4(const KvqAttnParams& p, long t, long c, int D, const floatx4_t& a) {
+  const long cols = long(p.Hq) * D;
   T* out = static_cast<T*>(p.out) + (p.out_tiled ? tiled_index(t, c, cols, sizeof(T)) : t * cols + c);
   if constexpr (sizeof(T) == 4)
-    *reinterpret_cast<UnalignedF4*>(out) = a * inv;
+    *reinterpret_cast<UnalignedF4*>(out) = a;
   else
-    *reinterpret_cast<UnalignedU2*>(out) = u32x2{f32x2_to_bf16(a[0] * inv, a[1] * inv), f32x2_to_bf16(a[2] * inv, a[3] * inv)};
+    *reinterpret_cast<UnalignedU2*>(out) = u32x2{f32x2_to_bf16(a[0], a[1]), f32x2_to_bf16(a[2], a[3])};
+}
+
+// 1 / L, 0 for a row that sees no key
+MOLT_DEV float inverse(float L) { return L == 0.f ? 0.f : 1.f / L; }
+
+// dims d0 .. + 3 of row r of (b, h)
+template <typename T>
+MOLT_DEV void store_out4(const KvqAttnParams& p, int b, int h, int r, int D, int d0, const floatx4_t& a, float L) {
+  store4<T>(p, long(b) * p.n + r / p.G, long(h * p.G + r % p.G) * D + d0, D, a * inverse(L));
 }
 
 // The work of slot `slot` of a row group (whose rows end before r1): part `part` of `parts` of sequence b, whose
@@ -275,16 +285,21 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
   const int lane = threadIdx.x % kWave, l16 = lane % 16, g4 = lane / 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   // The query rows are loaded first: behind the copies of keys and values they would wait for those. Wavefront i
-  // makes the operands of tile i.
-  const int qtile = F32 ? 0 : min(wave, NT - 1), qr = min(r0 + 16 * qtile + l16, p.R - 1);
-  const long qrow = ((long(b) * p.n + qr / p.G) * p.Hq + h * p.G + qr % p.G) * D;
-  u32x4 raw[D / 64][2];
-  if constexpr (!F32) {
-    const uint16_t* src = static_cast<const uint16_t*>(p.q) + qrow + 16 * g4;
+  // makes the operands of tiles i, i + W, ..
+  constexpr int QT = F32 ? 1 : (NT + W - 1) / W;
+  long qrow[QT];
+  u32x4 raw[QT][D / 64][2];
 #pragma unroll
-    for (int c = 0; c < D / 64; ++c)
+  for (int x = 0; x < QT; ++x) {
+    const int qr = min(r0 + (F32 ? 0 : 16 * min(wave + W * x, NT - 1)) + l16, p.R - 1);
+    qrow[x] = ((long(b) * p.n + qr / p.G) * p.Hq + h * p.G + qr % p.G) * D;
+    if constexpr (!F32) {
+      const uint16_t* src = static_cast<const uint16_t*>(p.q) + qrow[x] + 16 * g4;
 #pragma unroll
-      for (int v = 0; v < 2; ++v) raw[c][v] = *reinterpret_cast<const UnalignedU4*>(src + 64 * c + 8 * v);
+      for (int c = 0; c < D / 64; ++c)
+#pragma unroll
+        for (int v = 0; v < 2; ++v) raw[x][c][v] = *reinterpret_cast<const UnalignedU4*>(src + 64 * c + 8 * v);
+    }
   }
   const int ctx = p.ctx[b];
   const int end = visible_end(p, ctx, r1);
@@ -294,7 +309,8 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
   for (int i = 0; i < NT; ++i) lim[i] = visible_end(p, ctx, min(r0 + 16 * i + l16, p.R - 1) + 1) - 1;
   // the share's pairs of blocks, then the wavefront's
   const int s0 = int(long(npairs) * w.part / w.parts), s1 = int(long(npairs) * (w.part + 1) / w.parts);
-  const int p0 = s0 + (s1 - s0) * wave / W, p1 = s0 + (s1 - s0) * (wave + 1) / W;
+  const int each = (s1 - s0) / W, more = (s1 - s0) % W;
+  const int p0 = s0 + each * wave + min(wave, more), p1 = p0 + each + (wave < more ? 1 : 0);
   const int full_end = min(visible_end(p, ctx, r0 + 1), end);    // keys before are seen by every row
   uint8_t* ring = lds + wave * kLds;
   uint8_t* qlds = lds + W * kLds;
@@ -352,23 +368,27 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
   bf16x8_t qf[QP][KS];
   int qs[NT];                            // scale bytes of both fp8 parts
   if constexpr (F32) {
-    load_query_f32<D>(static_cast<const float*>(p.q) + qrow, r0 + l16 < p.R, g4, qf);
-  } else if (wave < NT) {
-    int32x8_t qp[D / 64];
-    int sc;
-    split_query_bf16<D>(raw, g4, qp, sc);
+    load_query_f32<D>(static_cast<const float*>(p.q) + qrow[0], r0 + l16 < p.R, g4, qf);
+  } else {
 #pragma unroll
-    for (int u = 0; u < D / 64; ++u) {
-      int32x4_t* dst = reinterpret_cast<int32x4_t*>(qlds + wave * QF + u * 2048 + lane * 16);
-      dst[0] = int32x4_t{qp[u][0], qp[u][1], qp[u][2], qp[u][3]};
-      dst[64] = int32x4_t{qp[u][4], qp[u][5], qp[u][6], qp[u][7]};
+    for (int x = 0; x < QT; ++x) {
+      const int tile = wave + W * x;
+      if (tile >= NT) break;
+      int32x8_t qp[D / 64];
+      int sc;
+      split_query_bf16<D>(raw[x], g4, qp, sc);
+#pragma unroll
+      for (int u = 0; u < D / 64; ++u) {
+        int32x4_t* dst = reinterpret_cast<int32x4_t*>(qlds + tile * QF + u * 2048 + lane * 16);
+        dst[0] = int32x4_t{qp[u][0], qp[u][1], qp[u][2], qp[u][3]};
+        dst[64] = int32x4_t{qp[u][4], qp[u][5], qp[u][6], qp[u][7]};
+      }
+      reinterpret_cast<int*>(ring + (kSlots - 1) * SLOT)[64 * x + lane] = sc;   // in a slot not yet in use
     }
-    *reinterpret_cast<int*>(ring + (kSlots - 1) * SLOT + lane * 4) = sc;   // in a slot not yet in use
-  }
-  if constexpr (!F32) {
     lds_barrier();
 #pragma unroll
-    for (int i = 0; i < NT; ++i) qs[i] = *reinterpret_cast<const int*>(lds + i * kLds + (kSlots - 1) * SLOT + lane * 4);
+    for (int i = 0; i < NT; ++i)
+      qs[i] = reinterpret_cast<const int*>(lds + i % W * kLds + (kSlots - 1) * SLOT)[64 * (i / W) + lane];
     lds_barrier();
   }
   floatx4_t o[NT][DT], ls[NT];           // O^T; the rows' sums (bf16: by MFMA, the same in every register and group)
@@ -598,6 +618,20 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no copy may outlive the ring
 
+  if constexpr (W == 1) {                // nothing to join
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      const float L = F32 ? rows_sum4(ls[i][0]) : ls[i][0];
+      const int r = r0 + 16 * i + l16;
+      if (r >= p.R) continue;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int t = 0; t < DT; t += 4)
+          store_out4<T>(p, b, h, r, D, D / 4 * g4 + DT * e + t, floatx4_t{o[i][t][e], o[i][t + 1][e], o[i][t + 2][e], o[i][t + 3][e]}, L);
+    }
+    return;
+  }
   // the wavefronts' shares joined through LDS, one 16-row tile at a time
   constexpr int RS = D + 4;              // floats of a row, then 16 maxima and 16 sums
   float* own = reinterpret_cast<float*>(ring);
@@ -745,10 +779,19 @@ constexpr int kMaxTiles = 3;             // 16-row tiles of a wavefront (bf16; o
 
 // Row groups of as few 16-row tiles as cover the R rows. Slots: one per sequence where that gives as many workgroups
 // as are resident (a cut for uneven lengths would cost 8% of even ones: the work of finding it, workgroups without a
-// part, the joining launch), or the tables are short (kMinCutBlocks), else room for as many parts as are resident.
-constexpr int kMinCutBlocks = 48;
-// Uncut calls of up to kFew workgroups, a compute unit for each, take kMoreWaves wavefronts in each.
-constexpr int kFew = 256, kMoreWaves = 8;
+// part, the joining launch), or the tables are short, else room for as many parts as are resident. Short: under
+// kMinCut pairs, and where each workgroup has a compute unit and 8 wavefronts (kFew) those beat a cut for longer: us
+// uncut and cut, with U workgroups at context 1000, 1400, 2000 and 3000, 1 sequence U = 4: 9.6, 10.7, 13.0, 16.9 and
+// 10.9, 11.2, 11.5, 11.4; 8 sequences U = 32: 13.1, 14.6, 17.5, 22.0 and 15.4, 17.0, 19.1, 20.0; 30 sequences U = 240 of
+// D = 64: 9.4, 10.6, 12.3, 15.3 and 16.6, 18.8, 19.5, 22.6.
+constexpr int kMinCut = 24, kFew = 256;
+// Wavefronts of an uncut workgroup, 1, 4 or 8: the fewer, the more workgroups run at a time and the less there is to
+// join, the more, the sooner a long key range is done. The rule weighs rounds of workgroups by what one takes; us of
+// calls with 1, 4 and 8: 19844 workgroups of up to 9 pairs (f32) 115, 256 and 544; 2016 of 1 pair (2.5 tiles) 27, 36
+// and 75; 1584 of 49 pairs (3 tiles) 167, 120 and 145; 48 of 32 pairs (f32) 35, 19.6 and 14.6; 8 of 4 pairs (3 tiles)
+// 12.7, 9.4 and 10.6.
+constexpr int kMoreWaves = 8;
+constexpr double kPairTime = 1.7;        // us of a wavefront for a pair of blocks
 void kvq_plan(KvqAttnParams& p, int D, bool f32) {
   p.G = p.Hq / p.Hkv;
   p.R = p.G * p.n;
@@ -759,17 +802,35 @@ void kvq_plan(KvqAttnParams& p, int D, bool f32) {
   p.resident = 256 * (D == 128 || nt == 3 ? 2 : f32 || nt == 2 ? 3 : 4);   // by LDS and registers
   const long per = long(p.Hkv) * p.nrg, pairs = (p.max_blocks + 1) / 2;
   const long slots = std::min(p.resident / per, p.B * ((pairs + kMinPairs - 1) / kMinPairs));
-  p.slots = slots > p.B && p.B <= kMaxCut && p.max_blocks >= kMinCutBlocks ? int(slots) : p.B;
+  const bool longer = p.B * per <= kFew ? pairs > 2 * kMinCut + p.B * per / 2 : pairs >= kMinCut;
+  p.slots = slots > p.B && p.B <= kMaxCut && longer ? int(slots) : p.B;
   p.spread = p.slots >= 64;
+  p.waves = kWaves;
+  if (p.slots == p.B) {
+    // how many workgroups run at a time, and the us of one
+    const int mem = kSlots * (32 * D + 256) + (f32 ? 0 : D / 64 * 2048 * nt);   // Lds of one wavefront
+    const double at_once[3] = {256.0 * std::min(8, 163840 / mem), double(p.resident), 256.0};
+    const double each[3] = {4.0 + kPairTime * pairs, 7.0 + kPairTime * pairs / 4, 8.2 + kPairTime * pairs / 8};
+    double best = 1e30;
+    for (int i = 0; i < 3; ++i) {
+      const double time = std::ceil(double(p.B) * per / at_once[i]) * each[i];
+      if (time < best) { best = time; p.waves = i == 0 ? 1 : i == 1 ? kWaves : kMoreWaves; }
+    }
+  }
+}
+
+template <int D, typename T, int NT, bool ONCE>
+void launch_w(const KvqAttnParams& p, unsigned grid, hipStream_t s) {
+  if (p.waves == 1) kvq_attn_kernel<D, T, NT, ONCE, 1><<<grid, kWave, 0, s>>>(p);
+  else if (p.waves == kWaves) kvq_attn_kernel<D, T, NT, ONCE, kWaves><<<grid, kWaves * kWave, 0, s>>>(p);
+  else kvq_attn_kernel<D, T, NT, ONCE, kMoreWaves><<<grid, kMoreWaves * kWave, 0, s>>>(p);
 }
 
 template <int D, typename T, int NT>
 void launch_nt(const KvqAttnParams& p, hipStream_t s) {
   const long units = p.spread ? (long(p.slots) + 7) / 8 * 8 * p.Hkv : (long(p.slots) * p.Hkv + 7) / 8 * 8;
-  const unsigned grid = unsigned(units * p.nrg);
-  if (p.nrg > 1) kvq_attn_kernel<D, T, NT, false, kWaves><<<grid, kWaves * kWave, 0, s>>>(p);
-  else if (p.slots > p.B || units > kFew) kvq_attn_kernel<D, T, NT, true, kWaves><<<grid, kWaves * kWave, 0, s>>>(p);
-  else kvq_attn_kernel<D, T, NT, true, kMoreWaves><<<grid, kMoreWaves * kWave, 0, s>>>(p);
+  if (p.nrg > 1) launch_w<D, T, NT, false>(p, unsigned(units * p.nrg), s);
+  else launch_w<D, T, NT, true>(p, unsigned(units), s);
 }
 
 template <int D, typename T>

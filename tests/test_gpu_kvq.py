@@ -295,10 +295,10 @@ def test_infinite_query(molt_lib):
 def test_nan_query_of_a_cut_sequence(molt_lib, dtype):
     """A row of NaN scores has no maximum in any part of its keys: the parts joined are NaN, not zeros."""
     rng = np.random.default_rng(31)
-    kc, vc, tables = _caches(molt_lib, rng, 1, 60, 1, 128)
+    kc, vc, tables = _caches(molt_lib, rng, 1, 200, 1, 128)
     _fill(rng, kc, vc, tables, [902], 128)
     args = (_t(kc), _t(vc), _t(tables), _t(np.array([900], np.int32)), 1)
-    assert molt_lib.paged_attention_kvq_workspace_size(1, 1, 3, 1, 128, 60) > 0
+    assert molt_lib.paged_attention_kvq_workspace_size(1, 1, 3, 1, 128, 200) > 0
     q, _ = _rows(rng, 2, 3, 128, dtype)
     base = molt_lib.paged_attention_kvq(q.cuda(), *args).view(2, 3, 128)
     q[0, 1, 3] = float("nan")
@@ -493,13 +493,13 @@ def test_graph_replays(molt_lib, dtype):
     """A captured step (write, attend with splits, read back) replayed with other inputs between eager work."""
     rng = np.random.default_rng(29)
     B, n, Hq, Hkv, D = 2, 2, 8, 2, 128
-    kc, vc, tables = _caches(molt_lib, rng, B, 60, Hkv, D)
+    kc, vc, tables = _caches(molt_lib, rng, B, 200, Hkv, D)
     ctx = np.array([200, 900], np.int32)
     _fill(rng, kc, vc, tables, ctx.tolist(), D)
     gk, gv, gt, gc = _t(kc), _t(vc), _t(tables), _t(ctx)
     draw = lambda H: _rows(rng, B * n, H, D, dtype)[0].cuda()
     q, k, v = draw(Hq), draw(Hkv), draw(Hkv)
-    ws = torch.empty(molt_lib.paged_attention_kvq_workspace_size(B, n - 1, Hq, Hkv, D, 60), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(molt_lib.paged_attention_kvq_workspace_size(B, n - 1, Hq, Hkv, D, 200), dtype=torch.uint8, device="cuda")
     assert ws.numel() > 0
 
     def step(gk, gv, ws=None):
