@@ -160,11 +160,6 @@ def _stream():
     return torch.cuda.current_stream().cuda_stream
 
 
-def _raw_stream(device):
-    """The current stream of a device (by index), without a torch.cuda.Stream object around it (2.6 us)."""
-    return torch._C._cuda_getCurrentRawStream(device)
-
-
 def _workspace(nbytes, device, ws=None):
     if nbytes == 0:
         return None, 0
@@ -363,17 +358,23 @@ def kvq_cache(num_blocks, n_kv_heads, head_dim, device="cuda"):
             torch.zeros(shape, dtype=torch.uint8, device=device))
 
 
+# The calls below take 3 to 8 us on the GPU where they are small, and as long on the host: they ask each tensor
+# for what they need once, and take the paths with messages only where something is wrong.
+_current_device = torch._C._cuda_getDevice
+_raw_stream = torch._C._cuda_getCurrentRawStream    # of a device index, without a torch.cuda.Stream around it (2.6 us)
+
+
 def _kvq_caches(k_cache, v_cache, block_tables, starts):
     """Checks of a pair of caches and the tables; returns (device index, B, num_blocks, n_kv_heads, head_dim,
     max_blocks)."""
     dev = k_cache.get_device()
     shape, table = k_cache.shape, block_tables.shape
-    if not (dev >= 0 and len(shape) == 3 and shape[2] * 2 % 17 == 0 and len(table) == 2 and starts.shape == table[:1]
-            and v_cache.shape == shape and k_cache.dtype is v_cache.dtype is torch.uint8
-            and block_tables.dtype is starts.dtype is torch.int32
+    if not (dev >= 0 and len(shape) == 3 and len(table) == 2 and v_cache.shape == shape
+            and starts.dim() == 1 and starts.numel() == table[0]
+            and k_cache.dtype is v_cache.dtype is torch.uint8 and block_tables.dtype is starts.dtype is torch.int32
             and v_cache.get_device() == block_tables.get_device() == starts.get_device() == dev
             and k_cache.is_contiguous() and v_cache.is_contiguous() and block_tables.is_contiguous()
-            and starts.is_contiguous()):
+            and starts.is_contiguous()) or shape[2] * 2 % 17:
         _dev(k_cache, torch.uint8, name="k_cache")
         if len(shape) != 3 or shape[2] * 2 % 17:
             raise MoltError(f"k_cache has shape {tuple(shape)}, expected [num_blocks, n_kv_heads, 17 * head_dim / 2]")
@@ -383,17 +384,26 @@ def _kvq_caches(k_cache, v_cache, block_tables, starts):
         if len(table) != 2 or table[0] != starts.shape[0]:
             raise MoltError(f"block_tables has shape {tuple(table)}, expected ({starts.shape[0]}, max_blocks)")
         raise MoltError("k_cache, v_cache, block_tables and context_lens must be on one device")
-    if dev != torch.cuda.current_device():
-        raise MoltError(f"the caches are on device {dev}, the current device is {torch.cuda.current_device()}")
+    if dev != _current_device():
+        raise MoltError(f"the caches are on device {dev}, the current device is {_current_device()}")
     return dev, table[0], shape[0], shape[1], shape[2] * 2 // 17, table[1]
 
 
 def _same_device(t, dev, name):
-    if t is not None and t.get_device() != dev:
+    if t.get_device() != dev:
         raise MoltError(f"{name} must be a GPU tensor on device {dev}, the caches', is on {t.device}")
 
 
-def _rows_stride(t, dtype, T, H, D, name):
+def _kvq_lens(lens, B, dev):
+    """Address of lens, or None."""
+    if lens is None:
+        return None
+    _dev(lens, torch.int32, (B,), "lens")
+    _same_device(lens, dev, "lens")
+    return lens.data_ptr()
+
+
+def _rows_stride(t, dtype, T, H, D, dev, name):
     """Row stride (elements) of rows [T, H, D] whose heads are contiguous, e.g. a slice of fused QKV rows."""
     if t.dtype is not dtype:
         raise MoltError(f"{name} has dtype {t.dtype}, expected {dtype}")
@@ -402,41 +412,43 @@ def _rows_stride(t, dtype, T, H, D, name):
     row, head, dim = t.stride()
     if dim != 1 or (H > 1 and head != D) or (T > 1 and row < H * D):
         raise MoltError(f"{name} must have contiguous heads in rows that do not overlap, strides are {t.stride()}")
+    _same_device(t, dev, name)
     return row if T > 1 else H * D
 
 
 def kvq_write(k, v, k_cache, v_cache, block_tables, context_lens, n, lens=None):
     """Writes rows k, v [B*n, Hkv, D] (f32|bf16; row-strided views will do) into the 4-bit cache at
     positions context_lens[b] + j, j < n (j < lens[b] if given)."""
-    lib = load()
+    lib = _lib or load()
     dev, B, nb, Hkv, D, maxb = _kvq_caches(k_cache, v_cache, block_tables, context_lens)
     dt = k.dtype
     if dt is not torch.bfloat16 and dt is not torch.float32:
         raise MoltError(f"k has dtype {dt}, expected float32 or bfloat16")
-    ks, vs = _rows_stride(k, dt, B * n, Hkv, D, "k"), _rows_stride(v, dt, B * n, Hkv, D, "v")
-    _dev(lens, torch.int32, (B,), "lens")
-    for t, name in ((k, "k"), (v, "v"), (lens, "lens")):
-        _same_device(t, dev, name)
-    _check(lib.molt_kvq_write(_ptr(k), _ptr(v), ks, vs, _ptr(k_cache), _ptr(v_cache), _ptr(block_tables),
-                              _ptr(context_lens), _ptr(lens), B, n, Hkv, D, maxb, nb, DTYPE_CODE[dt],
-                              _raw_stream(dev)), "molt_kvq_write")
+    ks, vs = _rows_stride(k, dt, B * n, Hkv, D, dev, "k"), _rows_stride(v, dt, B * n, Hkv, D, dev, "v")
+    status = lib.molt_kvq_write(k.data_ptr(), v.data_ptr(), ks, vs, k_cache.data_ptr(), v_cache.data_ptr(),
+                                block_tables.data_ptr(), context_lens.data_ptr(), _kvq_lens(lens, B, dev), B, n,
+                                Hkv, D, maxb, nb, DTYPE_CODE[dt], _raw_stream(dev))
+    if status:
+        _check(status, "molt_kvq_write")
 
 
 def kvq_read(k_cache, v_cache, block_tables, starts, n, lens=None, dtype=torch.bfloat16):
     """Positions starts[b] + j, j < n, of the 4-bit cache as (k, v) [B*n, Hkv, D] of dtype (bf16|f32); rows
     j >= lens[b], and rows without a place in the table, are zeros."""
-    lib = load()
+    lib = _lib or load()
     dev, B, nb, Hkv, D, maxb = _kvq_caches(k_cache, v_cache, block_tables, starts)
     if dtype is not torch.bfloat16 and dtype is not torch.float32:
         raise MoltError(f"dtype is {dtype}, expected float32 or bfloat16")
-    _dev(lens, torch.int32, (B,), "lens")
-    _same_device(lens, dev, "lens")
     if n < 1:
         raise MoltError(f"n = {n} must be >= 1")
+    lens = _kvq_lens(lens, B, dev)
     k = torch.empty(B * n, Hkv, D, dtype=dtype, device=k_cache.device)
-    v = torch.empty(B * n, Hkv, D, dtype=dtype, device=k_cache.device)
-    _check(lib.molt_kvq_read(_ptr(k_cache), _ptr(v_cache), _ptr(block_tables), _ptr(starts), _ptr(lens), B, n,
-                             Hkv, D, maxb, nb, DTYPE_CODE[dtype], _ptr(k), _ptr(v), _raw_stream(dev)), "molt_kvq_read")
+    v = torch.empty_like(k)
+    status = lib.molt_kvq_read(k_cache.data_ptr(), v_cache.data_ptr(), block_tables.data_ptr(), starts.data_ptr(),
+                               lens, B, n, Hkv, D, maxb, nb, DTYPE_CODE[dtype], k.data_ptr(), v.data_ptr(),
+                               _raw_stream(dev))
+    if status:
+        _check(status, "molt_kvq_read")
     return k, v
 
 
@@ -446,32 +458,32 @@ def paged_attention_kvq_workspace_size(B, k, n_q_heads, n_kv_heads, head_dim, ma
 
 def paged_attention_kvq(q, k_cache, v_cache, block_tables, context_lens, k, workspace=None):
     """paged_attention over a 4-bit cache: q [B*(1+k), Hq, D] (f32|bf16); returns [T, Hq*D] of q's dtype."""
-    lib = load()
+    lib = _lib or load()
     dev, B, nb, Hkv, D, maxb = _kvq_caches(k_cache, v_cache, block_tables, context_lens)
-    dt = q.dtype
+    dt, shape = q.dtype, q.shape
     if dt is not torch.bfloat16 and dt is not torch.float32:
         raise MoltError(f"q has dtype {dt}, expected float32 or bfloat16")
-    if q.dim() != 3:
-        raise MoltError(f"q has shape {tuple(q.shape)}, expected [B*(1+k), Hq, D]")
-    Hq = q.shape[1]
-    _dev(q, None, (B * (k + 1), Hq, D), "q")
+    if len(shape) != 3:
+        raise MoltError(f"q has shape {tuple(shape)}, expected [B*(1+k), Hq, D]")
+    T, Hq, _ = shape
+    if T != B * (k + 1) or shape[2] != D or not q.is_contiguous():
+        _dev(q, None, (B * (k + 1), Hq, D), "q")
     _same_device(q, dev, "q")
-    _same_device(workspace, dev, "workspace")
-    if workspace is not None and not workspace.is_contiguous():
-        raise MoltError("workspace must be contiguous")
-    out = torch.empty(q.shape[0], Hq * D, dtype=dt, device=q.device)
-
-    def call(ws, have):
-        return lib.molt_paged_attention_kvq(_ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(block_tables),
-                                            _ptr(context_lens), B, k, Hq, Hkv, D, maxb, nb, DTYPE_CODE[dt],
-                                            _ptr(out), _ptr(ws), have, _raw_stream(dev))
-
-    status = MOLT_ERR_WORKSPACE
+    ws, have = None, 0
     if workspace is not None:
-        status = call(workspace, workspace.numel() * workspace.element_size())
+        _same_device(workspace, dev, "workspace")
+        if not workspace.is_contiguous():
+            raise MoltError("workspace must be contiguous")
+        ws, have = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    out = q.new_empty(T, Hq * D)
+    args = (q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_tables.data_ptr(), context_lens.data_ptr(),
+            B, k, Hq, Hkv, D, maxb, nb, DTYPE_CODE[dt], out.data_ptr())
+    status = lib.molt_paged_attention_kvq(*args, ws, have, _raw_stream(dev))
     if status == MOLT_ERR_WORKSPACE:     # none, or one that is too small
-        status = call(*_workspace(lib.molt_paged_attention_kvq_workspace_size(B, k, Hq, Hkv, D, maxb), q.device))
-    _check(status, "molt_paged_attention_kvq")
+        own, have = _workspace(lib.molt_paged_attention_kvq_workspace_size(B, k, Hq, Hkv, D, maxb), q.device)
+        status = lib.molt_paged_attention_kvq(*args, _ptr(own), have, _raw_stream(dev))
+    if status:
+        _check(status, "molt_paged_attention_kvq")
     return out
 
 
