@@ -6,6 +6,25 @@
 // bf16 parts (24 bits); in bf16 one, with the sum taken of the rounded weights, by an MFMA with a row of ones.
 // That adds a rounding like the output's own: rms error 2.07e-3 of the output's rms against 1.66e-3 with two
 // parts, for which 128 sequences x 5 positions at context 8192 took 178 us, with one 135.
+//
+// A workgroup has one kv head of a sequence, or of a part of its keys, and a group of up to 48 rows. Each of its
+// wavefronts walks a range of pairs of 16-token blocks by itself, with running maxima and sums, and they join at the
+// end: no barrier in the loop, and each record byte is read once per row group. The records come by LDS-DMA three
+// pairs ahead (into registers they spilled: 257 us for the first call below). K goes into a scaled MFMA as it lies there
+// (255 us with K decoded to bf16, so 208, both before the DMA), V is decoded to bf16: its scale belongs to a token, the
+// product's sum index. The next pair's scores are computed beside this pair's weights and values.
+//
+// 32 query / 4 kv heads x 128, bf16, what bounds the call and what it takes:
+//   128 sequences x 5 positions at 8192: the records' 571 MB, 122 us, 4.7 TB/s (a large copy: 4.96; read requests 1.02
+//     times the records); VALU 64% and MFMA 39% of the cycles
+//   256 x 9 at 2048: 72 rows in groups of 3 and 2 tiles, the keys read twice (once through the L2), VALU issue, 148 us
+//   2 x 257 at 8100: 68 GFLOP in 344 workgroups where 512 fit, VALU issue, 114 us, 590 TFLOP/s
+//   16 x 5 at 32768-65536, cut: 428 MB in 99 us, 4.3 TB/s, and 4.7 for the join
+//   1 x 1 at 700: launch, four dependent loads and the join, 7.6 us
+// A loop iteration is 38 MFMAs and 300 VALU instructions at 3 tiles (of them 24 exp2 and 64 for the decoded values);
+// two wavefronts a SIMD, by registers, leave its time near the sum of both pipes. Tried: 5 tiles and one wavefront a
+// SIMD, so that 72 rows read keys once (185 us); 64 keys an iteration (125 of the first line); 3 slots (128);
+// MFMA and VALU interleaved by schedule groups (123-139); a persistent loop over workgroups (146).
 #include <algorithm>
 #include <cmath>
 

@@ -40,6 +40,9 @@ MOLT_DEV void store8(float* p, const uint32_t (&v)[4]) {
 
 // Both kernels: wavefront = one block of one sequence, and one kv head of 128 dims or two of 64, its keys and its
 // values. The block's place is found once, on the scalar unit, and all of a wavefront's loads are in flight together.
+// Bound by HBM, or by the launch and three dependent loads where there is little: 4 kv heads x 128, bf16, 128 sequences
+// x 5 rows written in 4.7 us and read in 3.7; f32, 4000 rows written in 5.8 us (18.6 MB, 3.2 TB/s) and 6000 read, a third
+// of them zeros, in 9.4; 144000 bf16 rows read, of 262144 with the zeros behind, in 123 us (5.0 TB/s; a large copy: 4.96).
 // Keys: instruction i, lane: an octet of dims of one token, 16 contiguous bytes of a bf16 row and 4 of the cache;
 // values: the lane has an octet of dims of the 4 tokens that share its 16 bytes of the cache.
 template <int D>
