@@ -78,20 +78,28 @@ MOLT_DEV int visible_end(const KvqAttnParams& p, int ctx, int r1) {
 typedef const __attribute__((address_space(1))) void* GlobalPtr;
 typedef __attribute__((address_space(3))) void* LdsPtr;
 template <bool ONCE>
-MOLT_DEV void copy_lds16(const uint8_t* src, uint8_t* dst) {
-  if constexpr (ONCE) __builtin_amdgcn_global_load_lds((GlobalPtr)src, (LdsPtr)dst, 16, 0, 2);
-  else __builtin_amdgcn_global_load_lds((GlobalPtr)src, (LdsPtr)dst, 16, 0, 0);
+MOLT_DEV void copy_lds16(const uint8_t* src, uint32_t dst) {
+  if constexpr (ONCE) __builtin_amdgcn_global_load_lds((GlobalPtr)src, (LdsPtr)uintptr_t(dst), 16, 0, 2);
+  else __builtin_amdgcn_global_load_lds((GlobalPtr)src, (LdsPtr)uintptr_t(dst), 16, 0, 0);
 }
 template <bool ONCE>
-MOLT_DEV void copy_lds4(const uint8_t* src, uint8_t* dst) {
-  if constexpr (ONCE) __builtin_amdgcn_global_load_lds((GlobalPtr)src, (LdsPtr)dst, 4, 0, 2);
-  else __builtin_amdgcn_global_load_lds((GlobalPtr)src, (LdsPtr)dst, 4, 0, 0);
+MOLT_DEV void copy_lds4(const uint8_t* src, uint32_t dst) {
+  if constexpr (ONCE) __builtin_amdgcn_global_load_lds((GlobalPtr)src, (LdsPtr)uintptr_t(dst), 4, 0, 2);
+  else __builtin_amdgcn_global_load_lds((GlobalPtr)src, (LdsPtr)uintptr_t(dst), 4, 0, 0);
 }
 
-// a wave-uniform value the compiler is to hold in scalar registers
-MOLT_DEV long uniform(long x) {
+// a wave-uniform value in scalar registers, whatever the compiler would make of how it came about
+MOLT_DEV uint32_t in_sgpr(uint32_t x) {
+  x = __builtin_amdgcn_readfirstlane(int(x));
+  asm("" : "+s"(x));
+  return x;
+}
+MOLT_DEV const uint8_t* in_sgpr(const uint8_t* p) {
+  const uint64_t x = reinterpret_cast<uint64_t>(p);
   const uint32_t lo = __builtin_amdgcn_readfirstlane(int(x)), hi = __builtin_amdgcn_readfirstlane(int(x >> 32));
-  return long(uint64_t(hi) << 32 | lo);
+  p = reinterpret_cast<const uint8_t*>(uint64_t(hi) << 32 | lo);
+  asm("" : "+s"(p));
+  return p;
 }
 
 // x as P bf16 values whose sum is x to 8 P bits
@@ -332,6 +340,7 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
   const int p0 = s0 + each * wave + min(wave, more), p1 = p0 + each + (wave < more ? 1 : 0);
   const int full_end = min(visible_end(p, ctx, r0 + 1), end);    // keys before are seen by every row
   uint8_t* ring = lds + wave * kLds;
+  const uint32_t ring_at = uint32_t(uintptr_t((LdsPtr)ring));     // its LDS address
   uint8_t* qlds = lds + W * kLds;
 
   // Copies of a pair into a slot of the wavefront's ring: [K codes of both blocks][V codes][scales of K, of
@@ -344,15 +353,15 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
   const uint32_t spart = lane / SR % 4;
   const uint8_t* sbase = (spart < 2 ? p.kc : p.vc) + Rec::kCodes + lane % SR * 4;
   auto issue = [&](int pi, const int (&id)[2]) __attribute__((always_inline)) {
-    uint8_t* dst = ring + (pi - p0) % kSlots * SLOT;
-    long rec[2];                         // kept in scalar registers: a uniform base and a lane offset per copy
+    const uint32_t dst = in_sgpr(ring_at + uint32_t(pi - p0) % kSlots * SLOT);
+    long rec[2];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) rec[u] = uniform((long(unsigned(id[u]) < unsigned(p.num_blocks) ? id[u] : 0) * p.Hkv + h) * Rec::kBytes);
-    if constexpr (D == 128) {
+    for (int u = 0; u < 2; ++u) rec[u] = (long(unsigned(id[u]) < unsigned(p.num_blocks) ? id[u] : 0) * p.Hkv + h) * Rec::kBytes;
+    if constexpr (D == 128) {            // a base in scalar registers and a lane offset per copy
 #pragma unroll
-      for (int u = 0; u < 2; ++u) copy_lds16<ONCE>(p.kc + rec[u] + ksrc, dst + 1024 * u);
+      for (int u = 0; u < 2; ++u) copy_lds16<ONCE>(in_sgpr(p.kc + rec[u]) + ksrc, dst + 1024 * u);
 #pragma unroll
-      for (int u = 0; u < 2; ++u) copy_lds16<ONCE>(p.vc + rec[u] + vsrc, dst + 2048 + 1024 * u);
+      for (int u = 0; u < 2; ++u) copy_lds16<ONCE>(in_sgpr(p.vc + rec[u]) + vsrc, dst + 2048 + 1024 * u);
     } else {
       const long r = lane < 32 ? rec[0] : rec[1];
       copy_lds16<ONCE>(p.kc + r + ksrc, dst);
@@ -411,10 +420,9 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
     lds_barrier();
   }
   floatx4_t o[NT][DT], ls[NT];           // O^T; the rows' sums (bf16: by MFMA, the same in every register and group)
-  float m[NT];                           // reference maximum (of raw scores)
+  float m[NT];                           // reference maximum (of scores in log2 units)
   float ref[NT];                         // m, or 0 for a row that has seen no key: its exp2(-inf) is 0
   float bound[NT];                       // scores above it raise m
-  const float slack = kRescaleSlack / p.c;
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
     m[i] = bound[i] = -INFINITY;
@@ -478,7 +486,20 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
   };
 
   // What follows a pair's scores: masks where a row may not see a key, and the reference maxima.
-  auto settle = [&](int pi, bool ok0, bool ok1, floatx4_t (&sv)[2][NT], uint32_t (&vs)[2]) __attribute__((always_inline)) {
+  auto settle = [&](int pi, bool ok0, bool ok1, const floatx4_t (&raw)[2][NT], floatx4_t (&sv)[2][NT],
+                    uint32_t (&vs)[2]) __attribute__((always_inline)) {
+    float mx[NT];
+    auto maxima = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+        mx[i] = fmaxf(fmaxf(fmaxf(sv[0][i][0], sv[0][i][1]), fmaxf(sv[0][i][2], sv[0][i][3])),
+                      fmaxf(fmaxf(sv[1][i][0], sv[1][i][1]), fmaxf(sv[1][i][2], sv[1][i][3])));
+    };
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < NT; ++i) sv[u][i] = raw[u][i] * p.c;
+    maxima();                            // beside the products, which the compiler knows to need no quieting
     if (32 * pi + 32 > full_end || !ok0 || !ok1) {
       // Keys that some row may not see: their scores are -inf for it, and their values must not reach it.
       // A probability of 0 does that, unless the value is NaN (scale byte 255, also in slots that were
@@ -517,22 +538,18 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
 #pragma unroll
           for (int t = 0; t < DT; ++t) o[i][t] += poison[i] ? __builtin_nanf("") : 0.f;
       }
+      maxima();
     }
-    float mx[NT];
     bool grow = false;
 #pragma unroll
-    for (int i = 0; i < NT; ++i) {
-      mx[i] = fmaxf(fmaxf(fmaxf(sv[0][i][0], sv[0][i][1]), fmaxf(sv[0][i][2], sv[0][i][3])),
-                    fmaxf(fmaxf(sv[1][i][0], sv[1][i][1]), fmaxf(sv[1][i][2], sv[1][i][3])));
-      grow |= mx[i] > bound[i];
-    }
+    for (int i = 0; i < NT; ++i) grow |= mx[i] > bound[i];
     if (__ballot(grow)) {
 #pragma unroll
       for (int i = 0; i < NT; ++i) {
         const float mn = fmaxf(m[i], rows_max4(mx[i]));
-        const float alpha = m[i] == -INFINITY ? 0.f : exp2f((m[i] - mn) * p.c);
+        const float alpha = m[i] == -INFINITY ? 0.f : exp2f(m[i] - mn);
         m[i] = mn;
-        bound[i] = mn + slack;
+        bound[i] = mn + kRescaleSlack;
         ref[i] = mn == -INFINITY ? 0.f : mn;
         ls[i] *= alpha;
 #pragma unroll
@@ -552,8 +569,9 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
   if (p0 < p1) {
     if (p0 + kSlots - 2 < p1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kSlots - 2) * kCopies) : "memory");
     else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    scores(p0, sv, vs);
-    settle(p0, have >> (2 * kSlots - 4) & 1u, have >> (2 * kSlots - 4) & 2u, sv, vs);
+    floatx4_t raw[2][NT];
+    scores(p0, raw, vs);
+    settle(p0, have >> (2 * kSlots - 4) & 1u, have >> (2 * kSlots - 4) & 2u, raw, sv, vs);
   }
   for (int pi = p0; pi < p1; ++pi) {
     arrive(pi + 1);
@@ -574,7 +592,7 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float w = __builtin_amdgcn_exp2f((sv[u][i][e] - ref[i]) * p.c);
+          const float w = __builtin_amdgcn_exp2f(sv[u][i][e] - ref[i]);
           if constexpr (F32) ps += w;
           __bf16 part[PP];
           split_bf16<PP>(w, part);
@@ -627,13 +645,9 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
         for (int q = 0; q < PP; ++q) o[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[i][q], o[i][t], 0, 0, 0);
     }
     __builtin_amdgcn_s_setprio(0);
-    if (pi + 1 < p1) settle(pi + 1, have >> (2 * kSlots - 4) & 1u, have >> (2 * kSlots - 4) & 2u, nsv, nvs);
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      vs[u] = nvs[u];
-#pragma unroll
-      for (int i = 0; i < NT; ++i) sv[u][i] = nsv[u][i];
-    }
+    if (pi + 1 < p1) settle(pi + 1, have >> (2 * kSlots - 4) & 1u, have >> (2 * kSlots - 4) & 2u, nsv, sv, nvs);
+    vs[0] = nvs[0];
+    vs[1] = nvs[1];
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no copy may outlive the ring
 
@@ -684,7 +698,7 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
     for (int w = 0; w < W; ++w) {
       const float* pw = part + w * (kLds / 4);
       const float mw = pw[16 * RS + row];
-      const float f = mw == -INFINITY ? 0.f : exp2f((mw - M) * p.c);
+      const float f = mw == -INFINITY ? 0.f : exp2f(mw - M);
       L += pw[16 * RS + 16 + row] * f;
       a[0] += *reinterpret_cast<const floatx4_t*>(pw + row * RS + d0) * f;
       a[1] += *reinterpret_cast<const floatx4_t*>(pw + row * RS + d0 + 4) * f;
@@ -759,14 +773,14 @@ __global__ __launch_bounds__(256) void kvq_merge_kernel(KvqAttnParams p) {
     for (int u = 0; u < kU; ++u) mn = fmaxf(mn, ml[u].x);
     // what has no maximum has seen no key, or NaN only: its factor is 0, its sum 0 or NaN
     const float ref = mn == -INFINITY ? 0.f : mn;
-    const float f0 = exp2f((M - ref) * p.c);
+    const float f0 = exp2f(M - ref);
     M = mn;
     L *= f0;
     a *= f0;
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
       const bool live = s0 + u * P < sp.y;
-      const float f = exp2f((ml[u].x - ref) * p.c);
+      const float f = exp2f(ml[u].x - ref);
       L += live ? ml[u].y * f : 0.f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) a[e] += live ? o[u][e] * f : 0.f;
@@ -786,7 +800,7 @@ __global__ __launch_bounds__(256) void kvq_merge_kernel(KvqAttnParams p) {
     a = floatx4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int u = 0; u < P; ++u) {
-      const float f = exp2f((stat[u].x - ref) * p.c);
+      const float f = exp2f(stat[u].x - ref);
       L += stat[u].y * f;
       a += sum[u * O + d] * f;
     }
