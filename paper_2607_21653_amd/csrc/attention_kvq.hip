@@ -102,6 +102,12 @@ MOLT_DEV const uint8_t* in_sgpr(const uint8_t* p) {
   return p;
 }
 
+// x, which the compiler is not to extend to 64 bits elsewhere: an offset beside a scalar base
+MOLT_DEV uint32_t here(uint32_t x) {
+  asm("" : "+v"(x));
+  return x;
+}
+
 // x as P bf16 values whose sum is x to 8 P bits
 template <int P>
 MOLT_DEV void split_bf16(float x, __bf16 (&part)[P]) {
@@ -352,6 +358,7 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
   const uint32_t vsrc = D == 128 ? lane * 16 : lane % 32 * 16;
   const uint32_t spart = lane / SR % 4;
   const uint8_t* sbase = (spart < 2 ? p.kc : p.vc) + Rec::kCodes + lane % SR * 4;
+  asm("" : "+v"(sbase));                 // (or the constant is added at every copy)
   auto issue = [&](int pi, const int (&id)[2]) __attribute__((always_inline)) {
     const uint32_t dst = in_sgpr(ring_at + uint32_t(pi - p0) % kSlots * SLOT);
     long rec[2];
@@ -359,9 +366,9 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
     for (int u = 0; u < 2; ++u) rec[u] = (long(unsigned(id[u]) < unsigned(p.num_blocks) ? id[u] : 0) * p.Hkv + h) * Rec::kBytes;
     if constexpr (D == 128) {            // a base in scalar registers and a lane offset per copy
 #pragma unroll
-      for (int u = 0; u < 2; ++u) copy_lds16<ONCE>(in_sgpr(p.kc + rec[u]) + ksrc, dst + 1024 * u);
+      for (int u = 0; u < 2; ++u) copy_lds16<ONCE>(in_sgpr(p.kc + rec[u]) + here(ksrc), dst + 1024 * u);
 #pragma unroll
-      for (int u = 0; u < 2; ++u) copy_lds16<ONCE>(in_sgpr(p.vc + rec[u]) + vsrc, dst + 2048 + 1024 * u);
+      for (int u = 0; u < 2; ++u) copy_lds16<ONCE>(in_sgpr(p.vc + rec[u]) + here(vsrc), dst + 2048 + 1024 * u);
     } else {
       const long r = lane < 32 ? rec[0] : rec[1];
       copy_lds16<ONCE>(p.kc + r + ksrc, dst);
@@ -492,8 +499,8 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
     auto maxima = [&]() __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < NT; ++i)
-        mx[i] = fmaxf(fmaxf(fmaxf(sv[0][i][0], sv[0][i][1]), fmaxf(sv[0][i][2], sv[0][i][3])),
-                      fmaxf(fmaxf(sv[1][i][0], sv[1][i][1]), fmaxf(sv[1][i][2], sv[1][i][3])));
+        mx[i] = fmaxf(fmaxf(fmaxf(fmaxf(sv[0][i][0], sv[0][i][1]), sv[0][i][2]), fmaxf(fmaxf(sv[0][i][3], sv[1][i][0]), sv[1][i][1])),
+                      fmaxf(sv[1][i][2], sv[1][i][3]));
     };
 #pragma unroll
     for (int u = 0; u < 2; ++u)
@@ -580,7 +587,7 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
     ids(pi + kSlots, nid);
     // scores of the next pair (past the last: of whatever its slot holds, not used), beside the
     // probabilities and values of this one
-    __builtin_amdgcn_s_setprio(1);
+    __builtin_amdgcn_s_setprio(0);
     floatx4_t nsv[2][NT];
     uint32_t nvs[2];
     scores(pi + 1, nsv, nvs);
@@ -644,7 +651,9 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
 #pragma unroll
         for (int q = 0; q < PP; ++q) o[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[i][q], o[i][t], 0, 0, 0);
     }
-    __builtin_amdgcn_s_setprio(0);
+    // the stretch without MFMAs goes first, so that the other wavefront's run beside it (2 x 257 positions at 8100: 102
+    // us, 104 with these two the other way round, 111 without)
+    __builtin_amdgcn_s_setprio(1);
     if (pi + 1 < p1) settle(pi + 1, have >> (2 * kSlots - 4) & 1u, have >> (2 * kSlots - 4) & 2u, nsv, sv, nvs);
     vs[0] = nvs[0];
     vs[1] = nvs[1];
