@@ -14,17 +14,18 @@
 // (255 us with K decoded to bf16, so 208, both before the DMA), V is decoded to bf16: its scale belongs to a token, the
 // product's sum index. The next pair's scores are computed beside this pair's weights and values.
 //
-// 32 query / 4 kv heads x 128, bf16, what bounds the call and what it takes:
-//   128 sequences x 5 positions at 8192: the records' 571 MB, 122 us, 4.7 TB/s (a large copy: 4.96; read requests 1.02
-//     times the records); VALU 64% and MFMA 39% of the cycles
-//   256 x 9 at 2048: 72 rows in groups of 3 and 2 tiles, the keys read twice (once through the L2), VALU issue, 148 us
-//   2 x 257 at 8100: 68 GFLOP in 344 workgroups where 512 fit, VALU issue, 114 us, 590 TFLOP/s
-//   16 x 5 at 32768-65536, cut: 428 MB in 99 us, 4.3 TB/s, and 4.7 for the join
-//   1 x 1 at 700: launch, four dependent loads and the join, 7.6 us
-// A loop iteration is 38 MFMAs and 300 VALU instructions at 3 tiles (of them 24 exp2 and 64 for the decoded values);
-// two wavefronts a SIMD, by registers, leave its time near the sum of both pipes. Tried: 5 tiles and one wavefront a
-// SIMD, so that 72 rows read keys once (185 us); 64 keys an iteration (125 of the first line); 3 slots (128);
-// MFMA and VALU interleaved by schedule groups (123-139); a persistent loop over workgroups (146).
+// 32 query / 4 kv heads x 128, bf16, what bounds the call and what it takes on new inputs:
+//   128 sequences x 5 positions at 8192: the records' 571 MB, 125 us, 4.6 TB/s (a large copy: 4.96; read requests 1.02
+//     times the records); VALU 59% and MFMA 42% of the cycles
+//   256 x 9 at 2048: 72 rows in groups of 3 and 2 tiles, the keys read twice (once through the L2), VALU and MFMA, 125 us
+//   2 x 257 at 8100: 68 GFLOP in 344 workgroups where 512 fit, VALU and MFMA, 91 us, 750 TFLOP/s
+//   16 x 5 at 32768-65536, cut: 429 MB in 101 us with the join's 5, 4.2 TB/s
+//   1 x 1 at 700: launch, four dependent loads and the join, 7 us
+// A loop iteration is 39 MFMAs and 207 VALU instructions at 3 tiles (of them 24 exp2 and 64 for the decoded values);
+// two wavefronts a SIMD, by registers, leave its time near the sum of both pipes. Tried, where the first line took 122
+// us: 5 tiles and one wavefront a SIMD, so that 72 rows read keys once (second, from 148); 64 keys an iteration
+// (125); 3 slots (128); MFMA and VALU interleaved by schedule groups (123-139); a persistent loop over workgroups (second
+// line 146); exponentials, scores and values in other orders (all within 3%).
 #include <algorithm>
 #include <cmath>
 
