@@ -872,8 +872,10 @@ void launch_w(const KvqAttnParams& p, unsigned grid, hipStream_t s) {
 template <int D, typename T, int NT>
 void launch_nt(const KvqAttnParams& p, hipStream_t s) {
   const long units = p.spread ? (long(p.slots) + 7) / 8 * 8 * p.Hkv : (long(p.slots) * p.Hkv + 7) / 8 * 8;
-  if (p.nrg > 1) launch_w<D, T, NT, false>(p, unsigned(units * p.nrg), s);
-  else launch_w<D, T, NT, true>(p, unsigned(units), s);
+  if constexpr (NT > 1 || sizeof(T) == 4) {      // (one tile of a bf16 row group is all there is)
+    if (p.nrg > 1) return launch_w<D, T, NT, false>(p, unsigned(units * p.nrg), s);
+  }
+  launch_w<D, T, NT, true>(p, unsigned(units), s);
 }
 
 template <int D, typename T>

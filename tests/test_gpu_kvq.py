@@ -224,6 +224,53 @@ def test_attention(molt_lib, dtype, B, k, Hq, Hkv, D, lo, hi):
     assert (err <= _tol(want, mag, dtype)).all()
 
 
+def _dense_check(molt, rng, ctx, k, Hq, Hkv, D, dtype):
+    """Sequences of random rows written and attended over, against a dense softmax of the rows read back. Blocks and
+    slots of no row hold NaN."""
+    B, n = len(ctx), k + 1
+    maxb = (max(ctx) + n + 15) // 16 + 1
+    tables = _t(rng.permutation(B * maxb + 3)[:B * maxb].reshape(B, maxb).astype(np.int32))
+    gk = torch.full((B * maxb + 3, Hkv, 17 * D // 2), 0xFF, dtype=torch.uint8, device="cuda")
+    gv = gk.clone()
+    zero = torch.zeros(1, dtype=torch.int32, device="cuda")
+    K, V = [], []
+    for b in range(B):
+        L, row = int(ctx[b]) + n, tables[b:b + 1]
+        molt.kvq_write(*(torch.from_numpy(rng.standard_normal((L, Hkv, D), np.float32)).cuda() for _ in range(2)),
+                       gk, gv, row, zero, L)
+        for x, to in zip(molt.kvq_read(gk, gv, row, zero, L, dtype=torch.float32), (K, V)):
+            to.append(x.double().cpu().numpy())
+    q, q64 = _rows(rng, B * n, Hq, D, dtype)
+    out = molt.paged_attention_kvq(q.cuda(), gk, gv, tables, _t(np.array(ctx, np.int32)), k).double().cpu().numpy()
+    out = out.reshape(B, n, Hkv, Hq // Hkv, D)
+    q64 = q64.reshape(out.shape)
+    for b in range(B):
+        score = np.einsum("jhgd,phd->jhgp", q64[b], K[b]) / np.sqrt(D)
+        seen = np.arange(len(K[b]))[None] <= ctx[b] + np.arange(n)[:, None]
+        w = np.where(seen[:, None, None], np.exp(score - score.max(axis=-1, keepdims=True)), 0.0)
+        w /= w.sum(axis=-1, keepdims=True)
+        want, mag = (np.einsum("jhgp,phd->jhgd", w, x) for x in (V[b], np.abs(V[b])))
+        assert (np.abs(out[b] - want) <= _tol(want, mag, dtype)).all()
+
+
+@pytest.mark.parametrize("lo,hi", [(0, 7), (33, 60), (150, 280), (2500, 3000)])
+@pytest.mark.parametrize("Hq,k", [(4, 0), (10, 3), (8, 9), (24, 4), (30, 4)])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_of_every_size(molt_lib, dtype, D, Hq, k, lo, hi):
+    """2, 20, 40, 60 and 75 rows of a kv head over short, middling and long key ranges and ones that are cut."""
+    _dense_check(molt_lib, np.random.default_rng(41), [lo, (lo + hi) // 2, hi], k, Hq, 2, D, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_two_long_sequences_among_many(molt_lib, dtype, D):
+    """70 sequences of which two are cut: few parts for most, joined by a thread each."""
+    ctx = [i % 90 for i in range(70)]
+    ctx[13] = ctx[69] = 3900
+    _dense_check(molt_lib, np.random.default_rng(43), ctx, 1, 6, 2, D, dtype)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("D", [64, 128])
 def test_large_scores(molt_lib, dtype, D):
