@@ -38,7 +38,10 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kRescaleSlack = 8.0f;   // probabilities may grow to 2^8 before O is rescaled
 constexpr int kWaves = 4;
-constexpr int kSlots = 4;               // pairs of blocks in a wavefront's ring
+// Pairs of blocks in a wavefront's ring. Workgroups of one wavefront are bound by how many fit in LDS: 201 sequences x
+// 180 positions x 8 heads at 0-404 took 138 us with 4, 109 with 3; the others wait for memory (122 us with 4, 128 with
+// 3 for the first call above).
+constexpr int slots_of(int wavefronts) { return wavefronts == 1 ? 3 : 4; }
 
 struct KvqAttnParams {
   const void* q;           // [B * n, Hq, D]
@@ -293,9 +296,10 @@ MOLT_DEV Share find_share(const KvqAttnParams& p, int r1, int slot, float* lds) 
   return w;
 }
 
-// bytes of LDS: the wavefronts' rings of kSlots pairs, later their results; the query operands (bf16)
+// bytes of LDS: the wavefronts' rings, later their results; the query operands (bf16)
 template <int D, typename T, int NT, int W>
 struct Lds {
+  static constexpr int kSlots = slots_of(W);
   static constexpr int kPair = 32 * D + 256;                  // bytes of a pair in the ring
   static constexpr int kJoin = (16 * (D + 4) + 32) * 4;       // a wavefront's results of one tile
   static constexpr int kWaveBytes = kSlots * kPair > kJoin ? kSlots * kPair : kJoin;
@@ -308,6 +312,7 @@ template <int D, typename T, int NT, bool ONCE, int W>
 MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h, int slot, const Share& w) {
   typedef KvqRecord<D> Rec;
   constexpr bool F32 = sizeof(T) == 4;
+  constexpr int kSlots = slots_of(W);
   constexpr int QP = 3;                  // bf16 parts of an f32 query element
   constexpr int PP = F32 ? 3 : 1;        // bf16 parts of a probability (see the top)
   constexpr int KS = D / 32;             // MFMA steps over the dims of a score
@@ -830,7 +835,7 @@ constexpr int kMaxTiles = 3;             // 16-row tiles of a wavefront (bf16; o
 constexpr int kMinCut = 24, kFew = 256;
 // Wavefronts of an uncut workgroup, 1, 4 or 8: the fewer, the more workgroups run at a time and the less there is to
 // join, the more, the sooner a long key range is done. The rule weighs rounds of workgroups by what one takes; us of
-// calls with 1, 4 and 8: 19844 workgroups of up to 9 pairs (f32) 115, 256 and 544; 2016 of 1 pair (2.5 tiles) 27, 36
+// calls with 1, 4 and 8: 19844 workgroups of up to 9 pairs (f32) 108, 256 and 544; 2016 of 1 pair (2.5 tiles) 26, 36
 // and 75; 1584 of 49 pairs (3 tiles) 167, 120 and 145; 48 of 32 pairs (f32) 35, 19.6 and 14.6; 8 of 4 pairs (3 tiles)
 // 12.7, 9.4 and 10.6.
 constexpr int kMoreWaves = 8;
@@ -851,7 +856,7 @@ void kvq_plan(KvqAttnParams& p, int D, bool f32) {
   p.waves = kWaves;
   if (p.slots == p.B) {
     // how many workgroups run at a time, and the us of one
-    const int mem = kSlots * (32 * D + 256) + (f32 ? 0 : D / 64 * 2048 * nt);   // Lds of one wavefront
+    const int mem = slots_of(1) * (32 * D + 256) + (f32 ? 0 : D / 64 * 2048 * nt);   // Lds of one wavefront
     const double at_once[3] = {256.0 * std::min(8, 163840 / mem), double(p.resident), 256.0};
     const double each[3] = {4.0 + kPairTime * pairs, 7.0 + kPairTime * pairs / 4, 8.2 + kPairTime * pairs / 8};
     double best = 1e30;
