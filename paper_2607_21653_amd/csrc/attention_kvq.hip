@@ -230,7 +230,7 @@ struct Share { int b, part, parts, first; };
 // wavefronts, kPartCost) over the workgroups that are resident, half a part more where they do not all fit at
 // once, and the joining launch (kJoinCost) if anything is cut. Of equal ones the longest c wins.
 constexpr int kMaxCut = 256, kMinPairs = 4;
-constexpr float kJoinCost = 30.f;
+constexpr float kJoinCost = 15.f;       // (73 x 9 positions x 16 heads at 824-1649: 30.0 us, 34.4 with 30; others alike)
 MOLT_DEV float cut(float pairs, float inv_c) { return fmaxf(1.f, ceilf(pairs * inv_c)); }
 
 template <int NT>
@@ -505,7 +505,8 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
     auto maxima = [&]() __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < NT; ++i)
-        mx[i] = fmaxf(fmaxf(fmaxf(fmaxf(sv[0][i][0], sv[0][i][1]), sv[0][i][2]), fmaxf(fmaxf(sv[0][i][3], sv[1][i][0]), sv[1][i][1])),
+        mx[i] = fmaxf(fmaxf(fmaxf(fmaxf(sv[0][i][0], sv[0][i][1]), sv[0][i][2]),
+                            fmaxf(fmaxf(sv[0][i][3], sv[1][i][0]), sv[1][i][1])),
                       fmaxf(sv[1][i][2], sv[1][i][3]));
     };
 #pragma unroll
@@ -676,7 +677,8 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
       for (int e = 0; e < 4; ++e)
 #pragma unroll
         for (int t = 0; t < DT; t += 4)
-          store_out4<T>(p, b, h, r, D, D / 4 * g4 + DT * e + t, floatx4_t{o[i][t][e], o[i][t + 1][e], o[i][t + 2][e], o[i][t + 3][e]}, L);
+          store_out4<T>(p, b, h, r, D, D / 4 * g4 + DT * e + t,
+                        floatx4_t{o[i][t][e], o[i][t + 1][e], o[i][t + 2][e], o[i][t + 3][e]}, L);
     }
     return;
   }
