@@ -113,7 +113,9 @@ def test_tiny_verify_step(molt_lib):
     (3, 4, 32, 4, 128, 5, 400),          # the RoPE-fused projection's head layout, splits of the attention's keys
     (2, 8, 8, 1, 128, 0, 60),            # 72 rows: two row groups
     (2, 20, 8, 4, 64, 30, 47),
-    (1, 2, 8, 2, 128, 1400, 1400),       # a cut key range
+    (1, 2, 8, 2, 128, 1400, 1400),       # a long key range
+    (1, 2, 8, 2, 128, 2200, 2200),       # a cut one
+    (2, 6, 16, 2, 64, 30, 2100),         # one of two cut, 56 rows
 ])
 def test_bf16_layer(molt_lib, B, k, Hq, Hkv, D, lo, hi):
     w = workloads.LAYER_BF16.scaled(batch=B, k=k, n_q_heads=Hq, n_kv_heads=Hkv, head_dim=D, ctx_lo=lo, ctx_hi=hi,
@@ -142,6 +144,51 @@ def test_bf16_layer(molt_lib, B, k, Hq, Hkv, D, lo, hi):
     err = np.abs(xd.cpu().numpy() - want)[same].max()
     print("residual", err, flush=True)
     assert err <= 2e-2
+
+
+def test_captured_layer(molt_lib):
+    """A captured call replayed on other inputs and contexts, eager calls between: the same bits as eager calls."""
+    B, k, Hq, Hkv, D = 2, 3, 8, 2, 128
+    w = workloads.LAYER_BF16.scaled(batch=B, k=k, n_q_heads=Hq, n_kv_heads=Hkv, head_dim=D, ctx_lo=2200, ctx_hi=2300,
+                                    d_model=512, n_experts=16, top_k=4, d_ff=256)
+    layout = workloads.make_kv_layout(w, 5)
+    model = molt_lib.Model([{n: dev(v) for n, v in workloads.make_layer_weights(w, 5, 0).items()}], None, n_q_heads=Hq,
+                           n_kv_heads=Hkv, head_dim=D, top_k=w.top_k, rms_eps=w.rms_eps, rope_theta=w.rope_theta)
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    draw = lambda *shape: torch.randn(*shape, generator=gen, device="cuda")
+    kc, vc = molt_lib.kvq_cache(int(layout.block_tables.max()) + 1, Hkv, D)
+    tables = dev(torch.from_numpy(layout.block_tables))
+    molt_lib.kvq_write(draw(B * 2300, Hkv, D), draw(B * 2300, Hkv, D), kc, vc, tables,
+                       torch.zeros(B, dtype=torch.int32, device="cuda"), 2300)
+    ctx = torch.tensor([2200, 40], dtype=torch.int32, device="cuda")
+    kv = molt_lib.KVCache([kc], [vc], tables, ctx)
+    size = molt_lib.decoder_workspace_size(model, B, k, tables.shape[1]) + kv.extra(model, B, k)
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+    x = torch.zeros(B * (k + 1), w.d_model, device="cuda")
+    inputs = [draw(B * (k + 1), w.d_model) for _ in range(4)]
+    contexts = [torch.tensor(c, dtype=torch.int32, device="cuda") for c in ([2200, 40], [100, 2290], [2250, -4], [0, 7])]
+
+    def step(own=None):
+        molt_lib.decoder_forward(model, kv, B, k, x, workspace=own)
+
+    step(ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(ws)
+    for xi, ci in zip(inputs, contexts):
+        before = kc.clone(), vc.clone()
+        ctx.copy_(ci)
+        x.copy_(xi)
+        step()
+        want = x.clone(), kc.clone(), vc.clone()
+        kc.copy_(before[0])
+        vc.copy_(before[1])
+        x.copy_(xi)
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, expected in zip((x, kc, vc), want):
+            assert torch.equal(got, expected)
 
 
 def test_serving_loop(molt_lib):
