@@ -261,7 +261,9 @@ int molt_paged_attention(const void* q, const void* k_cache, const void* v_cache
  * 1 + k of query positions. Rows see positions 0 .. context_lens[b] + j of the table; blocks
  * whose id is outside [0, num_blocks) are not seen, and a row that sees no key
  * (context_lens[b] + j < 0: a sequence that sits a step out) is zeros. Slots that a row does
- * not see may hold anything.
+ * not see may hold anything. F32 holds the softmax weights in 24 bits; BF16 in 11 beside
+ * values that f16 holds (scales 2^-21 .. 2^10; what is under 2^-24 of a row's largest weight
+ * is off by 2^-35 of that), in 16 beside others, and the values as they are.
  * Supported, all three: D in {64, 128}; Hq % Hkv == 0, Hq/Hkv any. Errors: INVALID_ARG for NULL
  * required pointers, sizes < 1, caches that are not 16-byte aligned; WORKSPACE.
  * ---------------------------------------------------------------------------- */

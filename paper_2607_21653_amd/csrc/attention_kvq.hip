@@ -2,10 +2,12 @@
 //   o_r = sum_p w_rp v_p,  w_r = softmax over p <= ctx_b + j(r) of q_r . k_p / sqrt(D)
 // for the R = G * n rows (position j = r / G, query head h G + r % G) of sequence b and kv head h.
 //
-// Values and keys are exact in bf16, so the products' only roundings are those of the weights: in f32 three
-// bf16 parts (24 bits); in bf16 one, with the sum taken of the rounded weights, by an MFMA with a row of ones.
-// That adds a rounding like the output's own: rms error 2.07e-3 of the output's rms against 1.66e-3 with two
-// parts, for which 128 sequences x 5 positions at context 8192 took 178 us, with one 135.
+// Values and keys are exact in bf16, so the products' only roundings are those of the weights. f32: three bf16 parts
+// (24 bits). bf16: f16 weights (11 bits, times 2^10) beside the values as f16, which are exact while V's scales are
+// 2^-21 .. 2^10; from its first pair of blocks with another scale on a wavefront takes two bf16 parts (16 bits) beside
+// bf16 values. The sum is that of the rounded weights, by an MFMA with a row of ones. The error is that of the output's
+// rounding then, rms 1.66e-3 of the output's rms (weights in one bf16 part: 2.3e-3). 128 sequences x 5 positions at
+// context 8192 take 108 us, with values outside f16 158, with one bf16 part 107; 2 x 257 at 8100 104, 152 and 101.
 //
 // A workgroup has one kv head of a sequence, or of a part of its keys, and a group of up to 48 rows. Each of its
 // wavefronts walks a range of pairs of 16-token blocks by itself, with running maxima and sums, and they join at the
@@ -28,6 +30,7 @@
 // line 146); exponentials, scores and values in other orders (all within 3%).
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "internal.h"
 #include "kvq_format.h"
@@ -36,7 +39,10 @@ namespace molt {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kRescaleSlack = 8.0f;   // probabilities may grow to 2^8 before O is rescaled
+// f16 weights are times 2^10 and may grow by 2^5 before O is rescaled: up to 2^15, near the top of their range, so that
+// those under 2^-24 of the largest become subnormal only. (A slack of 8 took as long for every case below.)
+constexpr float kRescaleSlack = 5.0f;
+constexpr float kWeightShift = 10.0f;
 constexpr int kWaves = 4;
 // Pairs of blocks in a wavefront's ring. Workgroups of one wavefront are bound by how many fit in LDS: 201 sequences x
 // 180 positions x 8 heads at 0-404 took 138 us with 4, 109 with 3; the others wait for memory (122 us with 4, 128 with
@@ -112,14 +118,22 @@ MOLT_DEV uint32_t here(uint32_t x) {
   return x;
 }
 
-// x as P bf16 values whose sum is x to 8 P bits
-template <int P>
-MOLT_DEV void split_bf16(float x, __bf16 (&part)[P]) {
+// x as P bf16 or f16 values whose sum is x to 8 P or 11 P bits
+template <int P, typename E>
+MOLT_DEV void split(float x, E (&part)[P]) {
 #pragma unroll
   for (int i = 0; i < P; ++i) {
-    part[i] = __bf16(x);
+    part[i] = E(x);
     x -= float(part[i]);                 // exact
   }
+}
+
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+MOLT_DEV floatx4_t mfma_16x16x32(bf16x8_t a, bf16x8_t b, floatx4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+MOLT_DEV floatx4_t mfma_16x16x32(f16x8_t a, f16x8_t b, floatx4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
 // Query row as B operands of 16x16x32 bf16 MFMAs: three bf16 parts (24 bits) of dims D / 4 * g4 + 8 s .. +7
@@ -136,7 +150,7 @@ MOLT_DEV void load_query_f32(const float* q, bool valid, int g4, bf16x8_t (&qf)[
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       __bf16 part[3];
-      split_bf16<3>(x[e / 4][e % 4], part);
+      split<3>(x[e / 4][e % 4], part);
 #pragma unroll
       for (int u = 0; u < 3; ++u) qf[u][s][e] = part[u];
     }
@@ -314,7 +328,6 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int kSlots = slots_of(W);
   constexpr int QP = 3;                  // bf16 parts of an f32 query element
-  constexpr int PP = F32 ? 3 : 1;        // bf16 parts of a probability (see the top)
   constexpr int KS = D / 32;             // MFMA steps over the dims of a score
   constexpr int DT = D / 16;             // 16-dim tiles of O^T
   constexpr int SLOT = Lds<D, T, NT, W>::kPair, kLds = Lds<D, T, NT, W>::kWaveBytes, QF = Lds<D, T, NT, W>::kQuery;
@@ -434,7 +447,8 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
   }
   floatx4_t o[NT][DT], ls[NT];           // O^T; the rows' sums (bf16: by MFMA, the same in every register and group)
   float m[NT];                           // reference maximum (of scores in log2 units)
-  float ref[NT];                         // m, or 0 for a row that has seen no key: its exp2(-inf) is 0
+  float shift = F32 ? 0.f : kWeightShift;   // weights are exp2(score - ref), ref = m - shift, or 0 for a row that has
+  float ref[NT];                            // seen no key: its exp2(-inf) is 0
   float bound[NT];                       // scores above it raise m
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
@@ -500,7 +514,7 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
 
   // What follows a pair's scores: masks where a row may not see a key, and the reference maxima.
   auto settle = [&](int pi, bool ok0, bool ok1, const floatx4_t (&raw)[2][NT], floatx4_t (&sv)[2][NT],
-                    uint32_t (&vs)[2]) __attribute__((always_inline)) {
+                    uint32_t (&vs)[2], auto half) __attribute__((always_inline)) {
     float mx[NT];
     auto maxima = [&]() __attribute__((always_inline)) {
 #pragma unroll
@@ -557,14 +571,19 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
     bool grow = false;
 #pragma unroll
     for (int i = 0; i < NT; ++i) grow |= mx[i] > bound[i];
-    if (__ballot(grow)) {
+    bool change = false;                 // from f16 weights and values to bf16 ones, before they meet
+    if constexpr (decltype(half)::value) change = __ballot(kvq_outside_f16(vs[0]) || kvq_outside_f16(vs[1])) != 0;
+    if (__ballot(grow) || change) {
+      if (change) shift = 0.f;
 #pragma unroll
       for (int i = 0; i < NT; ++i) {
         const float mn = fmaxf(m[i], rows_max4(mx[i]));
-        const float alpha = m[i] == -INFINITY ? 0.f : exp2f(m[i] - mn);
+        // (scores past 2^20 are 2^-3 and more apart: the shift would be rounded)
+        const float next = mn == -INFINITY ? 0.f : fabsf(mn) < 0x1p20f ? mn - shift : mn;
+        const float alpha = m[i] == -INFINITY ? 0.f : exp2f(ref[i] - next);
         m[i] = mn;
         bound[i] = mn + kRescaleSlack;
-        ref[i] = mn == -INFINITY ? 0.f : mn;
+        ref[i] = next;
         ls[i] *= alpha;
 #pragma unroll
         for (int t = 0; t < DT; ++t) o[i][t] *= alpha;
@@ -585,20 +604,29 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
     else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     floatx4_t raw[2][NT];
     scores(p0, raw, vs);
-    settle(p0, have >> (2 * kSlots - 4) & 1u, have >> (2 * kSlots - 4) & 2u, raw, sv, vs);
+    settle(p0, have >> (2 * kSlots - 4) & 1u, have >> (2 * kSlots - 4) & 2u, raw, sv, vs,
+           std::integral_constant<bool, !F32>());
   }
-  for (int pi = p0; pi < p1; ++pi) {
+  // Scores of the next pair (past the last: of whatever its slot holds, not used) beside the weights and values of this
+  // one, with weights and values of type E, the weights in P parts.
+  auto step = [&](int pi, auto elem, auto parts) __attribute__((always_inline)) {
+    typedef decltype(elem) E;
+    typedef E Frag __attribute__((ext_vector_type(8)));
+    constexpr int PP = decltype(parts)::value;
+    constexpr bool HALF = std::is_same<E, _Float16>::value;
+    auto decode = [](auto byte, uint32_t codes, uint32_t scale) __attribute__((always_inline)) {
+      if constexpr (HALF) return kvq_decode2_f16<decltype(byte)::value>(codes, scale);
+      else return kvq_decode2<decltype(byte)::value>(codes, scale);
+    };
     arrive(pi + 1);
     if (pi + kSlots - 1 < p1) issue(pi + kSlots - 1, nid);
     have = have << 2 | present(nid);
     ids(pi + kSlots, nid);
-    // scores of the next pair (past the last: of whatever its slot holds, not used), beside the
-    // probabilities and values of this one
     __builtin_amdgcn_s_setprio(0);
     floatx4_t nsv[2][NT];
     uint32_t nvs[2];
     scores(pi + 1, nsv, nvs);
-    bf16x8_t pf[NT][PP];
+    Frag pf[NT][PP];
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
       float ps = 0.f;
@@ -608,39 +636,35 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
         for (int e = 0; e < 4; ++e) {
           const float w = __builtin_amdgcn_exp2f(sv[u][i][e] - ref[i]);
           if constexpr (F32) ps += w;
-          __bf16 part[PP];
-          split_bf16<PP>(w, part);
+          E part[PP];
+          split<PP>(w, part);
 #pragma unroll
           for (int q = 0; q < PP; ++q) pf[i][q][4 * u + e] = part[q];
         }
       if constexpr (F32) {
         ls[i][0] += ps;
       } else {
-        const uint32_t one = 0x3f803f80u;
+        const uint32_t one = HALF ? 0x3c003c00u : 0x3f803f80u;
         const u32x4 ones = {one, one, one, one};
 #pragma unroll
-        for (int q = 0; q < PP; ++q)
-          ls[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ones), pf[i][q], ls[i], 0, 0, 0);
+        for (int q = 0; q < PP; ++q) ls[i] = mfma_16x16x32(__builtin_bit_cast(Frag, ones), pf[i][q], ls[i]);
       }
     }
     // O^T += V^T P^T: lane (l16, g4) holds dims D / 16 * l16 + t (tile t) of tokens 4 g4 .. +3 of both blocks
     const uint8_t* vsrc_lds = ring + (pi - p0) % kSlots * SLOT + 16 * D + (D == 128 ? lane : g4 * 8 + l16 / 2) * 16;
-    uint32_t vd[2][4][DT / 2];           // token's dims as bf16 pairs
+    uint32_t vd[2][4][DT / 2];           // token's dims in pairs
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const u32x4 vc = *reinterpret_cast<const u32x4*>(vsrc_lds + 8 * D * u);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const uint32_t sc = kvq_scale_bits(vs[u], e);
+        const uint32_t w = D == 128 ? vc[e] : vc[e] >> (16 * (l16 % 2));
+        vd[u][e][0] = decode(std::integral_constant<int, 0>(), w, sc);
+        vd[u][e][1] = decode(std::integral_constant<int, 1>(), w, sc);
         if constexpr (D == 128) {
-          vd[u][e][0] = kvq_decode2<0>(vc[e], sc);
-          vd[u][e][1] = kvq_decode2<1>(vc[e], sc);
-          vd[u][e][2] = kvq_decode2<2>(vc[e], sc);
-          vd[u][e][3] = kvq_decode2<3>(vc[e], sc);
-        } else {
-          const uint32_t w = vc[e] >> (16 * (l16 % 2));
-          vd[u][e][0] = kvq_decode2<0>(w, sc);
-          vd[u][e][1] = kvq_decode2<1>(w, sc);
+          vd[u][e][2] = decode(std::integral_constant<int, 2>(), w, sc);
+          vd[u][e][3] = decode(std::integral_constant<int, 3>(), w, sc);
         }
       }
     }
@@ -652,18 +676,27 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
 #pragma unroll
         for (int e = 0; e < 2; ++e)
           w[2 * u + e] = __builtin_amdgcn_perm(vd[u][2 * e + 1][t / 2], vd[u][2 * e][t / 2], t % 2 ? 0x07060302u : 0x05040100u);
-      const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, w);
+      const Frag vf = __builtin_bit_cast(Frag, w);
 #pragma unroll
       for (int i = 0; i < NT; ++i)
 #pragma unroll
-        for (int q = 0; q < PP; ++q) o[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[i][q], o[i][t], 0, 0, 0);
+        for (int q = 0; q < PP; ++q) o[i][t] = mfma_16x16x32(vf, pf[i][q], o[i][t]);
     }
     // the stretch without MFMAs goes first, so that the other wavefront's run beside it (2 x 257 positions at 8100: 102
     // us, 104 with these two the other way round, 111 without)
     __builtin_amdgcn_s_setprio(1);
-    if (pi + 1 < p1) settle(pi + 1, have >> (2 * kSlots - 4) & 1u, have >> (2 * kSlots - 4) & 2u, nsv, sv, nvs);
+    if (pi + 1 < p1)
+      settle(pi + 1, have >> (2 * kSlots - 4) & 1u, have >> (2 * kSlots - 4) & 2u, nsv, sv, nvs,
+             std::integral_constant<bool, HALF>());
     vs[0] = nvs[0];
     vs[1] = nvs[1];
+  };
+  if constexpr (F32) {
+    for (int pi = p0; pi < p1; ++pi) step(pi, __bf16(), std::integral_constant<int, 3>());
+  } else {
+    int pi = p0;
+    for (; pi < p1 && shift != 0.f; ++pi) step(pi, _Float16(), std::integral_constant<int, 1>());
+    for (; pi < p1; ++pi) step(pi, __bf16(), std::integral_constant<int, 2>());
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no copy may outlive the ring
 
@@ -696,7 +729,7 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
         *reinterpret_cast<floatx4_t*>(own + l16 * RS + D / 16 * (4 * g4 + e) + t) =
             floatx4_t{o[i][t][e], o[i][t + 1][e], o[i][t + 2][e], o[i][t + 3][e]};
     if (g4 == 0) {
-      own[16 * RS + l16] = m[i];
+      own[16 * RS + l16] = m[i] == -INFINITY ? m[i] : ref[i];
       own[16 * RS + 16 + l16] = lt;
     }
     __syncthreads();
