@@ -7,7 +7,7 @@
 // 2^-21 .. 2^10; from its first pair of blocks with another scale on a wavefront takes two bf16 parts (16 bits) beside
 // bf16 values. The sum is that of the rounded weights, by an MFMA with a row of ones. The error is that of the output's
 // rounding then, rms 1.66e-3 of the output's rms (weights in one bf16 part: 2.3e-3). 128 sequences x 5 positions at
-// context 8192 take 108 us, with values outside f16 158, with one bf16 part 107; 2 x 257 at 8100 104, 152 and 101.
+// context 8192 take 108 us, with values outside f16 158, with one bf16 part 107; 2 x 257 at 8100 106, 152 and 101.
 //
 // A workgroup has one kv head of a sequence, or of a part of its keys, and a group of up to 48 rows. Each of its
 // wavefronts walks a range of pairs of 16-token blocks by itself, with running maxima and sums, and they join at the
@@ -321,6 +321,80 @@ struct Lds {
   static constexpr int kBytes = W * kWaveBytes + NT * kQuery;
 };
 
+template <bool HALF, int I>
+MOLT_DEV uint32_t decode2(uint32_t codes, uint32_t scale_bits) {
+  if constexpr (HALF) return kvq_decode2_f16<I>(codes, scale_bits);
+  else return kvq_decode2<I>(codes, scale_bits);
+}
+
+// Adds a pair's weights exp2(sv - ref) to the rows' sums ls and its values, times them, to O^T. Both are taken as type E,
+// the weights in P parts. codes: the pair's V codes in LDS, vs: the lane's V scale bytes. (As a lambda within attend this
+// took 15 registers more of the f32 kernels: 143 us in place of 138 for 201 x 180 positions x 8 heads of 64 at 0-404.)
+template <int D, bool F32, int NT, int P, typename E>
+MOLT_DEV void add_pair(const floatx4_t (&sv)[2][NT], const float (&ref)[NT], const uint32_t (&vs)[2], const uint8_t* codes,
+                       int lane, floatx4_t (&ls)[NT], floatx4_t (&o)[NT][D / 16], E) {
+  typedef E Frag __attribute__((ext_vector_type(8)));
+  constexpr bool HALF = std::is_same<E, _Float16>::value;
+  constexpr int DT = D / 16;
+  const int l16 = lane % 16, g4 = lane / 16;
+  Frag pf[NT][P];
+#pragma unroll
+  for (int i = 0; i < NT; ++i) {
+    float ps = 0.f;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float w = __builtin_amdgcn_exp2f(sv[u][i][e] - ref[i]);
+        if constexpr (F32) ps += w;
+        E part[P];
+        split<P>(w, part);
+#pragma unroll
+        for (int q = 0; q < P; ++q) pf[i][q][4 * u + e] = part[q];
+      }
+    if constexpr (F32) {
+      ls[i][0] += ps;
+    } else {
+      const uint32_t one = HALF ? 0x3c003c00u : 0x3f803f80u;
+      const u32x4 ones = {one, one, one, one};
+#pragma unroll
+      for (int q = 0; q < P; ++q) ls[i] = mfma_16x16x32(__builtin_bit_cast(Frag, ones), pf[i][q], ls[i]);
+    }
+  }
+  // O^T += V^T P^T: lane (l16, g4) holds dims D / 16 * l16 + t (tile t) of tokens 4 g4 .. +3 of both blocks
+  const uint8_t* src = codes + (D == 128 ? lane : g4 * 8 + l16 / 2) * 16;
+  uint32_t vd[2][4][DT / 2];           // token's dims in pairs
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const u32x4 vc = *reinterpret_cast<const u32x4*>(src + 8 * D * u);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t sc = kvq_scale_bits(vs[u], e);
+      const uint32_t w = D == 128 ? vc[e] : vc[e] >> (16 * (l16 % 2));
+      vd[u][e][0] = decode2<HALF, 0>(w, sc);
+      vd[u][e][1] = decode2<HALF, 1>(w, sc);
+      if constexpr (D == 128) {
+        vd[u][e][2] = decode2<HALF, 2>(w, sc);
+        vd[u][e][3] = decode2<HALF, 3>(w, sc);
+      }
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < DT; ++t) {
+    u32x4 w;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        w[2 * u + e] = __builtin_amdgcn_perm(vd[u][2 * e + 1][t / 2], vd[u][2 * e][t / 2], t % 2 ? 0x07060302u : 0x05040100u);
+    const Frag vf = __builtin_bit_cast(Frag, w);
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+      for (int q = 0; q < P; ++q) o[i][t] = mfma_16x16x32(vf, pf[i][q], o[i][t]);
+  }
+}
+
 // Rows [r0, r0 + 16 NT) of kv head h over the keys of share w, by W wavefronts.
 template <int D, typename T, int NT, bool ONCE, int W>
 MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h, int slot, const Share& w) {
@@ -571,10 +645,10 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
     bool grow = false;
 #pragma unroll
     for (int i = 0; i < NT; ++i) grow |= mx[i] > bound[i];
-    bool change = false;                 // from f16 weights and values to bf16 ones, before they meet
-    if constexpr (decltype(half)::value) change = __ballot(kvq_outside_f16(vs[0]) || kvq_outside_f16(vs[1])) != 0;
-    if (__ballot(grow) || change) {
-      if (change) shift = 0.f;
+    bool wide = false;
+    if constexpr (decltype(half)::value) wide = kvq_outside_f16(vs[0], vs[1]) != 0;
+    if (__ballot(grow || wide)) {
+      if (__ballot(wide)) shift = 0.f;   // from f16 weights and values to bf16 ones, before they meet
 #pragma unroll
       for (int i = 0; i < NT; ++i) {
         const float mn = fmaxf(m[i], rows_max4(mx[i]));
@@ -591,6 +665,8 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
     }
   };
 
+  typedef std::conditional_t<F32, __bf16, _Float16> First;   // what weights and values are held in at first
+  constexpr std::integral_constant<bool, !F32> first{};       // (and whether that may change)
   floatx4_t sv[2][NT];
   uint32_t vs[2];
   // Pair pi is in when at most the copies of the pairs after it are in flight. The reads of pair pi - 2 are
@@ -604,99 +680,45 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
     else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     floatx4_t raw[2][NT];
     scores(p0, raw, vs);
-    settle(p0, have >> (2 * kSlots - 4) & 1u, have >> (2 * kSlots - 4) & 2u, raw, sv, vs,
-           std::integral_constant<bool, !F32>());
+    settle(p0, have >> (2 * kSlots - 4) & 1u, have >> (2 * kSlots - 4) & 2u, raw, sv, vs, first);
   }
-  // Scores of the next pair (past the last: of whatever its slot holds, not used) beside the weights and values of this
-  // one, with weights and values of type E, the weights in P parts.
-  auto step = [&](int pi, auto elem, auto parts) __attribute__((always_inline)) {
-    typedef decltype(elem) E;
-    typedef E Frag __attribute__((ext_vector_type(8)));
-    constexpr int PP = decltype(parts)::value;
-    constexpr bool HALF = std::is_same<E, _Float16>::value;
-    auto decode = [](auto byte, uint32_t codes, uint32_t scale) __attribute__((always_inline)) {
-      if constexpr (HALF) return kvq_decode2_f16<decltype(byte)::value>(codes, scale);
-      else return kvq_decode2<decltype(byte)::value>(codes, scale);
-    };
+  auto advance = [&](int pi) __attribute__((always_inline)) {
     arrive(pi + 1);
     if (pi + kSlots - 1 < p1) issue(pi + kSlots - 1, nid);
     have = have << 2 | present(nid);
     ids(pi + kSlots, nid);
+  };
+  // In each loop the scores of the next pair (past the last: of whatever its slot holds, not used) go beside the weights
+  // and values of this one. The stretch without MFMAs, settle, goes first, so that the other wavefront's run beside it
+  // (2 x 257 positions at 8100: 102 us, 104 with the priorities the other way round, 111 without).
+  int pi = p0;
+  for (; pi < p1 && (F32 || shift != 0.f); ++pi) {
+    advance(pi);
     __builtin_amdgcn_s_setprio(0);
     floatx4_t nsv[2][NT];
     uint32_t nvs[2];
     scores(pi + 1, nsv, nvs);
-    Frag pf[NT][PP];
-#pragma unroll
-    for (int i = 0; i < NT; ++i) {
-      float ps = 0.f;
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float w = __builtin_amdgcn_exp2f(sv[u][i][e] - ref[i]);
-          if constexpr (F32) ps += w;
-          E part[PP];
-          split<PP>(w, part);
-#pragma unroll
-          for (int q = 0; q < PP; ++q) pf[i][q][4 * u + e] = part[q];
-        }
-      if constexpr (F32) {
-        ls[i][0] += ps;
-      } else {
-        const uint32_t one = HALF ? 0x3c003c00u : 0x3f803f80u;
-        const u32x4 ones = {one, one, one, one};
-#pragma unroll
-        for (int q = 0; q < PP; ++q) ls[i] = mfma_16x16x32(__builtin_bit_cast(Frag, ones), pf[i][q], ls[i]);
-      }
-    }
-    // O^T += V^T P^T: lane (l16, g4) holds dims D / 16 * l16 + t (tile t) of tokens 4 g4 .. +3 of both blocks
-    const uint8_t* vsrc_lds = ring + (pi - p0) % kSlots * SLOT + 16 * D + (D == 128 ? lane : g4 * 8 + l16 / 2) * 16;
-    uint32_t vd[2][4][DT / 2];           // token's dims in pairs
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const u32x4 vc = *reinterpret_cast<const u32x4*>(vsrc_lds + 8 * D * u);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t sc = kvq_scale_bits(vs[u], e);
-        const uint32_t w = D == 128 ? vc[e] : vc[e] >> (16 * (l16 % 2));
-        vd[u][e][0] = decode(std::integral_constant<int, 0>(), w, sc);
-        vd[u][e][1] = decode(std::integral_constant<int, 1>(), w, sc);
-        if constexpr (D == 128) {
-          vd[u][e][2] = decode(std::integral_constant<int, 2>(), w, sc);
-          vd[u][e][3] = decode(std::integral_constant<int, 3>(), w, sc);
-        }
-      }
-    }
-#pragma unroll
-    for (int t = 0; t < DT; ++t) {
-      u32x4 w;
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-          w[2 * u + e] = __builtin_amdgcn_perm(vd[u][2 * e + 1][t / 2], vd[u][2 * e][t / 2], t % 2 ? 0x07060302u : 0x05040100u);
-      const Frag vf = __builtin_bit_cast(Frag, w);
-#pragma unroll
-      for (int i = 0; i < NT; ++i)
-#pragma unroll
-        for (int q = 0; q < PP; ++q) o[i][t] = mfma_16x16x32(vf, pf[i][q], o[i][t]);
-    }
-    // the stretch without MFMAs goes first, so that the other wavefront's run beside it (2 x 257 positions at 8100: 102
-    // us, 104 with these two the other way round, 111 without)
+    add_pair<D, F32, NT, F32 ? 3 : 1>(sv, ref, vs, ring + (pi - p0) % kSlots * SLOT + 16 * D, lane, ls, o, First());
     __builtin_amdgcn_s_setprio(1);
     if (pi + 1 < p1)
-      settle(pi + 1, have >> (2 * kSlots - 4) & 1u, have >> (2 * kSlots - 4) & 2u, nsv, sv, nvs,
-             std::integral_constant<bool, HALF>());
+      settle(pi + 1, have >> (2 * kSlots - 4) & 1u, have >> (2 * kSlots - 4) & 2u, nsv, sv, nvs, first);
     vs[0] = nvs[0];
     vs[1] = nvs[1];
-  };
-  if constexpr (F32) {
-    for (int pi = p0; pi < p1; ++pi) step(pi, __bf16(), std::integral_constant<int, 3>());
-  } else {
-    int pi = p0;
-    for (; pi < p1 && shift != 0.f; ++pi) step(pi, _Float16(), std::integral_constant<int, 1>());
-    for (; pi < p1; ++pi) step(pi, __bf16(), std::integral_constant<int, 2>());
+  }
+  if constexpr (!F32) {
+    for (; pi < p1; ++pi) {
+      advance(pi);
+      __builtin_amdgcn_s_setprio(0);
+      floatx4_t nsv[2][NT];
+      uint32_t nvs[2];
+      scores(pi + 1, nsv, nvs);
+      add_pair<D, F32, NT, 2>(sv, ref, vs, ring + (pi - p0) % kSlots * SLOT + 16 * D, lane, ls, o, __bf16());
+      __builtin_amdgcn_s_setprio(1);
+      if (pi + 1 < p1)
+        settle(pi + 1, have >> (2 * kSlots - 4) & 1u, have >> (2 * kSlots - 4) & 2u, nsv, sv, nvs, std::false_type());
+      vs[0] = nvs[0];
+      vs[1] = nvs[1];
+    }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no copy may outlive the ring
 
