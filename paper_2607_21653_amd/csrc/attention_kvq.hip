@@ -136,8 +136,9 @@ MOLT_DEV floatx4_t mfma_16x16x32(f16x8_t a, f16x8_t b, floatx4_t c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
-// Query row as B operands of 16x16x32 bf16 MFMAs: three bf16 parts (24 bits) of dims D / 4 * g4 + 8 s .. +7
-// for k-step s, the order in which a lane's K codes lie.
+// Query row as B operands of 16x16x32 bf16 MFMAs: three bf16 parts of dims D / 4 * g4 + 8 s .. +7 for k-step s, the
+// order in which a lane's K codes lie. The parts are cut off, not rounded: three times 8 bits are the element's 24, and
+// the largest elements do not round up to infinity.
 template <int D>
 MOLT_DEV void load_query_f32(const float* q, bool valid, int g4, bf16x8_t (&qf)[3][D / 32]) {
 #pragma unroll
@@ -149,10 +150,13 @@ MOLT_DEV void load_query_f32(const float* q, bool valid, int g4, bf16x8_t (&qf)[
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      __bf16 part[3];
-      split<3>(x[e / 4][e % 4], part);
+      float rest = x[e / 4][e % 4];
 #pragma unroll
-      for (int u = 0; u < 3; ++u) qf[u][s][e] = part[u];
+      for (int u = 0; u < 3; ++u) {
+        const float top = __uint_as_float(__float_as_uint(rest) & 0xffff0000u);
+        qf[u][s][e] = __bf16(top);         // exact
+        rest -= top;
+      }
     }
   }
 }

@@ -157,3 +157,26 @@ def test_largest_values(molt_lib, dtype, D):
         # keys: under 2^10 of them, weights of at most e^-48 < 2^-69, values under 2^3
         want = V[0][L // 2, 0]
         assert (np.abs(out - want) <= 2.0 ** (-8 if dtype == "bf16" else -20) * np.abs(want) + 2.0 ** -56).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_largest_queries(molt_lib, dtype, D):
+    """The largest finite query elements, on keys so small there that the scores are ordinary ones."""
+    rng = np.random.default_rng(59)
+    ctx, n, Hq = [90, 700], 2, 6
+    keys = [rng.standard_normal((c + n, 2, D), np.float32) for c in ctx]
+    for k in keys:
+        k[..., :32] = np.ldexp(k[..., :32], -124)      # times up to 2^128: terms of up to 2^7 / sqrt(D)
+    caches, K, V = _caches(molt_lib, rng, ctx, n, 2, D, key_rows=keys)
+    q, _ = _rows(rng, len(ctx) * n, Hq, D, dtype)
+    big = torch.finfo(DT[dtype]).max
+    q[:, :, 3] = big
+    q[:, 1::2, 30] = -big
+    if dtype == "f32":
+        q[0, :, 17], q[1, :, 17] = 3.3961e38, -3.3962e38   # either side of where bf16 rounds to infinity
+    # (a bf16 row's other elements are under 2^-22 of its largest: what is lost of them is under the row's bound)
+    tail = q[:, :, 32:]
+    if dtype == "bf16":
+        tail.zero_()
+    _check(molt_lib, q, q.double().numpy(), caches, K, V, ctx, n, dtype)
