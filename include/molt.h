@@ -264,8 +264,11 @@ int molt_paged_attention(const void* q, const void* k_cache, const void* v_cache
  * not see may hold anything. F32 holds the softmax weights in 24 bits; BF16 in 11 beside
  * values that f16 holds (scales 2^-21 .. 2^10; what is under 2^-24 of a row's largest weight
  * is off by 2^-35 of that), in 16 beside others, and the values as they are.
- * Supported, all three: D in {64, 128}; Hq % Hkv == 0, Hq/Hkv any. Errors: INVALID_ARG for NULL
- * required pointers, sizes < 1, caches that are not 16-byte aligned; WORKSPACE.
+ * Supported, all three: D in {64, 128}; Hq % Hkv == 0, Hq/Hkv any; what one launch holds: under
+ * 6e7 wavefronts of 16 positions x 128 dims, and in the attention under 1.4e7 groups of 16 (F32)
+ * or 48 (BF16) of a kv head's (1+k) * Hq/Hkv rows, tables of at most 2^26 blocks. Errors:
+ * INVALID_ARG for NULL required pointers, other sizes, caches that are not 16-byte aligned;
+ * WORKSPACE. The workspace size is 0 for sizes that no call takes.
  * ---------------------------------------------------------------------------- */
 int molt_kvq_write(const void* k, const void* v, long long k_stride, long long v_stride,
                    void* k_cache, void* v_cache, const int32_t* block_tables,

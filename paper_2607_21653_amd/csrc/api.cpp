@@ -514,6 +514,26 @@ int molt_paged_attention(const void* q, const void* k_cache, const void* v_cache
 
 // ------------------------------------------------------------------ 4-bit KV cache
 
+// Sizes that the attention over 4-bit caches takes: a launch holds 2^32 threads, in workgroups of 256 for a row group
+// (16 rows of a kv head in f32, 48 in bf16), and positions of a table are ints.
+static bool kvq_launch_fits(int B, int k, int Hq, int Hkv, molt_dtype dt) {
+  return double(B) * Hkv * (double(Hq / Hkv) * (double(k) + 1) / (dt == MOLT_F32 ? 16 : 48) + 1) < 1.4e7;
+}
+static bool kvq_table_fits(int max_blocks) { return max_blocks <= (1 << 26); }
+
+static int kvq_attention_ok(int B, int k, int Hq, int Hkv, int max_blocks, molt_dtype dt) {
+  REQUIRE(Hkv >= 1 && Hq >= Hkv && Hq % Hkv == 0, "n_q_heads %d must be a multiple of n_kv_heads %d", Hq, Hkv);
+  REQUIRE(kvq_launch_fits(B, k, Hq, Hkv, dt), "B * (1+k) * n_q_heads too large for 4-bit caches");
+  REQUIRE(kvq_table_fits(max_blocks), "max_blocks_per_seq = %d must be <= 2^26 for 4-bit caches", max_blocks);
+  return MOLT_OK;
+}
+
+// Whether a size function has an answer: what no call takes needs no workspace
+static bool kvq_sizes_ok(int B, int k, int Hq, int Hkv, int D, int max_blocks) {
+  return B >= 1 && k >= 0 && Hkv >= 1 && Hq >= Hkv && Hq % Hkv == 0 && (D == 64 || D == 128) && max_blocks >= 1 &&
+         kvq_launch_fits(B, k, Hq, Hkv, MOLT_BF16) && kvq_table_fits(max_blocks);
+}
+
 static int kvq_rows_ok(const void* k_cache, const void* v_cache, const int32_t* block_tables, const int32_t* start,
                        int B, int n, int Hkv, int D, int max_blocks, int num_blocks, molt_dtype dt) {
   REQUIRE(B >= 1, "B = %d must be >= 1", B);
@@ -561,7 +581,7 @@ int molt_kvq_read(const void* k_cache, const void* v_cache, const int32_t* block
 }
 
 size_t molt_paged_attention_kvq_workspace_size(int B, int k, int Hq, int Hkv, int D, int max_blocks) {
-  if (B < 1 || k < 0 || Hkv < 1 || Hq < Hkv || Hq % Hkv != 0 || D < 1 || max_blocks < 1) return 0;
+  if (!kvq_sizes_ok(B, k, Hq, Hkv, D, max_blocks)) return 0;
   return molt::kvq_attention_ws_bytes(B, k + 1, Hq, Hkv, D, max_blocks);
 }
 
@@ -572,11 +592,7 @@ int molt_paged_attention_kvq(const void* q, const void* k_cache, const void* v_c
   REQUIRE(k >= 0 && k < 0x7fffffff, "k = %d must be >= 0", k);
   if (int r = kvq_rows_ok(k_cache, v_cache, block_tables, context_lens, B, k + 1, Hkv, D, max_blocks, num_blocks, dtype))
     return r;
-  REQUIRE(Hq >= Hkv && Hq % Hkv == 0, "n_q_heads %d must be a multiple of n_kv_heads %d", Hq, Hkv);
-  // workgroups: row groups of 16 (f32) or 48 rows of a kv head
-  REQUIRE(double(B) * Hkv * (double(Hq / Hkv) * (k + 1) / (dtype == MOLT_F32 ? 16 : 48) + 1) < 1.4e7,
-          "B * (1+k) * n_q_heads too large");
-  REQUIRE(max_blocks <= (1 << 26), "max_blocks_per_seq = %d must be <= 2^26", max_blocks);
+  if (int r = kvq_attention_ok(B, k, Hq, Hkv, max_blocks, dtype)) return r;
   REQUIRE(q && out, "a required pointer is NULL");
   if (int r = check_ws(workspace, workspace_bytes, molt::kvq_attention_ws_bytes(B, k + 1, Hq, Hkv, D, max_blocks)))
     return r;
@@ -643,7 +659,14 @@ struct DecWs {
   void* kvq_ws;                   // workspace of the attention over 4-bit caches
 };
 
-// with `mx` also what 4-bit caches need besides
+// what 4-bit caches need besides: the QKV product, where it is not kept anyway, and the attention's workspace
+void carve_kvq(molt::Carver& c, const molt_model* m, int B, int k, int max_blocks, float*& qkv, void*& kvq_ws) {
+  const int D = m->head_dim, Hq = m->n_q_heads, Hkv = m->n_kv_heads;
+  if (m->dtype == MOLT_BF16 && D == 128) qkv = c.take<float>(long(B) * (k + 1) * (Hq + 2l * Hkv) * D);
+  kvq_ws = c.take<uint8_t>(molt::kvq_attention_ws_bytes(B, k + 1, Hq, Hkv, D, max_blocks));
+}
+
+// with `mx` also that
 DecWs carve_dec(molt::Carver& c, const molt_model* m, int B, int k, int max_blocks, bool fine, bool mx) {
   DecWs w{};
   w.fine = fine;
@@ -670,10 +693,7 @@ DecWs carve_dec(molt::Carver& c, const molt_model* m, int B, int k, int max_bloc
   w.part = c.take<float>(w.part_elems);
   w.rope = c.take<double>(T * D);
   w.kv_slot = c.take<int32_t>(T);
-  if (mx) {
-    if (!w.qkv && m->dtype == MOLT_BF16 && D == 128) w.qkv = c.take<float>(T * (Hq + 2 * Hkv) * D);
-    w.kvq_ws = c.take<uint8_t>(molt::kvq_attention_ws_bytes(B, k + 1, Hq, Hkv, D, max_blocks));
-  }
+  if (mx) carve_kvq(c, m, B, k, max_blocks, w.qkv, w.kvq_ws);
   return w;
 }
 
@@ -768,12 +788,14 @@ size_t molt_decoder_workspace_size(const molt_model* m, int B, int k, int max_bl
 }
 
 size_t molt_kvq_workspace_extra(const molt_model* m, int B, int k, int max_blocks) {
-  if (!m || B < 1 || k < 0 || max_blocks < 1 || m->n_kv_heads < 1 || m->n_q_heads < m->n_kv_heads ||
-      m->n_q_heads % m->n_kv_heads != 0 || !pair_ok(m->dtype, m->expert_dtype))
+  if (!m || !pair_ok(m->dtype, m->expert_dtype) ||
+      !kvq_sizes_ok(B, k, m->n_q_heads, m->n_kv_heads, m->head_dim, max_blocks))
     return 0;
-  // 256 bytes for each of the two aligned pieces
-  return carved_bytes(carve_dec, m, B, k, max_blocks, true, true) -
-         carved_bytes(carve_dec, m, B, k, max_blocks, true, false) + 512;
+  molt::Carver c(nullptr, 0);
+  float* qkv;
+  void* ws;
+  carve_kvq(c, m, B, k, max_blocks, qkv, ws);
+  return c.used + 512;                    // 256 bytes for each of the two aligned pieces
 }
 
 int molt_decoder_forward(const molt_model* m, const molt_kv* kv, int B, int k, float* x,
