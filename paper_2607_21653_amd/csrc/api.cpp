@@ -639,10 +639,14 @@ int model_ok(const molt_model* m, const molt_kv* kv, int B, int k, bool need_hea
   REQUIRE(kv->k_cache && kv->v_cache && kv->block_tables && kv->context_lens, "a kv pointer is NULL");
   for (int l = 0; l < m->n_layers; ++l)
     REQUIRE(kv->k_cache[l] && kv->v_cache[l], "layer %d: cache pointer is NULL", l);
-  if (kv->block_size & MOLT_KV_MX)
+  if (kv->block_size & MOLT_KV_MX) {
     for (int l = 0; l < m->n_layers; ++l)
       REQUIRE((reinterpret_cast<uintptr_t>(kv->k_cache[l]) | reinterpret_cast<uintptr_t>(kv->v_cache[l])) % 16 == 0,
               "layer %d: 4-bit caches must start at a multiple of 16 bytes", l);
+    if (int r = kvq_attention_ok(B, k, m->n_q_heads, m->n_kv_heads, kv->max_blocks_per_seq, m->dtype)) return r;
+    // (a workgroup of 256 threads writes a token's keys and values)
+    REQUIRE(double(B) * (double(k) + 1) < 1.6e7, "B * (1+k) too large for 4-bit caches");
+  }
   REQUIRE(kv->num_blocks >= 1, "num_blocks = %d must be >= 1", kv->num_blocks);
   return attn_shape_ok(B, k, m->n_q_heads, m->n_kv_heads, m->head_dim, kv->max_blocks_per_seq,
                        m->dtype);

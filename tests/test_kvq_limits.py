@@ -48,3 +48,49 @@ def test_extra_of_the_largest_sizes(L):
     for bad in (dict(n_experts=0), dict(top_k=0), dict(d_model=0)):      # not what the extra goes by
         m = _model(**bad)
         assert L.molt_kvq_workspace_extra(ctypes.byref(m), 2, 4, 40) >= 2 * 5 * (8 + 2 * 2) * 128 * 4
+
+
+@pytest.mark.parametrize("name", ["decoder", "verify", "prefill", "score", "draft"])
+@pytest.mark.parametrize("dtype", [_lib.MOLT_F32, _lib.MOLT_BF16])
+def test_model_calls_at_the_limits(L, name, dtype):
+    """Calls on a model refuse the sizes that the attention over 4-bit caches refuses, and take those just within."""
+    keep = []
+
+    def arr(v):
+        keep.append((ctypes.c_void_p * 1)(v))
+        return ctypes.cast(keep[-1], ctypes.c_void_p)
+
+    P = ctypes.c_void_p(0x1000)
+
+    def call(B, k, mb, Hq=8, Hkv=2, kind=16 | _lib.MOLT_KV_MX, d=64):
+        m = _model(dtype, n_q_heads=Hq, n_kv_heads=Hkv, head_dim=64, d_model=d, d_ff=64, vocab=64, top_k=1)
+        for key in ("attn_norm", "w_qkv", "w_o", "moe_norm", "w_router", "w_gate_up", "w_down"):
+            setattr(m, key, arr(0x4000))
+        m.embed, m.lm_head, m.final_norm = P, P, P
+        kv = _lib.MoltKV()
+        kv.k_cache, kv.v_cache = arr(0x8000), arr(0x9000)
+        kv.block_tables = kv.context_lens = P
+        kv.max_blocks_per_seq, kv.num_blocks, kv.block_size = mb, 99, kind
+        mr, kr = ctypes.byref(m), ctypes.byref(kv)
+        if name == "decoder":
+            return L.molt_decoder_forward(mr, kr, B, k, P, None, None, 0, None)
+        if name == "verify":
+            return L.molt_verify_step(mr, kr, B, k, P, None, P, None, P, P, None, None, None, None, 0, None)
+        if name == "prefill":
+            return L.molt_prefill(mr, kr, B, k + 1, P, P, P, None, None, None, 0, None)
+        if name == "score":
+            return L.molt_score_tokens(mr, kr, B, k, P, P, None, P, None, None, None, 0, None)
+        mtp = _lib.MoltMtp()
+        mtp.enorm = mtp.hnorm = mtp.eh_proj = mtp.final_norm = P
+        mtp.layer = ctypes.pointer(m)
+        return L.molt_mtp_draft_window(mr, ctypes.byref(mtp), kr, B, k + 1, 1, P, P, P, P, P, P, P, None, 0, None)
+
+    assert call(2, 4, 2 ** 26) == WORKSPACE
+    assert call(2, 4, 2 ** 26, kind=16) == WORKSPACE
+    assert call(2, 4, 2 ** 26 + 1) == INVALID and b"2^26" in L.molt_last_error()
+    assert call(2, 4, 2 ** 26 + 1, kind=16) == WORKSPACE               # other caches keep their own limits
+    rows = 16 if dtype == _lib.MOLT_F32 else 48
+    n = int(1.4e7 / 8 * rows / 64)                                     # 64 query heads a kv head, 8 kv heads
+    assert call(1, n, 4, Hq=512, Hkv=8) == INVALID and b"4-bit" in L.molt_last_error()
+    assert call(1, n - 2 * rows, 4, Hq=512, Hkv=8) == WORKSPACE
+    assert call(1, 16_000_000, 4, Hq=1, Hkv=1) == INVALID
