@@ -558,20 +558,50 @@ class KVCache:
             raise MoltError("the caches of all layers must be 4-bit ones, or none")
         s.block_size = 16 | MOLT_KV_MX if self.mx else 16
         self.struct = s
+        if self.mx:
+            self._look_over()
 
-    def check(self, model):
-        """4-bit caches have the model's heads."""
+    def _look_over(self):
+        """4-bit caches and their tables are whole tensors of one device: a call has addresses only, and would
+        take a slice of a pool for its first bytes."""
+        named = [(f"{n}[{i}]", t) for n, ts in (("k_caches", self.k_caches), ("v_caches", self.v_caches))
+                 for i, t in enumerate(ts)]
+        tables = [("block_tables", self.block_tables), ("context_lens", self.context_lens)]
+        for name, t in named + tables:
+            if not t.is_contiguous():
+                raise MoltError(f"{name} must be contiguous (shape {tuple(t.shape)}, strides {t.stride()})")
+            if t.get_device() != named[0][1].get_device():
+                raise MoltError(f"{name} is on {t.device}, k_caches[0] on {named[0][1].device}")
+        for (name, t), dim in zip(tables, (2, 1)):
+            if t.dtype is not torch.int32 or t.dim() != dim:
+                raise MoltError(f"{name} must be int32 with {dim} dimension(s), is {t.dtype} {tuple(t.shape)}")
+        self._shapes = {tuple(t.shape) for _, t in named}
+
+    def check(self, model, B=0):
+        """4-bit caches are the model's: its layers and heads, on the current device, tables of B sequences."""
+        if not self.mx:
+            return
         m = model.struct
         want = (self.struct.num_blocks, m.n_kv_heads, 17 * m.head_dim // 2)
-        if self.mx and any(tuple(t.shape) != want for t in [*self.k_caches, *self.v_caches]):
+        if self._shapes != {want}:
             raise MoltError(f"a 4-bit cache has shape {[tuple(t.shape) for t in [*self.k_caches, *self.v_caches]]}, "
                             f"expected {want}")
+        if not len(self._k) == len(self._v) == m.n_layers:
+            raise MoltError(f"{len(self._k)} and {len(self._v)} 4-bit caches for {m.n_layers} layers")
+        if min(self.block_tables.shape[0], self.context_lens.shape[0]) < B:
+            raise MoltError(f"block_tables has {self.block_tables.shape[0]} rows, context_lens "
+                            f"{self.context_lens.shape[0]}, the call has {B} sequences")
+        dev = self.k_caches[0].get_device()
+        if dev < 0:
+            raise MoltError("4-bit caches must be GPU tensors")
+        if dev != _current_device():
+            raise MoltError(f"the caches are on device {dev}, the current device is {_current_device()}")
 
     def extra(self, model, B, *ks):
         """Workspace bytes that 4-bit caches add to a call of B sequences of 1 + k positions, for each k of ks."""
         if not self.mx:
             return 0
-        self.check(model)
+        self.check(model, B)
         return sum(load().molt_kvq_workspace_extra(ctypes.byref(model.struct), B, k, self.struct.max_blocks_per_seq)
                    for k in ks)
 
