@@ -360,8 +360,11 @@ def kvq_cache(num_blocks, n_kv_heads, head_dim, device="cuda"):
 
 # The calls below take 3 to 8 us on the GPU where they are small, and as long on the host: they ask each tensor
 # for what they need once, and take the paths with messages only where something is wrong.
-_current_device = torch._C._cuda_getDevice
-_raw_stream = torch._C._cuda_getCurrentRawStream    # of a device index, without a torch.cuda.Stream around it (2.6 us)
+# (torch's own names for these two are not public, and missing where torch is built without GPU support, where the
+# package's host parts work all the same)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+# of a device index, without a torch.cuda.Stream around it (2.6 us)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
 def _kvq_caches(k_cache, v_cache, block_tables, starts):

@@ -1,4 +1,7 @@
 """KVCache of 4-bit caches: what a model call would read as something else is refused (host tensors will do here)."""
+import os
+import subprocess
+import sys
 import types
 
 import pytest
@@ -61,3 +64,25 @@ def test_other_caches_are_as_before():
                       torch.zeros(B, dtype=torch.int32))
     kv.check(_model(), B)
     assert kv.extra(_model(), B, 0) == 0
+
+
+def test_import_without_gpu_support():
+    """torch without its GPU functions: the package imports, its prefix cache works, GPU calls refuse host tensors."""
+    code = """
+import torch
+for name in ("_cuda_getDevice", "_cuda_getCurrentRawStream"):
+    if hasattr(torch._C, name):
+        delattr(torch._C, name)
+import paper_2607_21653_amd as molt
+molt.PrefixCache(8)
+cache = molt.kvq_cache(4, 2, 64, device="cpu")
+try:
+    molt.kvq_read(*cache, torch.zeros(1, 4, dtype=torch.int32), torch.zeros(1, dtype=torch.int32), 1)
+except molt.MoltError as e:
+    assert "GPU" in str(e), e
+else:
+    raise SystemExit("not refused")
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr
