@@ -901,7 +901,7 @@ constexpr int kMinCut = 24, kFew = 256;
 // 12.7, 9.4 and 10.6.
 constexpr int kMoreWaves = 8;
 constexpr double kPairTime = 1.7;        // us of a wavefront for a pair of blocks
-void kvq_plan(KvqAttnParams& p, int D, bool f32) {
+void set_plan(KvqAttnParams& p, int D, bool f32) {
   p.G = p.Hq / p.Hkv;
   p.R = p.G * p.n;
   const int tiles = (p.R + 15) / 16, most = f32 ? 1 : kMaxTiles;
@@ -971,13 +971,20 @@ void carve_parts(Carver& c, KvqAttnParams& p, int D) {
 
 }  // namespace
 
+KvqPlan kvq_plan(int B, int n, int Hq, int Hkv, int D, int max_blocks, bool f32) {
+  KvqAttnParams p{};
+  p.B = B; p.n = n; p.Hq = Hq; p.Hkv = Hkv; p.max_blocks = max_blocks;
+  set_plan(p, D, f32);
+  return {p.nrg, p.group, p.slots, p.waves};
+}
+
 // (of the type that needs more)
 size_t kvq_attention_ws_bytes(int B, int n, int Hq, int Hkv, int D, int max_blocks) {
   size_t most = 0;
   for (int f32 = 0; f32 < 2; ++f32) {
     KvqAttnParams p{};
     p.B = B; p.n = n; p.Hq = Hq; p.Hkv = Hkv; p.max_blocks = max_blocks;
-    kvq_plan(p, D, f32 != 0);
+    set_plan(p, D, f32 != 0);
     Carver c(nullptr, 0);
     carve_parts(c, p, D);
     if (c.used && c.used + 256 > most) most = c.used + 256;
@@ -997,7 +1004,7 @@ hipError_t launch_kvq_attention(const void* q, const void* kc, const void* vc, c
   p.B = B; p.n = n; p.Hq = Hq; p.Hkv = Hkv; p.max_blocks = max_blocks; p.num_blocks = num_blocks;
   p.c = kLog2e / sqrtf(float(D));
   p.out_tiled = out_tiled;
-  kvq_plan(p, D, dt == MOLT_F32);
+  set_plan(p, D, dt == MOLT_F32);
   Carver c(ws, 0);
   carve_parts(c, p, D);
   if (dt == MOLT_F32) {

@@ -176,6 +176,10 @@ hipError_t launch_rope_kvq_write(const float* qkv, int B, int k, int Hq, int Hkv
                                  molt_dtype dt, void* q_out, void* k_cache, void* v_cache, hipStream_t s);
 // k, v [B n, Hkv, D]; zeros where a row has no place in the cache
 hipError_t launch_kvq_read(const KvqRows& p, void* k, void* v, int D, molt_dtype dt, hipStream_t s);
+// How launch_kvq_attention does a call: row groups of a kv head, rows of one, workgroups of each (more than B: keys are
+// cut), wavefronts of a workgroup
+struct KvqPlan { int row_groups, group_rows, slots, waves; };
+KvqPlan kvq_plan(int B, int n, int Hq, int Hkv, int D, int max_blocks, bool f32);
 size_t kvq_attention_ws_bytes(int B, int n, int Hq, int Hkv, int D, int max_blocks);
 // n query positions per sequence; out as in launch_paged_attention
 hipError_t launch_kvq_attention(const void* q, const void* kc, const void* vc, const int32_t* bt,

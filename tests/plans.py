@@ -28,5 +28,15 @@ def gemm_plan(M, N, K, part_elems=1 << 62, rope=False):
     return _fn("_ZN4molt9gemm_planEiiilb", GemmPlan, [i, i, i, ctypes.c_long, ctypes.c_bool])(M, N, K, part_elems, rope)
 
 
+class KvqPlan(ctypes.Structure):
+    _fields_ = [("row_groups", ctypes.c_int), ("group_rows", ctypes.c_int), ("slots", ctypes.c_int),
+                ("waves", ctypes.c_int)]
+
+
+def kvq_plan(B, n, Hq, Hkv, D, max_blocks, f32):
+    i = ctypes.c_int
+    return _fn("_ZN4molt8kvq_planEiiiiiib", KvqPlan, [i] * 6 + [ctypes.c_bool])(B, n, Hq, Hkv, D, max_blocks, f32)
+
+
 def moe_plan(dtype, T, K, E, d, F):
     return _fn("_ZN4molt8moe_planE10molt_dtypeiiiii", MoePlan, [ctypes.c_int] * 6)(dtype, T, K, E, d, F)

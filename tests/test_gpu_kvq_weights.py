@@ -54,12 +54,15 @@ def _check(molt, q, q64, caches, K, V, ctx, n, dtype):
     out = out.reshape(q64.shape)
     worst = 0.0
     for b in range(len(ctx)):
-        score = np.einsum("jhgd,phd->jhgp", q64[b], K[b]) / np.sqrt(D)
-        seen = (np.arange(len(K[b]))[None] <= ctx[b] + np.arange(n)[:, None])[:, None, None]
+        rows = q64[b].transpose(1, 0, 2, 3).reshape(Hkv, -1, D)          # of a kv head: position, query head
+        k, v = (x[b].transpose(1, 0, 2) for x in (K, V))
+        score = rows @ k.transpose(0, 2, 1) / np.sqrt(D)
+        seen = np.arange(k.shape[1])[None] <= ctx[b] + np.arange(n)[:, None]
+        seen = np.repeat(seen, rows.shape[1] // n, axis=0)
         w = np.where(seen, np.exp(score - np.where(seen, score, -np.inf).max(axis=-1, keepdims=True)), 0.0)
         w /= w.sum(axis=-1, keepdims=True)
-        want, mag = (np.einsum("jhgp,phd->jhgd", w, x) for x in (V[b], np.abs(V[b])))
-        sum_v = np.einsum("jhgp,phd->jhgd", (w > 0).astype(float), np.abs(V[b]))
+        back = lambda x: x.reshape(Hkv, n, -1, D).transpose(1, 0, 2, 3)
+        want, mag, sum_v = back(w @ v), back(w @ np.abs(v)), back((w > 0).astype(float) @ np.abs(v))
         tol = _tol(want, mag, sum_v, dtype)
         err = np.abs(out[b] - want)
         assert np.isfinite(out[b]).all()
