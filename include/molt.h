@@ -263,7 +263,12 @@ int molt_paged_attention(const void* q, const void* k_cache, const void* v_cache
  * (context_lens[b] + j < 0: a sequence that sits a step out) is zeros. Slots that a row does
  * not see may hold anything. F32 holds the softmax weights in 24 bits; BF16 in 11 beside
  * values that f16 holds (scales 2^-21 .. 2^10; what is under 2^-24 of a row's largest weight
- * is off by 2^-35 of that), in 16 beside others, and the values as they are.
+ * is off by 2^-35 of that), in 16 beside others, and the values as they are. The same call gives
+ * the same bits; where keys are cut into parts, which goes by all sequences' lengths, a
+ * sequence's order of summation, and so its last bits, may change with its neighbours' lengths
+ * (molt_paged_attention's goes by B and the table's width only). Keys are cut where
+ * max_blocks_per_seq and B leave room for it, so a table no wider than the contexts need is
+ * planned best.
  * Supported, all three: D in {64, 128}; Hq % Hkv == 0, Hq/Hkv any; what one launch holds: under
  * 6e7 wavefronts of 16 positions x 128 dims, and in the attention under 1.4e7 groups of 16 (F32)
  * or 48 (BF16) of a kv head's (1+k) * Hq/Hkv rows, tables of at most 2^26 blocks. Errors:

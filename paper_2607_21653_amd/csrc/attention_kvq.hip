@@ -6,28 +6,29 @@
 // (24 bits). bf16: f16 weights (11 bits, times 2^10) beside the values as f16, which are exact while V's scales are
 // 2^-21 .. 2^10; from its first pair of blocks with another scale on a wavefront takes two bf16 parts (16 bits) beside
 // bf16 values. The sum is that of the rounded weights, by an MFMA with a row of ones. The error is that of the output's
-// rounding then, rms 1.66e-3 of the output's rms (weights in one bf16 part: 2.3e-3). 128 sequences x 5 positions at
-// context 8192 take 108 us, with values outside f16 158, with one bf16 part 107; 2 x 257 at 8100 106, 152 and 101.
+// rounding then, rms 1.66e-3 of the output's rms (weights in one bf16 part: 2.3e-3). Kernel times of 128 sequences x 5
+// positions at context 8192, and of 2 x 257 at 8100: 108 and 106 us, with values outside f16 158 and 152, with one bf16
+// part 107 and 101.
 //
 // A workgroup has one kv head of a sequence, or of a part of its keys, and a group of up to 48 rows. Each of its
 // wavefronts walks a range of pairs of 16-token blocks by itself, with running maxima and sums, and they join at the
 // end: no barrier in the loop, and each record byte is read once per row group. The records come by LDS-DMA three
-// pairs ahead (into registers they spilled: 257 us for the first call below). K goes into a scaled MFMA as it lies there
-// (255 us with K decoded to bf16, so 208, both before the DMA), V is decoded to bf16: its scale belongs to a token, the
-// product's sum index. The next pair's scores are computed beside this pair's weights and values.
+// pairs ahead (into registers they spilled: the first call below took twice as long). K goes into a scaled MFMA as it
+// lies there (decoded to bf16: a quarter more), V is decoded: its scale belongs to a token, the product's sum index. The
+// next pair's scores are computed beside this pair's weights and values.
 //
 // 32 query / 4 kv heads x 128, bf16, what bounds the call and what it takes on new inputs:
-//   128 sequences x 5 positions at 8192: the records' 571 MB, 125 us, 4.6 TB/s (a large copy: 4.96; read requests 1.02
-//     times the records); VALU 59% and MFMA 42% of the cycles
-//   256 x 9 at 2048: 72 rows in groups of 3 and 2 tiles, the keys read twice (once through the L2), VALU and MFMA, 125 us
-//   2 x 257 at 8100: 68 GFLOP in 344 workgroups where 512 fit, VALU and MFMA, 91 us, 750 TFLOP/s
-//   16 x 5 at 32768-65536, cut: 429 MB in 101 us with the join's 5, 4.2 TB/s
-//   1 x 1 at 700: launch, four dependent loads and the join, 7 us
-// A loop iteration is 39 MFMAs and 207 VALU instructions at 3 tiles (of them 24 exp2 and 64 for the decoded values);
-// two wavefronts a SIMD, by registers, leave its time near the sum of both pipes. Tried, where the first line took 122
-// us: 5 tiles and one wavefront a SIMD, so that 72 rows read keys once (second, from 148); 64 keys an iteration
-// (125); 3 slots (128); MFMA and VALU interleaved by schedule groups (123-139); a persistent loop over workgroups (second
-// line 146); exponentials, scores and values in other orders (all within 3%).
+//   128 sequences x 5 positions at 8192: the records' 571 MB, 127 us, 4.5 TB/s (a large copy: 4.96; read requests 1.03
+//     times the records); VALU 58% and MFMA 41% of the cycles
+//   256 x 9 at 2048: 72 rows in groups of 3 and 2 tiles, the keys read twice (once through the L2), VALU and MFMA, 130 us
+//   2 x 257 at 8100: 68 GFLOP in 344 workgroups where 512 fit, VALU and MFMA, 96 us, 710 TFLOP/s
+//   16 x 5 at 32768-65536, cut: 429 MB in 105 us with the join's 5, 4.1 TB/s
+//   1 x 1 at 700: launch, four dependent loads and the join, 7.2 us
+// A loop iteration is 39 MFMAs and 216 VALU instructions at 3 tiles (of them 24 exp2, 64 for the decoded values, 5 for
+// their scales' range); two wavefronts a SIMD, by registers, leave its time near the sum of both pipes. Tried, and what
+// the first line then took, in percent: 64 keys an iteration (+2), 3 slots (+5), MFMA and VALU interleaved by schedule
+// groups (+1 to 14), exponentials, scores and values in other orders (within 3); the second line: 5 tiles and one
+// wavefront a SIMD, so that 72 rows read keys once (+25), a persistent loop over workgroups (-1).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -45,8 +46,8 @@ constexpr float kRescaleSlack = 5.0f;
 constexpr float kWeightShift = 10.0f;
 constexpr int kWaves = 4;
 // Pairs of blocks in a wavefront's ring. Workgroups of one wavefront are bound by how many fit in LDS: 201 sequences x
-// 180 positions x 8 heads at 0-404 took 138 us with 4, 109 with 3; the others wait for memory (122 us with 4, 128 with
-// 3 for the first call above).
+// 180 positions x 8 heads at 0-404 took a quarter more with 4 than with 3; the others wait for memory (the first call
+// above: 5% more with 3 than with 4).
 constexpr int slots_of(int wavefronts) { return wavefronts == 1 ? 3 : 4; }
 
 struct KvqAttnParams {
@@ -72,7 +73,6 @@ struct KvqAttnParams {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef bf16x8_t UnalignedBf16x8 __attribute__((aligned(2)));
 typedef floatx4_t UnalignedF4 __attribute__((aligned(4)));
 typedef u32x4 UnalignedU4 __attribute__((aligned(2)));
 typedef u32x2 UnalignedU2 __attribute__((aligned(2)));
@@ -246,7 +246,9 @@ struct Share { int b, part, parts, first; };
 // place (a microsecond). Lane j weighs one of 64 values of c, from no cut at all down, by the time it would take, in
 // pairs of blocks: the longest part, or all parts and what each costs besides (its start and its join of
 // wavefronts, kPartCost) over the workgroups that are resident, half a part more where they do not all fit at
-// once, and the joining launch (kJoinCost) if anything is cut. Of equal ones the longest c wins.
+// once, and the joining launch (kJoinCost) if anything is cut. Of equal ones the longest c wins. The choice is flat about
+// these constants: with half and twice kPartCost, and with none or a whole part more for the second round, 11 cut calls
+// (1 to 100 sequences at contexts of 0 to 65536, both types) took within 4% of the same.
 constexpr int kMaxCut = 256, kMinPairs = 4;
 constexpr float kJoinCost = 15.f;       // (73 x 9 positions x 16 heads at 824-1649: 30.0 us, 34.4 with 30; others alike)
 MOLT_DEV float cut(float pairs, float inv_c) { return fmaxf(1.f, ceilf(pairs * inv_c)); }
@@ -694,7 +696,7 @@ MOLT_DEV void attend(const KvqAttnParams& p, uint8_t* lds, int rg, int r0, int h
   };
   // In each loop the scores of the next pair (past the last: of whatever its slot holds, not used) go beside the weights
   // and values of this one. The stretch without MFMAs, settle, goes first, so that the other wavefront's run beside it
-  // (2 x 257 positions at 8100: 102 us, 104 with the priorities the other way round, 111 without).
+  // (2 x 257 positions at 8100 took 2% more with the priorities the other way round, 9% without).
   int pi = p0;
   for (; pi < p1 && (F32 || shift != 0.f); ++pi) {
     advance(pi);
@@ -895,10 +897,11 @@ constexpr int kMaxTiles = 3;             // 16-row tiles of a wavefront (bf16; o
 // D = 64: 9.4, 10.6, 12.3, 15.3 and 16.6, 18.8, 19.5, 22.6.
 constexpr int kMinCut = 24, kFew = 256;
 // Wavefronts of an uncut workgroup, 1, 4 or 8: the fewer, the more workgroups run at a time and the less there is to
-// join, the more, the sooner a long key range is done. The rule weighs rounds of workgroups by what one takes; us of
-// calls with 1, 4 and 8: 19844 workgroups of up to 9 pairs (f32) 108, 256 and 544; 2016 of 1 pair (2.5 tiles) 26, 36
-// and 75; 1584 of 49 pairs (3 tiles) 167, 120 and 145; 48 of 32 pairs (f32) 35, 19.6 and 14.6; 8 of 4 pairs (3 tiles)
-// 12.7, 9.4 and 10.6.
+// join, the more, the sooner a long key range is done. The rule weighs rounds of workgroups by what one takes, a start and
+// join and its pairs, with constants that fit what calls took, in us with 1, 4 and 8 wavefronts: 8 workgroups (3 tiles) of
+// 1 pair 9.0, 9.0 and 9.5, of 4 pairs 12.2, 8.9 and 9.6, of 32 pairs 42, 17.4 and 15.4; 8 (f32, 64 dims) of 1 pair 5.2, 6.0
+// and 5.7, of 32 pairs 31, 12.3 and 10.4; 1600 (3 tiles) of 1 pair 25, 33 and 58, of 4 to 8 pairs 33, 39 and 66; 2016 of 1
+// pair (2.5 tiles) 26, 36 and 75; 1584 of 49 pairs (3 tiles) 167, 120 and 145; 19844 of up to 9 pairs (f32) 108, 256, 544.
 constexpr int kMoreWaves = 8;
 constexpr double kPairTime = 1.7;        // us of a wavefront for a pair of blocks
 void set_plan(KvqAttnParams& p, int D, bool f32) {

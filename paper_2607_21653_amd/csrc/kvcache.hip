@@ -41,8 +41,8 @@ MOLT_DEV void store8(float* p, const uint32_t (&v)[4]) {
 // Both kernels: wavefront = one block of one sequence, and one kv head of 128 dims or two of 64, its keys and its
 // values. The block's place is found once, on the scalar unit, and all of a wavefront's loads are in flight together.
 // Bound by HBM, or by the launch and three dependent loads where there is little: 4 kv heads x 128, bf16, 128 sequences
-// x 5 rows written in 4.7 us and read in 3.7; f32, 4000 rows written in 5.8 us (18.6 MB, 3.2 TB/s) and 6000 read, a third
-// of them zeros, in 9.4; 144000 bf16 rows read, of 262144 with the zeros behind, in 123 us (5.0 TB/s; a large copy: 4.96).
+// x 5 rows written in 4.6 us and read in 3.7; f32, 4000 rows written in 5.8 us (18.6 MB, 3.2 TB/s) and 6000 read, a third
+// of them zeros, in 8.6; 144000 bf16 rows read, of 262144 with the zeros behind, in 123 us (5.0 TB/s; a large copy: 4.96).
 // Keys: instruction i, lane: an octet of dims of one token, 16 contiguous bytes of a bf16 row and 4 of the cache;
 // values: the lane has an octet of dims of the 4 tokens that share its 16 bytes of the cache.
 template <int D>
@@ -211,7 +211,9 @@ __global__ __launch_bounds__(kThreads) void kvq_read_kernel(KvqRows p, int nblk,
 
 // The decoder's rows: workgroup = token t of the QKV projection's f32 rows, rotated in f64 with the step's table as for
 // the other caches. q -> q_out; thread = octet of a key (both halves of its pairs read, its own rotated) or value
-// head, rounded to the model's type, then quantised: the bytes that kvq_write makes of those rows.
+// head, rounded to the model's type, then quantised: the bytes that kvq_write makes of those rows. 640 tokens of 32 query
+// and 2 x 4 kv heads x 128, bf16: 10.9 us, 19 MB (the f32 rows in, q and the records out); the QKV product before it takes
+// 24.1, together 35 where the product that rotates and stores in its epilogue takes 32 for the bf16 cache.
 MOLT_DEV void store_q(uint16_t* p, float x) { *p = f32_to_bf16(x); }
 MOLT_DEV void store_q(float* p, float x) { *p = x; }
 template <int D, typename T>

@@ -15,7 +15,6 @@
 
 namespace molt {
 
-constexpr int kKvqGroup = 32;                 // elements per scale
 constexpr uint32_t kKvqScaleNan = 255u;
 
 template <int D>
@@ -69,7 +68,7 @@ MOLT_DEV uint32_t kvq_decode2_f16(uint32_t w, uint32_t scale_bits) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, __uint_as_float(scale_bits), I));
 }
 constexpr uint32_t kKvqF16First = 106u;      // 106 .. 137: 2^-21 .. 2^10
-// nonzero if one of 4 scale bytes is outside 106 .. 137 (a borrow from a byte's difference comes from one that is)
+// nonzero if one of 8 scale bytes is outside 106 .. 137 (a borrow from a byte's difference comes from one that is)
 MOLT_DEV uint32_t kvq_outside_f16(uint32_t a, uint32_t b) {
   return ((a - kKvqF16First * 0x01010101u) | (b - kKvqF16First * 0x01010101u)) & 0xe0e0e0e0u;
 }
