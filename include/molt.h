@@ -293,6 +293,108 @@ int molt_paged_attention_kvq(const void* q, const void* k_cache, const void* v_c
                              void* workspace, size_t workspace_bytes, molt_stream_t stream);
 
 /* ------------------------------------------------------------------------------
+ * Sparse attention over the paged cache: each query position attends to a few blocks, which a
+ * cheap score picks for it; and the upkeep of tables and caches that a decoding loop needs to
+ * run without the host. F32 and BF16 caches (layouts above), D in {64, 128}, Hq/Hkv any.
+ *
+ * molt_plan_blocks -- block tables that follow the lengths, and the new rows' slots.
+ *   block_tables [B, max_blocks_per_seq], n_blocks [B] i32, in/out: a sequence's blocks are the
+ *                first n_blocks[b] entries of its row
+ *   context_lens, n_new [B] i32: tokens cached, and rows that the next call adds (0 .. n), or
+ *                n_new[b] < 0: the sequence is finished
+ *   pool         [2 + num_blocks] i32, in/out: head, count, and a ring of num_blocks places that
+ *                holds the free blocks' ids from place `head` on
+ *   n_shared     [B] i32 or NULL (0): leading entries of a row that belong to others (a prefix
+ *                cache) and are not given back
+ *   out_slots    [B n] i32: row b n + j (j < n_new[b]) gets 16 * block + position % 16 of position
+ *                context_lens[b] + j, others -1
+ *   out_placed   [B] i32: n_new[b] of a sequence whose rows have slots, else 0
+ * A sequence needs ceil((context_lens[b] + n_new[b]) / 16) blocks if n_new[b] > 0; those beside
+ * its n_blocks[b] come from the head of the ring, sequence by sequence. From the first sequence
+ * on whose need, added to those before, the pool does not meet, sequences with a need get none and
+ * out_placed 0. Nor do those whose numbers are out of range: n_new[b] > n, context_lens[b] < 0, a
+ * table too narrow, n_blocks[b] outside [0, max_blocks_per_seq]; their state stays. Finished
+ * sequences give entries n_shared[b] .. n_blocks[b] - 1 back behind the ring's last place, in
+ * their order, and have n_blocks[b] = 0; what they give back is not taken in the same call. A
+ * slot is -1 where the block's id is outside [0, num_blocks). The result does not depend on
+ * timing. One launch for up to 1024 sequences and B n <= 8192, else two and a workspace.
+ *
+ * molt_kv_write -- rows into a cache by slot: row r of k and v ([rows, n_kv_heads, D], rows k_stride
+ * and v_stride elements apart) goes to token slots[r] % 16 of block slots[r] / 16; rows whose slot
+ * is outside [0, 16 num_blocks) are not written. Of rows with the same slot one stays, element by
+ * element.
+ *
+ * molt_key_bounds_update -- bounds of the keys of the blocks that hold positions starts[b] ..
+ * starts[b] + lens[b] - 1 (lens: [B] i32 in [0, n], or NULL: n), of their tokens up to the last of these
+ * positions. Call it after the rows are written. Where lens[b] is 0, a position is outside the
+ * table or a block's id outside [0, num_blocks), nothing is written. For a block and kv head let M_d and m_d
+ * be the largest and smallest key in dim d, a the largest |M_d|, |m_d|, e the smallest integer
+ * >= -100 with a <= 127 * 2^e: the codes are ceil(M_d / 2^e) and floor(m_d / 2^e), whole numbers in
+ * -127 .. 127. A block with an infinity or NaN has e = 127 and codes 0.
+ *   bounds  uint8 [num_blocks, n_kv_heads, 2 D + 16]: codes of M, codes of m, e (signed bytes),
+ *           15 bytes of 0; starts at a multiple of 16 bytes. All-zero records score 0.
+ * molt_key_bounds_read -- codes of blocks ids[i], i < M, as the values that they stand for:
+ * out_hi, out_lo [M, n_kv_heads, D] f32 (e = 127: +inf and -inf; ids outside [0, num_blocks): NaN).
+ *
+ * molt_select_blocks -- for each query position t = b (1+k) + j and kv head the n_select blocks of
+ * largest score of those that hold positions 0 .. context_lens[b] + j: out [T, n_kv_heads, n_select]
+ * i32, numbers of the sequence's blocks (columns of its table) in ascending order, then -1. A
+ * query row q (one head's D elements of dtype) has codes c_d = q_d / 2^f to the nearest integer, ties to even,
+ * f by the rule for e above (c = 0 where the row has an infinity or NaN); its score of a block is
+ *     2^min(max(e + f, -100), 100) * sum_d max(c_d * M-code_d, c_d * m-code_d),
+ * exact, +inf where e = 127; the kv head's is the largest of its Hq/Hkv rows'. So no key of a
+ * block that is left out has a larger product with a (rounded) query row than the least score of the list.
+ * Blocks 0 .. n_first - 1 and the last n_last that the position sees come before all others; equal
+ * scores go to the lower block. Rows j >= lens[b] ([B] i32, or NULL: all count) and rows that
+ * see no position have empty lists; a block whose id is outside [0, num_blocks) is in none.
+ * n_first >= 0, n_last >= 1, n_first + n_last <= n_select.
+ *
+ * molt_paged_attention_blocks -- molt_paged_attention where row t and kv head h see only the keys of
+ * the blocks blocks[t, h, :] ([T, n_kv_heads, n_list] i32, in any order): positions up to
+ * context_lens[b] + j of these. Entries outside [0, max_blocks_per_seq), blocks past the position
+ * and blocks whose id is outside [0, num_blocks) are passed over; a block listed twice counts
+ * twice; a row without a key is zeros. Keys and values that a row does not see may hold anything.
+ * Softmax weights are held in 16 bits (BF16) or 24 (F32), sums in f32; the same call gives the same
+ * bits.
+ *
+ * Errors, all: INVALID_ARG for NULL required pointers, sizes outside the above or past what a
+ * launch holds (2^32 threads), caches, bounds, q or out that are not 16-byte aligned; WORKSPACE. A
+ * workspace size is 0 where none is needed, and for sizes that no call takes.
+ * ---------------------------------------------------------------------------- */
+size_t molt_plan_blocks_workspace_size(int B, int n);
+int molt_plan_blocks(int32_t* block_tables, int32_t* n_blocks, const int32_t* context_lens,
+                     const int32_t* n_new, int32_t* pool, const int32_t* n_shared, int B, int n,
+                     int max_blocks_per_seq, int num_blocks, int32_t* out_slots,
+                     int32_t* out_placed, void* workspace, size_t workspace_bytes,
+                     molt_stream_t stream);
+int molt_kv_write(const void* k, const void* v, long long k_stride, long long v_stride,
+                  const int32_t* slots, int rows, int n_kv_heads, int head_dim, int num_blocks,
+                  molt_dtype dtype, void* k_cache, void* v_cache, molt_stream_t stream);
+int molt_key_bounds_update(const void* k_cache, void* bounds, const int32_t* block_tables,
+                           const int32_t* starts, const int32_t* lens, int B, int n,
+                           int n_kv_heads, int head_dim, int max_blocks_per_seq, int num_blocks,
+                           molt_dtype dtype, molt_stream_t stream);
+int molt_key_bounds_read(const void* bounds, const int32_t* ids, int M, int n_kv_heads,
+                         int head_dim, int num_blocks, float* out_hi, float* out_lo,
+                         molt_stream_t stream);
+size_t molt_select_blocks_workspace_size(int B, int k, int n_q_heads, int n_kv_heads, int head_dim,
+                                         int max_blocks_per_seq);
+int molt_select_blocks(const void* q, const void* bounds, const int32_t* block_tables,
+                       const int32_t* context_lens, const int32_t* lens, int B, int k,
+                       int n_q_heads, int n_kv_heads, int head_dim, int max_blocks_per_seq,
+                       int num_blocks, int n_select, int n_first, int n_last, molt_dtype dtype,
+                       int32_t* out, void* workspace, size_t workspace_bytes,
+                       molt_stream_t stream);
+size_t molt_paged_attention_blocks_workspace_size(int B, int k, int n_q_heads, int n_kv_heads,
+                                                  int head_dim, int n_list);
+int molt_paged_attention_blocks(const void* q, const void* k_cache, const void* v_cache,
+                                const int32_t* block_tables, const int32_t* context_lens,
+                                const int32_t* blocks, int B, int k, int n_q_heads,
+                                int n_kv_heads, int head_dim, int max_blocks_per_seq,
+                                int num_blocks, int n_list, molt_dtype dtype, void* out,
+                                void* workspace, size_t workspace_bytes, molt_stream_t stream);
+
+/* ------------------------------------------------------------------------------
  * molt_dense_gemm -- the dense projection of the verify step's decoder (QKV, O, router,
  * LM head): C[M, N] (f32, row-major) = A[M, K] * B[N, K]^T, or C += A * B^T with
  * accumulate != 0 (the O projection adds into the residual stream). A and B in `dtype`

@@ -72,6 +72,16 @@ _SIGS = {
     "molt_paged_attention_kvq": (c_int, [c_vp, c_vp, c_vp, c_vp, c_vp, c_int, c_int, c_int, c_int,
                                          c_int, c_int, c_int, c_int, c_vp, c_vp, c_size, c_vp]),
     "molt_kvq_workspace_extra": (c_size, [ctypes.POINTER(MoltModel), c_int, c_int, c_int]),
+    "molt_plan_blocks_workspace_size": (c_size, [c_int, c_int]),
+    "molt_plan_blocks": (c_int, [c_vp] * 6 + [c_int] * 4 + [c_vp, c_vp, c_vp, c_size, c_vp]),
+    "molt_kv_write": (c_int, [c_vp, c_vp, ctypes.c_longlong, ctypes.c_longlong, c_vp, c_int, c_int, c_int, c_int,
+                              c_int, c_vp, c_vp, c_vp]),
+    "molt_key_bounds_update": (c_int, [c_vp] * 5 + [c_int] * 7 + [c_vp]),
+    "molt_key_bounds_read": (c_int, [c_vp, c_vp, c_int, c_int, c_int, c_int, c_vp, c_vp, c_vp]),
+    "molt_select_blocks_workspace_size": (c_size, [c_int] * 6),
+    "molt_select_blocks": (c_int, [c_vp] * 5 + [c_int] * 11 + [c_vp, c_vp, c_size, c_vp]),
+    "molt_paged_attention_blocks_workspace_size": (c_size, [c_int] * 6),
+    "molt_paged_attention_blocks": (c_int, [c_vp] * 6 + [c_int] * 9 + [c_vp, c_vp, c_size, c_vp]),
     "molt_decoder_workspace_size": (c_size, [ctypes.POINTER(MoltModel), c_int, c_int, c_int]),
     "molt_decoder_forward": (c_int, [ctypes.POINTER(MoltModel), ctypes.POINTER(MoltKV), c_int,
                                      c_int, c_vp, c_vp, c_vp, c_size, c_vp]),
@@ -487,6 +497,228 @@ def paged_attention_kvq(q, k_cache, v_cache, block_tables, context_lens, k, work
         status = lib.molt_paged_attention_kvq(*args, _ptr(own), have, _raw_stream(dev))
     if status:
         _check(status, "molt_paged_attention_kvq")
+    return out
+
+
+# ------------------------------------------------------------------ sparse attention over listed blocks
+
+def _i32(t, shape, dev, name):
+    """Checks an int32 tensor of shape on device dev."""
+    if t.dtype is not torch.int32 or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        _dev(t, torch.int32, shape, name)
+        raise MoltError(f"{name} must be on device {dev}, is on {t.device}")
+
+
+def _float_dtype(t, name):
+    dt = t.dtype
+    if dt is not torch.bfloat16 and dt is not torch.float32:
+        raise MoltError(f"{name} has dtype {dt}, expected float32 or bfloat16")
+    return dt
+
+
+def _here(t, name):
+    """Index of a tensor's device, which must be the current one."""
+    dev = t.get_device()
+    if dev < 0:
+        raise MoltError(f"{name} must be a GPU tensor")
+    if dev != _current_device():
+        raise MoltError(f"{name} is on device {dev}, the current device is {_current_device()}")
+    return dev
+
+
+def _tables(block_tables, context_lens, dev):
+    """(B, max_blocks) of a table and its lengths on device dev."""
+    table = block_tables.shape
+    if len(table) != 2:
+        raise MoltError(f"block_tables has shape {tuple(table)}, expected (B, max_blocks)")
+    _i32(block_tables, table, dev, "block_tables")
+    _i32(context_lens, table[:1], dev, "context_lens")
+    return table
+
+
+def _cache_pair(k_cache, v_cache):
+    """(device, dtype, num_blocks, n_kv_heads, head_dim) of a bf16 or f32 cache."""
+    dev, dt, shape = _here(k_cache, "k_cache"), _float_dtype(k_cache, "k_cache"), k_cache.shape
+    if len(shape) != 4 or shape[2] != 16:
+        raise MoltError(f"k_cache has shape {tuple(shape)}, expected [num_blocks, n_kv_heads, 16, head_dim]")
+    nb, Hkv, _, D = shape
+    _dev(k_cache, dt, shape, "k_cache")
+    if v_cache is not None:
+        _dev(v_cache, dt, (nb, Hkv, D, 16), "v_cache")
+        _same_device(v_cache, dev, "v_cache")
+    return dev, dt, nb, Hkv, D
+
+
+def _bounds_shape(bounds):
+    """(num_blocks, n_kv_heads, head_dim) of key bounds."""
+    shape = bounds.shape
+    if len(shape) != 3 or shape[2] % 2:
+        raise MoltError(f"bounds has shape {tuple(shape)}, expected [num_blocks, n_kv_heads, 2 * head_dim + 16]")
+    _dev(bounds, torch.uint8, shape, "bounds")
+    return shape[0], shape[1], (shape[2] - 16) // 2
+
+
+def _given(workspace, dev):
+    """Address and bytes of a caller's workspace."""
+    if workspace is None:
+        return None, 0
+    _same_device(workspace, dev, "workspace")
+    if not workspace.is_contiguous():
+        raise MoltError("workspace must be contiguous")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def block_pool(num_blocks, device="cuda"):
+    """A pool for plan_blocks in which blocks 0 .. num_blocks - 1 are free: int32 [2 + num_blocks]."""
+    pool = torch.arange(-2, num_blocks, dtype=torch.int32, device=device)
+    pool[0], pool[1] = 0, num_blocks
+    return pool
+
+
+def plan_blocks(block_tables, n_blocks, context_lens, n_new, pool, n, n_shared=None):
+    """Lets the block tables follow the lengths (molt_plan_blocks), all on the GPU and in place: sequence b gets the
+    blocks that rows context_lens[b] .. + n_new[b] - 1 need from pool, or gives its own back where n_new[b] < 0.
+    Returns (slots [B*n] i32 for kv_write, -1 where there is no row; placed [B] i32, rows that have slots)."""
+    lib = _lib or load()
+    dev = _here(block_tables, "block_tables")
+    B, maxb = _tables(block_tables, context_lens, dev)
+    _i32(n_blocks, (B,), dev, "n_blocks")
+    _i32(n_new, (B,), dev, "n_new")
+    if pool.dim() != 1 or pool.numel() < 3:
+        raise MoltError(f"pool has shape {tuple(pool.shape)}, expected (2 + num_blocks,)")
+    _i32(pool, pool.shape, dev, "pool")
+    if n_shared is not None:
+        _i32(n_shared, (B,), dev, "n_shared")
+    if n < 1:
+        raise MoltError(f"n = {n} must be >= 1")
+    slots, placed = n_new.new_empty(B * n), n_new.new_empty(B)
+    ws, have = _workspace(lib.molt_plan_blocks_workspace_size(B, n), n_new.device)
+    status = lib.molt_plan_blocks(block_tables.data_ptr(), n_blocks.data_ptr(), context_lens.data_ptr(),
+                                  n_new.data_ptr(), pool.data_ptr(), _ptr(n_shared), B, n, maxb, pool.numel() - 2,
+                                  slots.data_ptr(), placed.data_ptr(), _ptr(ws), have, _raw_stream(dev))
+    if status:
+        _check(status, "molt_plan_blocks")
+    return slots, placed
+
+
+def kv_write(k, v, k_cache, v_cache, slots):
+    """Writes rows k, v [T, Hkv, D] (row-strided views will do) into a bf16 or f32 cache at slots [T] i32 (block * 16 +
+    token, as plan_blocks gives them); rows whose slot is outside the cache are left out."""
+    lib = _lib or load()
+    dev, dt, nb, Hkv, D = _cache_pair(k_cache, v_cache)
+    T = slots.numel()
+    _i32(slots, (T,), dev, "slots")
+    ks, vs = _rows_stride(k, dt, T, Hkv, D, dev, "k"), _rows_stride(v, dt, T, Hkv, D, dev, "v")
+    status = lib.molt_kv_write(k.data_ptr(), v.data_ptr(), ks, vs, slots.data_ptr(), T, Hkv, D, nb, DTYPE_CODE[dt],
+                               k_cache.data_ptr(), v_cache.data_ptr(), _raw_stream(dev))
+    if status:
+        _check(status, "molt_kv_write")
+
+
+def key_bounds(num_blocks, n_kv_heads, head_dim, device="cuda"):
+    """Empty bounds of a cache's keys (molt.h): uint8 [num_blocks, n_kv_heads, 2 D + 16]."""
+    return torch.zeros(num_blocks, n_kv_heads, 2 * head_dim + 16, dtype=torch.uint8, device=device)
+
+
+def key_bounds_update(k_cache, bounds, block_tables, starts, n, lens=None):
+    """Bounds of the keys of the blocks that hold positions starts[b] + j, j < n (j < lens[b] if given), after
+    kv_write of these rows."""
+    lib = _lib or load()
+    dev, dt, nb, Hkv, D = _cache_pair(k_cache, None)
+    B, maxb = _tables(block_tables, starts, dev)
+    _dev(bounds, torch.uint8, (nb, Hkv, 2 * D + 16), "bounds")
+    _same_device(bounds, dev, "bounds")
+    if lens is not None:
+        _i32(lens, (B,), dev, "lens")
+    status = lib.molt_key_bounds_update(k_cache.data_ptr(), bounds.data_ptr(), block_tables.data_ptr(),
+                                        starts.data_ptr(), _ptr(lens), B, n, Hkv, D, maxb, nb, DTYPE_CODE[dt],
+                                        _raw_stream(dev))
+    if status:
+        _check(status, "molt_key_bounds_update")
+
+
+def key_bounds_read(bounds, ids):
+    """The bounds of blocks ids [M] i32 of the cache as values: (largest, smallest) f32 [M, Hkv, D]."""
+    lib = _lib or load()
+    dev = _here(bounds, "bounds")
+    nb, Hkv, D = _bounds_shape(bounds)
+    M = ids.numel()
+    _i32(ids, (M,), dev, "ids")
+    hi = torch.empty(M, Hkv, D, dtype=torch.float32, device=bounds.device)
+    lo = torch.empty_like(hi)
+    status = lib.molt_key_bounds_read(bounds.data_ptr(), ids.data_ptr(), M, Hkv, D, nb, hi.data_ptr(), lo.data_ptr(),
+                                      _raw_stream(dev))
+    if status:
+        _check(status, "molt_key_bounds_read")
+    return hi, lo
+
+
+def _queries(q, B, k, D, dev):
+    """(dtype, n_q_heads) of query rows [B*(1+k), Hq, D]."""
+    dt, shape = _float_dtype(q, "q"), q.shape
+    if len(shape) != 3 or shape[0] != B * (k + 1) or shape[2] != D or not q.is_contiguous():
+        _dev(q, None, (B * (k + 1), shape[1] if len(shape) == 3 else "Hq", D), "q")
+    _same_device(q, dev, "q")
+    return dt, shape[1]
+
+
+def select_blocks_workspace_size(B, k, n_q_heads, n_kv_heads, head_dim, max_blocks):
+    return load().molt_select_blocks_workspace_size(B, k, n_q_heads, n_kv_heads, head_dim, max_blocks)
+
+
+def select_blocks(q, bounds, block_tables, context_lens, k, n_select, n_first=1, n_last=2, lens=None, workspace=None):
+    """For each query position (q [B*(1+k), Hq, D], f32|bf16, at context_lens[b] + j) and kv head the n_select blocks
+    of largest score by the keys' bounds (molt_select_blocks), the first n_first and last n_last among them: i32
+    [B*(1+k), Hkv, n_select], ascending, then -1. Rows j >= lens[b] have empty lists."""
+    lib = _lib or load()
+    dev = _here(bounds, "bounds")
+    nb, Hkv, D = _bounds_shape(bounds)
+    B, maxb = _tables(block_tables, context_lens, dev)
+    dt, Hq = _queries(q, B, k, D, dev)
+    if lens is not None:
+        _i32(lens, (B,), dev, "lens")
+    if n_select < 1:
+        raise MoltError(f"n_select = {n_select} must be >= 1")
+    ws, have = _given(workspace, dev)
+    out = block_tables.new_empty(B * (k + 1), Hkv, n_select)
+    args = (q.data_ptr(), bounds.data_ptr(), block_tables.data_ptr(), context_lens.data_ptr(), _ptr(lens), B, k, Hq,
+            Hkv, D, maxb, nb, n_select, n_first, n_last, DTYPE_CODE[dt], out.data_ptr())
+    status = lib.molt_select_blocks(*args, ws, have, _raw_stream(dev))
+    if status == MOLT_ERR_WORKSPACE:     # none, or one that is too small
+        own, have = _workspace(lib.molt_select_blocks_workspace_size(B, k, Hq, Hkv, D, maxb), q.device)
+        status = lib.molt_select_blocks(*args, _ptr(own), have, _raw_stream(dev))
+    if status:
+        _check(status, "molt_select_blocks")
+    return out
+
+
+def paged_attention_blocks_workspace_size(B, k, n_q_heads, n_kv_heads, head_dim, n_list):
+    return load().molt_paged_attention_blocks_workspace_size(B, k, n_q_heads, n_kv_heads, head_dim, n_list)
+
+
+def paged_attention_blocks(q, k_cache, v_cache, block_tables, context_lens, k, blocks, workspace=None):
+    """paged_attention over the blocks that blocks [B*(1+k), Hkv, N] i32 lists for each position and kv head
+    (select_blocks; -1: none): returns [B*(1+k), Hq*D] of q's dtype."""
+    lib = _lib or load()
+    dev, dt, nb, Hkv, D = _cache_pair(k_cache, v_cache)
+    B, maxb = _tables(block_tables, context_lens, dev)
+    qt, Hq = _queries(q, B, k, D, dev)
+    if qt is not dt:
+        raise MoltError(f"q has dtype {qt}, the caches {dt}")
+    if blocks.dim() != 3:
+        raise MoltError(f"blocks has shape {tuple(blocks.shape)}, expected ({B * (k + 1)}, {Hkv}, n_list)")
+    N = blocks.shape[2]
+    _i32(blocks, (B * (k + 1), Hkv, N), dev, "blocks")
+    ws, have = _given(workspace, dev)
+    out = q.new_empty(B * (k + 1), Hq * D)
+    args = (q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_tables.data_ptr(), context_lens.data_ptr(),
+            blocks.data_ptr(), B, k, Hq, Hkv, D, maxb, nb, N, DTYPE_CODE[dt], out.data_ptr())
+    status = lib.molt_paged_attention_blocks(*args, ws, have, _raw_stream(dev))
+    if status == MOLT_ERR_WORKSPACE:
+        own, have = _workspace(lib.molt_paged_attention_blocks_workspace_size(B, k, Hq, Hkv, D, N), q.device)
+        status = lib.molt_paged_attention_blocks(*args, _ptr(own), have, _raw_stream(dev))
+    if status:
+        _check(status, "molt_paged_attention_blocks")
     return out
 
 

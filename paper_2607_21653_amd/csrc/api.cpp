@@ -605,6 +605,176 @@ int molt_paged_attention_kvq(const void* q, const void* k_cache, const void* v_c
   return hip_status(e, "molt_paged_attention_kvq");
 }
 
+// ------------------------------------------------------------------ sparse attention over listed blocks
+
+// Slots are ints, positions of a table too; a launch holds 2^32 threads, of workgroups of 256
+constexpr int kMaxPoolBlocks = (1 << 27) - 1, kMaxTableBlocks = 1 << 26;
+constexpr double kMaxGroups = 1.6e7;
+
+static bool aligned16(const void* a, const void* b = nullptr, const void* c = nullptr, const void* d = nullptr) {
+  return (reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b) | reinterpret_cast<uintptr_t>(c) |
+          reinterpret_cast<uintptr_t>(d)) % 16 == 0;
+}
+
+static int blocks_sizes_ok(int Hkv, int D, int num_blocks) {
+  REQUIRE(D == 64 || D == 128, "head_dim = %d must be 64 or 128", D);
+  REQUIRE(Hkv >= 1 && double(Hkv) * D < 1.0e6, "n_kv_heads = %d must be >= 1, n_kv_heads * head_dim < 10^6", Hkv);
+  REQUIRE(num_blocks >= 1 && num_blocks <= kMaxPoolBlocks, "num_blocks = %d must be in [1, 2^27)", num_blocks);
+  return MOLT_OK;
+}
+static int blocks_table_ok(int B, int n, int max_blocks) {
+  REQUIRE(B >= 1, "B = %d must be >= 1", B);
+  REQUIRE(n >= 1, "n = %d rows of a sequence must be >= 1", n);
+  REQUIRE(double(B) * n < 2.0e9, "B = %d times n = %d rows is too large", B, n);
+  REQUIRE(max_blocks >= 1 && max_blocks <= kMaxTableBlocks, "max_blocks_per_seq = %d must be in [1, 2^26]", max_blocks);
+  return MOLT_OK;
+}
+
+size_t molt_plan_blocks_workspace_size(int B, int n) { return B < 1 || n < 1 ? 0 : molt::plan_ws_bytes(B, n); }
+
+int molt_plan_blocks(int32_t* block_tables, int32_t* n_blocks, const int32_t* context_lens, const int32_t* n_new,
+                     int32_t* pool, const int32_t* n_shared, int B, int n, int max_blocks, int num_blocks,
+                     int32_t* out_slots, int32_t* out_placed, void* workspace, size_t workspace_bytes,
+                     molt_stream_t stream) {
+  if (int r = blocks_table_ok(B, n, max_blocks)) return r;
+  REQUIRE(num_blocks >= 1 && num_blocks <= kMaxPoolBlocks, "num_blocks = %d must be in [1, 2^27)", num_blocks);
+  REQUIRE(double(B) * n / 256 + B < kMaxGroups, "B = %d sequences of n = %d rows are too many", B, n);
+  REQUIRE(block_tables && n_blocks && context_lens && n_new && pool && out_slots && out_placed,
+          "a required pointer is NULL");
+  if (int r = check_ws(workspace, workspace_bytes, molt::plan_ws_bytes(B, n))) return r;
+  return hip_status(molt::launch_plan_blocks(block_tables, n_blocks, context_lens, n_new, pool, n_shared, B, n, max_blocks,
+                                             num_blocks, out_slots, out_placed, workspace, workspace_bytes,
+                                             reinterpret_cast<hipStream_t>(stream)),
+                    "molt_plan_blocks");
+}
+
+int molt_kv_write(const void* k, const void* v, long long k_stride, long long v_stride, const int32_t* slots, int rows,
+                  int Hkv, int D, int num_blocks, molt_dtype dtype, void* k_cache, void* v_cache,
+                  molt_stream_t stream) {
+  if (int r = blocks_sizes_ok(Hkv, D, num_blocks)) return r;
+  REQUIRE(act_ok(dtype), "dtype must be F32 or BF16");
+  REQUIRE(rows >= 1, "rows = %d must be >= 1", rows);
+  REQUIRE((double(rows) + 15) / 16 * ((double(Hkv) * D + 127) / 128) / 4 < kMaxGroups,
+          "rows * n_kv_heads * head_dim too large");
+  REQUIRE(k && v && slots && k_cache && v_cache, "a required pointer is NULL");
+  REQUIRE(k_cache != v_cache, "k_cache and v_cache are the same");
+  REQUIRE(aligned16(k_cache, v_cache), "the caches must start at a multiple of 16 bytes");
+  REQUIRE(k_stride >= (long long)Hkv * D && v_stride >= (long long)Hkv * D,
+          "row strides %lld and %lld must be at least n_kv_heads * head_dim = %lld", k_stride, v_stride,
+          (long long)Hkv * D);
+  return hip_status(molt::launch_kv_write(k, k_stride, v, v_stride, slots, rows, Hkv, D, num_blocks, dtype, k_cache,
+                                          v_cache, reinterpret_cast<hipStream_t>(stream)),
+                    "molt_kv_write");
+}
+
+int molt_key_bounds_update(const void* k_cache, void* bounds, const int32_t* block_tables, const int32_t* starts,
+                           const int32_t* lens, int B, int n, int Hkv, int D, int max_blocks, int num_blocks,
+                           molt_dtype dtype, molt_stream_t stream) {
+  if (int r = blocks_sizes_ok(Hkv, D, num_blocks)) return r;
+  if (int r = blocks_table_ok(B, n, max_blocks)) return r;
+  REQUIRE(act_ok(dtype), "dtype must be F32 or BF16");
+  REQUIRE(double(B) * ((double(n) + 30) / 16) * Hkv / 4 < kMaxGroups, "B * n * n_kv_heads too large");
+  REQUIRE(k_cache && bounds && block_tables && starts, "a required pointer is NULL");
+  REQUIRE(aligned16(k_cache, bounds), "the cache and its bounds must start at a multiple of 16 bytes");
+  return hip_status(molt::launch_bounds_update(k_cache, bounds, block_tables, starts, lens, B, n, Hkv, D, max_blocks,
+                                               num_blocks, dtype, reinterpret_cast<hipStream_t>(stream)),
+                    "molt_key_bounds_update");
+}
+
+int molt_key_bounds_read(const void* bounds, const int32_t* ids, int M, int Hkv, int D, int num_blocks, float* out_hi,
+                         float* out_lo, molt_stream_t stream) {
+  if (int r = blocks_sizes_ok(Hkv, D, num_blocks)) return r;
+  REQUIRE(M >= 1, "M = %d must be >= 1", M);
+  REQUIRE(double(M) * Hkv * D / 1024 < kMaxGroups, "M * n_kv_heads * head_dim too large");
+  REQUIRE(bounds && ids && out_hi && out_lo, "a required pointer is NULL");
+  REQUIRE(aligned16(bounds, out_hi, out_lo), "bounds and outputs must start at a multiple of 16 bytes");
+  return hip_status(molt::launch_bounds_read(bounds, ids, M, Hkv, D, num_blocks, out_hi, out_lo,
+                                             reinterpret_cast<hipStream_t>(stream)),
+                    "molt_key_bounds_read");
+}
+
+// What the two calls on queries have in common; false where no call takes the sizes
+static int blocks_heads_ok(int B, int k, int Hq, int Hkv, int D) {
+  REQUIRE(B >= 1, "B = %d must be >= 1", B);
+  REQUIRE(k >= 0 && k < 0x7fffffff, "k = %d must be >= 0", k);
+  REQUIRE(D == 64 || D == 128, "head_dim = %d must be 64 or 128", D);
+  REQUIRE(Hkv >= 1 && Hq >= Hkv && Hq % Hkv == 0, "n_q_heads %d must be a multiple of n_kv_heads %d", Hq, Hkv);
+  REQUIRE(double(B) * (double(k) + 1) * Hq < 2.0e9, "B * (1+k) * n_q_heads too large");
+  return MOLT_OK;
+}
+static int select_sizes_ok(int B, int k, int Hq, int Hkv, int D, int max_blocks) {
+  if (int r = blocks_heads_ok(B, k, Hq, Hkv, D)) return r;
+  if (int r = blocks_table_ok(B, k + 1, max_blocks)) return r;
+  REQUIRE(molt::select_groups(B, k + 1, Hq, Hkv, max_blocks) < kMaxGroups,
+          "B * (1+k) * n_kv_heads * max_blocks_per_seq too large");
+  return MOLT_OK;
+}
+static int attend_sizes_ok(int B, int k, int Hq, int Hkv, int D, int n_list) {
+  if (int r = blocks_heads_ok(B, k, Hq, Hkv, D)) return r;
+  REQUIRE(n_list >= 1 && n_list <= kMaxTableBlocks, "n_list = %d must be in [1, 2^26]", n_list);
+  REQUIRE(molt::blocks_attention_groups(B, k + 1, Hq, Hkv, n_list) < kMaxGroups, "B * (1+k) * n_q_heads too large");
+  return MOLT_OK;
+}
+
+size_t molt_select_blocks_workspace_size(int B, int k, int Hq, int Hkv, int D, int max_blocks) {
+  const std::string said = g_err;
+  const bool fits = select_sizes_ok(B, k, Hq, Hkv, D, max_blocks) == MOLT_OK;
+  g_err = said;                                  // (a size function fails without a message)
+  return fits ? molt::select_ws_bytes(B, k + 1, Hkv, max_blocks) : 0;
+}
+
+int molt_select_blocks(const void* q, const void* bounds, const int32_t* block_tables, const int32_t* context_lens,
+                       const int32_t* lens, int B, int k, int Hq, int Hkv, int D, int max_blocks, int num_blocks,
+                       int n_select, int n_first, int n_last, molt_dtype dtype, int32_t* out, void* workspace,
+                       size_t workspace_bytes, molt_stream_t stream) {
+  if (int r = select_sizes_ok(B, k, Hq, Hkv, D, max_blocks)) return r;
+  if (int r = blocks_sizes_ok(Hkv, D, num_blocks)) return r;
+  REQUIRE(act_ok(dtype), "dtype must be F32 or BF16");
+  REQUIRE(n_select >= 1 && n_select <= kMaxTableBlocks, "n_select = %d must be in [1, 2^26]", n_select);
+  REQUIRE(n_first >= 0 && n_last >= 1 && n_first <= n_select && n_last <= n_select - n_first,
+          "n_first = %d >= 0 and n_last = %d >= 1 must fit n_select = %d", n_first, n_last, n_select);
+  REQUIRE(q && bounds && block_tables && context_lens && out, "a required pointer is NULL");
+  REQUIRE(aligned16(q, bounds), "q and bounds must start at a multiple of 16 bytes");
+  if (int r = check_ws(workspace, workspace_bytes, molt::select_ws_bytes(B, k + 1, Hkv, max_blocks))) return r;
+  hipError_t e;
+  {
+    ProfScope ps(MOLT_PROF_ATTENTION, reinterpret_cast<hipStream_t>(stream));
+    e = molt::launch_select_blocks(q, bounds, block_tables, context_lens, lens, B, k + 1, Hq, Hkv, D, max_blocks,
+                                   num_blocks, n_select, n_first, n_last, dtype, out, workspace, workspace_bytes,
+                                   reinterpret_cast<hipStream_t>(stream));
+  }
+  return hip_status(e, "molt_select_blocks");
+}
+
+size_t molt_paged_attention_blocks_workspace_size(int B, int k, int Hq, int Hkv, int D, int n_list) {
+  const std::string said = g_err;
+  const bool fits = attend_sizes_ok(B, k, Hq, Hkv, D, n_list) == MOLT_OK;
+  g_err = said;
+  return fits ? molt::blocks_attention_ws_bytes(B, k + 1, Hq, Hkv, D, n_list) : 0;
+}
+
+int molt_paged_attention_blocks(const void* q, const void* k_cache, const void* v_cache, const int32_t* block_tables,
+                                const int32_t* context_lens, const int32_t* blocks, int B, int k, int Hq, int Hkv,
+                                int D, int max_blocks, int num_blocks, int n_list, molt_dtype dtype, void* out,
+                                void* workspace, size_t workspace_bytes, molt_stream_t stream) {
+  if (int r = attend_sizes_ok(B, k, Hq, Hkv, D, n_list)) return r;
+  if (int r = blocks_sizes_ok(Hkv, D, num_blocks)) return r;
+  if (int r = blocks_table_ok(B, k + 1, max_blocks)) return r;
+  REQUIRE(act_ok(dtype), "dtype must be F32 or BF16");
+  REQUIRE(q && k_cache && v_cache && block_tables && context_lens && blocks && out, "a required pointer is NULL");
+  REQUIRE(aligned16(q, k_cache, v_cache, out), "q, out and the caches must start at a multiple of 16 bytes");
+  if (int r = check_ws(workspace, workspace_bytes, molt::blocks_attention_ws_bytes(B, k + 1, Hq, Hkv, D, n_list)))
+    return r;
+  hipError_t e;
+  {
+    ProfScope ps(MOLT_PROF_ATTENTION, reinterpret_cast<hipStream_t>(stream));
+    e = molt::launch_blocks_attention(q, k_cache, v_cache, block_tables, context_lens, blocks, B, k + 1, Hq, Hkv, D,
+                                      max_blocks, num_blocks, n_list, dtype, out, workspace, workspace_bytes,
+                                      reinterpret_cast<hipStream_t>(stream));
+  }
+  return hip_status(e, "molt_paged_attention_blocks");
+}
+
 // ------------------------------------------------------------------ decoder / verify step
 
 namespace {

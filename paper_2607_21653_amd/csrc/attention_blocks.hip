@@ -1,0 +1,370 @@
+// Attention over listed blocks of the paged cache.
+//   o_r = sum_p w_rp v_p,  w_r = softmax over the keys p <= ctx_b + j of the blocks that list (t, h) names
+// for the G query rows r of position j of sequence b (t = b n + j) and kv head h, scores q . k / sqrt(D).
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+#include "device_common.h"
+#include "internal.h"
+
+namespace molt {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct BlocksArgs {
+  const void* q; const void* kc; const void* vc; const int32_t* bt; const int32_t* ctx; const int32_t* blocks;
+  void* out;
+  float* part_o;                                 // [units, splits, 16, D] partial outputs of split lists
+  float* part_ml;                                // [units, splits, 16, 2] their maxima and sums
+  int B, n, Hq, Hkv, G, N, max_blocks, num_blocks;
+  int row_groups, splits, per_split;             // groups of 16 query rows of a kv head; parts of a list, pairs of one
+  float c;                                       // log2(e) / sqrt(D)
+};
+
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef u32x4_t UnalignedU4 __attribute__((aligned(2)));
+typedef floatx4_t UnalignedF4 __attribute__((aligned(4)));
+
+// Entry e of a list, e in [e0, e0 + 64): lane e - e0 holds its block's place in the cache (-1: none) and how many of
+// its 16 tokens the position sees.
+struct Entries { int id, seen; };
+MOLT_DEV Entries entries_of(const BlocksArgs& p, const int32_t* list, int e, bool there, int b, long pos) {
+  Entries r{-1, 0};
+  if (!there) return r;
+  const int blk = list[e];
+  if (blk < 0 || blk >= p.max_blocks || 16l * blk > pos) return r;
+  const int id = p.bt[long(b) * p.max_blocks + blk];
+  if (id < 0 || id >= p.num_blocks) return r;
+  r.id = id;
+  r.seen = int(min(16l, pos - 16l * blk + 1));
+  return r;
+}
+
+// Running softmax of a lane's query row (lane % 16): maximum of the scaled scores in units of log2, this lane's share
+// of the sum, and O^T: dims 16 d + 4 (lane / 16) + i
+template <int D>
+struct Running {
+  float m = -__builtin_inff(), l = 0.f;
+  floatx4_t o[D / 16];
+};
+
+// Scores s of a lane's M keys of one row (-inf: not seen) -> weights, with O and the sum rescaled
+template <int D, int M>
+MOLT_DEV void weigh(Running<D>& r, float (&s)[M], float c) {
+  float top = s[0];
+#pragma unroll
+  for (int i = 1; i < M; ++i) top = fmaxf(top, s[i]);
+  top = rows_max4(top) * c;
+  if (__any(top > r.m)) {
+    const float m = fmaxf(r.m, top), f = r.m == m ? 1.f : __builtin_amdgcn_exp2f(r.m - m);
+    r.m = m;
+    r.l *= f;
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) r.o[d] *= f;
+  }
+  const float base = r.m == -__builtin_inff() ? 0.f : r.m;
+#pragma unroll
+  for (int i = 0; i < M; ++i) {
+    s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -base));
+    r.l += s[i];
+  }
+}
+
+// bf16: two blocks at a time. Scores S^T = K Q^T by 16x16x32 MFMAs whose A rows are tokens in such an order that a
+// lane's 8 scores of the two tiles are those of 8 consecutive tokens of one block: rows 4 g + i of tile x are tokens
+// 8 (g % 2) + 4 x + i of block g / 2. They are then the B operand of O^T = V^T P^T as they lie, and V's A operand is
+// 16 contiguous bytes of the cache. Weights go in as two bf16 parts, 16 bits.
+template <int D>
+struct PairBf16 {
+  static constexpr int kBlocks = 2;
+  bf16x8_t q[D / 32];
+  MOLT_DEV void load_q(const void* qq, long row, bool there, int g) {
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s) {
+      u32x4_t w{0, 0, 0, 0};
+      if (there) w = *reinterpret_cast<const UnalignedU4*>(static_cast<const uint16_t*>(qq) + row * D + 32 * s + 8 * g);
+      q[s] = __builtin_bit_cast(bf16x8_t, w);
+    }
+  }
+  u32x4_t k[2][D / 32], v[D / 16];
+  MOLT_DEV void load(const BlocksArgs& p, const int (&id)[2], int h, int g, int col) {
+    const long kb = (long(col / 8 ? id[1] : id[0]) * p.Hkv + h) * 16 * D;
+    const long vb = (long(g / 2 ? id[1] : id[0]) * p.Hkv + h) * 16 * D;
+    const uint16_t* kp = static_cast<const uint16_t*>(p.kc) + kb + (col / 4 % 2 * 8 + col % 4) * D + 8 * g;
+    const uint16_t* vp = static_cast<const uint16_t*>(p.vc) + vb + col * 16 + g % 2 * 8;
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int s = 0; s < D / 32; ++s) k[x][s] = *reinterpret_cast<const u32x4_t*>(kp + 4 * x * D + 32 * s);
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) v[d] = *reinterpret_cast<const u32x4_t*>(vp + d * 256);
+  }
+  // tokens of the lane's 8 that are seen, of its block's
+  MOLT_DEV void use(Running<D>& r, const int (&seen)[2], int g, float c) {
+    floatx4_t s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i)
+        s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, k[x][i]), q[i], s[x], 0, 0, 0);
+    float w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = s[i / 4][i % 4];
+    if (seen[0] < 16 || seen[1] < 16) {          // wavefront-uniform
+      const int mine = (g / 2 ? seen[1] : seen[0]) - g % 2 * 8;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i >= mine) w[i] = -__builtin_inff();
+#pragma unroll
+      for (int d = 0; d < D / 16; ++d)           // what is not seen may be anything: 0 times it would be NaN
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (2 * i >= mine) v[d][i] = 0;
+          else if (2 * i + 1 >= mine) v[d][i] &= 0xffffu;
+        }
+    }
+    weigh<D, 8>(r, w, c);
+    bf16x8_t hi, lo;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      hi[i] = __bf16(w[i]);
+      lo[i] = __bf16(w[i] - float(hi[i]));
+    }
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) {
+      const bf16x8_t a = __builtin_bit_cast(bf16x8_t, v[d]);
+      r.o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, hi, r.o[d], 0, 0, 0);
+      r.o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, lo, r.o[d], 0, 0, 0);
+    }
+  }
+};
+
+// f32: one block at a time on 16x16x4 f32 MFMAs; step s of the scores takes dims D / 4 g + s, so that a lane's share of
+// a token is contiguous; step i of O^T takes tokens 4 g + i, those of the lane's i-th score.
+template <int D>
+struct BlockF32 {
+  static constexpr int kBlocks = 1;
+  floatx4_t q[D / 16];
+  MOLT_DEV void load_q(const void* qq, long row, bool there, int g) {
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+      q[s] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+      if (there) q[s] = *reinterpret_cast<const UnalignedF4*>(static_cast<const float*>(qq) + row * D + D / 4 * g + 4 * s);
+    }
+  }
+  floatx4_t k[D / 16], v[D / 16];
+  MOLT_DEV void load(const BlocksArgs& p, const int (&id)[1], int h, int g, int col) {
+    const long at = (long(id[0]) * p.Hkv + h) * 16 * D;
+    const float* kp = static_cast<const float*>(p.kc) + at + col * D + D / 4 * g;
+    const float* vp = static_cast<const float*>(p.vc) + at + col * 16 + 4 * g;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) k[s] = *reinterpret_cast<const floatx4_t*>(kp + 4 * s);
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) v[d] = *reinterpret_cast<const floatx4_t*>(vp + d * 256);
+  }
+  MOLT_DEV void use(Running<D>& r, const int (&seen)[1], int g, float c) {
+    floatx4_t s{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[i][e], q[i][e], s, 0, 0, 0);
+    float w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = s[i];
+    if (seen[0] < 16) {
+      const int mine = seen[0] - 4 * g;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i >= mine) {
+          w[i] = -__builtin_inff();
+#pragma unroll
+          for (int d = 0; d < D / 16; ++d) v[d][i] = 0.f;
+        }
+    }
+    weigh<D, 4>(r, w, c);
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r.o[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[d][i], w[i], r.o[d], 0, 0, 0);
+  }
+};
+
+MOLT_DEV void store4(uint16_t* p, floatx4_t x) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(f32x2_to_bf16(x[0], x[1]), f32x2_to_bf16(x[2], x[3]));
+}
+MOLT_DEV void store4(float* p, floatx4_t x) { *reinterpret_cast<floatx4_t*>(p) = x; }
+
+// Workgroup = one list (or a part of it) and 16 query rows; wavefronts take its units (pairs of blocks, or blocks) in
+// turn with running softmaxes of their own and join them in LDS.
+template <int D, typename T, int W>
+__global__ __launch_bounds__(W* kWave) void blocks_attention_kernel(BlocksArgs p) {
+  typedef std::conditional_t<sizeof(T) == 2, PairBf16<D>, BlockF32<D>> Unit;
+  constexpr int KB = Unit::kBlocks, PER = kWave / KB;                    // blocks of a unit; units that lanes hold
+  __shared__ float ml[W][2][16];
+  __shared__ floatx4_t acc[W > 1 ? W : 1][D / 16][kWave];
+  const int lane = threadIdx.x % kWave, g = lane / 16, col = lane % 16;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  uint32_t item = blockIdx.x;
+  const int split = int(item % p.splits);
+  item /= p.splits;
+  const int rg = int(item % p.row_groups);
+  item /= p.row_groups;
+  const int h = int(item % p.Hkv), t = int(item / p.Hkv), b = t / p.n, j = t % p.n;
+  const long pos = long(p.ctx[b]) + j;
+  const int32_t* list = p.blocks + (long(t) * p.Hkv + h) * p.N;
+  const int head = h * p.G + rg * 16 + col;
+  const bool there = rg * 16 + col < p.G;
+
+  Unit u;
+  u.load_q(p.q, long(t) * p.Hq + head, there, g);
+  Running<D> r;
+#pragma unroll
+  for (int d = 0; d < D / 16; ++d) r.o[d] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+  const int units = (p.N + KB - 1) / KB, u0 = split * p.per_split, u1 = min(units, u0 + p.per_split);
+  for (int base = u0; base < u1; base += W * PER) {
+    const int mine = base + wave + lane / KB * W, e = mine * KB + lane % KB;
+    const Entries en = entries_of(p, list, e, mine < u1 && e < p.N, b, pos);
+    for (int i = 0; i < PER && base + wave + i * W < u1; ++i) {
+      int id[KB], seen[KB], any = 0, some = 0;
+#pragma unroll
+      for (int x = 0; x < KB; ++x) {
+        id[x] = __builtin_amdgcn_readlane(en.id, i * KB + x);
+        seen[x] = __builtin_amdgcn_readlane(en.seen, i * KB + x);
+        any += seen[x];
+        if (id[x] >= 0) some = id[x];
+      }
+      if (any == 0) continue;
+#pragma unroll
+      for (int x = 0; x < KB; ++x)
+        if (id[x] < 0) id[x] = some;             // the other block's, unseen
+      u.load(p, id, h, g, col);
+      u.use(r, seen, g, p.c);
+    }
+  }
+
+  r.l = rows_sum4(r.l);
+  if (W > 1) {
+    if (g == 0) { ml[wave][0][col] = r.m; ml[wave][1][col] = r.l; }
+    __syncthreads();
+    float m = ml[0][0][col];
+#pragma unroll
+    for (int w = 1; w < W; ++w) m = fmaxf(m, ml[w][0][col]);
+    const float base = m == -__builtin_inff() ? 0.f : m, f = __builtin_amdgcn_exp2f(r.m - base);
+    float l = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) l += __builtin_amdgcn_exp2f(ml[w][0][col] - base) * ml[w][1][col];
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) acc[wave][d][lane] = r.o[d] * f;
+    __syncthreads();
+    r.m = m;
+    r.l = l;
+  }
+  // wavefront w stores dims 16 d .. + 15 for d = w, w + W, ..
+#pragma unroll
+  for (int d0 = 0; d0 < D / 16; d0 += W) {
+    const int d = d0 + wave;
+    if (d >= D / 16) break;
+    floatx4_t o;
+    if (W > 1) {
+      o = acc[0][d][lane];
+#pragma unroll
+      for (int w = 1; w < W; ++w) o += acc[w][d][lane];
+    } else {
+      o = r.o[d0];
+    }
+    if (p.splits > 1) {
+      const long at = (((long(t) * p.Hkv + h) * p.row_groups + rg) * p.splits + split) * 16 + col;
+      if (there) *reinterpret_cast<floatx4_t*>(p.part_o + at * D + 16 * d + 4 * g) = o;
+      if (there && d == 0 && g == 0) { p.part_ml[at * 2] = r.m; p.part_ml[at * 2 + 1] = r.l; }
+    } else if (there) {
+      // l is 0 only where no key has weight; NaN scores leave NaN
+      const float inv = r.l == 0.f ? 0.f : 1.f / r.l;
+      store4(static_cast<T*>(p.out) + (long(t) * p.Hq + head) * D + 16 * d + 4 * g, o * inv);
+    }
+  }
+}
+
+// Joins the parts of split lists: thread = 4 dims of a query row
+template <int D, typename T>
+__global__ __launch_bounds__(256) void blocks_join_kernel(BlocksArgs p) {
+  const long at = (long(blockIdx.x) * 256 + threadIdx.x) / (D / 4);
+  const int d = threadIdx.x % (D / 4) * 4;
+  if (at >= long(p.B) * p.n * p.Hq) return;
+  const long th = at / p.G;                      // list
+  const int row = int(at % p.G);
+  const long first = ((th * p.row_groups + row / 16) * p.splits) * 16 + row % 16;
+  float m = -__builtin_inff();
+  for (int s = 0; s < p.splits; ++s) m = fmaxf(m, p.part_ml[(first + 16 * s) * 2]);
+  const float base = m == -__builtin_inff() ? 0.f : m;
+  float l = 0.f;
+  floatx4_t o{0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < p.splits; ++s) {
+    const float f = __builtin_amdgcn_exp2f(p.part_ml[(first + 16 * s) * 2] - base);
+    l += f * p.part_ml[(first + 16 * s) * 2 + 1];
+    o += f * *reinterpret_cast<const floatx4_t*>(p.part_o + (first + 16 * s) * D + d);
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  store4(static_cast<T*>(p.out) + at * D + d, o * inv);
+}
+
+struct BlocksPlan { int row_groups, splits, per_split; };
+BlocksPlan blocks_plan(int B, int n, int Hq, int Hkv, int N) {
+  BlocksPlan pl{};
+  const int units = (N + 1) / 2;
+  pl.row_groups = (Hq / Hkv + 15) / 16;
+  const long lists = long(B) * n * Hkv * pl.row_groups;
+  // a split has 8 pairs at least, two for each wavefront
+  const long want = std::max(1l, std::min((512 + lists - 1) / lists, long(units) / 8));
+  pl.per_split = int((units + want - 1) / want);
+  pl.splits = (units + pl.per_split - 1) / pl.per_split;
+  return pl;
+}
+
+}  // namespace
+
+double blocks_attention_groups(int B, int n, int Hq, int Hkv, int N) {
+  const BlocksPlan pl = blocks_plan(B, n, Hq, Hkv, N);
+  return std::max(double(B) * n * Hkv * pl.row_groups * pl.splits, double(B) * n * Hq / 8);
+}
+
+size_t blocks_attention_ws_bytes(int B, int n, int Hq, int Hkv, int D, int N) {
+  const BlocksPlan pl = blocks_plan(B, n, Hq, Hkv, N);
+  if (pl.splits == 1) return 0;
+  const size_t rows = size_t(B) * n * Hkv * pl.row_groups * pl.splits * 16;
+  return rows * (D + 2) * sizeof(float) + 512;
+}
+
+hipError_t launch_blocks_attention(const void* q, const void* kc, const void* vc, const int32_t* bt, const int32_t* ctx,
+                                   const int32_t* blocks, int B, int n, int Hq, int Hkv, int D, int max_blocks,
+                                   int num_blocks, int N, molt_dtype dt, void* out, void* ws, size_t ws_bytes,
+                                   hipStream_t s) {
+  const BlocksPlan pl = blocks_plan(B, n, Hq, Hkv, N);
+  BlocksArgs p{q, kc, vc, bt, ctx, blocks, out, nullptr, nullptr, B, n, Hq, Hkv, Hq / Hkv, N, max_blocks, num_blocks,
+               pl.row_groups, pl.splits, dt == MOLT_F32 ? 2 * pl.per_split : pl.per_split,
+               kLog2e / std::sqrt(float(D))};
+  const size_t rows = size_t(B) * n * Hkv * pl.row_groups * pl.splits;
+  if (pl.splits > 1) {
+    Carver c(ws, ws_bytes);
+    p.part_o = c.take<float>(rows * 16 * D);
+    p.part_ml = c.take<float>(rows * 16 * 2);
+  }
+  constexpr int W = 4;
+  const unsigned grid = unsigned(rows), joins = unsigned((long(B) * n * Hq * (D / 4) + 255) / 256);
+  auto go = [&](auto d, auto* t) {
+    constexpr int DD = decltype(d)::value;
+    typedef std::remove_pointer_t<decltype(t)> T;
+    blocks_attention_kernel<DD, T, W><<<grid, W * kWave, 0, s>>>(p);
+    if (p.splits > 1) blocks_join_kernel<DD, T><<<joins, 256, 0, s>>>(p);
+  };
+  auto by_dim = [&](auto* t) {
+    if (D == 128) go(std::integral_constant<int, 128>{}, t);
+    else go(std::integral_constant<int, 64>{}, t);
+  };
+  if (dt == MOLT_F32) by_dim(static_cast<float*>(nullptr));
+  else by_dim(static_cast<uint16_t*>(nullptr));
+  return hipGetLastError();
+}
+
+}  // namespace molt

@@ -1,0 +1,471 @@
+// The paged cache's upkeep on the GPU: block tables that follow the lengths, rows written by slot, the bounds of
+// each block's keys.
+#include "bounds_format.h"
+#include "internal.h"
+
+namespace molt {
+namespace {
+
+constexpr int kThreads = 256;
+
+// ---------------------------------------------------------------- tables and slots
+
+constexpr int kPlanThreads = 1024;
+constexpr int kPlanWaves = kPlanThreads / kWave;
+
+// What a call does with sequence b's row of the table: entries have .. have + take - 1 come from the ring's places
+// first .. behind its head, entries keep .. have - 1 go to places back .. of it (-1: none do), rows 0 .. placed - 1 get
+// slots.
+struct PlanRow { int have, take, first, keep, back, placed; };
+
+struct PlanArgs {
+  int32_t* bt; int32_t* n_blocks; const int32_t* ctx; const int32_t* n_new; int32_t* pool; const int32_t* shared;
+  int B, n, max_blocks, num_blocks;
+  int32_t* slots; int32_t* placed;
+  PlanRow* rows;                                 // [B + 1]; the last one's `first` is the ring's head before the call
+};
+
+MOLT_DEV int ring_wrap(long at, int cap) { return int(at >= cap ? at - cap : at); }   // at < 2 cap
+
+// Row j of sequence b: its slot, and the table entry that it is the first to use. Entries of the pool are read from the
+// ring itself: nothing waits for the table.
+MOLT_DEV void plan_slot(const PlanArgs& p, const PlanRow& r, int b, int j, int head) {
+  const int cap = p.num_blocks;
+  const int32_t* ring = p.pool + 2;
+  int32_t* row = p.bt + long(b) * p.max_blocks;
+  int slot = -1;
+  if (j < r.placed) {
+    const int pos = p.ctx[b] + j, i = pos / 16;  // i < have + take
+    int id;
+    if (i >= r.have) {
+      id = ring[ring_wrap(long(head) + r.first + (i - r.have), cap)];
+      if (j == 0 || pos % 16 == 0) row[i] = id;
+    } else {
+      id = row[i];
+    }
+    if (id >= 0 && id < cap) slot = id * 16 + pos % 16;
+    if (j == 0)                                  // a table that lacks blocks of the cached tokens
+      for (int k = r.have; k < i; ++k) row[k] = ring[ring_wrap(long(head) + r.first + (k - r.have), cap)];
+  }
+  p.slots[long(b) * p.n + j] = slot;
+}
+
+// a finished sequence's entries into the ring, `threads` at a time
+MOLT_DEV void plan_return(const PlanArgs& p, const PlanRow& r, int b, int thread, int threads) {
+  const int32_t* row = p.bt + long(b) * p.max_blocks;
+  const int m = r.have - r.keep;
+  int i = thread;
+  for (; i + 3l * threads < m; i += 4 * threads) {
+    int id[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) id[u] = row[r.keep + i + u * threads];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) p.pool[2 + ring_wrap(long(r.back) + i + u * threads, p.num_blocks)] = id[u];
+  }
+  for (; i < m; i += threads) p.pool[2 + ring_wrap(long(r.back) + i, p.num_blocks)] = row[r.keep + i];
+}
+
+// Inclusive sum over the workgroup's threads of v in [0, 2^31), in 64 bits: its halves of 16 bits apart on DPP
+MOLT_DEV long plan_scan(int v, long* red, long& total) {
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const long s = (long(wave_scan_dpp(v >> 16)) << 16) + wave_scan_dpp(v & 0xffff);
+  __syncthreads();
+  if (lane == kWave - 1) red[wave] = s;
+  __syncthreads();
+  long before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kPlanWaves; ++w) {
+    if (w < wave) before += red[w];
+    all += red[w];
+  }
+  total = all;
+  return s + before;
+}
+
+// One workgroup. Who gets what is a matter of prefix sums of the rows' demands, in the rows' order: nothing depends on
+// timing. Taken places [head, head + taken) and returned ones behind head + count are apart, so both go on at once.
+// WHOLE: the slots and the entries too (up to kPlanThreads sequences), else plan_rows_kernel does them.
+template <bool WHOLE>
+__global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs p) {
+  __shared__ long red[kPlanWaves];
+  __shared__ unsigned long long ends[2];         // places taken and returned, as far as the pool goes
+  __shared__ PlanRow held[WHOLE ? kPlanThreads : 1];
+  const int cap = p.num_blocks;
+  const int head = int(uint32_t(p.pool[0]) % uint32_t(cap)), count = min(max(p.pool[1], 0), cap);
+  if (threadIdx.x < 2) ends[threadIdx.x] = 0;
+  long demanded = 0, given = 0;                  // of the rows before
+  for (int b0 = 0; b0 < p.B; b0 += kPlanThreads) {
+    const int b = b0 + int(threadIdx.x);
+    PlanRow r{0, 0, 0, 0, -1, 0};
+    int want = 0, give = 0;
+    bool fits = false, done = false;
+    if (b < p.B) {
+      const int ctx = p.ctx[b], m = p.n_new[b];
+      r.have = p.n_blocks[b];
+      const bool sound = r.have >= 0 && r.have <= p.max_blocks;
+      const long end = long(ctx) + m;
+      done = sound && m < 0;
+      fits = sound && m >= 0 && m <= p.n && ctx >= 0 && end <= 16l * p.max_blocks;
+      if (fits && m > 0) want = max(0, int((end + 15) / 16) - r.have);
+      if (done) {
+        r.keep = p.shared ? max(p.shared[b], 0) : 0;
+        give = max(0, r.have - r.keep);
+      }
+      if (fits) r.placed = m;
+    }
+    long all_want, all_give;
+    const long upto = demanded + plan_scan(want, red, all_want);
+    const long gave = given + plan_scan(give, red, all_give);
+    if (want && upto <= count) {
+      r.take = want;
+      r.first = int(upto - want);
+      atomicMax(&ends[0], (unsigned long long)upto);
+    } else if (want) {
+      r.placed = 0;                              // the pool does not reach so far
+    }
+    if (give && gave <= cap - count) {           // (a ring that would run over holds ids twice: they are dropped)
+      r.back = int((long(head) + count + gave - give) % cap);
+      atomicMax(&ends[1], (unsigned long long)gave);
+    }
+    if (b < p.B) {
+      p.placed[b] = r.placed;
+      if (done) p.n_blocks[b] = 0;
+      else if (r.take) p.n_blocks[b] = r.have + r.take;
+      if (WHOLE) held[threadIdx.x] = r;
+      else p.rows[b] = r;
+    }
+    demanded += all_want;
+    given += all_give;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    p.pool[0] = int((head + long(ends[0])) % cap);
+    p.pool[1] = count - int(ends[0]) + int(ends[1]);
+    if (!WHOLE) p.rows[p.B].first = head;
+  }
+  if (!WHOLE) return;
+  for (int at = threadIdx.x; at < p.B * p.n; at += kPlanThreads) plan_slot(p, held[at / p.n], at / p.n, at % p.n, head);
+  for (int b = threadIdx.x / kWave; b < p.B; b += kPlanWaves)
+    if (held[b].back >= 0) plan_return(p, held[b], b, threadIdx.x % kWave, kWave);
+}
+
+// after plan_kernel<false>: a thread per slot, then a workgroup per sequence for what it gives back
+__global__ __launch_bounds__(kThreads) void plan_rows_kernel(PlanArgs p, uint32_t slot_groups) {
+  if (blockIdx.x < slot_groups) {
+    const uint32_t at = blockIdx.x * kThreads + threadIdx.x;
+    const uint32_t b = at / uint32_t(p.n);
+    if (b < uint32_t(p.B)) plan_slot(p, p.rows[b], int(b), int(at - b * uint32_t(p.n)), p.rows[p.B].first);
+    return;
+  }
+  const int b = int(blockIdx.x - slot_groups);
+  const PlanRow r = p.rows[b];
+  if (r.back >= 0) plan_return(p, r, b, threadIdx.x, kThreads);
+}
+
+// One launch where it is enough for the slots
+bool plan_whole(int B, int n) { return B <= kPlanThreads && long(B) * n <= 8 * kPlanThreads; }
+
+// ---------------------------------------------------------------- rows by slot
+
+// two elements of a row at any element alignment, as the bits that the cache holds
+typedef uint32_t UnalignedU1 __attribute__((aligned(2)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+typedef u32x2_t UnalignedU2 __attribute__((aligned(4)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+
+// Wavefront = 16 rows of k and v and 128 dims: a head of 128 dims or two of 64; lane = two dims. The rows fall into
+// runs of consecutive slots of one block; a wavefront writes the runs that begin among its rows, up to their ends. A
+// run that fills its block's 16 slots leaves V, whose tokens are contiguous, in whole 16-byte stores; other runs leave
+// it in stores of 4 bytes where both tokens of a pair are there.
+template <int D, typename T>
+__global__ __launch_bounds__(kThreads) void kv_write_kernel(const T* __restrict__ k, long k_stride,
+                                                            const T* __restrict__ v, long v_stride,
+                                                            const int32_t* __restrict__ slots, int rows, int Hkv,
+                                                            int num_blocks, T* __restrict__ kc, T* __restrict__ vc) {
+  constexpr int HPW = 128 / D;
+  const int heads = (Hkv + HPW - 1) / HPW;
+  const uint32_t item = blockIdx.x * (kThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const uint32_t tile = item / uint32_t(heads);
+  const int r0 = int(tile) * 16, lane = threadIdx.x % kWave;
+  if (r0 >= rows) return;
+  const int h = int(item - tile * heads) * HPW + lane / (D / 2), d = lane % (D / 2) * 2;
+  // lane l: the slot of row r0 - 1 + l
+  const int row = r0 - 1 + lane;
+  const int slot = row >= 0 && row < rows && lane < 33 ? slots[row] : -1;
+  const bool good = slot >= 0 && slot / 16 < num_blocks;
+  const int before = __shfl_up(slot, 1);
+  const bool starts = good && (lane == 1 || before != slot - 1 || slot % 16 == 0 || before < 0);
+  // (row r0 continues a run of the tile before where its slot follows on)
+  const int prev = __shfl(slot, 0);
+  uint32_t begin = uint32_t(__ballot(starts) >> 1);                      // bit i: a run begins at row r0 + i
+  const uint32_t live = uint32_t(__ballot(good) >> 1);
+  const int s0 = __shfl(slot, 1);
+  if ((begin & 1) && prev >= 0 && prev == s0 - 1 && s0 % 16 != 0) begin &= ~1u;
+  const bool there = h < Hkv;
+  for (uint32_t left = begin & 0xffffu; left; left &= left - 1) {
+    const int i = __builtin_ctz(left);
+    const uint32_t stop = (begin | ~live) >> i >> 1;                     // what ends the run
+    const int len = min(stop ? __builtin_ctz(stop) + 1 : 32, 16);
+    const int s = __builtin_amdgcn_readlane(slot, i + 1), first = s % 16;
+    const long rec = (long(s / 16) * Hkv + h) * 16 * D;
+    if (!there) continue;
+    if constexpr (sizeof(T) == 2) {
+      uint32_t x[16], y[16];
+#pragma unroll
+      for (int t = 0; t < 16; ++t) {
+        const int at = t - first;
+        const long r = r0 + i + at;
+        x[t] = y[t] = 0;
+        if (at >= 0 && at < len) {
+          x[t] = *reinterpret_cast<const UnalignedU1*>(k + r * k_stride + h * D + d);
+          y[t] = *reinterpret_cast<const UnalignedU1*>(v + r * v_stride + h * D + d);
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < 16; ++t)
+        if (t >= first && t < first + len) *reinterpret_cast<uint32_t*>(kc + rec + t * D + d) = x[t];
+      T* out = vc + rec + d * 16;                                        // dims d and d + 1: 32 elements
+      uint32_t lo[8], hi[8];
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        lo[t] = (y[2 * t] & 0xffffu) | y[2 * t + 1] << 16;
+        hi[t] = y[2 * t] >> 16 | (y[2 * t + 1] & 0xffff0000u);
+      }
+      if (len == 16) {
+        u32x4_t* o = reinterpret_cast<u32x4_t*>(out);
+        o[0] = u32x4_t{lo[0], lo[1], lo[2], lo[3]};
+        o[1] = u32x4_t{lo[4], lo[5], lo[6], lo[7]};
+        o[2] = u32x4_t{hi[0], hi[1], hi[2], hi[3]};
+        o[3] = u32x4_t{hi[4], hi[5], hi[6], hi[7]};
+      } else {
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+          const bool a = 2 * t >= first && 2 * t < first + len, b = 2 * t + 1 >= first && 2 * t + 1 < first + len;
+          if (a && b) {
+            *reinterpret_cast<uint32_t*>(out + 2 * t) = lo[t];
+            *reinterpret_cast<uint32_t*>(out + 16 + 2 * t) = hi[t];
+          } else if (a) {
+            out[2 * t] = T(lo[t]);
+            out[16 + 2 * t] = T(hi[t]);
+          } else if (b) {
+            out[2 * t + 1] = T(lo[t] >> 16);
+            out[16 + 2 * t + 1] = T(hi[t] >> 16);
+          }
+        }
+      }
+    } else {
+      u32x2_t x[16], y[16];
+#pragma unroll
+      for (int t = 0; t < 16; ++t) {
+        const int at = t - first;
+        const long r = r0 + i + at;
+        x[t] = y[t] = u32x2_t{0, 0};
+        if (at >= 0 && at < len) {
+          x[t] = *reinterpret_cast<const UnalignedU2*>(k + r * k_stride + h * D + d);
+          y[t] = *reinterpret_cast<const UnalignedU2*>(v + r * v_stride + h * D + d);
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < 16; ++t)
+        if (t >= first && t < first + len) *reinterpret_cast<u32x2_t*>(kc + rec + t * D + d) = x[t];
+      uint32_t* out = reinterpret_cast<uint32_t*>(vc) + rec + d * 16;
+      if (len == 16) {
+        u32x4_t* o = reinterpret_cast<u32x4_t*>(out);
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+            o[4 * c + t] = u32x4_t{y[4 * t][c], y[4 * t + 1][c], y[4 * t + 2][c], y[4 * t + 3][c]};
+      } else {
+#pragma unroll
+        for (int t = 0; t < 16; ++t)
+          if (t >= first && t < first + len) { out[t] = y[t][0]; out[16 + t] = y[t][1]; }
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------- bounds of the keys
+
+MOLT_DEV void load_octet(const uint16_t* p, float (&x)[8]) {
+  const u32x4_t w = *reinterpret_cast<const u32x4_t*>(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(w[i] << 16);
+    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+MOLT_DEV void load_octet(const float* p, float (&x)[8]) {
+  const floatx4_t a = *reinterpret_cast<const floatx4_t*>(p), b = *reinterpret_cast<const floatx4_t*>(p + 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { x[i] = a[i]; x[4 + i] = b[i]; }
+}
+
+// Wavefront = one block of a sequence and one kv head: lane = an octet of dims of every (512 / D)-th token. The
+// block is read whole, cached tokens with it, so that what a record holds never depends on how it came about.
+template <int D, typename T>
+__global__ __launch_bounds__(kThreads) void bounds_update_kernel(const T* __restrict__ kc, uint8_t* __restrict__ bounds,
+                                                                 const int32_t* __restrict__ bt,
+                                                                 const int32_t* __restrict__ starts,
+                                                                 const int32_t* __restrict__ lens, int B, int n, int nblk,
+                                                                 int Hkv, int max_blocks, int num_blocks) {
+  typedef BoundsRecord<D> Rec;
+  constexpr int O = D / 8, TPI = kWave / O, NI = 16 / TPI;              // octets, tokens of a load, loads
+  const uint32_t item = blockIdx.x * (kThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const uint32_t rest = item / uint32_t(Hkv), b = rest / uint32_t(nblk);
+  const int h = int(item - rest * Hkv);
+  if (b >= uint32_t(B)) return;
+  const int start = starts[b], m = lens ? min(max(lens[b], 0), n) : n;
+  const long blk = (long(start) >> 4) + long(rest - b * nblk), end = long(start) + m;
+  if (m == 0 || blk < 0 || blk >= max_blocks || 16 * blk >= end) return;
+  const int id = bt[long(b) * max_blocks + blk];
+  if (id < 0 || id >= num_blocks) return;
+  const int seen = int(min(16l, end - 16 * blk));                        // tokens 0 .. seen - 1 of the block
+  const int lane = threadIdx.x % kWave, oct = lane % O;
+  const T* src = kc + (long(id) * Hkv + h) * 16 * D;
+  float x[NI][8];
+#pragma unroll
+  for (int i = 0; i < NI; ++i) load_octet(src + (i * TPI + lane / O) * D + oct * 8, x[i]);
+  float hi[8], lo[8];
+  uint32_t a = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    hi[e] = -__builtin_inff();
+    lo[e] = __builtin_inff();
+  }
+#pragma unroll
+  for (int i = 0; i < NI; ++i)
+    if (i * TPI + lane / O < seen) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        hi[e] = fmaxf(hi[e], x[i][e]);
+        lo[e] = fminf(lo[e], x[i][e]);
+        a = max(a, __float_as_uint(x[i][e]) & 0x7fffffffu);
+      }
+    }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    if (O == 8) {                                                        // lanes l, l ^ 8: a rotation of the 16-lane row
+      hi[e] = fmaxf(hi[e], __uint_as_float(dpp_u32<0x128, 0xF>(__float_as_uint(hi[e]), 0u)));
+      lo[e] = fminf(lo[e], __uint_as_float(dpp_u32<0x128, 0xF>(__float_as_uint(lo[e]), 0u)));
+    }
+    hi[e] = rows_max4(hi[e]);
+    lo[e] = -rows_max4(-lo[e]);
+  }
+  a = uint32_t(wave_max_dpp((unsigned long long)a));
+  const bool bad = a >= 0x7f800000u;
+  const int e = bad ? kBoundsNotFinite : bounds_exponent(a);
+  const float r = bad ? 0.f : pow2(-e);
+  int ch[8], cl[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    ch[i] = bad ? 0 : int(__builtin_ceilf(hi[i] * r));
+    cl[i] = bad ? 0 : int(__builtin_floorf(lo[i] * r));
+  }
+  uint8_t* rec = bounds + (long(id) * Hkv + h) * Rec::kBytes;
+  if (lane < O) {
+    u32x2_t* o = reinterpret_cast<u32x2_t*>(rec + oct * 8);
+    o[0] = u32x2_t{pack_codes(ch[0], ch[1], ch[2], ch[3]), pack_codes(ch[4], ch[5], ch[6], ch[7])};
+    o[D / 8] = u32x2_t{pack_codes(cl[0], cl[1], cl[2], cl[3]), pack_codes(cl[4], cl[5], cl[6], cl[7])};
+  }
+  if (lane == kWave - 1) *reinterpret_cast<u32x4_t*>(rec + Rec::kExponent) = u32x4_t{uint32_t(e) & 0xffu, 0, 0, 0};
+}
+
+// thread = four dims of a record
+template <int D>
+__global__ __launch_bounds__(kThreads) void bounds_read_kernel(const uint8_t* __restrict__ bounds,
+                                                               const int32_t* __restrict__ ids, long records, int Hkv,
+                                                               int num_blocks, float* __restrict__ hi,
+                                                               float* __restrict__ lo) {
+  typedef BoundsRecord<D> Rec;
+  const long at = (long(blockIdx.x) * kThreads + threadIdx.x) / (D / 4);
+  const int d = threadIdx.x % (D / 4) * 4;
+  if (at >= records) return;
+  const int id = ids[at / Hkv];
+  const float nan = __uint_as_float(0x7fc00000u), inf = __builtin_inff();
+  floatx4_t a{nan, nan, nan, nan}, b = a;
+  if (id >= 0 && id < num_blocks) {
+    const uint8_t* rec = bounds + (long(id) * Hkv + at % Hkv) * Rec::kBytes;
+    const int e = int(int8_t(rec[Rec::kExponent]));
+    const uint32_t x = *reinterpret_cast<const uint32_t*>(rec + d), y = *reinterpret_cast<const uint32_t*>(rec + D + d);
+    const float unit = pow2(min(max(e, kBoundsMinExponent), 121));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      a[i] = e == kBoundsNotFinite ? inf : float(int8_t(x >> 8 * i)) * unit;
+      b[i] = e == kBoundsNotFinite ? -inf : float(int8_t(y >> 8 * i)) * unit;
+    }
+  }
+  *reinterpret_cast<floatx4_t*>(hi + at * D + d) = a;
+  *reinterpret_cast<floatx4_t*>(lo + at * D + d) = b;
+}
+
+}  // namespace
+
+size_t plan_ws_bytes(int B, int n) { return plan_whole(B, n) ? 0 : (size_t(B) + 1) * sizeof(PlanRow) + 256; }
+
+hipError_t launch_plan_blocks(int32_t* bt, int32_t* n_blocks, const int32_t* ctx, const int32_t* n_new, int32_t* pool,
+                              const int32_t* shared, int B, int n, int max_blocks, int num_blocks, int32_t* slots,
+                              int32_t* placed, void* ws, size_t ws_bytes, hipStream_t s) {
+  PlanArgs p{bt, n_blocks, ctx, n_new, pool, shared, B, n, max_blocks, num_blocks, slots, placed, nullptr};
+  if (plan_whole(B, n)) {
+    plan_kernel<true><<<1, kPlanThreads, 0, s>>>(p);
+    return hipGetLastError();
+  }
+  Carver c(ws, ws_bytes);
+  p.rows = c.take<PlanRow>(size_t(B) + 1);
+  plan_kernel<false><<<1, kPlanThreads, 0, s>>>(p);
+  const uint32_t slot_groups = uint32_t((long(B) * n + kThreads - 1) / kThreads);
+  plan_rows_kernel<<<slot_groups + uint32_t(B), kThreads, 0, s>>>(p, slot_groups);
+  return hipGetLastError();
+}
+
+hipError_t launch_kv_write(const void* k, long k_stride, const void* v, long v_stride, const int32_t* slots, int rows,
+                           int Hkv, int D, int num_blocks, molt_dtype dt, void* kc, void* vc, hipStream_t s) {
+  const long waves = (long(rows) + 15) / 16 * ((Hkv * long(D) + 127) / 128);
+  const unsigned grid = unsigned((waves + kThreads / kWave - 1) / (kThreads / kWave));
+  auto go = [&](auto kernel, auto* t) {
+    typedef decltype(t) P;
+    kernel<<<grid, kThreads, 0, s>>>(static_cast<P>(const_cast<void*>(k)), k_stride, static_cast<P>(const_cast<void*>(v)),
+                                     v_stride, slots, rows, Hkv, num_blocks, static_cast<P>(kc), static_cast<P>(vc));
+  };
+  if (dt == MOLT_F32) {
+    float* t = nullptr;
+    if (D == 128) go(kv_write_kernel<128, float>, t); else go(kv_write_kernel<64, float>, t);
+  } else {
+    uint16_t* t = nullptr;
+    if (D == 128) go(kv_write_kernel<128, uint16_t>, t); else go(kv_write_kernel<64, uint16_t>, t);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_bounds_update(const void* kc, void* bounds, const int32_t* bt, const int32_t* starts,
+                                const int32_t* lens, int B, int n, int Hkv, int D, int max_blocks, int num_blocks,
+                                molt_dtype dt, hipStream_t s) {
+  const int nblk = int((long(n) + 30) / 16);                             // blocks that n positions may touch
+  const long waves = long(B) * nblk * Hkv;
+  const unsigned grid = unsigned((waves + kThreads / kWave - 1) / (kThreads / kWave));
+  auto go = [&](auto kernel, auto* c) {
+    kernel<<<grid, kThreads, 0, s>>>(c, static_cast<uint8_t*>(bounds), bt, starts, lens, B, n, nblk, Hkv, max_blocks,
+                                     num_blocks);
+  };
+  if (dt == MOLT_F32) {
+    auto* c = static_cast<const float*>(kc);
+    if (D == 128) go(bounds_update_kernel<128, float>, c); else go(bounds_update_kernel<64, float>, c);
+  } else {
+    auto* c = static_cast<const uint16_t*>(kc);
+    if (D == 128) go(bounds_update_kernel<128, uint16_t>, c); else go(bounds_update_kernel<64, uint16_t>, c);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_bounds_read(const void* bounds, const int32_t* ids, int M, int Hkv, int D, int num_blocks, float* hi,
+                              float* lo, hipStream_t s) {
+  const long records = long(M) * Hkv;
+  const unsigned grid = unsigned((records * (D / 4) + kThreads - 1) / kThreads);
+  auto* b = static_cast<const uint8_t*>(bounds);
+  if (D == 128) bounds_read_kernel<128><<<grid, kThreads, 0, s>>>(b, ids, records, Hkv, num_blocks, hi, lo);
+  else bounds_read_kernel<64><<<grid, kThreads, 0, s>>>(b, ids, records, Hkv, num_blocks, hi, lo);
+  return hipGetLastError();
+}
+
+}  // namespace molt

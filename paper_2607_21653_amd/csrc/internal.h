@@ -187,4 +187,30 @@ hipError_t launch_kvq_attention(const void* q, const void* kc, const void* vc, c
                                 int num_blocks, molt_dtype dt, void* out, bool out_tiled, void* ws,
                                 hipStream_t s);
 
+// ------------------------------------------------------------- sparse attention over listed blocks
+size_t plan_ws_bytes(int B, int n);
+hipError_t launch_plan_blocks(int32_t* bt, int32_t* n_blocks, const int32_t* ctx, const int32_t* n_new, int32_t* pool,
+                              const int32_t* shared, int B, int n, int max_blocks, int num_blocks, int32_t* slots,
+                              int32_t* placed, void* ws, size_t ws_bytes, hipStream_t s);
+hipError_t launch_kv_write(const void* k, long k_stride, const void* v, long v_stride, const int32_t* slots, int rows,
+                           int Hkv, int D, int num_blocks, molt_dtype dt, void* kc, void* vc, hipStream_t s);
+hipError_t launch_bounds_update(const void* kc, void* bounds, const int32_t* bt, const int32_t* starts,
+                                const int32_t* lens, int B, int n, int Hkv, int D, int max_blocks, int num_blocks,
+                                molt_dtype dt, hipStream_t s);
+hipError_t launch_bounds_read(const void* bounds, const int32_t* ids, int M, int Hkv, int D, int num_blocks, float* hi,
+                              float* lo, hipStream_t s);
+// n query positions per sequence; workgroups of the call's largest launch (for the host's check)
+double select_groups(int B, int n, int Hq, int Hkv, int max_blocks);
+size_t select_ws_bytes(int B, int n, int Hkv, int max_blocks);
+hipError_t launch_select_blocks(const void* q, const void* bounds, const int32_t* bt, const int32_t* ctx,
+                                const int32_t* lens, int B, int n, int Hq, int Hkv, int D, int max_blocks,
+                                int num_blocks, int N, int n_first, int n_last, molt_dtype dt, int32_t* out, void* ws,
+                                size_t ws_bytes, hipStream_t s);
+double blocks_attention_groups(int B, int n, int Hq, int Hkv, int N);
+size_t blocks_attention_ws_bytes(int B, int n, int Hq, int Hkv, int D, int N);
+hipError_t launch_blocks_attention(const void* q, const void* kc, const void* vc, const int32_t* bt, const int32_t* ctx,
+                                   const int32_t* blocks, int B, int n, int Hq, int Hkv, int D, int max_blocks,
+                                   int num_blocks, int N, molt_dtype dt, void* out, void* ws, size_t ws_bytes,
+                                   hipStream_t s);
+
 }  // namespace molt
