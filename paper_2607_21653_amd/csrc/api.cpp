@@ -705,7 +705,7 @@ static int blocks_heads_ok(int B, int k, int Hq, int Hkv, int D) {
 static int select_sizes_ok(int B, int k, int Hq, int Hkv, int D, int max_blocks) {
   if (int r = blocks_heads_ok(B, k, Hq, Hkv, D)) return r;
   if (int r = blocks_table_ok(B, k + 1, max_blocks)) return r;
-  REQUIRE(molt::select_groups(B, k + 1, Hq, Hkv, max_blocks) < kMaxGroups,
+  REQUIRE(molt::select_groups(B, k + 1, Hq, Hkv, D, max_blocks) < kMaxGroups,
           "B * (1+k) * n_kv_heads * max_blocks_per_seq too large");
   return MOLT_OK;
 }
@@ -720,7 +720,7 @@ size_t molt_select_blocks_workspace_size(int B, int k, int Hq, int Hkv, int D, i
   const std::string said = g_err;
   const bool fits = select_sizes_ok(B, k, Hq, Hkv, D, max_blocks) == MOLT_OK;
   g_err = said;                                  // (a size function fails without a message)
-  return fits ? molt::select_ws_bytes(B, k + 1, Hkv, max_blocks) : 0;
+  return fits ? molt::select_ws_bytes(B, k + 1, Hq, Hkv, D, max_blocks) : 0;
 }
 
 int molt_select_blocks(const void* q, const void* bounds, const int32_t* block_tables, const int32_t* context_lens,
@@ -735,7 +735,7 @@ int molt_select_blocks(const void* q, const void* bounds, const int32_t* block_t
           "n_first = %d >= 0 and n_last = %d >= 1 must fit n_select = %d", n_first, n_last, n_select);
   REQUIRE(q && bounds && block_tables && context_lens && out, "a required pointer is NULL");
   REQUIRE(aligned16(q, bounds), "q and bounds must start at a multiple of 16 bytes");
-  if (int r = check_ws(workspace, workspace_bytes, molt::select_ws_bytes(B, k + 1, Hkv, max_blocks))) return r;
+  if (int r = check_ws(workspace, workspace_bytes, molt::select_ws_bytes(B, k + 1, Hq, Hkv, D, max_blocks))) return r;
   hipError_t e;
   {
     ProfScope ps(MOLT_PROF_ATTENTION, reinterpret_cast<hipStream_t>(stream));

@@ -167,17 +167,19 @@ bool plan_whole(int B, int n) { return B <= kPlanThreads && long(B) * n <= 8 * k
 
 // ---------------------------------------------------------------- rows by slot
 
+constexpr int kWriteRows = 16;
+
 // two elements of a row at any element alignment, as the bits that the cache holds
 typedef uint32_t UnalignedU1 __attribute__((aligned(2)));
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 typedef u32x2_t UnalignedU2 __attribute__((aligned(4)));
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 
-// Wavefront = 16 rows of k and v and 128 dims: a head of 128 dims or two of 64; lane = two dims. The rows fall into
-// runs of consecutive slots of one block; a wavefront writes the runs that begin among its rows, up to their ends. A
-// run that fills its block's 16 slots leaves V, whose tokens are contiguous, in whole 16-byte stores; other runs leave
+// Wavefront = R rows of k and v and 128 dims: a head of 128 dims or two of 64; lane = two dims. The rows fall into
+// runs of consecutive slots of one block; a wavefront writes the runs that begin among its rows, up to their ends, one
+// after the other. A run that fills its block's 16 slots leaves V, whose tokens are contiguous, in whole 16-byte stores; other runs leave
 // it in stores of 4 bytes where both tokens of a pair are there.
-template <int D, typename T>
+template <int D, int R, typename T>
 __global__ __launch_bounds__(kThreads) void kv_write_kernel(const T* __restrict__ k, long k_stride,
                                                             const T* __restrict__ v, long v_stride,
                                                             const int32_t* __restrict__ slots, int rows, int Hkv,
@@ -186,23 +188,19 @@ __global__ __launch_bounds__(kThreads) void kv_write_kernel(const T* __restrict_
   const int heads = (Hkv + HPW - 1) / HPW;
   const uint32_t item = blockIdx.x * (kThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const uint32_t tile = item / uint32_t(heads);
-  const int r0 = int(tile) * 16, lane = threadIdx.x % kWave;
+  const int r0 = int(tile) * R, lane = threadIdx.x % kWave;
   if (r0 >= rows) return;
   const int h = int(item - tile * heads) * HPW + lane / (D / 2), d = lane % (D / 2) * 2;
-  // lane l: the slot of row r0 - 1 + l
+  // lane l: the slot of row r0 - 1 + l, up to the last row of a run that begins at r0 + R - 1
   const int row = r0 - 1 + lane;
-  const int slot = row >= 0 && row < rows && lane < 33 ? slots[row] : -1;
+  const int slot = row >= 0 && row < rows && lane <= R + 16 ? slots[row] : -1;
   const bool good = slot >= 0 && slot / 16 < num_blocks;
+  // (where it follows on from row r0 - 1 within a block, row r0 belongs to a run of the tile before)
   const int before = __shfl_up(slot, 1);
-  const bool starts = good && (lane == 1 || before != slot - 1 || slot % 16 == 0 || before < 0);
-  // (row r0 continues a run of the tile before where its slot follows on)
-  const int prev = __shfl(slot, 0);
-  uint32_t begin = uint32_t(__ballot(starts) >> 1);                      // bit i: a run begins at row r0 + i
-  const uint32_t live = uint32_t(__ballot(good) >> 1);
-  const int s0 = __shfl(slot, 1);
-  if ((begin & 1) && prev >= 0 && prev == s0 - 1 && s0 % 16 != 0) begin &= ~1u;
+  const bool starts = good && lane > 0 && (slot % 16 == 0 || before != slot - 1);
+  const uint32_t begin = uint32_t(__ballot(starts) >> 1), live = uint32_t(__ballot(good) >> 1);   // bit i: row r0 + i
   const bool there = h < Hkv;
-  for (uint32_t left = begin & 0xffffu; left; left &= left - 1) {
+  for (uint32_t left = begin & ((1u << R) - 1); left; left &= left - 1) {
     const int i = __builtin_ctz(left);
     const uint32_t stop = (begin | ~live) >> i >> 1;                     // what ends the run
     const int len = min(stop ? __builtin_ctz(stop) + 1 : 32, 16);
@@ -213,13 +211,9 @@ __global__ __launch_bounds__(kThreads) void kv_write_kernel(const T* __restrict_
       uint32_t x[16], y[16];
 #pragma unroll
       for (int t = 0; t < 16; ++t) {
-        const int at = t - first;
-        const long r = r0 + i + at;
-        x[t] = y[t] = 0;
-        if (at >= 0 && at < len) {
-          x[t] = *reinterpret_cast<const UnalignedU1*>(k + r * k_stride + h * D + d);
-          y[t] = *reinterpret_cast<const UnalignedU1*>(v + r * v_stride + h * D + d);
-        }
+        const long r = r0 + i + min(max(t - first, 0), len - 1);         // (some row of the run where t has none)
+        x[t] = *reinterpret_cast<const UnalignedU1*>(k + r * k_stride + h * D + d);
+        y[t] = *reinterpret_cast<const UnalignedU1*>(v + r * v_stride + h * D + d);
       }
 #pragma unroll
       for (int t = 0; t < 16; ++t)
@@ -257,13 +251,9 @@ __global__ __launch_bounds__(kThreads) void kv_write_kernel(const T* __restrict_
       u32x2_t x[16], y[16];
 #pragma unroll
       for (int t = 0; t < 16; ++t) {
-        const int at = t - first;
-        const long r = r0 + i + at;
-        x[t] = y[t] = u32x2_t{0, 0};
-        if (at >= 0 && at < len) {
-          x[t] = *reinterpret_cast<const UnalignedU2*>(k + r * k_stride + h * D + d);
-          y[t] = *reinterpret_cast<const UnalignedU2*>(v + r * v_stride + h * D + d);
-        }
+        const long r = r0 + i + min(max(t - first, 0), len - 1);         // (some row of the run where t has none)
+        x[t] = *reinterpret_cast<const UnalignedU2*>(k + r * k_stride + h * D + d);
+        y[t] = *reinterpret_cast<const UnalignedU2*>(v + r * v_stride + h * D + d);
       }
 #pragma unroll
       for (int t = 0; t < 16; ++t)
@@ -421,7 +411,8 @@ hipError_t launch_plan_blocks(int32_t* bt, int32_t* n_blocks, const int32_t* ctx
 
 hipError_t launch_kv_write(const void* k, long k_stride, const void* v, long v_stride, const int32_t* slots, int rows,
                            int Hkv, int D, int num_blocks, molt_dtype dt, void* kc, void* vc, hipStream_t s) {
-  const long waves = (long(rows) + 15) / 16 * ((Hkv * long(D) + 127) / 128);
+  constexpr int R = kWriteRows;
+  const long waves = (long(rows) + R - 1) / R * ((Hkv * long(D) + 127) / 128);
   const unsigned grid = unsigned((waves + kThreads / kWave - 1) / (kThreads / kWave));
   auto go = [&](auto kernel, auto* t) {
     typedef decltype(t) P;
@@ -430,10 +421,10 @@ hipError_t launch_kv_write(const void* k, long k_stride, const void* v, long v_s
   };
   if (dt == MOLT_F32) {
     float* t = nullptr;
-    if (D == 128) go(kv_write_kernel<128, float>, t); else go(kv_write_kernel<64, float>, t);
+    if (D == 128) go(kv_write_kernel<128, R, float>, t); else go(kv_write_kernel<64, R, float>, t);
   } else {
     uint16_t* t = nullptr;
-    if (D == 128) go(kv_write_kernel<128, uint16_t>, t); else go(kv_write_kernel<64, uint16_t>, t);
+    if (D == 128) go(kv_write_kernel<128, R, uint16_t>, t); else go(kv_write_kernel<64, R, uint16_t>, t);
   }
   return hipGetLastError();
 }

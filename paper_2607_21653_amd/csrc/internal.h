@@ -199,9 +199,9 @@ hipError_t launch_bounds_update(const void* kc, void* bounds, const int32_t* bt,
                                 molt_dtype dt, hipStream_t s);
 hipError_t launch_bounds_read(const void* bounds, const int32_t* ids, int M, int Hkv, int D, int num_blocks, float* hi,
                               float* lo, hipStream_t s);
-// n query positions per sequence; workgroups of the call's largest launch (for the host's check)
-double select_groups(int B, int n, int Hq, int Hkv, int max_blocks);
-size_t select_ws_bytes(int B, int n, int Hkv, int max_blocks);
+// n query positions per sequence; workgroups of the call's largest launch, as if of 256 threads (for the host's check)
+double select_groups(int B, int n, int Hq, int Hkv, int D, int max_blocks);
+size_t select_ws_bytes(int B, int n, int Hq, int Hkv, int D, int max_blocks);
 hipError_t launch_select_blocks(const void* q, const void* bounds, const int32_t* bt, const int32_t* ctx,
                                 const int32_t* lens, int B, int n, int Hq, int Hkv, int D, int max_blocks,
                                 int num_blocks, int N, int n_first, int n_last, molt_dtype dt, int32_t* out, void* ws,

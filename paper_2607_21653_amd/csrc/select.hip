@@ -13,9 +13,9 @@
 namespace molt {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / kWave;
-constexpr int kTiles = 4;                        // row tiles of a workgroup: 64 query rows
+constexpr int kWaves = 8;
+constexpr int kThreads = kWaves * kWave;
+constexpr size_t kFusedLds = 80 << 10;           // two workgroups a CU
 
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t UnalignedU4 __attribute__((ext_vector_type(4), aligned(2)));
@@ -26,6 +26,10 @@ struct SelectArgs {
   int B, n, Hq, Hkv, G, N, n_first, n_last, max_blocks, num_blocks;
   uint32_t* keys;                                // [B n, Hkv, max_blocks]
   int32_t* out;                                  // [B n, Hkv, N]
+  int f32;                                       // q's type
+  uint32_t block_bytes;                          // of a block's records
+  int pos_groups, chunks, chunk, by_xcd;         // launch: groups of positions, chunks of blocks and their size,
+                                                 // sequences by XCD
 };
 
 // Keys order as scores do, as unsigned numbers: 0 for a block that the position does not see, above every score those
@@ -66,14 +70,13 @@ MOLT_DEV void load16(const float* p, float (&x)[16]) {
 // A query row as the A operands of 16x16x64 8-bit MFMAs: lane's row r = lane % 16; dims 16 g .. + 15 of each 64, for
 // k-steps over the codes of hi (c+), then over those of lo (c-). Returns the row's exponent.
 template <int D, typename T>
-MOLT_DEV int query_codes(const T* q, bool there, int g, int32x4_t (&a)[D / 32]) {
+MOLT_DEV int query_codes(const T* q, int g, int32x4_t (&a)[D / 32]) {
   constexpr int S = D / 64;
   float x[S][16];
   uint32_t top = 0;
 #pragma unroll
   for (int s = 0; s < S; ++s) {
-    if (there) load16(q + 64 * s + 16 * g, x[s]);
-    else for (int i = 0; i < 16; ++i) x[s][i] = 0.f;
+    load16(q + 64 * s + 16 * g, x[s]);
 #pragma unroll
     for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(x[s][i]) & 0x7fffffffu);
   }
@@ -81,181 +84,529 @@ MOLT_DEV int query_codes(const T* q, bool there, int g, int32x4_t (&a)[D / 32]) 
   top = max(top, uint32_t(__shfl_xor(int(top), 32)));
   const bool bad = top >= 0x7f800000u;
   const int e = bad ? kBoundsMinExponent : bounds_exponent(top);
-  const float r = pow2(-e);
-#pragma unroll
+  const float r = pow2(-e), magic = 12582912.0f;   // 1.5 * 2^23: x r + magic rounds x r to a whole number, ties to
+#pragma unroll                                     // even, whose two's complement is in the sum's low bits
   for (int s = 0; s < S; ++s)
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      int c[4];
+      uint32_t c[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) c[i] = bad ? 0 : int(__builtin_rintf(x[s][4 * w + i] * r));
-      a[s][w] = int(pack_codes(max(c[0], 0), max(c[1], 0), max(c[2], 0), max(c[3], 0)));
-      a[S + s][w] = int(pack_codes(min(c[0], 0), min(c[1], 0), min(c[2], 0), min(c[3], 0)));
+      for (int i = 0; i < 4; ++i) c[i] = __float_as_uint(__builtin_fmaf(x[s][4 * w + i], r, magic));
+      uint32_t codes = (c[0] & 0xffu) | (c[1] & 0xffu) << 8 | (c[2] & 0xffu) << 16 | c[3] << 24;
+      if (bad) codes = 0;
+      const uint32_t sign = codes >> 7 & 0x01010101u, negative = (sign << 8) - sign;
+      a[s][w] = int(codes & ~negative);
+      a[S + s][w] = int(codes & negative);
     }
   return e;
 }
 
-// Scores of a workgroup's positions (GP rows of a tile each, the kv head's G query rows and rows that do not count)
-// against a chunk of a sequence's blocks; wavefront = 16 blocks in turn. G > 16: TPP tiles a position.
-template <int D, int GP, typename T>
-__global__ __launch_bounds__(kThreads) void score_kernel(SelectArgs p, int pos_groups, int chunks, int chunk) {
-  typedef BoundsRecord<D> Rec;
-  constexpr int S = D / 32, PPT = 16 / GP;       // MFMA steps, positions of a tile
-  const int lane = threadIdx.x % kWave, g = lane / 16, col = lane % 16;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  uint32_t item = blockIdx.x;
-  const int c0 = int(item % chunks) * chunk;
-  item /= chunks;
-  const int h = int(item % p.Hkv);
-  item /= p.Hkv;
-  const int group = int(item % pos_groups), b = int(item / pos_groups);
-  const int tpp = (p.G + 15) / 16;               // 1 where GP < 16
-  const int j0 = group * (tpp > 1 ? 1 : kTiles * PPT);
-  const int n_here = min(p.n - j0, tpp > 1 ? 1 : kTiles * PPT);
-  const int count = p.lens ? min(n_here, p.lens[b] - j0) : n_here;       // rows that count
-  const int end = count <= 0 ? 0 : min(visible_blocks(p, b, j0 + count - 1), c0 + chunk);
-  if (c0 >= end) return;
+// Query rows in tiles of 16: a position's rows are padded to GP = 4, 8 or 16 of them, and where G > 16 take several
+// tiles; padding repeats the last row, which leaves the maximum as it is. A workgroup has the rows of 64 / GP positions,
+// or of one.
+struct Tiling { int tpp, positions; };           // tiles of a position, positions of a workgroup
+template <int GP>
+MOLT_DEV Tiling tiling_of(int G) {
+  const int tpp = (G + 15) / 16;
+  return {tpp, tpp > 1 ? 1 : 64 / GP};
+}
 
-  const T* q = static_cast<const T*>(p.q);
-  for (int t0 = 0; t0 < tpp; t0 += kTiles) {     // one round but for G > 64
-    int32x4_t a[kTiles][S];
-    int eq[kTiles][4];
+// LDS of a workgroup: codes and exponents of its tiles of query rows, as MFMA operands; 16 records for each wavefront,
+// which go through it into the MFMA's order
+constexpr int kMaxTiles = 4;
+template <int D>
+struct ScoreLds {
+  uint8_t records[kWaves][16 * 2 * D];
+  int32x4_t a[kMaxTiles][D / 32][kWave];
+  int32x4_t e[kMaxTiles][4];
+};
+
+// Codes of tiles t0 .. t0 + 3 of the workgroup's rows into LDS, a wavefront a tile
+template <int D, int GP>
+MOLT_DEV void stage_codes(const SelectArgs& p, const Tiling& ti, int b, int h, int j0, int t0, int wave, int lane,
+                          ScoreLds<D>& lds) {
+  const int g = lane / 16, col = lane % 16;
+  if (wave < kMaxTiles) {
+    const int j = ti.tpp > 1 ? j0 : min(j0 + (wave * 16 + col) / GP, p.n - 1);
+    const int head = min(ti.tpp > 1 ? (t0 + wave) * 16 + col : col % GP, p.G - 1);
+    const long at = ((long(b) * p.n + j) * p.Hq + h * p.G + head) * D;
+    int32x4_t a[D / 32];
+    const int e = p.f32 ? query_codes<D>(static_cast<const float*>(p.q) + at, g, a)
+                        : query_codes<D>(static_cast<const uint16_t*>(p.q) + at, g, a);
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-      const int j = tpp > 1 ? j0 : j0 + t * PPT + col / GP, head = tpp > 1 ? (t0 + t) * 16 + col : col % GP;
-      const bool there = j < p.n && head < p.G;
-      const int e = query_codes<D, T>(q + ((long(b) * p.n + j) * p.Hq + h * p.G + head) * D, there, g, a[t]);
+    for (int s = 0; s < D / 32; ++s) lds.a[wave][s][lane] = a[s];
+    if (g == 0) reinterpret_cast<int*>(lds.e[wave])[col] = e;
+  }
+}
+
+// v_max_f32, which the compiler surrounds with instructions that quiet NaN: there is none here
+MOLT_DEV float max_of(float a, float b) {
+  float r;
+  asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+
+// 16 records on their way: 16 bytes a lane, a record's bytes by lanes side by side (as the MFMA takes them, 16 bytes
+// of 16 records by 16 lanes, each lane's would be a request of its own); lanes 0 .. 15 have a record's exponent.
+template <int D>
+struct Records {
+  static constexpr int L = 2 * D / 16, PB = kWave / L, S = D / 32;       // lanes a record, records a load, loads
+  int32x4_t w[S];
+  int e, block;                                  // of record lane % 16; block < 0: none
+  MOLT_DEV void load(const SelectArgs& p, const uint8_t* head, int id, int lane) {
+    block = id >= 0 && id < p.num_blocks ? id : -1;
+    const int use = max(block, 0);               // (block 0's in the place of one that is not there)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) eq[t][i] = __shfl(there ? e : 1000, 4 * g + i);   // of the accumulator's rows
+    for (int c = 0; c < S; ++c) {
+      const uint32_t r = uint32_t(__shfl(use, c * PB + lane / L));
+      w[c] = *reinterpret_cast<const int32x4_t*>(head + uint64_t(r) * p.block_bytes + lane % L * 16);
     }
-    for (int k0 = c0 + 16 * wave; k0 < end; k0 += 16 * kWaves) {
-      const int blk = k0 + col;
-      const int id = blk < end ? p.bt[long(b) * p.max_blocks + blk] : -1;
-      const bool good = id >= 0 && id < p.num_blocks;
-      const uint8_t* rec = p.bounds + (long(good ? id : 0) * p.Hkv + h) * Rec::kBytes;
-      int32x4_t w[S];
+    if (lane < 16) e = int(int8_t(head[uint64_t(uint32_t(use)) * p.block_bytes + BoundsRecord<D>::kExponent]));
+  }
+  // to LDS, the 16-byte chunks of record r at places chunk ^ r, so that both ways are free of conflicts
+  MOLT_DEV void store(uint8_t* to, int lane) const {
 #pragma unroll
-      for (int s = 0; s < S; ++s) w[s] = *reinterpret_cast<const int32x4_t*>(rec + 64 * s + 16 * g);
-      const int ek = int(int8_t(rec[Rec::kExponent]));
+    for (int c = 0; c < S; ++c) {
+      const int r = c * PB + lane / L;
+      *reinterpret_cast<int32x4_t*>(to + r * 2 * D + ((lane % L) ^ (r % L)) * 16) = w[c];
+    }
+  }
+  MOLT_DEV static void operand(const uint8_t* from, int lane, int32x4_t (&f)[S]) {
+    const int g = lane / 16, col = lane % 16;
 #pragma unroll
-      for (int t = 0; t < kTiles; ++t) {
-        const int first_j = tpp > 1 ? j0 : j0 + t * PPT;
-        if (first_j >= p.n || (tpp > 1 && t0 + t >= tpp)) continue;
-        int32x4_t acc{0, 0, 0, 0};
+    for (int s = 0; s < S; ++s)
+      f[s] = *reinterpret_cast<const int32x4_t*>(from + col * 2 * D + ((4 * s + g) ^ (col % L)) * 16);
+  }
+};
+
+// Keys of the workgroup's positions for blocks c0 .. end - 1 of the sequence, of position i at keys + i * stride, block
+// c0 + x at [x]. (Which of them the position sees, the pick knows.) Wavefront = 32 blocks in turn, the next 32 records in
+// registers, the places of the 32 after them.
+template <int D, int GP, typename Keys>
+MOLT_DEV void score_blocks(const SelectArgs& p, int b, int h, int j0, int c0, int end, int wave, int lane,
+                           ScoreLds<D>& lds, Keys keys, long stride) {
+  constexpr int S = D / 32, STEP = 32 * kWaves;
+  const int g = lane / 16, col = lane % 16;
+  const Tiling ti = tiling_of<GP>(p.G);
+  const int32_t* row = p.bt + long(b) * p.max_blocks;
+  const uint8_t* head = p.bounds + long(h) * BoundsRecord<D>::kBytes;
+  auto place = [&](int at) { return at < end ? row[at] : -1; };
+  for (int t0 = 0; t0 < ti.tpp; t0 += kMaxTiles) {   // one round but for G > 64
+    const int k1 = c0 + 32 * wave + col;
+    const int id0 = place(k1), id1 = place(k1 + 16);
+    int next0 = place(k1 + STEP), next1 = place(k1 + STEP + 16);
+    if (t0) __syncthreads();
+    stage_codes<D, GP>(p, ti, b, h, j0, t0, wave, lane, lds);
+    Records<D> r0, r1;
+    r0.load(p, head, id0, lane);
+    r1.load(p, head, id1, lane);
+    __syncthreads();
+    const int tiles = ti.tpp > 1 ? min(ti.tpp - t0, kMaxTiles) : min((p.n - j0 + 16 / GP - 1) / (16 / GP), kMaxTiles);
+    uint8_t* mine = lds.records[wave];
+    for (int k0 = k1; k0 - col < end; k0 += STEP) {
+      int32x4_t f0[S], f1[S];
+      r0.store(mine, lane);
+      Records<D>::operand(mine, lane, f0);
+      r1.store(mine, lane);
+      Records<D>::operand(mine, lane, f1);
+      const int ek0 = __shfl(r0.e, col), ek1 = __shfl(r1.e, col);
+      const bool no0 = r0.block < 0, no1 = r1.block < 0;
+      r0.load(p, head, next0, lane);
+      r1.load(p, head, next1, lane);
+      next0 = place(k0 + 2 * STEP);
+      next1 = place(k0 + 2 * STEP + 16);
+      float best0 = -__builtin_inff(), best1 = best0;
+      for (int t = 0; t < tiles; ++t) {
+        int32x4_t acc0{0, 0, 0, 0}, acc1{0, 0, 0, 0};
 #pragma unroll
-        for (int s = 0; s < S; ++s) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[t][s], w[s], acc, 0, 0, 0);
-        float f[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          f[i] = eq[t][i] == 1000 ? -__builtin_inff() : float(acc[i]) * pow2(min(max(eq[t][i] + ek, -100), 100));
-        // rows 4 g + i of the tile: the positions' maxima
-        constexpr int OUT = GP >= 4 ? 1 : 4 / GP;
-        float best[OUT];
-#pragma unroll
-        for (int o = 0; o < OUT; ++o) {
-          best[o] = f[o * (4 / OUT)];
-#pragma unroll
-          for (int i = 1; i < 4 / OUT; ++i) best[o] = fmaxf(best[o], f[o * (4 / OUT) + i]);
-          if (GP >= 8) best[o] = fmaxf(best[o], __shfl_xor(best[o], 16));
-          if (GP >= 16) best[o] = fmaxf(best[o], __shfl_xor(best[o], 32));
+        for (int s = 0; s < S; ++s) {
+          const int32x4_t a = lds.a[t][s][lane];
+          acc0 = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, f0[s], acc0, 0, 0, 0);
+          acc1 = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, f1[s], acc1, 0, 0, 0);
         }
-        const bool writes = GP <= 4 || (GP == 8 ? g % 2 == 0 : g == 0);
+        const int32x4_t eq = lds.e[t][g];        // of rows 4 g + i
+        float x0[4], x1[4];
 #pragma unroll
-        for (int o = 0; o < OUT; ++o) {
-          const int j = first_j + (GP >= 4 ? 4 * g / GP : 4 * g / GP + o);
-          if (!writes || j >= p.n || blk >= end) continue;
-          const int last = visible_blocks(p, b, j) - 1;
-          uint32_t key = 0;
-          if (good && blk <= last) {
-            key = ek == kBoundsNotFinite ? kKeyInfinite : order_key(best[o]);
-            if (blk < p.n_first || blk > last - p.n_last) key = kKeyHeld;
+        for (int i = 0; i < 4; ++i) {
+          x0[i] = __builtin_ldexpf(float(acc0[i]), min(max(eq[i] + ek0, -100), 100));
+          x1[i] = __builtin_ldexpf(float(acc1[i]), min(max(eq[i] + ek1, -100), 100));
+        }
+        float m0 = max_of(max_of(x0[0], x0[1]), max_of(x0[2], x0[3]));
+        float m1 = max_of(max_of(x1[0], x1[1]), max_of(x1[2], x1[3]));
+        if (GP >= 8) {                           // a position's rows are in 2 or 4 of the g
+          const auto y0 = __builtin_amdgcn_permlane16_swap(__float_as_uint(m0), __float_as_uint(m0), false, false);
+          const auto y1 = __builtin_amdgcn_permlane16_swap(__float_as_uint(m1), __float_as_uint(m1), false, false);
+          m0 = max_of(__uint_as_float(y0[0]), __uint_as_float(y0[1]));
+          m1 = max_of(__uint_as_float(y1[0]), __uint_as_float(y1[1]));
+        }
+        if (GP >= 16) {
+          const auto y0 = __builtin_amdgcn_permlane32_swap(__float_as_uint(m0), __float_as_uint(m0), false, false);
+          const auto y1 = __builtin_amdgcn_permlane32_swap(__float_as_uint(m1), __float_as_uint(m1), false, false);
+          m0 = max_of(__uint_as_float(y0[0]), __uint_as_float(y0[1]));
+          m1 = max_of(__uint_as_float(y1[0]), __uint_as_float(y1[1]));
+          if (ti.tpp > 1) {
+            best0 = m0 = max_of(best0, m0);
+            best1 = m1 = max_of(best1, m1);
+            if (t < tiles - 1) continue;
           }
-          uint32_t* to = p.keys + ((long(b) * p.n + j) * p.Hkv + h) * p.max_blocks + blk;
-          if (tpp > 1 && (t0 || t)) key = max(key, *to);
-          *to = key;
         }
+        const int i = ti.tpp > 1 ? 0 : (t * 16 + 4 * g) / GP;
+        if (4 * g % GP != 0 || j0 + i >= p.n) continue;
+        uint32_t key0 = ek0 == kBoundsNotFinite ? kKeyInfinite : order_key(m0);
+        uint32_t key1 = ek1 == kBoundsNotFinite ? kKeyInfinite : order_key(m1);
+        if (no0) key0 = 0;
+        if (no1) key1 = 0;
+        auto to = keys + i * stride + (k0 - c0);
+        if (GP == 16 && t0) {                    // over the rounds
+          if (k0 < end) key0 = max(key0, to[0]);
+          if (k0 + 16 < end) key1 = max(key1, to[16]);
+        }
+        if (k0 < end) to[0] = key0;
+        if (k0 + 16 < end) to[16] = key1;
       }
     }
   }
 }
 
-// Workgroup = one list. The N-th largest key by 8 bits at a time, from histograms in LDS; then the blocks above it and
-// the first of those equal to it, in their order.
-__global__ __launch_bounds__(kThreads) void pick_kernel(SelectArgs p) {
-  __shared__ int hist[256];
-  __shared__ int sums[2][kWaves];
-  __shared__ int digit, above;
+// What a list holds beside the scores: the first blocks and the last that the position sees, before all others
+MOLT_DEV uint32_t list_key(const SelectArgs& p, uint32_t key, int blk, int seen) {
+  return key != 0 && (blk < p.n_first || blk >= seen - p.n_last) ? kKeyHeld : key;
+}
+
+// Sum over the wavefront of four numbers at once; PACKED: of numbers that sum to less than 2^16
+struct Four { uint32_t x[4]; };
+template <bool PACKED>
+MOLT_DEV Four wave_sum4(const Four& c) {
+  auto total = [](uint32_t v) { return uint32_t(__builtin_amdgcn_readlane(wave_scan_dpp(int(v)), 63)); };
+  if (PACKED) {
+    const uint32_t a = total(c.x[0] | c.x[1] << 16), b = total(c.x[2] | c.x[3] << 16);
+    return Four{{a & 0xffffu, a >> 16, b & 0xffffu, b >> 16}};
+  }
+  return Four{{total(c.x[0]), total(c.x[1]), total(c.x[2]), total(c.x[3])}};
+}
+MOLT_DEV uint32_t wave_max_u32(uint32_t v) {
+  v = max(v, dpp_u32<0x111, 0xF>(v, 0u));
+  v = max(v, dpp_u32<0x112, 0xF>(v, 0u));
+  v = max(v, dpp_u32<0x114, 0xF>(v, 0u));
+  v = max(v, dpp_u32<0x118, 0xF>(v, 0u));
+  v = max(v, dpp_u32<0x142, 0xA>(v, 0u));
+  v = max(v, dpp_u32<0x143, 0xC>(v, 0u));
+  return lane63(v);
+}
+
+// The border of the N largest keys: keys >= lo are in, and of those equal to `equal_key` (if `equal` > 0) the first
+// `equal`. It is searched between the smallest and the largest key, three borders at a time, which ends as soon as just
+// N keys are not below one; only where equal keys straddle the border does it run down to that key.
+struct Border { uint32_t lo, equal_key; int equal; };
+
+// A step of the search: more than N keys are >= lo (c_lo of them), fewer than N are >= hi (c_hi); or N are >= lo
+struct Search {
+  uint32_t lo, hi;
+  int c_lo, c_hi;
+  bool exact;
+  // counts of keys >= each of the three borders, from `count`
+  template <typename Count>
+  MOLT_DEV void step(int N, Count count) {
+    const uint32_t w = max((hi - lo) / 4, 1u), b0 = lo + w, b1 = b0 + w, b2 = b1 + w;
+    const Four c = count(b0, b1, b2);
+    const int c0 = int(c.x[0]), c1 = int(c.x[1]), c2 = int(c.x[2]);
+    exact = c0 == N || c1 == N || c2 == N;
+    if (exact) lo = c0 == N ? b0 : c1 == N ? b1 : b2;
+    else if (c0 < N) { hi = b0; c_hi = c0; }
+    else if (c1 < N) { lo = b0; c_lo = c0; hi = b1; c_hi = c1; }
+    else if (c2 < N) { lo = b1; c_lo = c1; hi = b2; c_hi = c2; }
+    else { lo = b2; c_lo = c2; }                 // (a border past hi has fewer than N keys)
+  }
+  MOLT_DEV bool done() const { return exact || hi - lo <= 1; }
+  MOLT_DEV Border border(int N) const {
+    if (exact) return {lo, 0u, 0};
+    return {lo + 1, lo, N - c_hi};
+  }
+};
+template <int M>
+MOLT_DEV Search wave_search(Search s, const uint32_t (&key)[M], int N) {
+  while (!s.done())
+    s.step(N, [&](uint32_t b0, uint32_t b1, uint32_t b2) __attribute__((always_inline)) {
+      Four c{{0, 0, 0, 0}};
+#pragma unroll
+      for (int i = 0; i < M; ++i) {
+        c.x[0] += key[i] >= b0;
+        c.x[1] += key[i] >= b1;
+        c.x[2] += key[i] >= b2;
+      }
+      return wave_sum4<true>(c);
+    });
+  return s;
+}
+
+// What the keys of m per lane are: how many, how many that a list holds anyway, the largest of the others and of their
+// complements
+struct Range { uint32_t some, held, top, low; };
+template <typename Key>
+MOLT_DEV Range range_of(int m, Key key) {
+  Range r{0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < m; ++i) {
+    const uint32_t k = key(i);
+    r.some += k != 0;
+    r.held += k == kKeyHeld;
+    if (k != 0 && k != kKeyHeld) {
+      r.top = max(r.top, k);
+      r.low = max(r.low, ~k);
+    }
+  }
+  return r;
+}
+MOLT_DEV Search search_of(const Range& r, int N) {
+  return {~r.low, r.top + 1, int(r.some), int(r.held), false};
+}
+
+// The blocks of keys within the border, in ascending order: a wavefront has those of blocks first + 64 i + lane. `at` of
+// them, and `match` equal ones, are in front of it.
+template <typename Key>
+MOLT_DEV void emit(int m, Key key, const Border& b, int32_t* out, int first, int lane, int at, int match) {
+  const unsigned long long below = (1ull << lane) - 1;
+#pragma unroll
+  for (int i = 0; i < m; ++i) {
+    const uint32_t k = key(i);
+    bool in = k >= b.lo;
+    const unsigned long long mi = __ballot(in);
+    int to = at + __popcll(mi & below);
+    at += __popcll(mi);
+    if (b.equal) {
+      const unsigned long long me = __ballot(k == b.equal_key);
+      const int rank = match + __popcll(me & below);
+      to += min(rank, b.equal);
+      in = in || (k == b.equal_key && rank < b.equal);
+      match += __popcll(me);
+    }
+    if (in) out[to] = first + 64 * i + lane;
+  }
+}
+
+// A workgroup's place: sequence, kv head, position group and chunk of blocks. A sequence's heads, whose records lie side
+// by side, run on one XCD where that leaves none idle.
+struct Item { int b, h, group, chunk; };
+MOLT_DEV Item item_of(const SelectArgs& p) {
+  uint32_t at = blockIdx.x;
+  const uint32_t inner = uint32_t(p.pos_groups) * p.Hkv * p.chunks;
+  Item it;
+  if (p.by_xcd) {
+    const uint32_t slot = at / 8;
+    it.b = int(slot / inner * 8 + at % 8);
+    at = slot % inner;
+  } else {
+    it.b = int(at / inner);
+    at %= inner;
+  }
+  it.h = int(at % p.Hkv);
+  at /= p.Hkv;
+  it.chunk = int(at % p.chunks);
+  it.group = int(at / p.chunks);
+  return it;
+}
+
+// Tables of up to 1024 blocks whose keys fit in LDS: scores and lists in one launch; a wavefront a list
+constexpr int kFusedBlocks = 1024;
+template <int D, int GP>
+__global__ __launch_bounds__(kThreads, 4) void select_kernel(SelectArgs p) {
+  extern __shared__ __align__(16) char dyn[];
+  ScoreLds<D>& lds = *reinterpret_cast<ScoreLds<D>*>(dyn);
+  uint32_t* keys = reinterpret_cast<uint32_t*>(dyn + sizeof(ScoreLds<D>));
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const Item it = item_of(p);
+  if (it.b >= p.B) return;
+  const int positions = tiling_of<GP>(p.G).positions, j0 = it.group * positions, here = min(p.n - j0, positions);
+  const int counted = p.lens ? min(here, p.lens[it.b] - j0) : here;
+  const int end = counted > 0 ? visible_blocks(p, it.b, j0 + counted - 1) : 0;
+  score_blocks<D, GP>(p, it.b, it.h, j0, 0, end, wave, lane, lds, keys, p.max_blocks);
+  __syncthreads();
+  for (int i = wave; i < here; i += kWaves) {
+    const int seen = visible_blocks(p, it.b, j0 + i);
+    int32_t* out = p.out + ((long(it.b) * p.n + j0 + i) * p.Hkv + it.h) * p.N;
+    const uint32_t* mine = keys + i * p.max_blocks;
+    auto go = [&](auto m) {
+      constexpr int M = decltype(m)::value;
+      uint32_t key[M];
+#pragma unroll
+      for (int x = 0; x < M; ++x) {
+        const int blk = x * kWave + lane;
+        key[x] = blk < seen ? list_key(p, mine[blk], blk, seen) : 0u;
+      }
+      auto at = [&](int x) { return key[x]; };
+      Range r = range_of(M, at);
+      const Four n = wave_sum4<true>(Four{{r.some, r.held, 0, 0}});
+      Border border{1, 0, 0};
+      if (int(n.x[0]) > p.N) {
+        r = Range{n.x[0], n.x[1], wave_max_u32(r.top), wave_max_u32(r.low)};
+        if (int(r.held) == p.N) border.lo = kKeyHeld;
+        else border = wave_search<M>(search_of(r, p.N), key, p.N).border(p.N);
+      }
+      emit(M, at, border, out, 0, lane, 0, 0);
+      for (int x = min(int(n.x[0]), p.N) + lane; x < p.N; x += kWave) out[x] = -1;
+    };
+    if (seen <= 4 * kWave) go(std::integral_constant<int, 4>{});
+    else if (seen <= 9 * kWave) go(std::integral_constant<int, 9>{});
+    else go(std::integral_constant<int, 16>{});
+  }
+}
+
+// Longer tables: keys of chunks of blocks into the workspace ..
+template <int D, int GP>
+__global__ __launch_bounds__(kThreads, 4) void score_kernel(SelectArgs p) {
+  __shared__ ScoreLds<D> lds;
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const Item it = item_of(p);
+  if (it.b >= p.B) return;
+  const int positions = tiling_of<GP>(p.G).positions, j0 = it.group * positions, here = min(p.n - j0, positions);
+  const int counted = p.lens ? min(here, p.lens[it.b] - j0) : here, c0 = it.chunk * p.chunk;
+  const int end = counted > 0 ? min(visible_blocks(p, it.b, j0 + counted - 1), c0 + p.chunk) : 0;
+  if (c0 >= end) return;
+  score_blocks<D, GP>(p, it.b, it.h, j0, c0, end, wave, lane, lds,
+                      p.keys + ((long(it.b) * p.n + j0) * p.Hkv + it.h) * p.max_blocks + c0, long(p.Hkv) * p.max_blocks);
+}
+
+// .. and a workgroup a list, M keys to a thread (0: tables past 2^13 blocks, the keys read again for each count). Once
+// few keys lie between the borders they go to LDS, and every wavefront ends the search by itself.
+constexpr int kPickThreads = 512, kPickWaves = kPickThreads / kWave, kFew = 8 * kWave;
+template <int M>
+__global__ __launch_bounds__(kPickThreads) void pick_kernel(SelectArgs p) {
+  __shared__ Four part[2][kPickWaves];
+  __shared__ uint32_t few[kFew];
+  __shared__ int n_few;
   const long list = blockIdx.x;
-  const int t = int(list / p.Hkv), b = t / p.n, j = t % p.n;
-  const int seen = visible_blocks(p, b, j);
+  const int t = int(list / p.Hkv), b = t / p.n, j = t % p.n, lane = threadIdx.x % kWave;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const uint32_t* keys = p.keys + list * p.max_blocks;
+  int m = M, first = wave * M * kWave;
+  uint32_t key[M ? M : 1];
+#pragma unroll
+  for (int x = 0; x < M; ++x) {                  // (before it is known how many of them count)
+    const int i = first + x * kWave + lane;
+    key[x] = i < p.max_blocks ? keys[i] : 0u;
+  }
+  if (threadIdx.x == 0) n_few = 0;
+  const int seen = visible_blocks(p, b, j);
+#pragma unroll
+  for (int x = 0; x < M; ++x) {
+    const int i = first + x * kWave + lane;
+    key[x] = i < seen ? list_key(p, key[x], i, seen) : 0u;
+  }
+  if (M == 0) {
+    m = (seen + kPickThreads - 1) / kPickThreads;
+    first = wave * m * kWave;
+  }
+  auto at = [&](int x) __attribute__((always_inline)) {
+    if (M) return key[M ? x : 0];
+    const int i = first + x * kWave + lane;
+    return i < seen ? list_key(p, keys[i], i, seen) : 0u;
+  };
+  int turn = 0;                                  // two sets of numbers in turn: one barrier an exchange
+  auto exchange = [&](const Four& c) {
+    turn ^= 1;
+    if (lane == 0) part[turn][wave] = c;
+    __syncthreads();
+  };
+  auto sum = [&](const Four& c) {
+    exchange(c);
+    Four all{{0, 0, 0, 0}};
+#pragma unroll
+    for (int w = 0; w < kPickWaves; ++w)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) all.x[u] += part[turn][w].x[u];
+    return all;
+  };
+  Range r = range_of(m, at);
+  const Four n = wave_sum4<M != 0>(Four{{r.some, r.held, 0, 0}});
+  exchange(Four{{n.x[0], n.x[1], wave_max_u32(r.top), wave_max_u32(r.low)}});
+  r = Range{0, 0, 0, 0};
+#pragma unroll
+  for (int w = 0; w < kPickWaves; ++w) {
+    const Four x = part[turn][w];
+    r = Range{r.some + x.x[0], r.held + x.x[1], max(r.top, x.x[2]), max(r.low, x.x[3])};
+  }
+  Border border{1, 0, 0};
+  if (int(r.some) > p.N) {
+    Search s = search_of(r, p.N);
+    if (int(r.held) == p.N) {
+      border.lo = kKeyHeld;
+    } else {
+      while (!s.done() && s.c_lo - s.c_hi > kFew)
+        s.step(p.N, [&](uint32_t b0, uint32_t b1, uint32_t b2) __attribute__((always_inline)) {
+          Four c{{0, 0, 0, 0}};
+#pragma unroll
+          for (int x = 0; x < m; ++x) {
+            const uint32_t k = at(x);
+            c.x[0] += k >= b0;
+            c.x[1] += k >= b1;
+            c.x[2] += k >= b2;
+          }
+          return sum(wave_sum4<M != 0>(c));
+        });
+      if (!s.done()) {
+#pragma unroll
+        for (int x = 0; x < m; ++x) {
+          const uint32_t k = at(x);
+          if (k >= s.lo && k < s.hi) few[atomicAdd(&n_few, 1)] = k;      // in any order: they are counted only
+        }
+        __syncthreads();
+        uint32_t some[kFew / kWave];
+#pragma unroll
+        for (int x = 0; x < kFew / kWave; ++x) some[x] = x * kWave + lane < n_few ? few[x * kWave + lane] : 0u;
+        const int above = s.c_hi;
+        s.c_lo -= above;
+        s.c_hi = 0;
+        s = wave_search<kFew / kWave>(s, some, p.N - above);
+        s.c_hi += above;
+      }
+      border = s.border(p.N);
+    }
+  }
+  Four c{{0, 0, 0, 0}};
+#pragma unroll
+  for (int x = 0; x < m; ++x) {
+    const uint32_t k = at(x);
+    c.x[0] += k >= border.lo;
+    c.x[1] += k == border.equal_key;
+  }
+  c = wave_sum4<M != 0>(c);
+  exchange(c);
+  int in = 0, equal = 0;                         // in front of the wavefront
+#pragma unroll
+  for (int w = 0; w < kPickWaves; ++w)
+    if (w < wave) { in += int(part[turn][w].x[0]); equal += int(part[turn][w].x[1]); }
   int32_t* out = p.out + list * p.N;
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  uint32_t floor_key = 0;                        // keys under it are out, those above it in
-  int equal = 0;                                 // of those equal to it, the first so many are in
-  if (seen > p.N) {
-    uint32_t prefix = 0;
-    int need = p.N;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      hist[threadIdx.x] = 0;
-      __syncthreads();
-      for (int i = threadIdx.x; i < seen; i += kThreads) {
-        const uint32_t key = keys[i];
-        if (shift == 24 || key >> (shift + 8) == prefix >> (shift + 8)) atomicAdd(&hist[key >> shift & 255], 1);
-      }
-      __syncthreads();
-      // keys of larger digits than 255 - thread
-      const int mine = hist[255 - threadIdx.x];
-      int s = wave_scan_dpp(mine);
-      if (lane == kWave - 1) sums[0][wave] = s;
-      __syncthreads();
-      for (int w = 0; w < wave; ++w) s += sums[0][w];
-      if (s >= need && s - mine < need) {
-        digit = 255 - int(threadIdx.x);
-        above = s - mine;
-      }
-      __syncthreads();
-      prefix |= uint32_t(digit) << shift;
-      need -= above;
-    }
-    floor_key = prefix;
-    equal = need;
-  }
-  if (floor_key == 0) equal = 0;                 // what a position does not see is never taken
-  int base_above = 0, base_equal = 0;
-  for (int i0 = 0; i0 < seen; i0 += kThreads) {
-    const int i = i0 + int(threadIdx.x);
-    const uint32_t key = i < seen ? keys[i] : 0u;
-    const bool in = key > floor_key, eq = key == floor_key && key != 0;
-    const unsigned long long mi = __ballot(in), me = __ballot(eq), below = (1ull << lane) - 1;
-    __syncthreads();
-    if (lane == 0) { sums[0][wave] = __popcll(mi); sums[1][wave] = __popcll(me); }
-    __syncthreads();
-    int ai = base_above + __popcll(mi & below), ae = base_equal + __popcll(me & below);
-    for (int w = 0; w < kWaves; ++w) {
-      if (w < wave) { ai += sums[0][w]; ae += sums[1][w]; }
-      base_above += sums[0][w];
-      base_equal += sums[1][w];
-    }
-    if (in || (eq && ae < equal)) out[ai + min(ae, equal)] = i;
-  }
-  for (int i = base_above + min(base_equal, equal) + int(threadIdx.x); i < p.N; i += kThreads) out[i] = -1;
+  emit(m, at, border, out, first, lane, in, equal);
+  for (int x = min(int(r.some), p.N) + int(threadIdx.x); x < p.N; x += kPickThreads) out[x] = -1;
 }
 
-int pow2_rows(int G) { return G <= 1 ? 1 : G <= 2 ? 2 : G <= 4 ? 4 : G <= 8 ? 8 : 16; }
+int padded_rows(int G) { return G <= 4 ? 4 : G <= 8 ? 8 : 16; }
+int score_positions(int G) { return G > 16 ? 1 : 64 / padded_rows(G); }
 
-// Positions of a workgroup of score_kernel, and blocks
-int score_positions(int G) { return G > 16 ? 1 : kTiles * 16 / pow2_rows(G); }
-constexpr int kScoreChunk = 16 * kWaves * 2;
+// LDS of a call in one launch; 0 where it takes two
+size_t fused_lds(int n, int G, int D, int max_blocks) {
+  const size_t fixed = D == 128 ? sizeof(ScoreLds<128>) : sizeof(ScoreLds<64>);
+  const size_t bytes = fixed + size_t(std::min(n, score_positions(G))) * max_blocks * sizeof(uint32_t);
+  return max_blocks <= kFusedBlocks && bytes <= kFusedLds ? bytes : 0;
+}
+
+// Chunks of blocks of a call in two launches: as many as fill the chip once, of 256 blocks or more
+int score_chunks(int B, int n, int G, int Hkv, int max_blocks) {
+  const long groups = long(B) * Hkv * ((long(n) + score_positions(G) - 1) / score_positions(G));
+  const int rounds = (max_blocks + 32 * kWaves - 1) / (32 * kWaves);
+  return int(std::max(1l, std::min(long(rounds), 512 / groups)));
+}
 
 }  // namespace
 
-double select_groups(int B, int n, int Hq, int Hkv, int max_blocks) {
-  const double at = score_positions(Hq / Hkv);
-  return std::max(double(B) * std::ceil(n / at) * Hkv * std::ceil(max_blocks / double(kScoreChunk)), double(B) * n * Hkv);
+double select_groups(int B, int n, int Hq, int Hkv, int D, int max_blocks) {
+  const int G = Hq / Hkv;
+  const double chunks = fused_lds(n, G, D, max_blocks) ? 1 : score_chunks(B, n, G, Hkv, max_blocks);
+  return 2 * std::max((double(B) + 7) * std::ceil(n / double(score_positions(G))) * Hkv * chunks, double(B) * n * Hkv);
 }
 
-size_t select_ws_bytes(int B, int n, int Hkv, int max_blocks) {
+size_t select_ws_bytes(int B, int n, int Hq, int Hkv, int D, int max_blocks) {
+  if (fused_lds(n, Hq / Hkv, D, max_blocks)) return 0;
   return size_t(B) * n * Hkv * max_blocks * sizeof(uint32_t) + 256;
 }
 
@@ -263,32 +614,48 @@ hipError_t launch_select_blocks(const void* q, const void* bounds, const int32_t
                                 const int32_t* lens, int B, int n, int Hq, int Hkv, int D, int max_blocks,
                                 int num_blocks, int N, int n_first, int n_last, molt_dtype dt, int32_t* out, void* ws,
                                 size_t ws_bytes, hipStream_t s) {
-  Carver c(ws, ws_bytes);
-  SelectArgs p{q, static_cast<const uint8_t*>(bounds), bt, ctx, lens, B, n, Hq, Hkv, Hq / Hkv, N, n_first, n_last,
-               max_blocks, num_blocks, c.take<uint32_t>(size_t(B) * n * Hkv * max_blocks), out};
-  const int gp = pow2_rows(p.G), per_group = score_positions(p.G), pos_groups = int((long(n) + per_group - 1) / per_group);
-  const int chunk = kScoreChunk, chunks = (max_blocks + chunk - 1) / chunk;
-  const unsigned grid = unsigned(long(B) * pos_groups * Hkv * chunks);
-  auto go = [&](auto kernel) { kernel<<<grid, kThreads, 0, s>>>(p, pos_groups, chunks, chunk); };
-  auto by_rows = [&](auto d, auto* t) {
-    constexpr int DD = decltype(d)::value;
-    typedef std::remove_pointer_t<decltype(t)> T;
-    switch (gp) {
-      case 1: go(score_kernel<DD, 1, T>); break;
-      case 2: go(score_kernel<DD, 2, T>); break;
-      case 4: go(score_kernel<DD, 4, T>); break;
-      case 8: go(score_kernel<DD, 8, T>); break;
-      default: go(score_kernel<DD, 16, T>);
-    }
+  SelectArgs p{};
+  p.q = q; p.bounds = static_cast<const uint8_t*>(bounds); p.bt = bt; p.ctx = ctx; p.lens = lens;
+  p.B = B; p.n = n; p.Hq = Hq; p.Hkv = Hkv; p.G = Hq / Hkv; p.N = N; p.n_first = n_first; p.n_last = n_last;
+  p.max_blocks = max_blocks; p.num_blocks = num_blocks; p.out = out;
+  p.f32 = dt == MOLT_F32;
+  const size_t lds = fused_lds(n, p.G, D, max_blocks);
+  const bool fused = lds != 0;
+  const int positions = score_positions(p.G);
+  p.pos_groups = int((long(n) + positions - 1) / positions);
+  p.chunks = 1;
+  p.block_bytes = uint32_t(Hkv) * (2 * D + 16);
+  p.by_xcd = B % 8 == 0 || B >= 48;
+  if (!fused) {
+    const int most = score_chunks(B, n, p.G, Hkv, max_blocks), rounds = (max_blocks + 32 * kWaves - 1) / (32 * kWaves);
+    p.chunk = (rounds + most - 1) / most * 32 * kWaves;
+    p.chunks = (max_blocks + p.chunk - 1) / p.chunk;
+    Carver c(ws, ws_bytes);
+    p.keys = c.take<uint32_t>(size_t(B) * n * Hkv * max_blocks);
+  }
+  const long inner = long(p.pos_groups) * Hkv * p.chunks;
+  const unsigned grid = unsigned((p.by_xcd ? (long(B) + 7) / 8 * 8 : long(B)) * inner);
+  auto go = [&](auto d, auto gp) {
+    constexpr int DD = decltype(d)::value, GP = decltype(gp)::value;
+    if (fused) select_kernel<DD, GP><<<grid, kThreads, lds, s>>>(p);
+    else score_kernel<DD, GP><<<grid, kThreads, 0, s>>>(p);
   };
-  auto by_dim = [&](auto* t) {
-    if (D == 128) by_rows(std::integral_constant<int, 128>{}, t);
-    else by_rows(std::integral_constant<int, 64>{}, t);
+  auto by_rows = [&](auto d) {
+    const int gp = padded_rows(p.G);
+    if (gp == 4) go(d, std::integral_constant<int, 4>{});
+    else if (gp == 8) go(d, std::integral_constant<int, 8>{});
+    else go(d, std::integral_constant<int, 16>{});
   };
-  if (dt == MOLT_F32) by_dim(static_cast<float*>(nullptr));
-  else by_dim(static_cast<uint16_t*>(nullptr));
+  if (D == 128) by_rows(std::integral_constant<int, 128>{});
+  else by_rows(std::integral_constant<int, 64>{});
   if (hipError_t e = hipGetLastError()) return e;
-  pick_kernel<<<unsigned(long(B) * n * Hkv), kThreads, 0, s>>>(p);
+  if (fused) return hipSuccess;
+  const unsigned lists = unsigned(long(B) * n * Hkv);
+  const int per = (max_blocks + kPickThreads - 1) / kPickThreads;
+  if (per <= 4) pick_kernel<4><<<lists, kPickThreads, 0, s>>>(p);
+  else if (per <= 9) pick_kernel<9><<<lists, kPickThreads, 0, s>>>(p);
+  else if (per <= 16) pick_kernel<16><<<lists, kPickThreads, 0, s>>>(p);
+  else pick_kernel<0><<<lists, kPickThreads, 0, s>>>(p);
   return hipGetLastError();
 }
 

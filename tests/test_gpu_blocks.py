@@ -262,7 +262,7 @@ def test_select_of_lengths(molt_lib, dtype, B, n, maxb, N, first, last):
     _select_both(molt_lib, _queries(rng, B, n, 4, 64, dtype), bounds, tables, ctx, n, N, first, last, lens)
 
 
-@pytest.mark.parametrize("maxb", [30, 1500, 5000])
+@pytest.mark.parametrize("maxb", [30, 1500, 5000, 17000])
 def test_select_of_equal_scores(molt_lib, maxb):
     """Few different scores, many ties, all equal ones, zeros: the lowest blocks of them."""
     rng = np.random.default_rng(maxb)
