@@ -19,13 +19,12 @@ struct BlocksArgs {
   float* part_o;                                 // [units, splits, 16, D] partial outputs of split lists
   float* part_ml;                                // [units, splits, 16, 2] their maxima and sums
   int B, n, Hq, Hkv, G, N, max_blocks, num_blocks;
-  int row_groups, splits, per_split;             // groups of 16 query rows of a kv head; parts of a list, pairs of one
+  int row_groups, splits, per_split;             // groups of 16 query rows of a kv head; parts of a list, units of one
+  int by_xcd;
   float c;                                       // log2(e) / sqrt(D)
 };
 
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
-typedef u32x4_t UnalignedU4 __attribute__((aligned(2)));
-typedef floatx4_t UnalignedF4 __attribute__((aligned(4)));
 
 // Entry e of a list, e in [e0, e0 + 64): lane e - e0 holds its block's place in the cache (-1: none) and how many of
 // its 16 tokens the position sees.
@@ -72,58 +71,82 @@ MOLT_DEV void weigh(Running<D>& r, float (&s)[M], float c) {
   }
 }
 
+// A block's keys or values of one kv head on their way to LDS: 16 bytes a lane, in the cache's order, so that lanes side
+// by side ask for bytes side by side. (As the MFMAs take them, 16 bytes of 16 tokens or dims by 16 lanes, each lane's are
+// a request of its own: the loads are then bound by requests, at 20 bytes a cycle and CU.)
+template <int D, typename T>
+struct Raw {
+  static constexpr int kBytes = 16 * D * int(sizeof(T)), kLoads = kBytes / 1024;
+  u32x4_t w[kLoads];
+  MOLT_DEV void load(const void* cache, long block_head, int lane) {
+    const uint8_t* from = static_cast<const uint8_t*>(cache) + block_head * kBytes;
+#pragma unroll
+    for (int c = 0; c < kLoads; ++c) w[c] = *reinterpret_cast<const u32x4_t*>(from + c * 1024 + lane * 16);
+  }
+};
+
 // bf16: two blocks at a time. Scores S^T = K Q^T by 16x16x32 MFMAs whose A rows are tokens in such an order that a
 // lane's 8 scores of the two tiles are those of 8 consecutive tokens of one block: rows 4 g + i of tile x are tokens
 // 8 (g % 2) + 4 x + i of block g / 2. They are then the B operand of O^T = V^T P^T as they lie, and V's A operand is
-// 16 contiguous bytes of the cache. Weights go in as two bf16 parts, 16 bits.
+// 16 contiguous bytes. Weights go in as two bf16 parts, 16 bits. In LDS a token's 16-byte chunks of K lie at chunk ^ f
+// and a dim's two of V at half ^ f, with f of the token or dim, so that reads are free of bank conflicts.
 template <int D>
 struct PairBf16 {
   static constexpr int kBlocks = 2;
-  bf16x8_t q[D / 32];
-  MOLT_DEV void load_q(const void* qq, long row, bool there, int g) {
+  static constexpr int kLds = 2 * 2 * Raw<D, uint16_t>::kBytes;
+  static constexpr int KC = D / 8;               // chunks of a token
+  struct Query { bf16x8_t q[D / 32]; };
+  MOLT_DEV static void load_q(Query& r, const void* qq, long row, bool there, int g) {
 #pragma unroll
     for (int s = 0; s < D / 32; ++s) {
       u32x4_t w{0, 0, 0, 0};
-      if (there) w = *reinterpret_cast<const UnalignedU4*>(static_cast<const uint16_t*>(qq) + row * D + 32 * s + 8 * g);
-      q[s] = __builtin_bit_cast(bf16x8_t, w);
+      if (there) w = *reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(qq) + row * D + 32 * s + 8 * g);
+      r.q[s] = __builtin_bit_cast(bf16x8_t, w);
     }
   }
-  u32x4_t k[2][D / 32], v[D / 16];
-  MOLT_DEV void load(const BlocksArgs& p, const int (&id)[2], int h, int g, int col) {
-    const long kb = (long(col / 8 ? id[1] : id[0]) * p.Hkv + h) * 16 * D;
-    const long vb = (long(g / 2 ? id[1] : id[0]) * p.Hkv + h) * 16 * D;
-    const uint16_t* kp = static_cast<const uint16_t*>(p.kc) + kb + (col / 4 % 2 * 8 + col % 4) * D + 8 * g;
-    const uint16_t* vp = static_cast<const uint16_t*>(p.vc) + vb + col * 16 + g % 2 * 8;
-#pragma unroll
-    for (int x = 0; x < 2; ++x)
-#pragma unroll
-      for (int s = 0; s < D / 32; ++s) k[x][s] = *reinterpret_cast<const u32x4_t*>(kp + 4 * x * D + 32 * s);
-#pragma unroll
-    for (int d = 0; d < D / 16; ++d) v[d] = *reinterpret_cast<const u32x4_t*>(vp + d * 256);
+  MOLT_DEV static int key_at(int block, int token, int chunk) {
+    const int f = ((token & 3) | (token >> 3 & 1) << 2 | (token >> 2 & 1) << 3) & (KC - 1);
+    return (block * 16 + token) * KC * 16 + (chunk ^ f) * 16;
   }
-  // tokens of the lane's 8 that are seen, of its block's
-  MOLT_DEV void use(Running<D>& r, const int (&seen)[2], int g, float c) {
+  MOLT_DEV static int value_at(int block, int dim, int half) {
+    return 2 * Raw<D, uint16_t>::kBytes + (block * D + dim) * 32 + (half ^ (dim >> 2 & 1)) * 16;
+  }
+  Raw<D, uint16_t> k[2], v[2];
+  MOLT_DEV void load(const BlocksArgs& p, const int (&id)[2], int h, int lane) {
+#pragma unroll
+    for (int y = 0; y < 2; ++y) k[y].load(p.kc, long(id[y]) * p.Hkv + h, lane);
+#pragma unroll
+    for (int y = 0; y < 2; ++y) v[y].load(p.vc, long(id[y]) * p.Hkv + h, lane);
+  }
+  MOLT_DEV void store(uint8_t* lds, int lane) const {
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+#pragma unroll
+      for (int c = 0; c < Raw<D, uint16_t>::kLoads; ++c) {
+        const int at = c * 64 + lane;
+        *reinterpret_cast<u32x4_t*>(lds + key_at(y, at / KC, at % KC)) = k[y].w[c];
+        *reinterpret_cast<u32x4_t*>(lds + value_at(y, at / 2, at % 2)) = v[y].w[c];
+      }
+  }
+  // seen: tokens of the blocks that the row sees
+  MOLT_DEV static void use(const uint8_t* lds, const Query& q, const int (&seen)[2], Running<D>& r, int g, int col, float c) {
     floatx4_t s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
     for (int x = 0; x < 2; ++x)
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i)
-        s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, k[x][i]), q[i], s[x], 0, 0, 0);
+      for (int i = 0; i < D / 32; ++i) {
+        const bf16x8_t k = *reinterpret_cast<const bf16x8_t*>(lds + key_at(col / 8, col / 4 % 2 * 8 + 4 * x + col % 4, 4 * i + g));
+        s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q.q[i], s[x], 0, 0, 0);
+      }
     float w[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) w[i] = s[i / 4][i % 4];
-    if (seen[0] < 16 || seen[1] < 16) {          // wavefront-uniform
-      const int mine = (g / 2 ? seen[1] : seen[0]) - g % 2 * 8;
+    const bool cut = seen[0] < 16 || seen[1] < 16;                       // wavefront-uniform
+    const int mine = (g / 2 ? seen[1] : seen[0]) - g % 2 * 8;            // of the lane's 8 tokens
+    if (cut) {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
         if (i >= mine) w[i] = -__builtin_inff();
-#pragma unroll
-      for (int d = 0; d < D / 16; ++d)           // what is not seen may be anything: 0 times it would be NaN
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (2 * i >= mine) v[d][i] = 0;
-          else if (2 * i + 1 >= mine) v[d][i] &= 0xffffu;
-        }
     }
     weigh<D, 8>(r, w, c);
     bf16x8_t hi, lo;
@@ -134,7 +157,12 @@ struct PairBf16 {
     }
 #pragma unroll
     for (int d = 0; d < D / 16; ++d) {
-      const bf16x8_t a = __builtin_bit_cast(bf16x8_t, v[d]);
+      u32x4_t v = *reinterpret_cast<const u32x4_t*>(lds + value_at(g / 2, 16 * d + col, g % 2));
+      if (cut) {                                 // what is not seen may be anything: 0 times it would be NaN
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = 2 * i >= mine ? 0 : 2 * i + 1 >= mine ? v[i] & 0xffffu : v[i];
+      }
+      const bf16x8_t a = __builtin_bit_cast(bf16x8_t, v);
       r.o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, hi, r.o[d], 0, 0, 0);
       r.o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, lo, r.o[d], 0, 0, 0);
     }
@@ -146,48 +174,62 @@ struct PairBf16 {
 template <int D>
 struct BlockF32 {
   static constexpr int kBlocks = 1;
-  floatx4_t q[D / 16];
-  MOLT_DEV void load_q(const void* qq, long row, bool there, int g) {
+  static constexpr int kLds = 2 * Raw<D, float>::kBytes;
+  static constexpr int KC = D / 4;
+  struct Query { floatx4_t q[D / 16]; };
+  MOLT_DEV static void load_q(Query& r, const void* qq, long row, bool there, int g) {
 #pragma unroll
     for (int s = 0; s < D / 16; ++s) {
-      q[s] = floatx4_t{0.f, 0.f, 0.f, 0.f};
-      if (there) q[s] = *reinterpret_cast<const UnalignedF4*>(static_cast<const float*>(qq) + row * D + D / 4 * g + 4 * s);
+      r.q[s] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+      if (there) r.q[s] = *reinterpret_cast<const floatx4_t*>(static_cast<const float*>(qq) + row * D + D / 4 * g + 4 * s);
     }
   }
-  floatx4_t k[D / 16], v[D / 16];
-  MOLT_DEV void load(const BlocksArgs& p, const int (&id)[1], int h, int g, int col) {
-    const long at = (long(id[0]) * p.Hkv + h) * 16 * D;
-    const float* kp = static_cast<const float*>(p.kc) + at + col * D + D / 4 * g;
-    const float* vp = static_cast<const float*>(p.vc) + at + col * 16 + 4 * g;
-#pragma unroll
-    for (int s = 0; s < D / 16; ++s) k[s] = *reinterpret_cast<const floatx4_t*>(kp + 4 * s);
-#pragma unroll
-    for (int d = 0; d < D / 16; ++d) v[d] = *reinterpret_cast<const floatx4_t*>(vp + d * 256);
+  MOLT_DEV static int key_at(int token, int chunk) { return token * KC * 16 + (chunk ^ (token & 7)) * 16; }
+  MOLT_DEV static int value_at(int dim, int chunk) {
+    return Raw<D, float>::kBytes + dim * 64 + (chunk ^ (dim >> 1 & 3)) * 16;
   }
-  MOLT_DEV void use(Running<D>& r, const int (&seen)[1], int g, float c) {
+  Raw<D, float> k, v;
+  MOLT_DEV void load(const BlocksArgs& p, const int (&id)[1], int h, int lane) {
+    k.load(p.kc, long(id[0]) * p.Hkv + h, lane);
+    v.load(p.vc, long(id[0]) * p.Hkv + h, lane);
+  }
+  MOLT_DEV void store(uint8_t* lds, int lane) const {
+#pragma unroll
+    for (int c = 0; c < Raw<D, float>::kLoads; ++c) {
+      const int at = c * 64 + lane;
+      *reinterpret_cast<u32x4_t*>(lds + key_at(at / KC, at % KC)) = k.w[c];
+      *reinterpret_cast<u32x4_t*>(lds + value_at(at / 4, at % 4)) = v.w[c];
+    }
+  }
+  MOLT_DEV static void use(const uint8_t* lds, const Query& q, const int (&seen)[1], Running<D>& r, int g, int col, float c) {
     floatx4_t s{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i)
+    for (int i = 0; i < D / 16; ++i) {
+      const floatx4_t k = *reinterpret_cast<const floatx4_t*>(lds + key_at(col, D / 16 * g + i));
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[i][e], q[i][e], s, 0, 0, 0);
+      for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[e], q.q[i][e], s, 0, 0, 0);
+    }
     float w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = s[i];
+    const int mine = seen[0] - 4 * g;
     if (seen[0] < 16) {
-      const int mine = seen[0] - 4 * g;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (i >= mine) {
-          w[i] = -__builtin_inff();
-#pragma unroll
-          for (int d = 0; d < D / 16; ++d) v[d][i] = 0.f;
-        }
+        if (i >= mine) w[i] = -__builtin_inff();
     }
     weigh<D, 4>(r, w, c);
 #pragma unroll
-    for (int d = 0; d < D / 16; ++d)
+    for (int d = 0; d < D / 16; ++d) {
+      floatx4_t v = *reinterpret_cast<const floatx4_t*>(lds + value_at(16 * d + col, g));
+      if (seen[0] < 16) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) r.o[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[d][i], w[i], r.o[d], 0, 0, 0);
+        for (int i = 0; i < 4; ++i)
+          if (i >= mine) v[i] = 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r.o[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[i], w[i], r.o[d], 0, 0, 0);
+    }
   }
 };
 
@@ -197,28 +239,37 @@ MOLT_DEV void store4(uint16_t* p, floatx4_t x) {
 MOLT_DEV void store4(float* p, floatx4_t x) { *reinterpret_cast<floatx4_t*>(p) = x; }
 
 // Workgroup = one list (or a part of it) and 16 query rows; wavefronts take its units (pairs of blocks, or blocks) in
-// turn with running softmaxes of their own and join them in LDS.
+// turn, a unit ahead in registers, with running softmaxes of their own, and join them in LDS.
 template <int D, typename T, int W>
-__global__ __launch_bounds__(W* kWave) void blocks_attention_kernel(BlocksArgs p) {
+__global__ __launch_bounds__(W* kWave, 2) void blocks_attention_kernel(BlocksArgs p) {
   typedef std::conditional_t<sizeof(T) == 2, PairBf16<D>, BlockF32<D>> Unit;
   constexpr int KB = Unit::kBlocks, PER = kWave / KB;                    // blocks of a unit; units that lanes hold
+  constexpr int kAcc = D / 16 * kWave * 16;                              // a wavefront's O for the join
+  __shared__ __attribute__((aligned(16))) uint8_t lds[W][Unit::kLds > kAcc ? Unit::kLds : kAcc];
   __shared__ float ml[W][2][16];
-  __shared__ floatx4_t acc[W > 1 ? W : 1][D / 16][kWave];
   const int lane = threadIdx.x % kWave, g = lane / 16, col = lane % 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  uint32_t item = blockIdx.x;
-  const int split = int(item % p.splits);
-  item /= p.splits;
-  const int rg = int(item % p.row_groups);
-  item /= p.row_groups;
-  const int h = int(item % p.Hkv), t = int(item / p.Hkv), b = t / p.n, j = t % p.n;
+  // all of a sequence's and kv head's lists on one XCD where that leaves none idle: neighbouring positions list much
+  // the same blocks
+  uint32_t item = blockIdx.x, bh;
+  const uint32_t inner = uint32_t(p.n) * p.row_groups * p.splits;
+  if (p.by_xcd) {
+    bh = item / 8 / inner * 8 + item % 8;
+    item = item / 8 % inner;
+    if (bh >= uint32_t(p.B) * p.Hkv) return;
+  } else {
+    bh = item / inner;
+    item %= inner;
+  }
+  const int split = int(item % p.splits), rg = int(item / p.splits % p.row_groups);
+  const int j = int(item / p.splits / p.row_groups), h = int(bh % p.Hkv), b = int(bh / p.Hkv), t = b * p.n + j;
   const long pos = long(p.ctx[b]) + j;
   const int32_t* list = p.blocks + (long(t) * p.Hkv + h) * p.N;
   const int head = h * p.G + rg * 16 + col;
   const bool there = rg * 16 + col < p.G;
 
-  Unit u;
-  u.load_q(p.q, long(t) * p.Hq + head, there, g);
+  typename Unit::Query q;
+  Unit::load_q(q, p.q, long(t) * p.Hq + head, there, g);
   Running<D> r;
 #pragma unroll
   for (int d = 0; d < D / 16; ++d) r.o[d] = floatx4_t{0.f, 0.f, 0.f, 0.f};
@@ -226,21 +277,36 @@ __global__ __launch_bounds__(W* kWave) void blocks_attention_kernel(BlocksArgs p
   for (int base = u0; base < u1; base += W * PER) {
     const int mine = base + wave + lane / KB * W, e = mine * KB + lane % KB;
     const Entries en = entries_of(p, list, e, mine < u1 && e < p.N, b, pos);
-    for (int i = 0; i < PER && base + wave + i * W < u1; ++i) {
-      int id[KB], seen[KB], any = 0, some = 0;
+    unsigned long long left = __ballot(en.seen > 0);                     // units with a key, by the lane of their first
+    if (KB == 2) left = (left | left >> 1) & 0x5555555555555555ull;      // block
+    if (!left) continue;
+    Unit u;
+    int seen[KB];
+    auto fetch = [&]() __attribute__((always_inline)) {
+      const int i = __builtin_ctzll(left);
+      left &= left - 1;
+      int id[KB], some = 0;
 #pragma unroll
-      for (int x = 0; x < KB; ++x) {
-        id[x] = __builtin_amdgcn_readlane(en.id, i * KB + x);
-        seen[x] = __builtin_amdgcn_readlane(en.seen, i * KB + x);
-        any += seen[x];
-        if (id[x] >= 0) some = id[x];
+      for (int y = 0; y < KB; ++y) {
+        id[y] = __builtin_amdgcn_readlane(en.id, i + y);
+        seen[y] = __builtin_amdgcn_readlane(en.seen, i + y);
+        if (id[y] >= 0) some = id[y];
       }
-      if (any == 0) continue;
 #pragma unroll
-      for (int x = 0; x < KB; ++x)
-        if (id[x] < 0) id[x] = some;             // the other block's, unseen
-      u.load(p, id, h, g, col);
-      u.use(r, seen, g, p.c);
+      for (int y = 0; y < KB; ++y)
+        if (id[y] < 0) id[y] = some;             // the other block's, unseen
+      u.load(p, id, h, lane);
+    };
+    fetch();
+    for (;;) {
+      int now[KB];
+#pragma unroll
+      for (int y = 0; y < KB; ++y) now[y] = seen[y];
+      u.store(lds[wave], lane);
+      const bool more = left != 0;
+      if (more) fetch();
+      Unit::use(lds[wave], q, now, r, g, col, p.c);
+      if (!more) break;
     }
   }
 
@@ -256,7 +322,7 @@ __global__ __launch_bounds__(W* kWave) void blocks_attention_kernel(BlocksArgs p
 #pragma unroll
     for (int w = 0; w < W; ++w) l += __builtin_amdgcn_exp2f(ml[w][0][col] - base) * ml[w][1][col];
 #pragma unroll
-    for (int d = 0; d < D / 16; ++d) acc[wave][d][lane] = r.o[d] * f;
+    for (int d = 0; d < D / 16; ++d) reinterpret_cast<floatx4_t*>(lds[wave])[d * kWave + lane] = r.o[d] * f;
     __syncthreads();
     r.m = m;
     r.l = l;
@@ -268,9 +334,9 @@ __global__ __launch_bounds__(W* kWave) void blocks_attention_kernel(BlocksArgs p
     if (d >= D / 16) break;
     floatx4_t o;
     if (W > 1) {
-      o = acc[0][d][lane];
+      o = reinterpret_cast<const floatx4_t*>(lds[0])[d * kWave + lane];
 #pragma unroll
-      for (int w = 1; w < W; ++w) o += acc[w][d][lane];
+      for (int w = 1; w < W; ++w) o += reinterpret_cast<const floatx4_t*>(lds[w])[d * kWave + lane];
     } else {
       o = r.o[d0];
     }
@@ -309,14 +375,15 @@ __global__ __launch_bounds__(256) void blocks_join_kernel(BlocksArgs p) {
   store4(static_cast<T*>(p.out) + at * D + d, o * inv);
 }
 
-struct BlocksPlan { int row_groups, splits, per_split; };
+struct BlocksPlan { int row_groups, splits, per_split, waves; };
 BlocksPlan blocks_plan(int B, int n, int Hq, int Hkv, int N) {
   BlocksPlan pl{};
   const int units = (N + 1) / 2;
   pl.row_groups = (Hq / Hkv + 15) / 16;
   const long lists = long(B) * n * Hkv * pl.row_groups;
-  // a split has 8 pairs at least, two for each wavefront
-  const long want = std::max(1l, std::min((512 + lists - 1) / lists, long(units) / 8));
+  pl.waves = lists * 4 >= 2048 || units < 16 ? 4 : 8;
+  // a split has two units at least for each wavefront
+  const long want = std::max(1l, std::min((2048 / pl.waves / 2 + lists - 1) / lists, long(units) / (2 * pl.waves)));
   pl.per_split = int((units + want - 1) / want);
   pl.splits = (units + pl.per_split - 1) / pl.per_split;
   return pl;
@@ -326,7 +393,7 @@ BlocksPlan blocks_plan(int B, int n, int Hq, int Hkv, int N) {
 
 double blocks_attention_groups(int B, int n, int Hq, int Hkv, int N) {
   const BlocksPlan pl = blocks_plan(B, n, Hq, Hkv, N);
-  return std::max(double(B) * n * Hkv * pl.row_groups * pl.splits, double(B) * n * Hq / 8);
+  return 2 * std::max((double(B) * Hkv + 7) * n * pl.row_groups * pl.splits, double(B) * n * Hq / 8);
 }
 
 size_t blocks_attention_ws_bytes(int B, int n, int Hq, int Hkv, int D, int N) {
@@ -341,8 +408,10 @@ hipError_t launch_blocks_attention(const void* q, const void* kc, const void* vc
                                    int num_blocks, int N, molt_dtype dt, void* out, void* ws, size_t ws_bytes,
                                    hipStream_t s) {
   const BlocksPlan pl = blocks_plan(B, n, Hq, Hkv, N);
+  const long bh = long(B) * Hkv;
+  const int by_xcd = n > 1 && (bh % 8 == 0 || bh >= 48);
   BlocksArgs p{q, kc, vc, bt, ctx, blocks, out, nullptr, nullptr, B, n, Hq, Hkv, Hq / Hkv, N, max_blocks, num_blocks,
-               pl.row_groups, pl.splits, dt == MOLT_F32 ? 2 * pl.per_split : pl.per_split,
+               pl.row_groups, pl.splits, dt == MOLT_F32 ? 2 * pl.per_split : pl.per_split, by_xcd,
                kLog2e / std::sqrt(float(D))};
   const size_t rows = size_t(B) * n * Hkv * pl.row_groups * pl.splits;
   if (pl.splits > 1) {
@@ -350,12 +419,12 @@ hipError_t launch_blocks_attention(const void* q, const void* kc, const void* vc
     p.part_o = c.take<float>(rows * 16 * D);
     p.part_ml = c.take<float>(rows * 16 * 2);
   }
-  constexpr int W = 4;
-  const unsigned grid = unsigned(rows), joins = unsigned((long(B) * n * Hq * (D / 4) + 255) / 256);
+  const unsigned grid = unsigned((by_xcd ? (bh + 7) / 8 * 8 : bh) * n * pl.row_groups * pl.splits), joins = unsigned((long(B) * n * Hq * (D / 4) + 255) / 256);
   auto go = [&](auto d, auto* t) {
     constexpr int DD = decltype(d)::value;
     typedef std::remove_pointer_t<decltype(t)> T;
-    blocks_attention_kernel<DD, T, W><<<grid, W * kWave, 0, s>>>(p);
+    if (pl.waves == 4) blocks_attention_kernel<DD, T, 4><<<grid, 4 * kWave, 0, s>>>(p);
+    else blocks_attention_kernel<DD, T, 8><<<grid, 8 * kWave, 0, s>>>(p);
     if (p.splits > 1) blocks_join_kernel<DD, T><<<joins, 256, 0, s>>>(p);
   };
   auto by_dim = [&](auto* t) {
