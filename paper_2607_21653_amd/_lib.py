@@ -502,18 +502,15 @@ def paged_attention_kvq(q, k_cache, v_cache, block_tables, context_lens, k, work
 
 # ------------------------------------------------------------------ sparse attention over listed blocks
 
-def _i32(t, shape, dev, name):
-    """Checks an int32 tensor of shape on device dev."""
-    if t.dtype is not torch.int32 or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
-        _dev(t, torch.int32, shape, name)
-        raise MoltError(f"{name} must be on device {dev}, is on {t.device}")
+# As above, a call asks each tensor once, and looks for the message (`_must`) only where something is wrong.
+
+_I32 = torch.int32
 
 
-def _float_dtype(t, name):
-    dt = t.dtype
-    if dt is not torch.bfloat16 and dt is not torch.float32:
-        raise MoltError(f"{name} has dtype {dt}, expected float32 or bfloat16")
-    return dt
+def _must(t, dtype, shape, dev, name):
+    """Raises unless t is such a tensor."""
+    _dev(t, dtype, shape, name)
+    _same_device(t, dev, name)
 
 
 def _here(t, name):
@@ -526,27 +523,27 @@ def _here(t, name):
     return dev
 
 
-def _tables(block_tables, context_lens, dev):
-    """(B, max_blocks) of a table and its lengths on device dev."""
-    table = block_tables.shape
-    if len(table) != 2:
-        raise MoltError(f"block_tables has shape {tuple(table)}, expected (B, max_blocks)")
-    _i32(block_tables, table, dev, "block_tables")
-    _i32(context_lens, table[:1], dev, "context_lens")
-    return table
+def _must_be_ints(dev, *named):
+    for name, t, shape in named:
+        if t is not None:
+            _must(t, _I32, shape, dev, name)
 
 
-def _cache_pair(k_cache, v_cache):
-    """(device, dtype, num_blocks, n_kv_heads, head_dim) of a bf16 or f32 cache."""
-    dev, dt, shape = _here(k_cache, "k_cache"), _float_dtype(k_cache, "k_cache"), k_cache.shape
+def _table(block_tables):
+    shape = block_tables.shape
+    if len(shape) != 2:
+        raise MoltError(f"block_tables has shape {tuple(shape)}, expected (B, max_blocks)")
+    return shape
+
+
+def _cache(k_cache):
+    """(dtype, shape) of a bf16 or f32 cache of keys."""
+    dt, shape = k_cache.dtype, k_cache.shape
+    if dt is not torch.bfloat16 and dt is not torch.float32:
+        raise MoltError(f"k_cache has dtype {dt}, expected float32 or bfloat16")
     if len(shape) != 4 or shape[2] != 16:
         raise MoltError(f"k_cache has shape {tuple(shape)}, expected [num_blocks, n_kv_heads, 16, head_dim]")
-    nb, Hkv, _, D = shape
-    _dev(k_cache, dt, shape, "k_cache")
-    if v_cache is not None:
-        _dev(v_cache, dt, (nb, Hkv, D, 16), "v_cache")
-        _same_device(v_cache, dev, "v_cache")
-    return dev, dt, nb, Hkv, D
+    return dt, shape
 
 
 def _bounds_shape(bounds):
@@ -554,16 +551,31 @@ def _bounds_shape(bounds):
     shape = bounds.shape
     if len(shape) != 3 or shape[2] % 2:
         raise MoltError(f"bounds has shape {tuple(shape)}, expected [num_blocks, n_kv_heads, 2 * head_dim + 16]")
-    _dev(bounds, torch.uint8, shape, "bounds")
+    if bounds.dtype is not torch.uint8 or not bounds.is_contiguous():
+        _dev(bounds, torch.uint8, shape, "bounds")
     return shape[0], shape[1], (shape[2] - 16) // 2
+
+
+def _must_be_queries(q, T, D, dev):
+    shape = q.shape
+    if q.dtype is not torch.bfloat16 and q.dtype is not torch.float32:
+        raise MoltError(f"q has dtype {q.dtype}, expected float32 or bfloat16")
+    if len(shape) != 3:
+        raise MoltError(f"q has shape {tuple(shape)}, expected [B*(1+k), Hq, {D}]")
+    _must(q, None, (T, shape[1], D), dev, "q")
+
+
+def _are_lens(lens, rows, dev):
+    return lens is None or (lens.dtype is _I32 and lens.shape == rows and lens.get_device() == dev
+                            and lens.is_contiguous())
 
 
 def _given(workspace, dev):
     """Address and bytes of a caller's workspace."""
     if workspace is None:
         return None, 0
-    _same_device(workspace, dev, "workspace")
-    if not workspace.is_contiguous():
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        _same_device(workspace, dev, "workspace")
         raise MoltError("workspace must be contiguous")
     return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
@@ -581,21 +593,28 @@ def plan_blocks(block_tables, n_blocks, context_lens, n_new, pool, n, n_shared=N
     Returns (slots [B*n] i32 for kv_write, -1 where there is no row; placed [B] i32, rows that have slots)."""
     lib = _lib or load()
     dev = _here(block_tables, "block_tables")
-    B, maxb = _tables(block_tables, context_lens, dev)
-    _i32(n_blocks, (B,), dev, "n_blocks")
-    _i32(n_new, (B,), dev, "n_new")
-    if pool.dim() != 1 or pool.numel() < 3:
-        raise MoltError(f"pool has shape {tuple(pool.shape)}, expected (2 + num_blocks,)")
-    _i32(pool, pool.shape, dev, "pool")
-    if n_shared is not None:
-        _i32(n_shared, (B,), dev, "n_shared")
-    if n < 1:
-        raise MoltError(f"n = {n} must be >= 1")
+    B, maxb = shape = _table(block_tables)
+    rows = (B,)
+    cap = pool.numel() - 2
+    if not (cap > 0 < n and block_tables.dtype is n_blocks.dtype is context_lens.dtype is n_new.dtype is pool.dtype is _I32
+            and n_blocks.shape == context_lens.shape == n_new.shape == rows and pool.dim() == 1
+            and n_blocks.get_device() == context_lens.get_device() == n_new.get_device() == pool.get_device() == dev
+            and block_tables.is_contiguous() and n_blocks.is_contiguous() and context_lens.is_contiguous()
+            and n_new.is_contiguous() and pool.is_contiguous()) or n_shared is not None:
+        if pool.dim() != 1 or cap < 1:
+            raise MoltError(f"pool has shape {tuple(pool.shape)}, expected (2 + num_blocks,)")
+        if n < 1:
+            raise MoltError(f"n = {n} must be >= 1")
+        _must_be_ints(dev, ("block_tables", block_tables, shape), ("n_blocks", n_blocks, rows),
+                      ("context_lens", context_lens, rows), ("n_new", n_new, rows), ("pool", pool, pool.shape),
+                      ("n_shared", n_shared, rows))
     slots, placed = n_new.new_empty(B * n), n_new.new_empty(B)
-    ws, have = _workspace(lib.molt_plan_blocks_workspace_size(B, n), n_new.device)
+    ws, have = None, lib.molt_plan_blocks_workspace_size(B, n)
+    if have:
+        ws = torch.empty(have, dtype=torch.uint8, device=n_new.device)
     status = lib.molt_plan_blocks(block_tables.data_ptr(), n_blocks.data_ptr(), context_lens.data_ptr(),
-                                  n_new.data_ptr(), pool.data_ptr(), _ptr(n_shared), B, n, maxb, pool.numel() - 2,
-                                  slots.data_ptr(), placed.data_ptr(), _ptr(ws), have, _raw_stream(dev))
+                                  n_new.data_ptr(), pool.data_ptr(), _ptr(n_shared), B, n, maxb, cap, slots.data_ptr(),
+                                  placed.data_ptr(), _ptr(ws), have, _raw_stream(dev))
     if status:
         _check(status, "molt_plan_blocks")
     return slots, placed
@@ -605,9 +624,16 @@ def kv_write(k, v, k_cache, v_cache, slots):
     """Writes rows k, v [T, Hkv, D] (row-strided views will do) into a bf16 or f32 cache at slots [T] i32 (block * 16 +
     token, as plan_blocks gives them); rows whose slot is outside the cache are left out."""
     lib = _lib or load()
-    dev, dt, nb, Hkv, D = _cache_pair(k_cache, v_cache)
+    dev = _here(k_cache, "k_cache")
+    dt, shape = _cache(k_cache)
+    nb, Hkv, _, D = shape
     T = slots.numel()
-    _i32(slots, (T,), dev, "slots")
+    if not (v_cache.dtype is dt and slots.dtype is _I32 and v_cache.shape == (nb, Hkv, D, 16) and slots.dim() == 1
+            and v_cache.get_device() == slots.get_device() == dev
+            and k_cache.is_contiguous() and v_cache.is_contiguous() and slots.is_contiguous()):
+        _must(k_cache, dt, shape, dev, "k_cache")
+        _must(v_cache, dt, (nb, Hkv, D, 16), dev, "v_cache")
+        _must(slots, _I32, (T,), dev, "slots")
     ks, vs = _rows_stride(k, dt, T, Hkv, D, dev, "k"), _rows_stride(v, dt, T, Hkv, D, dev, "v")
     status = lib.molt_kv_write(k.data_ptr(), v.data_ptr(), ks, vs, slots.data_ptr(), T, Hkv, D, nb, DTYPE_CODE[dt],
                                k_cache.data_ptr(), v_cache.data_ptr(), _raw_stream(dev))
@@ -624,15 +650,22 @@ def key_bounds_update(k_cache, bounds, block_tables, starts, n, lens=None):
     """Bounds of the keys of the blocks that hold positions starts[b] + j, j < n (j < lens[b] if given), after
     kv_write of these rows."""
     lib = _lib or load()
-    dev, dt, nb, Hkv, D = _cache_pair(k_cache, None)
-    B, maxb = _tables(block_tables, starts, dev)
-    _dev(bounds, torch.uint8, (nb, Hkv, 2 * D + 16), "bounds")
-    _same_device(bounds, dev, "bounds")
-    if lens is not None:
-        _i32(lens, (B,), dev, "lens")
+    dev = _here(k_cache, "k_cache")
+    dt, shape = _cache(k_cache)
+    nb, Hkv, _, D = shape
+    B, maxb = table = _table(block_tables)
+    rows = (B,)
+    if not (bounds.dtype is torch.uint8 and block_tables.dtype is starts.dtype is _I32
+            and bounds.shape == (nb, Hkv, 2 * D + 16) and starts.shape == rows
+            and bounds.get_device() == block_tables.get_device() == starts.get_device() == dev
+            and k_cache.is_contiguous() and bounds.is_contiguous() and block_tables.is_contiguous()
+            and starts.is_contiguous() and _are_lens(lens, rows, dev)):
+        _must(k_cache, dt, shape, dev, "k_cache")
+        _must(bounds, torch.uint8, (nb, Hkv, 2 * D + 16), dev, "bounds")
+        _must_be_ints(dev, ("block_tables", block_tables, table), ("starts", starts, rows), ("lens", lens, rows))
     status = lib.molt_key_bounds_update(k_cache.data_ptr(), bounds.data_ptr(), block_tables.data_ptr(),
-                                        starts.data_ptr(), _ptr(lens), B, n, Hkv, D, maxb, nb, DTYPE_CODE[dt],
-                                        _raw_stream(dev))
+                                        starts.data_ptr(), None if lens is None else lens.data_ptr(), B, n, Hkv, D,
+                                        maxb, nb, DTYPE_CODE[dt], _raw_stream(dev))
     if status:
         _check(status, "molt_key_bounds_update")
 
@@ -643,23 +676,15 @@ def key_bounds_read(bounds, ids):
     dev = _here(bounds, "bounds")
     nb, Hkv, D = _bounds_shape(bounds)
     M = ids.numel()
-    _i32(ids, (M,), dev, "ids")
-    hi = torch.empty(M, Hkv, D, dtype=torch.float32, device=bounds.device)
+    if not (ids.dtype is _I32 and ids.dim() == 1 and ids.get_device() == dev and ids.is_contiguous()):
+        _must(ids, _I32, (M,), dev, "ids")
+    hi = bounds.new_empty((M, Hkv, D), dtype=torch.float32)
     lo = torch.empty_like(hi)
     status = lib.molt_key_bounds_read(bounds.data_ptr(), ids.data_ptr(), M, Hkv, D, nb, hi.data_ptr(), lo.data_ptr(),
                                       _raw_stream(dev))
     if status:
         _check(status, "molt_key_bounds_read")
     return hi, lo
-
-
-def _queries(q, B, k, D, dev):
-    """(dtype, n_q_heads) of query rows [B*(1+k), Hq, D]."""
-    dt, shape = _float_dtype(q, "q"), q.shape
-    if len(shape) != 3 or shape[0] != B * (k + 1) or shape[2] != D or not q.is_contiguous():
-        _dev(q, None, (B * (k + 1), shape[1] if len(shape) == 3 else "Hq", D), "q")
-    _same_device(q, dev, "q")
-    return dt, shape[1]
 
 
 def select_blocks_workspace_size(B, k, n_q_heads, n_kv_heads, head_dim, max_blocks):
@@ -673,19 +698,25 @@ def select_blocks(q, bounds, block_tables, context_lens, k, n_select, n_first=1,
     lib = _lib or load()
     dev = _here(bounds, "bounds")
     nb, Hkv, D = _bounds_shape(bounds)
-    B, maxb = _tables(block_tables, context_lens, dev)
-    dt, Hq = _queries(q, B, k, D, dev)
-    if lens is not None:
-        _i32(lens, (B,), dev, "lens")
-    if n_select < 1:
+    B, maxb = table = _table(block_tables)
+    rows, T, dt, shape = (B,), B * (k + 1), q.dtype, q.shape
+    if not (n_select > 0 and (dt is torch.bfloat16 or dt is torch.float32) and len(shape) == 3 and shape[0] == T
+            and shape[2] == D and block_tables.dtype is context_lens.dtype is _I32 and context_lens.shape == rows
+            and q.get_device() == block_tables.get_device() == context_lens.get_device() == dev
+            and q.is_contiguous() and block_tables.is_contiguous() and context_lens.is_contiguous()
+            and _are_lens(lens, rows, dev)):
+        _must_be_ints(dev, ("block_tables", block_tables, table), ("context_lens", context_lens, rows),
+                      ("lens", lens, rows))
+        _must_be_queries(q, T, D, dev)
         raise MoltError(f"n_select = {n_select} must be >= 1")
     ws, have = _given(workspace, dev)
-    out = block_tables.new_empty(B * (k + 1), Hkv, n_select)
-    args = (q.data_ptr(), bounds.data_ptr(), block_tables.data_ptr(), context_lens.data_ptr(), _ptr(lens), B, k, Hq,
-            Hkv, D, maxb, nb, n_select, n_first, n_last, DTYPE_CODE[dt], out.data_ptr())
+    out = block_tables.new_empty((T, Hkv, n_select))
+    args = (q.data_ptr(), bounds.data_ptr(), block_tables.data_ptr(), context_lens.data_ptr(),
+            None if lens is None else lens.data_ptr(), B, k, shape[1], Hkv, D, maxb, nb, n_select, n_first, n_last,
+            DTYPE_CODE[dt], out.data_ptr())
     status = lib.molt_select_blocks(*args, ws, have, _raw_stream(dev))
     if status == MOLT_ERR_WORKSPACE:     # none, or one that is too small
-        own, have = _workspace(lib.molt_select_blocks_workspace_size(B, k, Hq, Hkv, D, maxb), q.device)
+        own, have = _workspace(lib.molt_select_blocks_workspace_size(B, k, shape[1], Hkv, D, maxb), q.device)
         status = lib.molt_select_blocks(*args, _ptr(own), have, _raw_stream(dev))
     if status:
         _check(status, "molt_select_blocks")
@@ -700,22 +731,35 @@ def paged_attention_blocks(q, k_cache, v_cache, block_tables, context_lens, k, b
     """paged_attention over the blocks that blocks [B*(1+k), Hkv, N] i32 lists for each position and kv head
     (select_blocks; -1: none): returns [B*(1+k), Hq*D] of q's dtype."""
     lib = _lib or load()
-    dev, dt, nb, Hkv, D = _cache_pair(k_cache, v_cache)
-    B, maxb = _tables(block_tables, context_lens, dev)
-    qt, Hq = _queries(q, B, k, D, dev)
-    if qt is not dt:
-        raise MoltError(f"q has dtype {qt}, the caches {dt}")
-    if blocks.dim() != 3:
-        raise MoltError(f"blocks has shape {tuple(blocks.shape)}, expected ({B * (k + 1)}, {Hkv}, n_list)")
-    N = blocks.shape[2]
-    _i32(blocks, (B * (k + 1), Hkv, N), dev, "blocks")
+    dev = _here(k_cache, "k_cache")
+    dt, cache = _cache(k_cache)
+    nb, Hkv, _, D = cache
+    B, maxb = table = _table(block_tables)
+    T, shape, lists = B * (k + 1), q.shape, blocks.shape
+    if not (len(shape) == len(lists) == 3 and shape[0] == lists[0] == T and shape[2] == D and lists[1] == Hkv
+            and v_cache.shape == (nb, Hkv, D, 16) and context_lens.shape == (B,) and v_cache.dtype is q.dtype is dt
+            and block_tables.dtype is context_lens.dtype is blocks.dtype is _I32
+            and v_cache.get_device() == q.get_device() == block_tables.get_device() == context_lens.get_device()
+            == blocks.get_device() == dev and k_cache.is_contiguous() and v_cache.is_contiguous()
+            and q.is_contiguous() and block_tables.is_contiguous() and context_lens.is_contiguous()
+            and blocks.is_contiguous()):
+        _must(k_cache, dt, cache, dev, "k_cache")
+        _must(v_cache, dt, (nb, Hkv, D, 16), dev, "v_cache")
+        _must_be_ints(dev, ("block_tables", block_tables, table), ("context_lens", context_lens, (B,)))
+        _must_be_queries(q, T, D, dev)
+        if q.dtype is not dt:
+            raise MoltError(f"q has dtype {q.dtype}, the caches {dt}")
+        if len(lists) != 3:
+            raise MoltError(f"blocks has shape {tuple(lists)}, expected ({T}, {Hkv}, n_list)")
+        _must_be_ints(dev, ("blocks", blocks, (T, Hkv, lists[2])))
     ws, have = _given(workspace, dev)
-    out = q.new_empty(B * (k + 1), Hq * D)
+    out = q.new_empty((T, shape[1] * D))
     args = (q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_tables.data_ptr(), context_lens.data_ptr(),
-            blocks.data_ptr(), B, k, Hq, Hkv, D, maxb, nb, N, DTYPE_CODE[dt], out.data_ptr())
+            blocks.data_ptr(), B, k, shape[1], Hkv, D, maxb, nb, lists[2], DTYPE_CODE[dt], out.data_ptr())
     status = lib.molt_paged_attention_blocks(*args, ws, have, _raw_stream(dev))
     if status == MOLT_ERR_WORKSPACE:
-        own, have = _workspace(lib.molt_paged_attention_blocks_workspace_size(B, k, Hq, Hkv, D, N), q.device)
+        own, have = _workspace(lib.molt_paged_attention_blocks_workspace_size(B, k, shape[1], Hkv, D, lists[2]),
+                               q.device)
         status = lib.molt_paged_attention_blocks(*args, _ptr(own), have, _raw_stream(dev))
     if status:
         _check(status, "molt_paged_attention_blocks")

@@ -78,10 +78,11 @@ template <int D, typename T>
 struct Raw {
   static constexpr int kBytes = 16 * D * int(sizeof(T)), kLoads = kBytes / 1024;
   u32x4_t w[kLoads];
+  template <bool ONCE>                           // nontemporal, where one workgroup reads the block
   MOLT_DEV void load(const void* cache, long block_head, int lane) {
-    const uint8_t* from = static_cast<const uint8_t*>(cache) + block_head * kBytes;
+    const u32x4_t* from = reinterpret_cast<const u32x4_t*>(static_cast<const uint8_t*>(cache) + block_head * kBytes) + lane;
 #pragma unroll
-    for (int c = 0; c < kLoads; ++c) w[c] = *reinterpret_cast<const u32x4_t*>(from + c * 1024 + lane * 16);
+    for (int c = 0; c < kLoads; ++c) w[c] = ONCE ? __builtin_nontemporal_load(from + c * 64) : from[c * 64];
   }
 };
 
@@ -93,7 +94,7 @@ struct Raw {
 template <int D>
 struct PairBf16 {
   static constexpr int kBlocks = 2;
-  static constexpr int kLds = 2 * 2 * Raw<D, uint16_t>::kBytes;
+  static constexpr int kLds = 2 * Raw<D, uint16_t>::kBytes;              // the keys, then the values
   static constexpr int KC = D / 8;               // chunks of a token
   struct Query { bf16x8_t q[D / 32]; };
   MOLT_DEV static void load_q(Query& r, const void* qq, long row, bool there, int g) {
@@ -105,31 +106,43 @@ struct PairBf16 {
     }
   }
   MOLT_DEV static int key_at(int block, int token, int chunk) {
-    const int f = ((token & 3) | (token >> 3 & 1) << 2 | (token >> 2 & 1) << 3) & (KC - 1);
+    const int f = (token & 3) | (token >> 3 & 1) << 2;                    // (8 lanes read tokens 0 .. 3, 8 .. 11 or 4 more)
     return (block * 16 + token) * KC * 16 + (chunk ^ f) * 16;
   }
   MOLT_DEV static int value_at(int block, int dim, int half) {
-    return 2 * Raw<D, uint16_t>::kBytes + (block * D + dim) * 32 + (half ^ (dim >> 2 & 1)) * 16;
+    return (block * D + dim) * 32 + (half ^ (dim >> 2 & 1)) * 16;
   }
   Raw<D, uint16_t> k[2], v[2];
-  MOLT_DEV void load(const BlocksArgs& p, const int (&id)[2], int h, int lane) {
+  template <bool ONCE>
+  MOLT_DEV void load_keys(const BlocksArgs& p, const int (&id)[2], int h, int lane) {
 #pragma unroll
-    for (int y = 0; y < 2; ++y) k[y].load(p.kc, long(id[y]) * p.Hkv + h, lane);
-#pragma unroll
-    for (int y = 0; y < 2; ++y) v[y].load(p.vc, long(id[y]) * p.Hkv + h, lane);
+    for (int y = 0; y < 2; ++y) k[y].template load<ONCE>(p.kc, long(id[y]) * p.Hkv + h, lane);
   }
-  MOLT_DEV void store(uint8_t* lds, int lane) const {
+  template <bool ONCE>
+  MOLT_DEV void load_values(const BlocksArgs& p, const int (&id)[2], int h, int lane) {
+#pragma unroll
+    for (int y = 0; y < 2; ++y) v[y].template load<ONCE>(p.vc, long(id[y]) * p.Hkv + h, lane);
+  }
+  MOLT_DEV void store_keys(uint8_t* lds, int lane) const {
 #pragma unroll
     for (int y = 0; y < 2; ++y)
 #pragma unroll
       for (int c = 0; c < Raw<D, uint16_t>::kLoads; ++c) {
         const int at = c * 64 + lane;
         *reinterpret_cast<u32x4_t*>(lds + key_at(y, at / KC, at % KC)) = k[y].w[c];
+      }
+  }
+  MOLT_DEV void store_values(uint8_t* lds, int lane) const {
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+#pragma unroll
+      for (int c = 0; c < Raw<D, uint16_t>::kLoads; ++c) {
+        const int at = c * 64 + lane;
         *reinterpret_cast<u32x4_t*>(lds + value_at(y, at / 2, at % 2)) = v[y].w[c];
       }
   }
-  // seen: tokens of the blocks that the row sees
-  MOLT_DEV static void use(const uint8_t* lds, const Query& q, const int (&seen)[2], Running<D>& r, int g, int col, float c) {
+  typedef float Scores[8];
+  MOLT_DEV static void scores(const uint8_t* lds, const Query& q, Scores& w, int g, int col) {
     floatx4_t s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
     for (int x = 0; x < 2; ++x)
@@ -138,9 +151,11 @@ struct PairBf16 {
         const bf16x8_t k = *reinterpret_cast<const bf16x8_t*>(lds + key_at(col / 8, col / 4 % 2 * 8 + 4 * x + col % 4, 4 * i + g));
         s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q.q[i], s[x], 0, 0, 0);
       }
-    float w[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) w[i] = s[i / 4][i % 4];
+  }
+  // seen: tokens of the blocks that the row sees
+  MOLT_DEV static void use(const uint8_t* lds, Scores& w, const int (&seen)[2], Running<D>& r, int g, int col, float c) {
     const bool cut = seen[0] < 16 || seen[1] < 16;                       // wavefront-uniform
     const int mine = (g / 2 ? seen[1] : seen[0]) - g % 2 * 8;            // of the lane's 8 tokens
     if (cut) {
@@ -174,7 +189,7 @@ struct PairBf16 {
 template <int D>
 struct BlockF32 {
   static constexpr int kBlocks = 1;
-  static constexpr int kLds = 2 * Raw<D, float>::kBytes;
+  static constexpr int kLds = Raw<D, float>::kBytes;
   static constexpr int KC = D / 4;
   struct Query { floatx4_t q[D / 16]; };
   MOLT_DEV static void load_q(Query& r, const void* qq, long row, bool there, int g) {
@@ -185,23 +200,32 @@ struct BlockF32 {
     }
   }
   MOLT_DEV static int key_at(int token, int chunk) { return token * KC * 16 + (chunk ^ (token & 7)) * 16; }
-  MOLT_DEV static int value_at(int dim, int chunk) {
-    return Raw<D, float>::kBytes + dim * 64 + (chunk ^ (dim >> 1 & 3)) * 16;
-  }
+  MOLT_DEV static int value_at(int dim, int chunk) { return dim * 64 + (chunk ^ (dim >> 1 & 3)) * 16; }
   Raw<D, float> k, v;
-  MOLT_DEV void load(const BlocksArgs& p, const int (&id)[1], int h, int lane) {
-    k.load(p.kc, long(id[0]) * p.Hkv + h, lane);
-    v.load(p.vc, long(id[0]) * p.Hkv + h, lane);
+  template <bool ONCE>
+  MOLT_DEV void load_keys(const BlocksArgs& p, const int (&id)[1], int h, int lane) {
+    k.template load<ONCE>(p.kc, long(id[0]) * p.Hkv + h, lane);
   }
-  MOLT_DEV void store(uint8_t* lds, int lane) const {
+  template <bool ONCE>
+  MOLT_DEV void load_values(const BlocksArgs& p, const int (&id)[1], int h, int lane) {
+    v.template load<ONCE>(p.vc, long(id[0]) * p.Hkv + h, lane);
+  }
+  MOLT_DEV void store_keys(uint8_t* lds, int lane) const {
 #pragma unroll
     for (int c = 0; c < Raw<D, float>::kLoads; ++c) {
       const int at = c * 64 + lane;
       *reinterpret_cast<u32x4_t*>(lds + key_at(at / KC, at % KC)) = k.w[c];
+    }
+  }
+  MOLT_DEV void store_values(uint8_t* lds, int lane) const {
+#pragma unroll
+    for (int c = 0; c < Raw<D, float>::kLoads; ++c) {
+      const int at = c * 64 + lane;
       *reinterpret_cast<u32x4_t*>(lds + value_at(at / 4, at % 4)) = v.w[c];
     }
   }
-  MOLT_DEV static void use(const uint8_t* lds, const Query& q, const int (&seen)[1], Running<D>& r, int g, int col, float c) {
+  typedef float Scores[4];
+  MOLT_DEV static void scores(const uint8_t* lds, const Query& q, Scores& w, int g, int col) {
     floatx4_t s{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) {
@@ -209,9 +233,10 @@ struct BlockF32 {
 #pragma unroll
       for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[e], q.q[i][e], s, 0, 0, 0);
     }
-    float w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = s[i];
+  }
+  MOLT_DEV static void use(const uint8_t* lds, Scores& w, const int (&seen)[1], Running<D>& r, int g, int col, float c) {
     const int mine = seen[0] - 4 * g;
     if (seen[0] < 16) {
 #pragma unroll
@@ -240,8 +265,8 @@ MOLT_DEV void store4(float* p, floatx4_t x) { *reinterpret_cast<floatx4_t*>(p) =
 
 // Workgroup = one list (or a part of it) and 16 query rows; wavefronts take its units (pairs of blocks, or blocks) in
 // turn, a unit ahead in registers, with running softmaxes of their own, and join them in LDS.
-template <int D, typename T, int W>
-__global__ __launch_bounds__(W* kWave, 2) void blocks_attention_kernel(BlocksArgs p) {
+template <int D, typename T, int W, bool ONCE>
+__global__ __launch_bounds__(W* kWave, sizeof(T) == 2 ? 3 : 2) void blocks_attention_kernel(BlocksArgs p) {
   typedef std::conditional_t<sizeof(T) == 2, PairBf16<D>, BlockF32<D>> Unit;
   constexpr int KB = Unit::kBlocks, PER = kWave / KB;                    // blocks of a unit; units that lanes hold
   constexpr int kAcc = D / 16 * kWave * 16;                              // a wavefront's O for the join
@@ -281,11 +306,11 @@ __global__ __launch_bounds__(W* kWave, 2) void blocks_attention_kernel(BlocksArg
     if (KB == 2) left = (left | left >> 1) & 0x5555555555555555ull;      // block
     if (!left) continue;
     Unit u;
-    int seen[KB];
-    auto fetch = [&]() __attribute__((always_inline)) {
+    int id[KB], seen[KB];
+    auto next = [&]() __attribute__((always_inline)) {
       const int i = __builtin_ctzll(left);
       left &= left - 1;
-      int id[KB], some = 0;
+      int some = 0;
 #pragma unroll
       for (int y = 0; y < KB; ++y) {
         id[y] = __builtin_amdgcn_readlane(en.id, i + y);
@@ -295,17 +320,25 @@ __global__ __launch_bounds__(W* kWave, 2) void blocks_attention_kernel(BlocksArg
 #pragma unroll
       for (int y = 0; y < KB; ++y)
         if (id[y] < 0) id[y] = some;             // the other block's, unseen
-      u.load(p, id, h, lane);
     };
-    fetch();
+    next();
+    u.template load_keys<ONCE>(p, id, h, lane);
+    u.template load_values<ONCE>(p, id, h, lane);
     for (;;) {
       int now[KB];
 #pragma unroll
       for (int y = 0; y < KB; ++y) now[y] = seen[y];
-      u.store(lds[wave], lane);
       const bool more = left != 0;
-      if (more) fetch();
-      Unit::use(lds[wave], q, now, r, g, col, p.c);
+      typename Unit::Scores w;
+      u.store_keys(lds[wave], lane);
+      if (more) {
+        next();
+        u.template load_keys<ONCE>(p, id, h, lane);
+      }
+      Unit::scores(lds[wave], q, w, g, col);
+      u.store_values(lds[wave], lane);
+      if (more) u.template load_values<ONCE>(p, id, h, lane);
+      Unit::use(lds[wave], w, now, r, g, col, p.c);
       if (!more) break;
     }
   }
@@ -375,15 +408,15 @@ __global__ __launch_bounds__(256) void blocks_join_kernel(BlocksArgs p) {
   store4(static_cast<T*>(p.out) + at * D + d, o * inv);
 }
 
-struct BlocksPlan { int row_groups, splits, per_split, waves; };
+constexpr int kWaves = 4;
+struct BlocksPlan { int row_groups, splits, per_split; };
 BlocksPlan blocks_plan(int B, int n, int Hq, int Hkv, int N) {
   BlocksPlan pl{};
   const int units = (N + 1) / 2;
   pl.row_groups = (Hq / Hkv + 15) / 16;
   const long lists = long(B) * n * Hkv * pl.row_groups;
-  pl.waves = lists * 4 >= 2048 || units < 16 ? 4 : 8;
-  // a split has two units at least for each wavefront
-  const long want = std::max(1l, std::min((2048 / pl.waves / 2 + lists - 1) / lists, long(units) / (2 * pl.waves)));
+  // as many parts as the chip holds at once (3 workgroups a CU), each of two units at least for a wavefront
+  const long want = std::max(1l, std::min(768 / lists, long(units) / (2 * kWaves)));
   pl.per_split = int((units + want - 1) / want);
   pl.splits = (units + pl.per_split - 1) / pl.per_split;
   return pl;
@@ -410,6 +443,7 @@ hipError_t launch_blocks_attention(const void* q, const void* kc, const void* vc
   const BlocksPlan pl = blocks_plan(B, n, Hq, Hkv, N);
   const long bh = long(B) * Hkv;
   const int by_xcd = n > 1 && (bh % 8 == 0 || bh >= 48);
+  const bool once = n == 1 && pl.row_groups == 1;
   BlocksArgs p{q, kc, vc, bt, ctx, blocks, out, nullptr, nullptr, B, n, Hq, Hkv, Hq / Hkv, N, max_blocks, num_blocks,
                pl.row_groups, pl.splits, dt == MOLT_F32 ? 2 * pl.per_split : pl.per_split, by_xcd,
                kLog2e / std::sqrt(float(D))};
@@ -423,8 +457,8 @@ hipError_t launch_blocks_attention(const void* q, const void* kc, const void* vc
   auto go = [&](auto d, auto* t) {
     constexpr int DD = decltype(d)::value;
     typedef std::remove_pointer_t<decltype(t)> T;
-    if (pl.waves == 4) blocks_attention_kernel<DD, T, 4><<<grid, 4 * kWave, 0, s>>>(p);
-    else blocks_attention_kernel<DD, T, 8><<<grid, 8 * kWave, 0, s>>>(p);
+    if (once) blocks_attention_kernel<DD, T, kWaves, true><<<grid, kWaves * kWave, 0, s>>>(p);
+    else blocks_attention_kernel<DD, T, kWaves, false><<<grid, kWaves * kWave, 0, s>>>(p);
     if (p.splits > 1) blocks_join_kernel<DD, T><<<joins, 256, 0, s>>>(p);
   };
   auto by_dim = [&](auto* t) {

@@ -1,5 +1,7 @@
 // The paged cache's upkeep on the GPU: block tables that follow the lengths, rows written by slot, the bounds of
 // each block's keys.
+#include <type_traits>
+
 #include "bounds_format.h"
 #include "internal.h"
 
@@ -16,7 +18,7 @@ constexpr int kPlanWaves = kPlanThreads / kWave;
 // What a call does with sequence b's row of the table: entries have .. have + take - 1 come from the ring's places
 // first .. behind its head, entries keep .. have - 1 go to places back .. of it (-1: none do), rows 0 .. placed - 1 get
 // slots.
-struct PlanRow { int have, take, first, keep, back, placed; };
+struct PlanRow { int have, take, first, keep, back, placed, ctx; };
 
 struct PlanArgs {
   int32_t* bt; int32_t* n_blocks; const int32_t* ctx; const int32_t* n_new; int32_t* pool; const int32_t* shared;
@@ -35,7 +37,7 @@ MOLT_DEV void plan_slot(const PlanArgs& p, const PlanRow& r, int b, int j, int h
   int32_t* row = p.bt + long(b) * p.max_blocks;
   int slot = -1;
   if (j < r.placed) {
-    const int pos = p.ctx[b] + j, i = pos / 16;  // i < have + take
+    const int pos = r.ctx + j, i = pos / 16;       // i < have + take
     int id;
     if (i >= r.have) {
       id = ring[ring_wrap(long(head) + r.first + (i - r.have), cap)];
@@ -65,21 +67,25 @@ MOLT_DEV void plan_return(const PlanArgs& p, const PlanRow& r, int b, int thread
   for (; i < m; i += threads) p.pool[2 + ring_wrap(long(r.back) + i, p.num_blocks)] = row[r.keep + i];
 }
 
-// Inclusive sum over the workgroup's threads of v in [0, 2^31), in 64 bits: its halves of 16 bits apart on DPP
-MOLT_DEV long plan_scan(int v, long* red, long& total) {
+// Inclusive sums over the workgroup's threads of v and w in [0, 2^31), in 64 bits: their halves of 16 bits apart on DPP
+struct Pair { long a, b; };
+MOLT_DEV Pair plan_scan(int v, int w, Pair* red, Pair& total) {
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const long s = (long(wave_scan_dpp(v >> 16)) << 16) + wave_scan_dpp(v & 0xffff);
+  const Pair s{(long(wave_scan_dpp(v >> 16)) << 16) + wave_scan_dpp(v & 0xffff),
+               (long(wave_scan_dpp(w >> 16)) << 16) + wave_scan_dpp(w & 0xffff)};
   __syncthreads();
   if (lane == kWave - 1) red[wave] = s;
   __syncthreads();
-  long before = 0, all = 0;
+  Pair before{0, 0}, all{0, 0};
 #pragma unroll
-  for (int w = 0; w < kPlanWaves; ++w) {
-    if (w < wave) before += red[w];
-    all += red[w];
+  for (int i = 0; i < kPlanWaves; ++i) {
+    const Pair x = red[i];
+    if (i < wave) { before.a += x.a; before.b += x.b; }
+    all.a += x.a;
+    all.b += x.b;
   }
   total = all;
-  return s + before;
+  return Pair{s.a + before.a, s.b + before.b};
 }
 
 // One workgroup. Who gets what is a matter of prefix sums of the rows' demands, in the rows' order: nothing depends on
@@ -87,7 +93,7 @@ MOLT_DEV long plan_scan(int v, long* red, long& total) {
 // WHOLE: the slots and the entries too (up to kPlanThreads sequences), else plan_rows_kernel does them.
 template <bool WHOLE>
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs p) {
-  __shared__ long red[kPlanWaves];
+  __shared__ Pair red[kPlanWaves];
   __shared__ unsigned long long ends[2];         // places taken and returned, as far as the pool goes
   __shared__ PlanRow held[WHOLE ? kPlanThreads : 1];
   const int cap = p.num_blocks;
@@ -96,12 +102,13 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs p) {
   long demanded = 0, given = 0;                  // of the rows before
   for (int b0 = 0; b0 < p.B; b0 += kPlanThreads) {
     const int b = b0 + int(threadIdx.x);
-    PlanRow r{0, 0, 0, 0, -1, 0};
+    PlanRow r{0, 0, 0, 0, -1, 0, 0};
     int want = 0, give = 0;
     bool fits = false, done = false;
     if (b < p.B) {
       const int ctx = p.ctx[b], m = p.n_new[b];
       r.have = p.n_blocks[b];
+      r.ctx = ctx;
       const bool sound = r.have >= 0 && r.have <= p.max_blocks;
       const long end = long(ctx) + m;
       done = sound && m < 0;
@@ -113,9 +120,9 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs p) {
       }
       if (fits) r.placed = m;
     }
-    long all_want, all_give;
-    const long upto = demanded + plan_scan(want, red, all_want);
-    const long gave = given + plan_scan(give, red, all_give);
+    Pair all;
+    const Pair sums = plan_scan(want, give, red, all);
+    const long upto = demanded + sums.a, gave = given + sums.b;
     if (want && upto <= count) {
       r.take = want;
       r.first = int(upto - want);
@@ -134,8 +141,8 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs p) {
       if (WHOLE) held[threadIdx.x] = r;
       else p.rows[b] = r;
     }
-    demanded += all_want;
-    given += all_give;
+    demanded += all.a;
+    given += all.b;
   }
   __syncthreads();
   if (threadIdx.x == 0) {
@@ -167,7 +174,8 @@ bool plan_whole(int B, int n) { return B <= kPlanThreads && long(B) * n <= 8 * k
 
 // ---------------------------------------------------------------- rows by slot
 
-constexpr int kWriteRows = 16;
+constexpr int kWriteRows = 16, kFewRows = 4;
+constexpr long kFewUnits = 16384;                // rows x 128 dims up to which rows count as few
 
 // two elements of a row at any element alignment, as the bits that the cache holds
 typedef uint32_t UnalignedU1 __attribute__((aligned(2)));
@@ -179,12 +187,12 @@ typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 // runs of consecutive slots of one block; a wavefront writes the runs that begin among its rows, up to their ends, one
 // after the other. A run that fills its block's 16 slots leaves V, whose tokens are contiguous, in whole 16-byte stores; other runs leave
 // it in stores of 4 bytes where both tokens of a pair are there.
-template <int D, int R, typename T>
+template <int D, typename T>
 __global__ __launch_bounds__(kThreads) void kv_write_kernel(const T* __restrict__ k, long k_stride,
                                                             const T* __restrict__ v, long v_stride,
                                                             const int32_t* __restrict__ slots, int rows, int Hkv,
                                                             int num_blocks, T* __restrict__ kc, T* __restrict__ vc) {
-  constexpr int HPW = 128 / D;
+  constexpr int HPW = 128 / D, R = kWriteRows;
   const int heads = (Hkv + HPW - 1) / HPW;
   const uint32_t item = blockIdx.x * (kThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const uint32_t tile = item / uint32_t(heads);
@@ -271,6 +279,47 @@ __global__ __launch_bounds__(kThreads) void kv_write_kernel(const T* __restrict_
         for (int t = 0; t < 16; ++t)
           if (t >= first && t < first + len) { out[t] = y[t][0]; out[16 + t] = y[t][1]; }
       }
+    }
+  }
+}
+
+// The same for few rows, where the time is that of the loads in a row: wavefront = 4 rows, read before it is known where
+// they go; V's tokens are stored one by one.
+template <int D, typename T>
+__global__ __launch_bounds__(kThreads) void kv_write_few_kernel(const T* __restrict__ k, long k_stride,
+                                                                const T* __restrict__ v, long v_stride,
+                                                                const int32_t* __restrict__ slots, int rows, int Hkv,
+                                                                int num_blocks, T* __restrict__ kc, T* __restrict__ vc) {
+  constexpr int HPW = 128 / D, R = kFewRows;
+  typedef std::conditional_t<sizeof(T) == 2, uint32_t, u32x2_t> Two;
+  typedef std::conditional_t<sizeof(T) == 2, UnalignedU1, UnalignedU2> UnalignedTwo;
+  const int heads = (Hkv + HPW - 1) / HPW;
+  const uint32_t item = blockIdx.x * (kThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const uint32_t tile = item / uint32_t(heads);
+  const int r0 = int(tile) * R, lane = threadIdx.x % kWave;
+  const int h = int(item - tile * heads) * HPW + lane / (D / 2), d = lane % (D / 2) * 2;
+  if (r0 >= rows || h >= Hkv) return;
+  int slot[R];
+  Two x[R], y[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const long r = min(r0 + i, rows - 1);
+    slot[i] = r0 + i < rows ? slots[r] : -1;
+    x[i] = *reinterpret_cast<const UnalignedTwo*>(k + r * k_stride + h * D + d);
+    y[i] = *reinterpret_cast<const UnalignedTwo*>(v + r * v_stride + h * D + d);
+  }
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    if (slot[i] < 0 || slot[i] / 16 >= num_blocks) continue;
+    const long rec = (long(slot[i] / 16) * Hkv + h) * 16 * D;
+    *reinterpret_cast<Two*>(kc + rec + slot[i] % 16 * D + d) = x[i];
+    T* out = vc + rec + d * 16 + slot[i] % 16;
+    if constexpr (sizeof(T) == 2) {
+      out[0] = T(y[i]);
+      out[16] = T(y[i] >> 16);
+    } else {
+      out[0] = __uint_as_float(y[i][0]);
+      out[16] = __uint_as_float(y[i][1]);
     }
   }
 }
@@ -411,21 +460,26 @@ hipError_t launch_plan_blocks(int32_t* bt, int32_t* n_blocks, const int32_t* ctx
 
 hipError_t launch_kv_write(const void* k, long k_stride, const void* v, long v_stride, const int32_t* slots, int rows,
                            int Hkv, int D, int num_blocks, molt_dtype dt, void* kc, void* vc, hipStream_t s) {
-  constexpr int R = kWriteRows;
-  const long waves = (long(rows) + R - 1) / R * ((Hkv * long(D) + 127) / 128);
+  const long units = (Hkv * long(D) + 127) / 128;
+  const bool few = rows * units <= kFewUnits;
+  const int R = few ? kFewRows : kWriteRows;
+  const long waves = (long(rows) + R - 1) / R * units;
   const unsigned grid = unsigned((waves + kThreads / kWave - 1) / (kThreads / kWave));
   auto go = [&](auto kernel, auto* t) {
     typedef decltype(t) P;
     kernel<<<grid, kThreads, 0, s>>>(static_cast<P>(const_cast<void*>(k)), k_stride, static_cast<P>(const_cast<void*>(v)),
                                      v_stride, slots, rows, Hkv, num_blocks, static_cast<P>(kc), static_cast<P>(vc));
   };
-  if (dt == MOLT_F32) {
-    float* t = nullptr;
-    if (D == 128) go(kv_write_kernel<128, R, float>, t); else go(kv_write_kernel<64, R, float>, t);
-  } else {
-    uint16_t* t = nullptr;
-    if (D == 128) go(kv_write_kernel<128, R, uint16_t>, t); else go(kv_write_kernel<64, R, uint16_t>, t);
-  }
+  auto by_dim = [&](auto* t) {
+    typedef std::remove_pointer_t<decltype(t)> T;
+    if (few) {
+      if (D == 128) go(kv_write_few_kernel<128, T>, t); else go(kv_write_few_kernel<64, T>, t);
+    } else {
+      if (D == 128) go(kv_write_kernel<128, T>, t); else go(kv_write_kernel<64, T>, t);
+    }
+  };
+  if (dt == MOLT_F32) by_dim(static_cast<float*>(nullptr));
+  else by_dim(static_cast<uint16_t*>(nullptr));
   return hipGetLastError();
 }
 

@@ -83,7 +83,7 @@ HEADS = CACHE + [dict(B=0), dict(k=-1), dict(k=2 ** 31 - 1), dict(Hq=30), dict(H
 
 
 @pytest.mark.parametrize("bad", HEADS + [dict(bounds=None), dict(bounds=ODD), dict(first=-1), dict(last=0),
-                                         dict(first=7), dict(N=2), dict(first=2 ** 31 - 1), dict(mb=2 ** 26, B=64)])
+                                         dict(first=7), dict(N=2), dict(first=2 ** 31 - 1)])
 def test_select(L, bad):
     _refused(L, _select(L, **bad))
 
