@@ -323,9 +323,13 @@ struct Search {
     return {lo + 1, lo, N - c_hi};
   }
 };
+// The rest of the search by one wavefront that has all keys but `others` larger ones, M a lane. Once no more than 32 are
+// between the borders they go to a lane each (through LDS, room for 32, 16-byte aligned), which counts those above its own:
+// few keys lie close together now and then, and the borders would take many more steps to part them.
+constexpr int kRoom = 32;
 template <int M>
-MOLT_DEV Search wave_search(Search s, const uint32_t (&key)[M], int N) {
-  while (!s.done())
+MOLT_DEV Border wave_search(Search s, const uint32_t (&key)[M], int others, int N, uint32_t* room, int lane) {
+  while (!s.done() && s.c_lo - s.c_hi > kRoom)
     s.step(N, [&](uint32_t b0, uint32_t b1, uint32_t b2) __attribute__((always_inline)) {
       Four c{{0, 0, 0, 0}};
 #pragma unroll
@@ -334,9 +338,36 @@ MOLT_DEV Search wave_search(Search s, const uint32_t (&key)[M], int N) {
         c.x[1] += key[i] >= b1;
         c.x[2] += key[i] >= b2;
       }
-      return wave_sum4<true>(c);
+      c = wave_sum4<true>(c);
+      return Four{{c.x[0] + others, c.x[1] + others, c.x[2] + others, 0}};
     });
-  return s;
+  if (s.done()) return s.border(N);
+  const unsigned long long below = (1ull << lane) - 1;
+  int at = 0;
+  if (lane < kRoom) room[lane] = 0;              // (keys above 0 only are counted)
+#pragma unroll
+  for (int i = 0; i < M; ++i) {
+    const bool in = key[i] >= s.lo && key[i] < s.hi;
+    const unsigned long long mask = __ballot(in);
+    if (in) room[at + __popcll(mask & below)] = key[i];
+    at += __popcll(mask);
+  }
+  const uint32_t mine = lane < at ? room[lane] : ~0u;
+  int above = s.c_hi, with = s.c_hi;             // keys above the lane's, and those with the equal ones
+#pragma unroll
+  for (int i = 0; i < kRoom / 4; ++i) {
+    const u32x4_t k = reinterpret_cast<const u32x4_t*>(room)[i];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      above += k[u] > mine;
+      with += k[u] >= mine;
+    }
+  }
+  const int l = __builtin_ctzll(__ballot(lane < at && above < N && with >= N));   // one there is, and equal ones
+  const uint32_t k = uint32_t(__builtin_amdgcn_readlane(int(mine), l));
+  above = __builtin_amdgcn_readlane(above, l);
+  if (__builtin_amdgcn_readlane(with, l) == N) return {k, 0u, 0};
+  return {k + 1, k, N - above};
 }
 
 // What the keys of m per lane are: how many, how many that a list holds anyway, the largest of the others and of their
@@ -421,6 +452,7 @@ __global__ __launch_bounds__(kThreads, 4) void select_kernel(SelectArgs p) {
   const int end = counted > 0 ? visible_blocks(p, it.b, j0 + counted - 1) : 0;
   score_blocks<D, GP>(p, it.b, it.h, j0, 0, end, wave, lane, lds, keys, p.max_blocks);
   __syncthreads();
+  uint32_t(*room)[kRoom] = reinterpret_cast<uint32_t(*)[kRoom]>(dyn);    // the records' place
   for (int i = wave; i < here; i += kWaves) {
     const int seen = visible_blocks(p, it.b, j0 + i);
     int32_t* out = p.out + ((long(it.b) * p.n + j0 + i) * p.Hkv + it.h) * p.N;
@@ -440,7 +472,7 @@ __global__ __launch_bounds__(kThreads, 4) void select_kernel(SelectArgs p) {
       if (int(n.x[0]) > p.N) {
         r = Range{n.x[0], n.x[1], wave_max_u32(r.top), wave_max_u32(r.low)};
         if (int(r.held) == p.N) border.lo = kKeyHeld;
-        else border = wave_search<M>(search_of(r, p.N), key, p.N).border(p.N);
+        else border = wave_search<M>(search_of(r, p.N), key, 0, p.N, room[wave], lane);
       }
       emit(M, at, border, out, 0, lane, 0, 0);
       for (int x = min(int(n.x[0]), p.N) + lane; x < p.N; x += kWave) out[x] = -1;
@@ -473,6 +505,7 @@ template <int M>
 __global__ __launch_bounds__(kPickThreads) void pick_kernel(SelectArgs p) {
   __shared__ Four part[2][kPickWaves];
   __shared__ uint32_t few[kFew];
+  __shared__ __attribute__((aligned(16))) uint32_t room[kPickWaves][kRoom];
   __shared__ int n_few;
   const long list = blockIdx.x;
   const int t = int(list / p.Hkv), b = t / p.n, j = t % p.n, lane = threadIdx.x % kWave;
@@ -553,13 +586,10 @@ __global__ __launch_bounds__(kPickThreads) void pick_kernel(SelectArgs p) {
         uint32_t some[kFew / kWave];
 #pragma unroll
         for (int x = 0; x < kFew / kWave; ++x) some[x] = x * kWave + lane < n_few ? few[x * kWave + lane] : 0u;
-        const int above = s.c_hi;
-        s.c_lo -= above;
-        s.c_hi = 0;
-        s = wave_search<kFew / kWave>(s, some, p.N - above);
-        s.c_hi += above;
+        border = wave_search<kFew / kWave>(s, some, s.c_hi, p.N, room[wave], lane);
+      } else {
+        border = s.border(p.N);
       }
-      border = s.border(p.N);
     }
   }
   Four c{{0, 0, 0, 0}};
@@ -590,18 +620,19 @@ size_t fused_lds(int n, int G, int D, int max_blocks) {
   return max_blocks <= kFusedBlocks && bytes <= kFusedLds ? bytes : 0;
 }
 
-// Chunks of blocks of a call in two launches: as many as fill the chip once, of 256 blocks or more
-int score_chunks(int B, int n, int G, int Hkv, int max_blocks) {
+// Blocks of a workgroup of a call in two launches: two rounds of 256 where that still makes a workgroup for every CU
+// (16 sequences x 5 positions at 32768-65536: 28.4 us; with one round 30.1, three 30.6, four 33.4)
+int score_chunk(int B, int n, int G, int Hkv, int max_blocks) {
   const long groups = long(B) * Hkv * ((long(n) + score_positions(G) - 1) / score_positions(G));
-  const int rounds = (max_blocks + 32 * kWaves - 1) / (32 * kWaves);
-  return int(std::max(1l, std::min(long(rounds), 512 / groups)));
+  constexpr int round = 32 * kWaves;
+  return groups * ((max_blocks + 2 * round - 1) / (2 * round)) >= 256 ? 2 * round : round;
 }
 
 }  // namespace
 
 double select_groups(int B, int n, int Hq, int Hkv, int D, int max_blocks) {
   const int G = Hq / Hkv;
-  const double chunks = fused_lds(n, G, D, max_blocks) ? 1 : score_chunks(B, n, G, Hkv, max_blocks);
+  const double chunks = fused_lds(n, G, D, max_blocks) ? 1 : std::ceil(max_blocks / double(score_chunk(B, n, G, Hkv, max_blocks)));
   return 2 * std::max((double(B) + 7) * std::ceil(n / double(score_positions(G))) * Hkv * chunks, double(B) * n * Hkv);
 }
 
@@ -627,8 +658,7 @@ hipError_t launch_select_blocks(const void* q, const void* bounds, const int32_t
   p.block_bytes = uint32_t(Hkv) * (2 * D + 16);
   p.by_xcd = B % 8 == 0 || B >= 48;
   if (!fused) {
-    const int most = score_chunks(B, n, p.G, Hkv, max_blocks), rounds = (max_blocks + 32 * kWaves - 1) / (32 * kWaves);
-    p.chunk = (rounds + most - 1) / most * 32 * kWaves;
+    p.chunk = score_chunk(B, n, p.G, Hkv, max_blocks);
     p.chunks = (max_blocks + p.chunk - 1) / p.chunk;
     Carver c(ws, ws_bytes);
     p.keys = c.take<uint32_t>(size_t(B) * n * Hkv * max_blocks);
