@@ -354,8 +354,9 @@ int molt_paged_attention_kvq(const void* q, const void* k_cache, const void* v_c
  * context_lens[b] + j of these. Entries outside [0, max_blocks_per_seq), blocks past the position
  * and blocks whose id is outside [0, num_blocks) are passed over; a block listed twice counts
  * twice; a row without a key is zeros. Keys and values that a row does not see may hold anything.
- * Softmax weights are held in 16 bits (BF16) or 24 (F32), sums in f32; the same call gives the same
- * bits.
+ * Softmax weights are held in 16 bits (BF16, as two bf16 parts) or 24 (F32), sums in f32; an infinite
+ * value that a row sees gives an infinity or NaN in its dim, a NaN gives NaN. The same call gives the
+ * same bits.
  *
  * Errors, all: INVALID_ARG for NULL required pointers, sizes outside the above or past what a
  * launch holds (2^32 threads), caches, bounds, q or out that are not 16-byte aligned; WORKSPACE. A

@@ -696,10 +696,13 @@ def select_blocks(q, bounds, block_tables, context_lens, k, n_select, n_first=1,
     of largest score by the keys' bounds (molt_select_blocks), the first n_first and last n_last among them: i32
     [B*(1+k), Hkv, n_select], ascending, then -1. Rows j >= lens[b] have empty lists."""
     lib = _lib or load()
-    dev = _here(bounds, "bounds")
+    dev, table, dt, shape = bounds.get_device(), block_tables.shape, q.dtype, q.shape
+    if dev < 0 or dev != _current_device() or len(table) != 2:
+        _here(bounds, "bounds")
+        _table(block_tables)
     nb, Hkv, D = _bounds_shape(bounds)
-    B, maxb = table = _table(block_tables)
-    rows, T, dt, shape = (B,), B * (k + 1), q.dtype, q.shape
+    B, maxb = table
+    rows, T = (B,), B * (k + 1)
     if not (n_select > 0 and (dt is torch.bfloat16 or dt is torch.float32) and len(shape) == 3 and shape[0] == T
             and shape[2] == D and block_tables.dtype is context_lens.dtype is _I32 and context_lens.shape == rows
             and q.get_device() == block_tables.get_device() == context_lens.get_device() == dev
@@ -731,18 +734,24 @@ def paged_attention_blocks(q, k_cache, v_cache, block_tables, context_lens, k, b
     """paged_attention over the blocks that blocks [B*(1+k), Hkv, N] i32 lists for each position and kv head
     (select_blocks; -1: none): returns [B*(1+k), Hq*D] of q's dtype."""
     lib = _lib or load()
-    dev = _here(k_cache, "k_cache")
-    dt, cache = _cache(k_cache)
+    dev, dt, cache, table, shape, lists = (k_cache.get_device(), k_cache.dtype, k_cache.shape, block_tables.shape,
+                                           q.shape, blocks.shape)
+    if dev < 0 or dev != _current_device() or len(cache) != 4 or len(table) != 2:
+        _here(k_cache, "k_cache")
+        _cache(k_cache)
+        _table(block_tables)
     nb, Hkv, _, D = cache
-    B, maxb = table = _table(block_tables)
-    T, shape, lists = B * (k + 1), q.shape, blocks.shape
+    B, maxb = table
+    T = B * (k + 1)
     if not (len(shape) == len(lists) == 3 and shape[0] == lists[0] == T and shape[2] == D and lists[1] == Hkv
-            and v_cache.shape == (nb, Hkv, D, 16) and context_lens.shape == (B,) and v_cache.dtype is q.dtype is dt
+            and cache[2] == 16 and v_cache.shape == (nb, Hkv, D, 16) and context_lens.shape == (B,)
+            and v_cache.dtype is q.dtype is dt and (dt is torch.bfloat16 or dt is torch.float32)
             and block_tables.dtype is context_lens.dtype is blocks.dtype is _I32
             and v_cache.get_device() == q.get_device() == block_tables.get_device() == context_lens.get_device()
             == blocks.get_device() == dev and k_cache.is_contiguous() and v_cache.is_contiguous()
             and q.is_contiguous() and block_tables.is_contiguous() and context_lens.is_contiguous()
             and blocks.is_contiguous()):
+        _cache(k_cache)
         _must(k_cache, dt, cache, dev, "k_cache")
         _must(v_cache, dt, (nb, Hkv, D, 16), dev, "v_cache")
         _must_be_ints(dev, ("block_tables", block_tables, table), ("context_lens", context_lens, (B,)))

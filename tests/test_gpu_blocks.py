@@ -374,6 +374,65 @@ def test_attention_over_odd_lists(molt_lib, dtype):
     assert (got[0, :G * D] == 0).all() and (got[6:8] == 0).all()
 
 
+def _ascending(lists):
+    """The lists as select_blocks leaves them: each block once, ascending, then -1."""
+    out = np.full_like(lists, -1)
+    for i in np.ndindex(lists.shape[:2]):
+        row = np.unique(lists[i][lists[i] >= 0])
+        out[i][:len(row)] = row
+    return out
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,n,H,G,D,N,maxb", [(1, 2, 1, 8, 128, 1, 3), (2, 5, 2, 8, 128, 24, 40), (3, 4, 1, 7, 64, 63, 70),
+                                              (1, 2, 3, 1, 64, 9, 12), (1, 9, 1, 5, 128, 130, 300), (2, 3, 2, 2, 128, 512, 520),
+                                              (1, 2, 1, 4, 64, 513, 520)])
+def test_attention_over_ascending_lists(molt_lib, dtype, B, n, H, G, D, N, maxb):
+    """What neighbouring positions list in common, and what they do not: no block, a few, all."""
+    rng = np.random.default_rng(maxb)
+    nb = B * maxb
+    kc, vc = _cache(rng, nb, H, D, dtype)
+    tables = rng.permutation(nb).reshape(B, maxb).astype(np.int32)
+    ctx = np.linspace(16 * maxb - n, 30, B).astype(np.int32)
+    common = rng.permutation(maxb)
+    lists = np.empty((B * n, H, N), np.int32)
+    for t in range(B * n):
+        for h in range(H):
+            own = rng.permutation(maxb)[:N]
+            keep = [N, N // 2, 0][(t + h) % 3]
+            lists[t, h] = np.concatenate([common[:keep], own[keep:], np.full(N, -1)])[:N]
+    _attend_both(molt_lib, _queries(rng, B, n, H * G, D, dtype), kc, vc, tables, ctx, n, _ascending(lists), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N", [5, 200])
+def test_attention_where_only_a_neighbour_sees_nan(molt_lib, dtype, N):
+    """A NaN or infinity in a block that the next position lists, or at its own token, leaves a row as it is."""
+    rng = np.random.default_rng(12)
+    H, G, D, maxb, n = 2, 8, 128, 220, 5
+    kc, vc = _cache(rng, maxb, H, D, dtype)
+    tables = rng.permutation(maxb).astype(np.int32)[None]
+    q = _queries(rng, 1, n, H * G, D, dtype)
+    lists = np.tile(np.arange(10, 10 + N, dtype=np.int32), (n, H, 1))
+    lists[:, :, 0], lists[:, :, -1] = 3, 219
+    ctx = [16 * 219 + 4]
+    clean = molt_lib.paged_attention_blocks(q.cuda(), kc.cuda(), vc.cuda(), _t(tables), _i32(ctx), n - 1, _t(lists))
+    lists[1, 0, 0], lists[4, 1, 0] = 4, 5                            # others list block 3, or nothing of 4 and 5
+    vc[tables[0, 4], 0, 7, 3], kc[tables[0, 5], 1, 2, 8] = float("nan"), float("inf")
+    vc[tables[0, 219], 1, 100, 7] = float("-inf")                    # the token of position 3
+    got = molt_lib.paged_attention_blocks(q.cuda(), kc.cuda(), vc.cuda(), _t(tables), _i32(ctx), n - 1, _t(lists))
+    got, clean = got.view(n, H, G, D), clean.view(n, H, G, D)
+    for j, h in ((0, 0), (2, 0), (3, 0), (4, 0), (0, 1), (1, 1), (2, 1)):
+        err = (got[j, h].double() - clean[j, h].double()).abs().max().item()
+        assert err <= 2.0 ** -7 * clean[j, h].abs().max().item(), (j, h, err)
+    assert got[1, 0, :, 7].isnan().all() and not got[1, 0, :, 8:].isnan().any()
+    # (bf16 weights go in as two parts, the smaller of any sign or 0: an infinite value gives an infinity or NaN)
+    assert not got[3, 1, :, 100].isfinite().any() and not got[3, 1, :, :100].isnan().any()
+    assert not got[3, 1, :, 101:].isnan().any()
+    up = q.view(n, H, G, D)[4, 1, :, 8].float() > 0                  # heads whose score of the infinite key is +inf
+    assert got[4, 1][up].isnan().all() and up.any()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("N", [3, 200])
 def test_attention_of_values_that_are_not_finite(molt_lib, dtype, N):
