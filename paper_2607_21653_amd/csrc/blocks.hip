@@ -365,48 +365,52 @@ __global__ __launch_bounds__(kThreads) void bounds_update_kernel(const T* __rest
   float x[NI][8];
 #pragma unroll
   for (int i = 0; i < NI; ++i) load_octet(src + (i * TPI + lane / O) * D + oct * 8, x[i]);
-  float hi[8], lo[8];
-  uint32_t a = 0;
+  float hi[8], lo[8], finite = 0.f;              // lo: of the negated keys; finite: 0 as long as all keys are
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    hi[e] = -__builtin_inff();
-    lo[e] = __builtin_inff();
-  }
+  for (int e = 0; e < 8; ++e) hi[e] = lo[e] = -__builtin_inff();
 #pragma unroll
   for (int i = 0; i < NI; ++i)
     if (i * TPI + lane / O < seen) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         hi[e] = fmaxf(hi[e], x[i][e]);
-        lo[e] = fminf(lo[e], x[i][e]);
-        a = max(a, __float_as_uint(x[i][e]) & 0x7fffffffu);
+        lo[e] = fmaxf(lo[e], -x[i][e]);
+        finite = __builtin_fmaf(x[i][e], 0.f, finite);
       }
     }
+  if (O == 8) {                                  // lanes l, l ^ 8: a rotation of the 16-lane row
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    if (O == 8) {                                                        // lanes l, l ^ 8: a rotation of the 16-lane row
+    for (int e = 0; e < 8; ++e) {
       hi[e] = fmaxf(hi[e], __uint_as_float(dpp_u32<0x128, 0xF>(__float_as_uint(hi[e]), 0u)));
-      lo[e] = fminf(lo[e], __uint_as_float(dpp_u32<0x128, 0xF>(__float_as_uint(lo[e]), 0u)));
+      lo[e] = fmaxf(lo[e], __uint_as_float(dpp_u32<0x128, 0xF>(__float_as_uint(lo[e]), 0u)));
     }
-    hi[e] = rows_max4(hi[e]);
-    lo[e] = -rows_max4(-lo[e]);
   }
-  a = uint32_t(wave_max_dpp((unsigned long long)a));
-  const bool bad = a >= 0x7f800000u;
-  const int e = bad ? kBoundsNotFinite : bounds_exponent(a);
-  const float r = bad ? 0.f : pow2(-e);
-  int ch[8], cl[8];
+  // Over the 16-lane rows, each of which ends with its share: rows 0 and 1 the octet's first and second 4 of hi, rows 2
+  // and 3 those of lo. A row swap brings two values' partners together, so that one maximum serves both.
+  float w[4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    ch[i] = bad ? 0 : int(__builtin_ceilf(hi[i] * r));
-    cl[i] = bad ? 0 : int(__builtin_floorf(lo[i] * r));
+  for (int e = 0; e < 4; ++e) {
+    const auto u = __builtin_amdgcn_permlane16_swap(__float_as_uint(hi[e]), __float_as_uint(hi[e + 4]), false, false);
+    const auto v = __builtin_amdgcn_permlane16_swap(__float_as_uint(lo[e]), __float_as_uint(lo[e + 4]), false, false);
+    const float hh = fmaxf(__uint_as_float(u[0]), __uint_as_float(u[1]));
+    const float ll = fmaxf(__uint_as_float(v[0]), __uint_as_float(v[1]));
+    const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(hh), __float_as_uint(ll), false, false);
+    w[e] = fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+  }
+  const bool bad = __any(finite != 0.f);         // (NaN is)
+  const float a = wave_max_dpp(fmaxf(fmaxf(fabsf(w[0]), fabsf(w[1])), fmaxf(fabsf(w[2]), fabsf(w[3]))));
+  const int e = bad ? kBoundsNotFinite : bounds_exponent(__float_as_uint(a));
+  const float r = bad ? 0.f : pow2(-e);
+  const bool low = lane >= 32;
+  int c[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int up = bad ? 0 : int(__builtin_ceilf(w[i] * r));
+    c[i] = low ? -up : up;                       // floor(x) = -ceil(-x)
   }
   uint8_t* rec = bounds + (long(id) * Hkv + h) * Rec::kBytes;
-  if (lane < O) {
-    u32x2_t* o = reinterpret_cast<u32x2_t*>(rec + oct * 8);
-    o[0] = u32x2_t{pack_codes(ch[0], ch[1], ch[2], ch[3]), pack_codes(ch[4], ch[5], ch[6], ch[7])};
-    o[D / 8] = u32x2_t{pack_codes(cl[0], cl[1], cl[2], cl[3]), pack_codes(cl[4], cl[5], cl[6], cl[7])};
-  }
+  if (O == 16 || lane % 16 < O)
+    *reinterpret_cast<uint32_t*>(rec + (low ? D : 0) + oct * 8 + lane / 16 % 2 * 4) = pack_codes(c[0], c[1], c[2], c[3]);
   if (lane == kWave - 1) *reinterpret_cast<u32x4_t*>(rec + Rec::kExponent) = u32x4_t{uint32_t(e) & 0xffu, 0, 0, 0};
 }
 

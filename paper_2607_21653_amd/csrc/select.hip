@@ -577,10 +577,20 @@ __global__ __launch_bounds__(kPickThreads) void pick_kernel(SelectArgs p) {
           return sum(wave_sum4<M != 0>(c));
         });
       if (!s.done()) {
+        int mine = 0;
 #pragma unroll
         for (int x = 0; x < m; ++x) {
           const uint32_t k = at(x);
-          if (k >= s.lo && k < s.hi) few[atomicAdd(&n_few, 1)] = k;      // in any order: they are counted only
+          mine += k >= s.lo && k < s.hi;
+        }
+        const int upto = wave_scan_dpp(mine);
+        int to = 0;                              // (the wavefronts in any order: the keys are counted only)
+        if (lane == kWave - 1 && upto) to = atomicAdd(&n_few, upto);
+        to = __builtin_amdgcn_readlane(to, kWave - 1) + upto - mine;
+#pragma unroll
+        for (int x = 0; x < m; ++x) {
+          const uint32_t k = at(x);
+          if (k >= s.lo && k < s.hi) few[to++] = k;
         }
         __syncthreads();
         uint32_t some[kFew / kWave];
