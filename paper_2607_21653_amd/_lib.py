@@ -12,6 +12,7 @@ import torch
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libmolt.so")
+CALLS_PATH = os.path.join(HERE, "_calls.so")
 
 MOLT_F32, MOLT_BF16, MOLT_FP8_E4M3 = 0, 1, 2
 MOLT_ERR_WORKSPACE = -3
@@ -21,6 +22,7 @@ DTYPE_CODE = {torch.float32: MOLT_F32, torch.bfloat16: MOLT_BF16, torch.uint8: M
 NAME_CODE = {"f32": MOLT_F32, "bf16": MOLT_BF16, "fp8": MOLT_FP8_E4M3}
 
 _lib = None
+_calls = None                     # the module of csrc/binding/calls.cpp
 
 c_int, c_size, c_vp, c_float = ctypes.c_int, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_float
 
@@ -124,17 +126,22 @@ class MoltError(RuntimeError):
 
 def load(path=LIB_PATH):
     """Loads the library (once). Raises if it has not been built."""
-    global _lib
+    global _lib, _calls
     if _lib is not None:
         return _lib
-    if not os.path.exists(path):
-        raise MoltError(f"{path} is missing: build it with `python -m paper_2607_21653_amd.build`")
+    for need in (path, CALLS_PATH):
+        if not os.path.exists(need):
+            raise MoltError(f"{need} is missing: build it with `python -m paper_2607_21653_amd.build`")
     lib = ctypes.CDLL(path)
     for name, (res, args) in _SIGS.items():
         fn = getattr(lib, name)
         fn.restype = res
         fn.argtypes = args
-    _lib = lib
+    from . import _calls as calls
+    calls.set_entries(MoltError, *(ctypes.cast(getattr(lib, "molt_" + name), c_vp).value for name in (
+        "last_error", "plan_blocks", "plan_blocks_workspace_size", "kv_write", "key_bounds_update", "key_bounds_read",
+        "select_blocks", "select_blocks_workspace_size", "paged_attention_blocks", "paged_attention_blocks_workspace_size")))
+    _lib, _calls = lib, calls
     return lib
 
 
@@ -502,16 +509,8 @@ def paged_attention_kvq(q, k_cache, v_cache, block_tables, context_lens, k, work
 
 # ------------------------------------------------------------------ sparse attention over listed blocks
 
-# As above, a call asks each tensor once, and looks for the message (`_must`) only where something is wrong.
-
-_I32 = torch.int32
-
-
-def _must(t, dtype, shape, dev, name):
-    """Raises unless t is such a tensor."""
-    _dev(t, dtype, shape, name)
-    _same_device(t, dev, name)
-
+# The calls below take 3 to 8 us on the GPU where they are small. They go through _calls, which looks their arguments over
+# in C++ and returns None where it does not take them: then `_why` finds the reason, tensor by tensor.
 
 def _here(t, name):
     """Index of a tensor's device, which must be the current one."""
@@ -523,61 +522,24 @@ def _here(t, name):
     return dev
 
 
-def _must_be_ints(dev, *named):
-    for name, t, shape in named:
-        if t is not None:
-            _must(t, _I32, shape, dev, name)
-
-
-def _table(block_tables):
-    shape = block_tables.shape
-    if len(shape) != 2:
-        raise MoltError(f"block_tables has shape {tuple(shape)}, expected (B, max_blocks)")
-    return shape
-
-
-def _cache(k_cache):
-    """(dtype, shape) of a bf16 or f32 cache of keys."""
-    dt, shape = k_cache.dtype, k_cache.shape
-    if dt is not torch.bfloat16 and dt is not torch.float32:
-        raise MoltError(f"k_cache has dtype {dt}, expected float32 or bfloat16")
-    if len(shape) != 4 or shape[2] != 16:
-        raise MoltError(f"k_cache has shape {tuple(shape)}, expected [num_blocks, n_kv_heads, 16, head_dim]")
-    return dt, shape
-
-
-def _bounds_shape(bounds):
-    """(num_blocks, n_kv_heads, head_dim) of key bounds."""
-    shape = bounds.shape
-    if len(shape) != 3 or shape[2] % 2:
-        raise MoltError(f"bounds has shape {tuple(shape)}, expected [num_blocks, n_kv_heads, 2 * head_dim + 16]")
-    if bounds.dtype is not torch.uint8 or not bounds.is_contiguous():
-        _dev(bounds, torch.uint8, shape, "bounds")
-    return shape[0], shape[1], (shape[2] - 16) // 2
-
-
-def _must_be_queries(q, T, D, dev):
-    shape = q.shape
-    if q.dtype is not torch.bfloat16 and q.dtype is not torch.float32:
-        raise MoltError(f"q has dtype {q.dtype}, expected float32 or bfloat16")
-    if len(shape) != 3:
-        raise MoltError(f"q has shape {tuple(shape)}, expected [B*(1+k), Hq, {D}]")
-    _must(q, None, (T, shape[1], D), dev, "q")
-
-
-def _are_lens(lens, rows, dev):
-    return lens is None or (lens.dtype is _I32 and lens.shape == rows and lens.get_device() == dev
-                            and lens.is_contiguous())
-
-
-def _given(workspace, dev):
-    """Address and bytes of a caller's workspace."""
-    if workspace is None:
-        return None, 0
-    if workspace.get_device() != dev or not workspace.is_contiguous():
-        _same_device(workspace, dev, "workspace")
-        raise MoltError("workspace must be contiguous")
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+def _why(call, dev, *named):
+    """Raises the reason why a call of _calls did not take its arguments: the first of named (name, tensor, dtype, shape)
+    that is not so (a shape's None stands for any size), else its numbers."""
+    for name, t, dtype, shape in named:
+        if t is None:
+            continue
+        if not isinstance(t, torch.Tensor):
+            raise MoltError(f"{name} must be a GPU tensor, is {type(t).__name__}")
+        want = tuple(shape) if shape is not None else t.shape
+        if len(want) != t.dim() or any(w is not None and w != s for w, s in zip(want, t.shape)):
+            raise MoltError(f"{name} has shape {tuple(t.shape)}, expected {want}")
+        if dtype is float:
+            dtype = t.dtype
+            if dtype is not torch.bfloat16 and dtype is not torch.float32:
+                raise MoltError(f"{name} has dtype {dtype}, expected float32 or bfloat16")
+        _dev(t, dtype, None, name)
+        _same_device(t, dev, name)
+    raise MoltError(f"{call}: a number among its arguments is not whole, or not in 0 .. 2^31 - 1")
 
 
 def block_pool(num_blocks, device="cuda"):
@@ -591,54 +553,39 @@ def plan_blocks(block_tables, n_blocks, context_lens, n_new, pool, n, n_shared=N
     """Lets the block tables follow the lengths (molt_plan_blocks), all on the GPU and in place: sequence b gets the
     blocks that rows context_lens[b] .. + n_new[b] - 1 need from pool, or gives its own back where n_new[b] < 0.
     Returns (slots [B*n] i32 for kv_write, -1 where there is no row; placed [B] i32, rows that have slots)."""
-    lib = _lib or load()
+    _lib or load()
     dev = _here(block_tables, "block_tables")
-    B, maxb = shape = _table(block_tables)
-    rows = (B,)
-    cap = pool.numel() - 2
-    if not (cap > 0 < n and block_tables.dtype is n_blocks.dtype is context_lens.dtype is n_new.dtype is pool.dtype is _I32
-            and n_blocks.shape == context_lens.shape == n_new.shape == rows and pool.dim() == 1
-            and n_blocks.get_device() == context_lens.get_device() == n_new.get_device() == pool.get_device() == dev
-            and block_tables.is_contiguous() and n_blocks.is_contiguous() and context_lens.is_contiguous()
-            and n_new.is_contiguous() and pool.is_contiguous()) or n_shared is not None:
-        if pool.dim() != 1 or cap < 1:
-            raise MoltError(f"pool has shape {tuple(pool.shape)}, expected (2 + num_blocks,)")
+    done = _calls.plan(block_tables, n_blocks, context_lens, n_new, pool, n, n_shared, dev, _raw_stream(dev))
+    if done is None:
+        i32, rows = torch.int32, block_tables.shape[:1]
         if n < 1:
             raise MoltError(f"n = {n} must be >= 1")
-        _must_be_ints(dev, ("block_tables", block_tables, shape), ("n_blocks", n_blocks, rows),
-                      ("context_lens", context_lens, rows), ("n_new", n_new, rows), ("pool", pool, pool.shape),
-                      ("n_shared", n_shared, rows))
-    slots, placed = n_new.new_empty(B * n), n_new.new_empty(B)
-    ws, have = None, lib.molt_plan_blocks_workspace_size(B, n)
-    if have:
-        ws = torch.empty(have, dtype=torch.uint8, device=n_new.device)
-    status = lib.molt_plan_blocks(block_tables.data_ptr(), n_blocks.data_ptr(), context_lens.data_ptr(),
-                                  n_new.data_ptr(), pool.data_ptr(), _ptr(n_shared), B, n, maxb, cap, slots.data_ptr(),
-                                  placed.data_ptr(), _ptr(ws), have, _raw_stream(dev))
-    if status:
-        _check(status, "molt_plan_blocks")
-    return slots, placed
+        if pool.numel() < 3:
+            raise MoltError(f"pool has shape {tuple(pool.shape)}, expected (2 + num_blocks,)")
+        _why("molt_plan_blocks", dev, ("block_tables", block_tables, i32, (None, None)), ("n_blocks", n_blocks, i32, rows),
+             ("context_lens", context_lens, i32, rows), ("n_new", n_new, i32, rows), ("pool", pool, i32, (None,)),
+             ("n_shared", n_shared, i32, rows))
+    return done
 
 
 def kv_write(k, v, k_cache, v_cache, slots):
     """Writes rows k, v [T, Hkv, D] (row-strided views will do) into a bf16 or f32 cache at slots [T] i32 (block * 16 +
     token, as plan_blocks gives them); rows whose slot is outside the cache are left out."""
-    lib = _lib or load()
+    _lib or load()
     dev = _here(k_cache, "k_cache")
-    dt, shape = _cache(k_cache)
-    nb, Hkv, _, D = shape
-    T = slots.numel()
-    if not (v_cache.dtype is dt and slots.dtype is _I32 and v_cache.shape == (nb, Hkv, D, 16) and slots.dim() == 1
-            and v_cache.get_device() == slots.get_device() == dev
-            and k_cache.is_contiguous() and v_cache.is_contiguous() and slots.is_contiguous()):
-        _must(k_cache, dt, shape, dev, "k_cache")
-        _must(v_cache, dt, (nb, Hkv, D, 16), dev, "v_cache")
-        _must(slots, _I32, (T,), dev, "slots")
-    ks, vs = _rows_stride(k, dt, T, Hkv, D, dev, "k"), _rows_stride(v, dt, T, Hkv, D, dev, "v")
-    status = lib.molt_kv_write(k.data_ptr(), v.data_ptr(), ks, vs, slots.data_ptr(), T, Hkv, D, nb, DTYPE_CODE[dt],
-                               k_cache.data_ptr(), v_cache.data_ptr(), _raw_stream(dev))
-    if status:
-        _check(status, "molt_kv_write")
+    if _calls.write(k, v, k_cache, v_cache, slots, dev, _raw_stream(dev)) is None:
+        dt, shape = k_cache.dtype, k_cache.shape
+        values = (shape[0], shape[1], shape[3], 16) if len(shape) == 4 else (None,) * 4
+        named = [("k_cache", k_cache, float, (None, None, 16, None)), ("v_cache", v_cache, dt, values),
+                 ("slots", slots, torch.int32, (None,))]
+        if len(shape) == 4 and dt in DTYPE_CODE and k.dim() == v.dim() == 3:
+            for name, t in (("k", k), ("v", v)):
+                if t.get_device() < 0:
+                    raise MoltError(f"{name} must be a GPU tensor")
+                _rows_stride(t, dt, slots.numel(), shape[1], shape[3], dev, name)
+        else:
+            named += [("k", k, dt, (None,) * 3), ("v", v, dt, (None,) * 3)]
+        _why("molt_kv_write", dev, *named)
 
 
 def key_bounds(num_blocks, n_kv_heads, head_dim, device="cuda"):
@@ -649,42 +596,26 @@ def key_bounds(num_blocks, n_kv_heads, head_dim, device="cuda"):
 def key_bounds_update(k_cache, bounds, block_tables, starts, n, lens=None):
     """Bounds of the keys of the blocks that hold positions starts[b] + j, j < n (j < lens[b] if given), after
     kv_write of these rows."""
-    lib = _lib or load()
+    _lib or load()
     dev = _here(k_cache, "k_cache")
-    dt, shape = _cache(k_cache)
-    nb, Hkv, _, D = shape
-    B, maxb = table = _table(block_tables)
-    rows = (B,)
-    if not (bounds.dtype is torch.uint8 and block_tables.dtype is starts.dtype is _I32
-            and bounds.shape == (nb, Hkv, 2 * D + 16) and starts.shape == rows
-            and bounds.get_device() == block_tables.get_device() == starts.get_device() == dev
-            and k_cache.is_contiguous() and bounds.is_contiguous() and block_tables.is_contiguous()
-            and starts.is_contiguous() and _are_lens(lens, rows, dev)):
-        _must(k_cache, dt, shape, dev, "k_cache")
-        _must(bounds, torch.uint8, (nb, Hkv, 2 * D + 16), dev, "bounds")
-        _must_be_ints(dev, ("block_tables", block_tables, table), ("starts", starts, rows), ("lens", lens, rows))
-    status = lib.molt_key_bounds_update(k_cache.data_ptr(), bounds.data_ptr(), block_tables.data_ptr(),
-                                        starts.data_ptr(), None if lens is None else lens.data_ptr(), B, n, Hkv, D,
-                                        maxb, nb, DTYPE_CODE[dt], _raw_stream(dev))
-    if status:
-        _check(status, "molt_key_bounds_update")
+    if _calls.update(k_cache, bounds, block_tables, starts, n, lens, dev, _raw_stream(dev)) is None:
+        i32, shape, rows = torch.int32, k_cache.shape, block_tables.shape[:1]
+        records = (shape[0], shape[1], 2 * shape[3] + 16) if len(shape) == 4 else (None,) * 3
+        _why("molt_key_bounds_update", dev, ("k_cache", k_cache, float, (None, None, 16, None)),
+             ("bounds", bounds, torch.uint8, records), ("block_tables", block_tables, i32, (None, None)),
+             ("starts", starts, i32, rows), ("lens", lens, i32, rows))
 
 
 def key_bounds_read(bounds, ids):
     """The bounds of blocks ids [M] i32 of the cache as values: (largest, smallest) f32 [M, Hkv, D]."""
-    lib = _lib or load()
+    _lib or load()
     dev = _here(bounds, "bounds")
-    nb, Hkv, D = _bounds_shape(bounds)
-    M = ids.numel()
-    if not (ids.dtype is _I32 and ids.dim() == 1 and ids.get_device() == dev and ids.is_contiguous()):
-        _must(ids, _I32, (M,), dev, "ids")
-    hi = bounds.new_empty((M, Hkv, D), dtype=torch.float32)
-    lo = torch.empty_like(hi)
-    status = lib.molt_key_bounds_read(bounds.data_ptr(), ids.data_ptr(), M, Hkv, D, nb, hi.data_ptr(), lo.data_ptr(),
-                                      _raw_stream(dev))
-    if status:
-        _check(status, "molt_key_bounds_read")
-    return hi, lo
+    done = _calls.read(bounds, ids, dev, _raw_stream(dev))
+    if done is None:
+        if ids.numel() < 1:
+            raise MoltError("ids is empty")
+        _why("molt_key_bounds_read", dev, ("bounds", bounds, torch.uint8, (None,) * 3), ("ids", ids, torch.int32, (None,)))
+    return done
 
 
 def select_blocks_workspace_size(B, k, n_q_heads, n_kv_heads, head_dim, max_blocks):
@@ -695,35 +626,20 @@ def select_blocks(q, bounds, block_tables, context_lens, k, n_select, n_first=1,
     """For each query position (q [B*(1+k), Hq, D], f32|bf16, at context_lens[b] + j) and kv head the n_select blocks
     of largest score by the keys' bounds (molt_select_blocks), the first n_first and last n_last among them: i32
     [B*(1+k), Hkv, n_select], ascending, then -1. Rows j >= lens[b] have empty lists."""
-    lib = _lib or load()
-    dev, table, dt, shape = bounds.get_device(), block_tables.shape, q.dtype, q.shape
-    if dev < 0 or dev != _current_device() or len(table) != 2:
-        _here(bounds, "bounds")
-        _table(block_tables)
-    nb, Hkv, D = _bounds_shape(bounds)
-    B, maxb = table
-    rows, T = (B,), B * (k + 1)
-    if not (n_select > 0 and (dt is torch.bfloat16 or dt is torch.float32) and len(shape) == 3 and shape[0] == T
-            and shape[2] == D and block_tables.dtype is context_lens.dtype is _I32 and context_lens.shape == rows
-            and q.get_device() == block_tables.get_device() == context_lens.get_device() == dev
-            and q.is_contiguous() and block_tables.is_contiguous() and context_lens.is_contiguous()
-            and _are_lens(lens, rows, dev)):
-        _must_be_ints(dev, ("block_tables", block_tables, table), ("context_lens", context_lens, rows),
-                      ("lens", lens, rows))
-        _must_be_queries(q, T, D, dev)
-        raise MoltError(f"n_select = {n_select} must be >= 1")
-    ws, have = _given(workspace, dev)
-    out = block_tables.new_empty((T, Hkv, n_select))
-    args = (q.data_ptr(), bounds.data_ptr(), block_tables.data_ptr(), context_lens.data_ptr(),
-            None if lens is None else lens.data_ptr(), B, k, shape[1], Hkv, D, maxb, nb, n_select, n_first, n_last,
-            DTYPE_CODE[dt], out.data_ptr())
-    status = lib.molt_select_blocks(*args, ws, have, _raw_stream(dev))
-    if status == MOLT_ERR_WORKSPACE:     # none, or one that is too small
-        own, have = _workspace(lib.molt_select_blocks_workspace_size(B, k, shape[1], Hkv, D, maxb), q.device)
-        status = lib.molt_select_blocks(*args, _ptr(own), have, _raw_stream(dev))
-    if status:
-        _check(status, "molt_select_blocks")
-    return out
+    _lib or load()
+    dev = _here(bounds, "bounds")
+    done = _calls.select(q, bounds, block_tables, context_lens, k, n_select, n_first, n_last, lens, workspace, dev,
+                         _raw_stream(dev))
+    if done is None:
+        i32, rows = torch.int32, block_tables.shape[:1]
+        if n_select < 1:
+            raise MoltError(f"n_select = {n_select} must be >= 1")
+        D = (bounds.shape[2] - 16) // 2 if bounds.dim() == 3 else None
+        _why("molt_select_blocks", dev, ("bounds", bounds, torch.uint8, (None,) * 3),
+             ("block_tables", block_tables, i32, (None, None)), ("context_lens", context_lens, i32, rows),
+             ("q", q, float, (block_tables.shape[0] * (k + 1), None, D)), ("lens", lens, i32, rows),
+             ("workspace", workspace, None, None))
+    return done
 
 
 def paged_attention_blocks_workspace_size(B, k, n_q_heads, n_kv_heads, head_dim, n_list):
@@ -733,46 +649,18 @@ def paged_attention_blocks_workspace_size(B, k, n_q_heads, n_kv_heads, head_dim,
 def paged_attention_blocks(q, k_cache, v_cache, block_tables, context_lens, k, blocks, workspace=None):
     """paged_attention over the blocks that blocks [B*(1+k), Hkv, N] i32 lists for each position and kv head
     (select_blocks; -1: none): returns [B*(1+k), Hq*D] of q's dtype."""
-    lib = _lib or load()
-    dev, dt, cache, table, shape, lists = (k_cache.get_device(), k_cache.dtype, k_cache.shape, block_tables.shape,
-                                           q.shape, blocks.shape)
-    if dev < 0 or dev != _current_device() or len(cache) != 4 or len(table) != 2:
-        _here(k_cache, "k_cache")
-        _cache(k_cache)
-        _table(block_tables)
-    nb, Hkv, _, D = cache
-    B, maxb = table
-    T = B * (k + 1)
-    if not (len(shape) == len(lists) == 3 and shape[0] == lists[0] == T and shape[2] == D and lists[1] == Hkv
-            and cache[2] == 16 and v_cache.shape == (nb, Hkv, D, 16) and context_lens.shape == (B,)
-            and v_cache.dtype is q.dtype is dt and (dt is torch.bfloat16 or dt is torch.float32)
-            and block_tables.dtype is context_lens.dtype is blocks.dtype is _I32
-            and v_cache.get_device() == q.get_device() == block_tables.get_device() == context_lens.get_device()
-            == blocks.get_device() == dev and k_cache.is_contiguous() and v_cache.is_contiguous()
-            and q.is_contiguous() and block_tables.is_contiguous() and context_lens.is_contiguous()
-            and blocks.is_contiguous()):
-        _cache(k_cache)
-        _must(k_cache, dt, cache, dev, "k_cache")
-        _must(v_cache, dt, (nb, Hkv, D, 16), dev, "v_cache")
-        _must_be_ints(dev, ("block_tables", block_tables, table), ("context_lens", context_lens, (B,)))
-        _must_be_queries(q, T, D, dev)
-        if q.dtype is not dt:
-            raise MoltError(f"q has dtype {q.dtype}, the caches {dt}")
-        if len(lists) != 3:
-            raise MoltError(f"blocks has shape {tuple(lists)}, expected ({T}, {Hkv}, n_list)")
-        _must_be_ints(dev, ("blocks", blocks, (T, Hkv, lists[2])))
-    ws, have = _given(workspace, dev)
-    out = q.new_empty((T, shape[1] * D))
-    args = (q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_tables.data_ptr(), context_lens.data_ptr(),
-            blocks.data_ptr(), B, k, shape[1], Hkv, D, maxb, nb, lists[2], DTYPE_CODE[dt], out.data_ptr())
-    status = lib.molt_paged_attention_blocks(*args, ws, have, _raw_stream(dev))
-    if status == MOLT_ERR_WORKSPACE:
-        own, have = _workspace(lib.molt_paged_attention_blocks_workspace_size(B, k, shape[1], Hkv, D, lists[2]),
-                               q.device)
-        status = lib.molt_paged_attention_blocks(*args, _ptr(own), have, _raw_stream(dev))
-    if status:
-        _check(status, "molt_paged_attention_blocks")
-    return out
+    _lib or load()
+    dev = _here(k_cache, "k_cache")
+    done = _calls.attend(q, k_cache, v_cache, block_tables, context_lens, k, blocks, workspace, dev, _raw_stream(dev))
+    if done is None:
+        i32, shape, rows, dt = torch.int32, k_cache.shape, block_tables.shape[:1], k_cache.dtype
+        nb, Hkv, _, D = shape if len(shape) == 4 else (None,) * 4
+        T = block_tables.shape[0] * (k + 1)
+        _why("molt_paged_attention_blocks", dev, ("k_cache", k_cache, float, (None, None, 16, None)),
+             ("v_cache", v_cache, dt, (nb, Hkv, D, 16)), ("block_tables", block_tables, i32, (None, None)),
+             ("context_lens", context_lens, i32, rows), ("q", q, dt, (T, None, D)), ("blocks", blocks, i32, (T, Hkv, None)),
+             ("workspace", workspace, None, None))
+    return done
 
 
 # ------------------------------------------------------------------ model / decoder / step

@@ -4,7 +4,8 @@
 
 Every source under csrc/ is compiled to an object in _build/ (in parallel), then
 linked into paper_2607_21653_amd/libmolt.so. Packed-fp32 instructions are disabled
-for all device code."""
+for all device code. csrc/binding/calls.cpp, host code on torch's headers, becomes the
+Python module _calls.so beside it."""
 import argparse
 import concurrent.futures as cf
 import glob
@@ -17,6 +18,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libmolt.so")
+CALLS = os.path.join(HERE, "_calls.so")
 ARCH = "gfx950"
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
@@ -42,12 +44,33 @@ def _compile(src):
     return obj
 
 
+def _module():
+    """The Python module _calls."""
+    import sysconfig
+
+    import torch
+    from torch.utils.cpp_extension import include_paths, library_paths
+    tmp = CALLS + ".tmp"
+    cmd = [shutil.which("g++") or "g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", sysconfig.get_paths()["include"]]
+    for p in include_paths():
+        cmd += ["-isystem", p]
+    cmd += [os.path.join(CSRC, "binding", "calls.cpp"), "-o", tmp]
+    cmd += [f"-L{p}" for p in library_paths()] + ["-ltorch_python", "-ltorch_cpu", "-lc10"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"compile failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
+    os.replace(tmp, CALLS)
+
+
 def build(jobs=None, verbose=True):
     os.makedirs(BUILD, exist_ok=True)
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")) + glob.glob(os.path.join(CSRC, "*.cpp")))
     jobs = jobs or min(8, os.cpu_count() or 4)
     with cf.ThreadPoolExecutor(jobs) as ex:
+        module = ex.submit(_module)
         objs = list(ex.map(_compile, srcs))
+        module.result()
     tmp = LIB + ".tmp"
     cmd = [hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)
