@@ -15,7 +15,7 @@ namespace {
 
 constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * kWave;
-constexpr size_t kFusedLds = 80 << 10;           // two workgroups a CU
+constexpr size_t kFusedLds = 112 << 10;          // 128 x 5 positions, 2000 blocks: 80.3 us, in two launches 84.6
 
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t UnalignedU4 __attribute__((ext_vector_type(4), aligned(2)));
@@ -437,8 +437,8 @@ MOLT_DEV Item item_of(const SelectArgs& p) {
   return it;
 }
 
-// Tables of up to 1024 blocks whose keys fit in LDS: scores and lists in one launch; a wavefront a list
-constexpr int kFusedBlocks = 1024;
+// Short tables whose keys fit in LDS: scores and lists in one launch; a wavefront a list
+constexpr int kFusedBlocks = 2048;
 template <int D, int GP>
 __global__ __launch_bounds__(kThreads, 4) void select_kernel(SelectArgs p) {
   extern __shared__ __align__(16) char dyn[];
@@ -479,7 +479,8 @@ __global__ __launch_bounds__(kThreads, 4) void select_kernel(SelectArgs p) {
     };
     if (seen <= 4 * kWave) go(std::integral_constant<int, 4>{});
     else if (seen <= 9 * kWave) go(std::integral_constant<int, 9>{});
-    else go(std::integral_constant<int, 16>{});
+    else if (seen <= 16 * kWave) go(std::integral_constant<int, 16>{});
+    else go(std::integral_constant<int, kFusedBlocks / kWave>{});
   }
 }
 
@@ -498,11 +499,12 @@ __global__ __launch_bounds__(kThreads, 4) void score_kernel(SelectArgs p) {
                       p.keys + ((long(it.b) * p.n + j0) * p.Hkv + it.h) * p.max_blocks + c0, long(p.Hkv) * p.max_blocks);
 }
 
-// .. and a workgroup a list, M keys to a thread (0: tables past 2^13 blocks, the keys read again for each count). Once
-// few keys lie between the borders they go to LDS, and every wavefront ends the search by itself.
-constexpr int kPickThreads = 512, kPickWaves = kPickThreads / kWave, kFew = 8 * kWave;
-template <int M>
-__global__ __launch_bounds__(kPickThreads) void pick_kernel(SelectArgs p) {
+// .. and a workgroup a list, M keys to a thread (0: of tables of any size, the keys read again for each count). Once few
+// keys lie between the borders they go to LDS, and every wavefront ends the search by itself.
+constexpr int kFew = 8 * kWave;
+template <int M, int kPickWaves>
+__global__ __launch_bounds__(kPickWaves* kWave) void pick_kernel(SelectArgs p) {
+  constexpr int kPickThreads = kPickWaves * kWave;
   __shared__ Four part[2][kPickWaves];
   __shared__ uint32_t few[kFew];
   __shared__ __attribute__((aligned(16))) uint32_t room[kPickWaves][kRoom];
@@ -620,14 +622,20 @@ __global__ __launch_bounds__(kPickThreads) void pick_kernel(SelectArgs p) {
   for (int x = min(int(r.some), p.N) + int(threadIdx.x); x < p.N; x += kPickThreads) out[x] = -1;
 }
 
+constexpr unsigned kManyLists = 1024;
 int padded_rows(int G) { return G <= 4 ? 4 : G <= 8 ? 8 : 16; }
 int score_positions(int G) { return G > 16 ? 1 : 64 / padded_rows(G); }
 
-// LDS of a call in one launch; 0 where it takes two
-size_t fused_lds(int n, int G, int D, int max_blocks) {
+// LDS of a call in one launch; 0 where it takes two. One launch is the faster one where it makes a workgroup for every CU
+// (64 sequences x 1 position, 4 kv heads x 128: 600 blocks 15.9 us, two launches 18.5; 1300 blocks 27.7 and 28.6; 128 x 5:
+// 27.0 and 50.3, 47.8 and 68.7), and else for tables so short that one workgroup is done with them before a second launch
+// would begin (1 x 1: 300 blocks 8.9 and 10.7, 600 blocks 12.0 and 11.1).
+size_t fused_lds(int B, int n, int G, int Hkv, int D, int max_blocks) {
+  const long groups = long(B) * Hkv * ((long(n) + score_positions(G) - 1) / score_positions(G));
+  if (max_blocks > (groups >= 256 ? kFusedBlocks : 448)) return 0;
   const size_t fixed = D == 128 ? sizeof(ScoreLds<128>) : sizeof(ScoreLds<64>);
   const size_t bytes = fixed + size_t(std::min(n, score_positions(G))) * max_blocks * sizeof(uint32_t);
-  return max_blocks <= kFusedBlocks && bytes <= kFusedLds ? bytes : 0;
+  return bytes <= kFusedLds ? bytes : 0;
 }
 
 // Blocks of a workgroup of a call in two launches: two rounds of 256 where that still makes a workgroup for every CU
@@ -642,12 +650,12 @@ int score_chunk(int B, int n, int G, int Hkv, int max_blocks) {
 
 double select_groups(int B, int n, int Hq, int Hkv, int D, int max_blocks) {
   const int G = Hq / Hkv;
-  const double chunks = fused_lds(n, G, D, max_blocks) ? 1 : std::ceil(max_blocks / double(score_chunk(B, n, G, Hkv, max_blocks)));
+  const double chunks = fused_lds(B, n, G, Hkv, D, max_blocks) ? 1 : std::ceil(max_blocks / double(score_chunk(B, n, G, Hkv, max_blocks)));
   return 2 * std::max((double(B) + 7) * std::ceil(n / double(score_positions(G))) * Hkv * chunks, double(B) * n * Hkv);
 }
 
 size_t select_ws_bytes(int B, int n, int Hq, int Hkv, int D, int max_blocks) {
-  if (fused_lds(n, Hq / Hkv, D, max_blocks)) return 0;
+  if (fused_lds(B, n, Hq / Hkv, Hkv, D, max_blocks)) return 0;
   return size_t(B) * n * Hkv * max_blocks * sizeof(uint32_t) + 256;
 }
 
@@ -660,7 +668,7 @@ hipError_t launch_select_blocks(const void* q, const void* bounds, const int32_t
   p.B = B; p.n = n; p.Hq = Hq; p.Hkv = Hkv; p.G = Hq / Hkv; p.N = N; p.n_first = n_first; p.n_last = n_last;
   p.max_blocks = max_blocks; p.num_blocks = num_blocks; p.out = out;
   p.f32 = dt == MOLT_F32;
-  const size_t lds = fused_lds(n, p.G, D, max_blocks);
+  const size_t lds = fused_lds(B, n, p.G, Hkv, D, max_blocks);
   const bool fused = lds != 0;
   const int positions = score_positions(p.G);
   p.pos_groups = int((long(n) + positions - 1) / positions);
@@ -691,11 +699,17 @@ hipError_t launch_select_blocks(const void* q, const void* bounds, const int32_t
   if (hipError_t e = hipGetLastError()) return e;
   if (fused) return hipSuccess;
   const unsigned lists = unsigned(long(B) * n * Hkv);
-  const int per = (max_blocks + kPickThreads - 1) / kPickThreads;
-  if (per <= 4) pick_kernel<4><<<lists, kPickThreads, 0, s>>>(p);
-  else if (per <= 9) pick_kernel<9><<<lists, kPickThreads, 0, s>>>(p);
-  else if (per <= 16) pick_kernel<16><<<lists, kPickThreads, 0, s>>>(p);
-  else pick_kernel<0><<<lists, kPickThreads, 0, s>>>(p);
+  auto pick = [&](auto m, auto waves) {
+    constexpr int M = decltype(m)::value, W = decltype(waves)::value;
+    pick_kernel<M, W><<<lists, W * kWave, 0, s>>>(p);
+  };
+  // many lists: few wavefronts each, which wait less for each other; few: as many as shorten the list's own time
+  if (lists >= kManyLists && max_blocks <= 16 * 2 * kWave) pick(std::integral_constant<int, 16>{}, std::integral_constant<int, 2>{});
+  else if (lists >= kManyLists && max_blocks <= 16 * 4 * kWave) pick(std::integral_constant<int, 16>{}, std::integral_constant<int, 4>{});
+  else if (max_blocks <= 4 * 8 * kWave) pick(std::integral_constant<int, 4>{}, std::integral_constant<int, 8>{});
+  else if (max_blocks <= 9 * 8 * kWave) pick(std::integral_constant<int, 9>{}, std::integral_constant<int, 8>{});
+  else if (max_blocks <= 16 * 8 * kWave) pick(std::integral_constant<int, 16>{}, std::integral_constant<int, 8>{});
+  else pick(std::integral_constant<int, 0>{}, std::integral_constant<int, 8>{});
   return hipGetLastError();
 }
 

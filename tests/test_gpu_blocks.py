@@ -262,6 +262,52 @@ def test_select_of_lengths(molt_lib, dtype, B, n, maxb, N, first, last):
     _select_both(molt_lib, _queries(rng, B, n, 4, 64, dtype), bounds, tables, ctx, n, N, first, last, lens)
 
 
+@pytest.mark.parametrize("G", [1, 3, 8, 16])
+@pytest.mark.parametrize("B,n,maxb,N", [(150, 1, 60, 9), (70, 9, 20, 5), (260, 1, 130, 40), (9, 130, 33, 7)])
+def test_select_of_many_sequences(molt_lib, G, B, n, maxb, N):
+    """Launches of many workgroups, also by XCD with a number of sequences that 8 does not divide; a sample is checked
+    against the oracle, all rows against the same sequences in calls of their own."""
+    rng = np.random.default_rng(B)
+    H, D = 2, 64
+    bounds = _random_bounds(rng, B * maxb + 1, H, D, 2)
+    tables = rng.permutation(B * maxb).reshape(B, maxb).astype(np.int32)
+    ctx = rng.integers(0, 16 * maxb - n, B).astype(np.int32)
+    q = _queries(rng, B, n, G * H, D, "bf16")
+    gq, gb, gt, gc = q.cuda(), _t(bounds), _t(tables), _i32(ctx)
+    got = molt_lib.select_blocks(gq, gb, gt, gc, n - 1, N)
+    for b in range(0, B, 7):
+        one = molt_lib.select_blocks(gq[b * n:(b + 1) * n], gb, gt[b:b + 1], gc[b:b + 1], n - 1, N)
+        assert torch.equal(got[b * n:(b + 1) * n], one), b
+    b, j = B - 1, n - 1
+    want = ob.select(_val(q)[b * n + j:b * n + j + 1], bounds, tables[b:], [int(ctx[b]) + j], 1, N, 1, 2)
+    assert np.array_equal(got[b * n + j:].cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("B,H,maxb", [(260, 1, 1100), (2, 130, 2100), (260, 4, 2060), (260, 4, 4100), (1, 2, 5000)])
+def test_select_of_long_tables(molt_lib, B, H, maxb):
+    """One launch or two, many lists or few: against a sort of the scores, which are those of one dim here."""
+    rng = np.random.default_rng(maxb)
+    D, N = 64, 33
+    rec = np.zeros((maxb, H, 2 * D + 16), np.int8)
+    rec[:, :, 0] = rng.integers(-120, 121, (maxb, H))
+    rec[:, :, D] = rec[:, :, 0]
+    rec[:, :, 2 * D] = rng.integers(-3, 4, (maxb, H))
+    bounds = torch.from_numpy(rec.view(np.uint8)).cuda()
+    table = torch.randperm(maxb, dtype=torch.int32).cuda()
+    q = torch.zeros(B, H, D)
+    q[:, :, 0] = torch.from_numpy(rng.choice([-1.0, 1.0], (B, H)).astype(np.float32))
+    ctx = rng.integers(16 * 64, 16 * maxb, B).astype(np.int32)
+    got = molt_lib.select_blocks(q.cuda(), bounds, table.expand(B, maxb).contiguous(), _i32(ctx), 0, N).cpu().numpy()
+    value = (rec[:, :, 0].astype(float) * 2.0 ** rec[:, :, 2 * D])[table.cpu().numpy()]
+    for b in range(0, B, 13):
+        last = ctx[b] // 16
+        for h in range(H):
+            s = q[b, h, 0].item() * value[:last + 1, h]
+            s[0], s[last - 1:] = np.inf, np.inf
+            order = np.lexsort((np.arange(last + 1), -s))[:N]
+            assert np.array_equal(got[b, h], np.sort(order)), (b, h)
+
+
 @pytest.mark.parametrize("maxb", [30, 1500, 5000, 17000])
 def test_select_of_equal_scores(molt_lib, maxb):
     """Few different scores, many ties, all equal ones, zeros: the lowest blocks of them."""
