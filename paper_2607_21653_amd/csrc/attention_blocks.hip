@@ -266,7 +266,7 @@ MOLT_DEV void store4(float* p, floatx4_t x) { *reinterpret_cast<floatx4_t*>(p) =
 // Workgroup = one list (or a part of it) and 16 query rows; wavefronts take its units (pairs of blocks, or blocks) in
 // turn, a unit ahead in registers, with running softmaxes of their own, and join them in LDS.
 template <int D, typename T, int W, bool ONCE>
-__global__ __launch_bounds__(W* kWave, sizeof(T) == 2 ? 3 : 2) void blocks_attention_kernel(BlocksArgs p) {
+__global__ __launch_bounds__(W* kWave, W == 8 || sizeof(T) == 4 ? 2 : 3) void blocks_attention_kernel(BlocksArgs p) {
   typedef std::conditional_t<sizeof(T) == 2, PairBf16<D>, BlockF32<D>> Unit;
   constexpr int KB = Unit::kBlocks, PER = kWave / KB;                    // blocks of a unit; units that lanes hold
   constexpr int kAcc = D / 16 * kWave * 16;                              // a wavefront's O for the join
@@ -408,16 +408,20 @@ __global__ __launch_bounds__(256) void blocks_join_kernel(BlocksArgs p) {
   store4(static_cast<T*>(p.out) + at * D + d, o * inv);
 }
 
-constexpr int kWaves = 4;
-struct BlocksPlan { int row_groups, splits, per_split; };
+// How a call is launched. A list's time is that of its wavefronts' units one after the other (1.3 us each): few lists get 8
+// wavefronts each, and parts, joined by a second launch, up to one workgroup a CU (1 x 1 position, 4 kv heads: 128 blocks
+// 12.2 us, uncut 18.1; with 4 wavefronts and up to 3 parts a CU 12.5). More lists get 4 wavefronts, three workgroups to a
+// CU, and parts where these leave 8 units to a wavefront (16 x 5: 256 blocks 46.8 us, uncut 55.4; 64 blocks 22.5 and
+// 19.4). 64 x 1, 64 blocks: 8 wavefronts 24.7 us, 4 and parts 29.4.
+struct BlocksPlan { int row_groups, splits, per_split, waves; };
 BlocksPlan blocks_plan(int B, int n, int Hq, int Hkv, int N) {
   BlocksPlan pl{};
   const int units = (N + 1) / 2;
   pl.row_groups = (Hq / Hkv + 15) / 16;
   const long lists = long(B) * n * Hkv * pl.row_groups;
-  // as many parts as the chip holds at once (3 workgroups a CU), each of two units at least for a wavefront
-  const long want = std::max(1l, std::min(768 / lists, long(units) / (2 * kWaves)));
-  pl.per_split = int((units + want - 1) / want);
+  pl.waves = lists <= 256 ? 8 : 4;
+  const long parts = pl.waves == 8 ? std::min(256 / lists, long(units) / 8) : std::min(768 / lists, long(units) / 32);
+  pl.per_split = int((units + std::max(1l, parts) - 1) / std::max(1l, parts));
   pl.splits = (units + pl.per_split - 1) / pl.per_split;
   return pl;
 }
@@ -457,8 +461,14 @@ hipError_t launch_blocks_attention(const void* q, const void* kc, const void* vc
   auto go = [&](auto d, auto* t) {
     constexpr int DD = decltype(d)::value;
     typedef std::remove_pointer_t<decltype(t)> T;
-    if (once) blocks_attention_kernel<DD, T, kWaves, true><<<grid, kWaves * kWave, 0, s>>>(p);
-    else blocks_attention_kernel<DD, T, kWaves, false><<<grid, kWaves * kWave, 0, s>>>(p);
+    auto run = [&](auto w, auto o) {
+      constexpr int W = decltype(w)::value;
+      blocks_attention_kernel<DD, T, W, decltype(o)::value><<<grid, W * kWave, 0, s>>>(p);
+    };
+    typedef std::integral_constant<int, 4> Four;
+    typedef std::integral_constant<int, 8> Eight;
+    if (pl.waves == 4) once ? run(Four{}, std::true_type{}) : run(Four{}, std::false_type{});
+    else once ? run(Eight{}, std::true_type{}) : run(Eight{}, std::false_type{});
     if (p.splits > 1) blocks_join_kernel<DD, T><<<joins, 256, 0, s>>>(p);
   };
   auto by_dim = [&](auto* t) {
