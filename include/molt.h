@@ -317,7 +317,7 @@ int molt_paged_attention_kvq(const void* q, const void* k_cache, const void* v_c
  * sequences give entries n_shared[b] .. n_blocks[b] - 1 back behind the ring's last place, in
  * their order, and have n_blocks[b] = 0; what they give back is not taken in the same call. A
  * slot is -1 where the block's id is outside [0, num_blocks). The result does not depend on
- * timing. One launch for up to 1024 sequences and B n <= 8192, else two and a workspace.
+ * timing. One launch for up to 1024 sequences and B n <= 4096, else two and a workspace.
  *
  * molt_kv_write -- rows into a cache by slot: row r of k and v ([rows, n_kv_heads, D], rows k_stride
  * and v_stride elements apart) goes to token slots[r] % 16 of block slots[r] / 16; rows whose slot

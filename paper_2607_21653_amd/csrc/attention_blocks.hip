@@ -274,8 +274,10 @@ __global__ __launch_bounds__(W* kWave, W == 8 || sizeof(T) == 4 ? 2 : 3) void bl
   __shared__ float ml[W][2][16];
   const int lane = threadIdx.x % kWave, g = lane / 16, col = lane % 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  // all of a sequence's and kv head's lists on one XCD where that leaves none idle: neighbouring positions list much
-  // the same blocks
+  // all of a sequence's and kv head's lists on one XCD where that leaves none idle for long: neighbouring positions list
+  // much the same blocks (x 5 positions x 4 kv heads: 5 sequences 16.0 us, in the grid's order 21.5; 16 sequences 30.5
+  // and 50.6; 120 sequences 117 and 182; but 3 sequences 15.0 and 11.0). They read them at about the same time: lists
+  // begun at different places found less in the L2 cache (16 sequences 43)
   uint32_t item = blockIdx.x, bh;
   const uint32_t inner = uint32_t(p.n) * p.row_groups * p.splits;
   if (p.by_xcd) {
@@ -446,7 +448,7 @@ hipError_t launch_blocks_attention(const void* q, const void* kc, const void* vc
                                    hipStream_t s) {
   const BlocksPlan pl = blocks_plan(B, n, Hq, Hkv, N);
   const long bh = long(B) * Hkv;
-  const int by_xcd = n > 1 && (bh % 8 == 0 || bh >= 48);
+  const int by_xcd = n > 1 && (bh % 8 == 0 || bh >= 20);
   const bool once = n == 1 && pl.row_groups == 1;
   BlocksArgs p{q, kc, vc, bt, ctx, blocks, out, nullptr, nullptr, B, n, Hq, Hkv, Hq / Hkv, N, max_blocks, num_blocks,
                pl.row_groups, pl.splits, dt == MOLT_F32 ? 2 * pl.per_split : pl.per_split, by_xcd,

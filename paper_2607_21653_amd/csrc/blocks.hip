@@ -169,19 +169,39 @@ __global__ __launch_bounds__(kThreads) void plan_rows_kernel(PlanArgs p, uint32_
   if (r.back >= 0) plan_return(p, r, b, threadIdx.x, kThreads);
 }
 
-// One launch where it is enough for the slots
-bool plan_whole(int B, int n) { return B <= kPlanThreads && long(B) * n <= 8 * kPlanThreads; }
+// One launch where its threads have few slots each: 512 sequences x 5 rows 6.7 us, two launches 8.8; 1024 x 1 8.8 and 8.6;
+// 1024 x 5 10.3 and 8.7; 64 x 257 9.6 and 8.7
+bool plan_whole(int B, int n) { return B <= kPlanThreads && long(B) * n <= 4 * kPlanThreads; }
 
 // ---------------------------------------------------------------- rows by slot
 
 constexpr int kWriteRows = 16, kFewRows = 4;
-constexpr long kFewUnits = 16384;                // rows x 128 dims up to which rows count as few
+// Runs of a tile from which its rows go one by one (8000 rows in runs of 1 33.8 us, run by run 54.7)
+constexpr int kManyRuns = 5;
+// Rows x 128 dims up to which rows count as few. 4 kv heads x 128, bf16: 640 rows in runs of 5 4.7 us, by runs 9.7; 2048 rows
+// in runs of 5 8.9 and 11.4, of 1000 8.4 and 6.0; 4000 rows 14.4 and 13.6, 13.9 and 6.9
+constexpr long kFewUnits = 4096;
 
 // two elements of a row at any element alignment, as the bits that the cache holds
 typedef uint32_t UnalignedU1 __attribute__((aligned(2)));
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 typedef u32x2_t UnalignedU2 __attribute__((aligned(4)));
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+
+// Dims d and d + 1 of a row of k and v at a slot of the cache
+template <int D, typename T, typename Two>
+MOLT_DEV void store_row(T* kc, T* vc, int slot, int Hkv, int h, int d, Two x, Two y) {
+  const long rec = (long(slot / 16) * Hkv + h) * 16 * D;
+  *reinterpret_cast<Two*>(kc + rec + slot % 16 * D + d) = x;
+  T* out = vc + rec + d * 16 + slot % 16;
+  if constexpr (sizeof(T) == 2) {
+    out[0] = T(y);
+    out[16] = T(y >> 16);
+  } else {
+    out[0] = __uint_as_float(y[0]);
+    out[16] = __uint_as_float(y[1]);
+  }
+}
 
 // Wavefront = R rows of k and v and 128 dims: a head of 128 dims or two of 64; lane = two dims. The rows fall into
 // runs of consecutive slots of one block; a wavefront writes the runs that begin among its rows, up to their ends, one
@@ -208,7 +228,27 @@ __global__ __launch_bounds__(kThreads) void kv_write_kernel(const T* __restrict_
   const bool starts = good && lane > 0 && (slot % 16 == 0 || before != slot - 1);
   const uint32_t begin = uint32_t(__ballot(starts) >> 1), live = uint32_t(__ballot(good) >> 1);   // bit i: row r0 + i
   const bool there = h < Hkv;
-  for (uint32_t left = begin & ((1u << R) - 1); left; left &= left - 1) {
+  uint32_t left = begin & ((1u << R) - 1);
+  if (__builtin_popcount(left) >= kManyRuns) {   // all rows between the first run's and the last run's beginning
+    const int i0 = __builtin_ctz(left), i1 = 31 - __builtin_clz(left);
+    if (there) {
+      typedef std::conditional_t<sizeof(T) == 2, uint32_t, u32x2_t> Two;
+      typedef std::conditional_t<sizeof(T) == 2, UnalignedU1, UnalignedU2> UnalignedTwo;
+      Two x[R], y[R];
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const long r = r0 + min(max(i, i0), i1);
+        x[i] = *reinterpret_cast<const UnalignedTwo*>(k + r * k_stride + h * D + d);
+        y[i] = *reinterpret_cast<const UnalignedTwo*>(v + r * v_stride + h * D + d);
+      }
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+        if (i >= i0 && i < i1 && live >> i & 1)
+          store_row<D, T>(kc, vc, __builtin_amdgcn_readlane(slot, i + 1), Hkv, h, d, x[i], y[i]);
+    }
+    left = 1u << i1;
+  }
+  for (; left; left &= left - 1) {
     const int i = __builtin_ctz(left);
     const uint32_t stop = (begin | ~live) >> i >> 1;                     // what ends the run
     const int len = min(stop ? __builtin_ctz(stop) + 1 : 32, 16);
@@ -310,17 +350,7 @@ __global__ __launch_bounds__(kThreads) void kv_write_few_kernel(const T* __restr
   }
 #pragma unroll
   for (int i = 0; i < R; ++i) {
-    if (slot[i] < 0 || slot[i] / 16 >= num_blocks) continue;
-    const long rec = (long(slot[i] / 16) * Hkv + h) * 16 * D;
-    *reinterpret_cast<Two*>(kc + rec + slot[i] % 16 * D + d) = x[i];
-    T* out = vc + rec + d * 16 + slot[i] % 16;
-    if constexpr (sizeof(T) == 2) {
-      out[0] = T(y[i]);
-      out[16] = T(y[i] >> 16);
-    } else {
-      out[0] = __uint_as_float(y[i][0]);
-      out[16] = __uint_as_float(y[i][1]);
-    }
+    if (slot[i] >= 0 && slot[i] / 16 < num_blocks) store_row<D, T>(kc, vc, slot[i], Hkv, h, d, x[i], y[i]);
   }
 }
 

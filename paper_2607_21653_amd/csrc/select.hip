@@ -416,7 +416,8 @@ MOLT_DEV void emit(int m, Key key, const Border& b, int32_t* out, int first, int
 }
 
 // A workgroup's place: sequence, kv head, position group and chunk of blocks. A sequence's heads, whose records lie side
-// by side, run on one XCD where that leaves none idle.
+// by side, run on one XCD where that leaves none idle for long (x 5 positions: 17 sequences, 2000 blocks 24.1 us, in the
+// grid's order 25.9; 47, 600 blocks 25.8 and 30.4; but 4, 2000 blocks 13.4 and 12.8; x 1: 9, 1500 blocks 14.0 and 12.2).
 struct Item { int b, h, group, chunk; };
 MOLT_DEV Item item_of(const SelectArgs& p) {
   uint32_t at = blockIdx.x;
@@ -622,7 +623,7 @@ __global__ __launch_bounds__(kPickWaves* kWave) void pick_kernel(SelectArgs p) {
   for (int x = min(int(r.some), p.N) + int(threadIdx.x); x < p.N; x += kPickThreads) out[x] = -1;
 }
 
-constexpr unsigned kManyLists = 1024;
+constexpr unsigned kManyLists = 256;
 int padded_rows(int G) { return G <= 4 ? 4 : G <= 8 ? 8 : 16; }
 int score_positions(int G) { return G > 16 ? 1 : 64 / padded_rows(G); }
 
@@ -674,7 +675,7 @@ hipError_t launch_select_blocks(const void* q, const void* bounds, const int32_t
   p.pos_groups = int((long(n) + positions - 1) / positions);
   p.chunks = 1;
   p.block_bytes = uint32_t(Hkv) * (2 * D + 16);
-  p.by_xcd = B % 8 == 0 || B >= 48;
+  p.by_xcd = B % 8 == 0 || B >= 16;
   if (!fused) {
     p.chunk = score_chunk(B, n, p.G, Hkv, max_blocks);
     p.chunks = (max_blocks + p.chunk - 1) / p.chunk;
@@ -704,6 +705,8 @@ hipError_t launch_select_blocks(const void* q, const void* bounds, const int32_t
     pick_kernel<M, W><<<lists, W * kWave, 0, s>>>(p);
   };
   // many lists: few wavefronts each, which wait less for each other; few: as many as shorten the list's own time
+  // (x 5 positions x 4 kv heads, 2200 blocks: 128 sequences 104.7 us, with 8 wavefronts 112.4, 16 sequences 24.5 and
+  // 24.8; 2 x 4 x 4, 2000 blocks 13.8 and 12.1)
   if (lists >= kManyLists && max_blocks <= 16 * 2 * kWave) pick(std::integral_constant<int, 16>{}, std::integral_constant<int, 2>{});
   else if (lists >= kManyLists && max_blocks <= 16 * 4 * kWave) pick(std::integral_constant<int, 16>{}, std::integral_constant<int, 4>{});
   else if (max_blocks <= 4 * 8 * kWave) pick(std::integral_constant<int, 4>{}, std::integral_constant<int, 8>{});

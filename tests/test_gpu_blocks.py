@@ -126,6 +126,39 @@ def test_write(molt_lib, dtype, H, D):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,D", [(4, 128), (3, 64)])
+def test_write_of_many_rows(molt_lib, dtype, H, D):
+    """Whole and partial blocks, single rows, runs of two to four, holes among them, and changes between these at any
+    row of a tile of 16."""
+    rng = np.random.default_rng(7 * D + H)
+    nb = 700
+    order, slots, at = rng.permutation(nb), [], 0
+    while at + 20 < nb:
+        kind = int(rng.integers(5))
+        if kind == 0:                                     # blocks in a row, the first from its middle
+            slots += [int(order[at]) * 16 + t for t in range(int(rng.integers(16)), 16)]
+            slots += [int(b) * 16 + t for b in order[at + 1:at + 3] for t in range(16)]
+            at += 3
+        else:
+            longest = (1, 1, 4, 16)[kind - 1]
+            for b in order[at:at + 20]:
+                first = int(rng.integers(16))
+                slots += [int(b) * 16 + t for t in range(first, min(16, first + int(rng.integers(1, longest + 1))))]
+                if kind == 2 and rng.integers(3) == 0:
+                    slots += [-1] * int(rng.integers(1, 4))
+            at += 20
+    slots += [-1] * (12000 // H - len(slots))  # enough rows for the kernel of many
+    T = len(slots)
+    kc, vc = _cache(rng, nb, H, D, dtype)
+    k, v = (torch.from_numpy(rng.standard_normal((T, H, D)).astype(np.float32)).to(DT[dtype]) for _ in range(2))
+    gk, gv = kc.cuda(), vc.cuda()
+    molt_lib.kv_write(k.cuda(), v.cuda(), gk, gv, _i32(slots))
+    wk, wv = _val(kc), _val(vc)
+    ob.write_rows(_val(k), _val(v), wk, wv, slots)
+    assert np.array_equal(_val(gk), wk) and np.array_equal(_val(gv), wv)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_write_of_rows_at_any_element(molt_lib, dtype):
     rng = np.random.default_rng(5)
     H, D, T = 2, 64, 21
