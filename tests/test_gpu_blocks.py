@@ -296,7 +296,7 @@ def test_select_of_lengths(molt_lib, dtype, B, n, maxb, N, first, last):
 
 
 @pytest.mark.parametrize("G", [1, 3, 8, 16])
-@pytest.mark.parametrize("B,n,maxb,N", [(150, 1, 60, 9), (70, 9, 20, 5), (260, 1, 130, 40), (9, 130, 33, 7)])
+@pytest.mark.parametrize("B,n,maxb,N", [(150, 1, 60, 9), (70, 9, 20, 5), (260, 1, 130, 40), (9, 130, 33, 7), (17, 3, 500, 30)])
 def test_select_of_many_sequences(molt_lib, G, B, n, maxb, N):
     """Launches of many workgroups, also by XCD with a number of sequences that 8 does not divide; a sample is checked
     against the oracle, all rows against the same sequences in calls of their own."""
@@ -316,7 +316,7 @@ def test_select_of_many_sequences(molt_lib, G, B, n, maxb, N):
     assert np.array_equal(got[b * n + j:].cpu().numpy(), want)
 
 
-@pytest.mark.parametrize("B,H,maxb", [(260, 1, 1100), (2, 130, 2100), (260, 4, 2060), (260, 4, 4100), (1, 2, 5000)])
+@pytest.mark.parametrize("B,H,maxb", [(260, 1, 1100), (2, 130, 2100), (260, 4, 2060), (260, 4, 4100), (1, 2, 4000), (1, 2, 5000)])
 def test_select_of_long_tables(molt_lib, B, H, maxb):
     """One launch or two, many lists or few: against a sort of the scores, which are those of one dim here."""
     rng = np.random.default_rng(maxb)
@@ -412,7 +412,9 @@ def _attend_both(molt, q, kc, vc, tables, ctx, n, lists, dtype, **kw):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("B,n,H,G,D,N,maxb", [(1, 1, 1, 1, 64, 1, 1), (2, 3, 2, 4, 128, 5, 9), (3, 1, 4, 8, 128, 16, 30),
                                               (1, 2, 2, 7, 64, 33, 60), (2, 5, 1, 16, 128, 8, 20), (1, 1, 2, 17, 64, 12, 20),
-                                              (1, 3, 1, 80, 128, 7, 10), (1, 1, 1, 8, 128, 300, 400), (1, 2, 4, 2, 64, 130, 200)])
+                                              (1, 3, 1, 80, 128, 7, 10), (1, 1, 1, 8, 128, 300, 400), (1, 2, 4, 2, 64, 130, 200),
+                                              (7, 9, 3, 2, 64, 12, 20), (33, 3, 3, 8, 128, 24, 30), (20, 5, 3, 1, 64, 130, 140),
+                                              (90, 1, 3, 2, 128, 9, 12)])
 def test_attention(molt_lib, dtype, B, n, H, G, D, N, maxb):
     rng = np.random.default_rng(N)
     nb = B * maxb + 2
