@@ -295,64 +295,48 @@ MOLT_DEV uint32_t wave_max_u32(uint32_t v) {
 }
 
 // The border of the N largest keys: keys >= lo are in, and of those equal to `equal_key` (if `equal` > 0) the first
-// `equal`. It is searched between the smallest and the largest key, three borders at a time, which ends as soon as just
-// N keys are not below one; only where equal keys straddle the border does it run down to that key.
+// `equal`. It is searched between the smallest and the largest key, by the counts of 256 parts of what is left, which ends as
+// soon as just N keys are not below a part's start; only where equal keys straddle the border does it run down to that key.
 struct Border { uint32_t lo, equal_key; int equal; };
+constexpr int kBins = 4 * kWave;
 
-// A step of the search: more than N keys are >= lo (c_lo of them), fewer than N are >= hi (c_hi); or N are >= lo
+// More than N keys are >= lo (c_lo of them), fewer than N are >= hi (c_hi); or N are >= lo
 struct Search {
   uint32_t lo, hi;
   int c_lo, c_hi;
   bool exact;
-  // counts of keys >= each of the three borders, from `count`
-  template <typename Count>
-  MOLT_DEV void step(int N, Count count) {
-    const uint32_t w = max((hi - lo) / 4, 1u), b0 = lo + w, b1 = b0 + w, b2 = b1 + w;
-    const Four c = count(b0, b1, b2);
-    const int c0 = int(c.x[0]), c1 = int(c.x[1]), c2 = int(c.x[2]);
-    exact = c0 == N || c1 == N || c2 == N;
-    if (exact) lo = c0 == N ? b0 : c1 == N ? b1 : b2;
-    else if (c0 < N) { hi = b0; c_hi = c0; }
-    else if (c1 < N) { lo = b0; c_lo = c0; hi = b1; c_hi = c1; }
-    else if (c2 < N) { lo = b1; c_lo = c1; hi = b2; c_hi = c2; }
-    else { lo = b2; c_lo = c2; }                 // (a border past hi has fewer than N keys)
-  }
   MOLT_DEV bool done() const { return exact || hi - lo <= 1; }
+  MOLT_DEV int shift() const { return max(24 - __builtin_clz(hi - lo - 1), 0); }     // a part's size
+  MOLT_DEV void add(uint32_t* bins, int shift, uint32_t key) const {
+    if (key >= lo && key < hi) atomicAdd(&bins[(key - lo) >> shift], 1u);
+  }
+  // to the part that the border is in (16-byte aligned bins)
+  MOLT_DEV void narrow(const uint32_t* bins, int shift, int N, int lane) {
+    const u32x4_t b = reinterpret_cast<const u32x4_t*>(bins)[lane];
+    const int upto = wave_scan_dpp(int(b[0] + b[1] + b[2] + b[3]));
+    // keys from the start of each of the lane's parts on
+    const int c3 = c_lo - upto + int(b[3]), c2 = c3 + int(b[2]), c1 = c2 + int(b[1]), c0 = c1 + int(b[0]);
+    const int l = 63 - __builtin_clzll(__ballot(c0 >= N));                           // (lane 0's are c_lo)
+    const int u = c3 >= N ? 3 : c2 >= N ? 2 : c1 >= N ? 1 : 0;
+    const int from = c3 >= N ? c3 : c2 >= N ? c2 : c1 >= N ? c1 : c0;
+    const int here = int(c3 >= N ? b[3] : c2 >= N ? b[2] : c1 >= N ? b[1] : b[0]);
+    lo += uint32_t(__builtin_amdgcn_readlane(4 * lane + u, l)) << shift;
+    if (hi - lo > 1u << shift) hi = lo + (1u << shift);
+    c_lo = __builtin_amdgcn_readlane(from, l);
+    c_hi = c_lo - __builtin_amdgcn_readlane(here, l);
+    exact = c_lo == N;
+  }
   MOLT_DEV Border border(int N) const {
     if (exact) return {lo, 0u, 0};
     return {lo + 1, lo, N - c_hi};
   }
 };
-// The rest of the search by one wavefront that has all keys but `others` larger ones, M a lane. Once no more than 32 are
-// between the borders they go to a lane each (through LDS, room for 32, 16-byte aligned), which counts those above its own:
-// few keys lie close together now and then, and the borders would take many more steps to part them.
+// The end of a search, once no more than 32 keys are between the borders: few keys lie close together now and then, and
+// parting them would take many more steps. They go to a lane each (room: these keys, then 0; 16-byte aligned), which
+// counts those above its own.
 constexpr int kRoom = 32;
-template <int M>
-MOLT_DEV Border wave_search(Search s, const uint32_t (&key)[M], int others, int N, uint32_t* room, int lane) {
-  while (!s.done() && s.c_lo - s.c_hi > kRoom)
-    s.step(N, [&](uint32_t b0, uint32_t b1, uint32_t b2) __attribute__((always_inline)) {
-      Four c{{0, 0, 0, 0}};
-#pragma unroll
-      for (int i = 0; i < M; ++i) {
-        c.x[0] += key[i] >= b0;
-        c.x[1] += key[i] >= b1;
-        c.x[2] += key[i] >= b2;
-      }
-      c = wave_sum4<true>(c);
-      return Four{{c.x[0] + others, c.x[1] + others, c.x[2] + others, 0}};
-    });
-  if (s.done()) return s.border(N);
-  const unsigned long long below = (1ull << lane) - 1;
-  int at = 0;
-  if (lane < kRoom) room[lane] = 0;              // (keys above 0 only are counted)
-#pragma unroll
-  for (int i = 0; i < M; ++i) {
-    const bool in = key[i] >= s.lo && key[i] < s.hi;
-    const unsigned long long mask = __ballot(in);
-    if (in) room[at + __popcll(mask & below)] = key[i];
-    at += __popcll(mask);
-  }
-  const uint32_t mine = lane < at ? room[lane] : ~0u;
+MOLT_DEV Border rank_room(const Search& s, const uint32_t* room, int N, int lane) {
+  const uint32_t own = lane < kRoom ? room[lane] : 0u, mine = own ? own : ~0u;
   int above = s.c_hi, with = s.c_hi;             // keys above the lane's, and those with the equal ones
 #pragma unroll
   for (int i = 0; i < kRoom / 4; ++i) {
@@ -363,11 +347,40 @@ MOLT_DEV Border wave_search(Search s, const uint32_t (&key)[M], int others, int 
       with += k[u] >= mine;
     }
   }
-  const int l = __builtin_ctzll(__ballot(lane < at && above < N && with >= N));   // one there is, and equal ones
+  const int l = __builtin_ctzll(__ballot(own != 0 && above < N && with >= N));       // one there is, and equal ones
   const uint32_t k = uint32_t(__builtin_amdgcn_readlane(int(mine), l));
   above = __builtin_amdgcn_readlane(above, l);
   if (__builtin_amdgcn_readlane(with, l) == N) return {k, 0u, 0};
   return {k + 1, k, N - above};
+}
+// A search by one wavefront that has all keys, M a lane
+struct SearchLds { uint32_t bins[kBins], room[kRoom]; };
+template <int M>
+MOLT_DEV Border wave_search(Search s, const uint32_t (&key)[M], int N, SearchLds& lds, int lane) {
+  while (!s.done() && s.c_lo - s.c_hi > kRoom) {
+    const int shift = s.shift();
+    reinterpret_cast<u32x4_t*>(lds.bins)[lane] = u32x4_t{0, 0, 0, 0};
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < M; ++i) s.add(lds.bins, shift, key[i]);
+    __builtin_amdgcn_wave_barrier();
+    s.narrow(lds.bins, shift, N, lane);
+    __builtin_amdgcn_wave_barrier();
+  }
+  if (s.done()) return s.border(N);
+  const unsigned long long below = (1ull << lane) - 1;
+  int at = 0;
+  if (lane < kRoom) lds.room[lane] = 0;
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int i = 0; i < M; ++i) {
+    const bool in = key[i] >= s.lo && key[i] < s.hi;
+    const unsigned long long mask = __ballot(in);
+    if (in) lds.room[at + __popcll(mask & below)] = key[i];
+    at += __popcll(mask);
+  }
+  __builtin_amdgcn_wave_barrier();
+  return rank_room(s, lds.room, N, lane);
 }
 
 // What the keys of m per lane are: how many, how many that a list holds anyway, the largest of the others and of their
@@ -453,7 +466,8 @@ __global__ __launch_bounds__(kThreads, 4) void select_kernel(SelectArgs p) {
   const int end = counted > 0 ? visible_blocks(p, it.b, j0 + counted - 1) : 0;
   score_blocks<D, GP>(p, it.b, it.h, j0, 0, end, wave, lane, lds, keys, p.max_blocks);
   __syncthreads();
-  uint32_t(*room)[kRoom] = reinterpret_cast<uint32_t(*)[kRoom]>(dyn);    // the records' place
+  SearchLds* of_wave = reinterpret_cast<SearchLds*>(dyn);                // the records' place
+  static_assert(sizeof(ScoreLds<D>) >= kWaves * sizeof(SearchLds));
   for (int i = wave; i < here; i += kWaves) {
     const int seen = visible_blocks(p, it.b, j0 + i);
     int32_t* out = p.out + ((long(it.b) * p.n + j0 + i) * p.Hkv + it.h) * p.N;
@@ -473,7 +487,7 @@ __global__ __launch_bounds__(kThreads, 4) void select_kernel(SelectArgs p) {
       if (int(n.x[0]) > p.N) {
         r = Range{n.x[0], n.x[1], wave_max_u32(r.top), wave_max_u32(r.low)};
         if (int(r.held) == p.N) border.lo = kKeyHeld;
-        else border = wave_search<M>(search_of(r, p.N), key, 0, p.N, room[wave], lane);
+        else border = wave_search<M>(search_of(r, p.N), key, p.N, of_wave[wave], lane);
       }
       emit(M, at, border, out, 0, lane, 0, 0);
       for (int x = min(int(n.x[0]), p.N) + lane; x < p.N; x += kWave) out[x] = -1;
@@ -500,16 +514,13 @@ __global__ __launch_bounds__(kThreads, 4) void score_kernel(SelectArgs p) {
                       p.keys + ((long(it.b) * p.n + j0) * p.Hkv + it.h) * p.max_blocks + c0, long(p.Hkv) * p.max_blocks);
 }
 
-// .. and a workgroup a list, M keys to a thread (0: of tables of any size, the keys read again for each count). Once few
-// keys lie between the borders they go to LDS, and every wavefront ends the search by itself.
-constexpr int kFew = 8 * kWave;
+// .. and a workgroup a list, M keys to a thread (0: of tables of any size, the keys read again for each count)
 template <int M, int kPickWaves>
 __global__ __launch_bounds__(kPickWaves* kWave) void pick_kernel(SelectArgs p) {
   constexpr int kPickThreads = kPickWaves * kWave;
   __shared__ Four part[2][kPickWaves];
-  __shared__ uint32_t few[kFew];
-  __shared__ __attribute__((aligned(16))) uint32_t room[kPickWaves][kRoom];
-  __shared__ int n_few;
+  __shared__ __attribute__((aligned(16))) uint32_t bins[3][kBins], room[kRoom];
+  __shared__ int n_room;
   const long list = blockIdx.x;
   const int t = int(list / p.Hkv), b = t / p.n, j = t % p.n, lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -521,7 +532,9 @@ __global__ __launch_bounds__(kPickWaves* kWave) void pick_kernel(SelectArgs p) {
     const int i = first + x * kWave + lane;
     key[x] = i < p.max_blocks ? keys[i] : 0u;
   }
-  if (threadIdx.x == 0) n_few = 0;
+  if (threadIdx.x == 0) n_room = 0;
+  if (threadIdx.x < kRoom) room[threadIdx.x] = 0;
+  for (int x = threadIdx.x; x < kBins; x += kPickThreads) bins[0][x] = 0;
   const int seen = visible_blocks(p, b, j);
 #pragma unroll
   for (int x = 0; x < M; ++x) {
@@ -543,15 +556,6 @@ __global__ __launch_bounds__(kPickWaves* kWave) void pick_kernel(SelectArgs p) {
     if (lane == 0) part[turn][wave] = c;
     __syncthreads();
   };
-  auto sum = [&](const Four& c) {
-    exchange(c);
-    Four all{{0, 0, 0, 0}};
-#pragma unroll
-    for (int w = 0; w < kPickWaves; ++w)
-#pragma unroll
-      for (int u = 0; u < 4; ++u) all.x[u] += part[turn][w].x[u];
-    return all;
-  };
   Range r = range_of(m, at);
   const Four n = wave_sum4<M != 0>(Four{{r.some, r.held, 0, 0}});
   exchange(Four{{n.x[0], n.x[1], wave_max_u32(r.top), wave_max_u32(r.low)}});
@@ -567,18 +571,15 @@ __global__ __launch_bounds__(kPickWaves* kWave) void pick_kernel(SelectArgs p) {
     if (int(r.held) == p.N) {
       border.lo = kKeyHeld;
     } else {
-      while (!s.done() && s.c_lo - s.c_hi > kFew)
-        s.step(p.N, [&](uint32_t b0, uint32_t b1, uint32_t b2) __attribute__((always_inline)) {
-          Four c{{0, 0, 0, 0}};
+      for (int now = 0; !s.done() && s.c_lo - s.c_hi > kRoom;) {         // three sets of bins in turn: one barrier a step
+        const int next = now == 2 ? 0 : now + 1, shift = s.shift();
+        for (int x = threadIdx.x; x < kBins; x += kPickThreads) bins[next][x] = 0;
 #pragma unroll
-          for (int x = 0; x < m; ++x) {
-            const uint32_t k = at(x);
-            c.x[0] += k >= b0;
-            c.x[1] += k >= b1;
-            c.x[2] += k >= b2;
-          }
-          return sum(wave_sum4<M != 0>(c));
-        });
+        for (int x = 0; x < m; ++x) s.add(bins[now], shift, at(x));
+        __syncthreads();
+        s.narrow(bins[now], shift, p.N, lane);
+        now = next;
+      }
       if (!s.done()) {
         int mine = 0;
 #pragma unroll
@@ -588,18 +589,15 @@ __global__ __launch_bounds__(kPickWaves* kWave) void pick_kernel(SelectArgs p) {
         }
         const int upto = wave_scan_dpp(mine);
         int to = 0;                              // (the wavefronts in any order: the keys are counted only)
-        if (lane == kWave - 1 && upto) to = atomicAdd(&n_few, upto);
+        if (lane == kWave - 1 && upto) to = atomicAdd(&n_room, upto);
         to = __builtin_amdgcn_readlane(to, kWave - 1) + upto - mine;
 #pragma unroll
         for (int x = 0; x < m; ++x) {
           const uint32_t k = at(x);
-          if (k >= s.lo && k < s.hi) few[to++] = k;
+          if (k >= s.lo && k < s.hi) room[to++] = k;
         }
         __syncthreads();
-        uint32_t some[kFew / kWave];
-#pragma unroll
-        for (int x = 0; x < kFew / kWave; ++x) some[x] = x * kWave + lane < n_few ? few[x * kWave + lane] : 0u;
-        border = wave_search<kFew / kWave>(s, some, s.c_hi, p.N, room[wave], lane);
+        border = rank_room(s, room, p.N, lane);
       } else {
         border = s.border(p.N);
       }
