@@ -15,7 +15,7 @@ namespace {
 
 constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * kWave;
-constexpr size_t kFusedLds = 112 << 10;          // 128 x 5 positions, 2000 blocks: 80.3 us, in two launches 84.6
+constexpr size_t kFusedLds = 112 << 10;          // 128 x 5 positions, 2000 blocks: 76.5 us, in two launches 81.6
 
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t UnalignedU4 __attribute__((ext_vector_type(4), aligned(2)));
@@ -626,9 +626,10 @@ int padded_rows(int G) { return G <= 4 ? 4 : G <= 8 ? 8 : 16; }
 int score_positions(int G) { return G > 16 ? 1 : 64 / padded_rows(G); }
 
 // LDS of a call in one launch; 0 where it takes two. One launch is the faster one where it makes a workgroup for every CU
-// (64 sequences x 1 position, 4 kv heads x 128: 600 blocks 15.9 us, two launches 18.5; 1300 blocks 27.7 and 28.6; 128 x 5:
-// 27.0 and 50.3, 47.8 and 68.7), and else for tables so short that one workgroup is done with them before a second launch
-// would begin (1 x 1: 300 blocks 8.9 and 10.7, 600 blocks 12.0 and 11.1).
+// (64 sequences x 1 position, 4 kv heads x 128: 600 blocks 15.2 us, two launches 19.2; 1300 blocks 26.0 and 28.5; 128 x 5:
+// 25.9 and 37.2, 44.9 and 56.0), and else for tables so short that one workgroup is done with them before a second launch
+// would begin (1 x 1: 300 blocks 8.1 and 9.3, 600 blocks 10.9 and 9.7; 16 x 5: 400 blocks 11.3 and 13.2, 600 blocks 14.1
+// and 13.6).
 size_t fused_lds(int B, int n, int G, int Hkv, int D, int max_blocks) {
   const long groups = long(B) * Hkv * ((long(n) + score_positions(G) - 1) / score_positions(G));
   if (max_blocks > (groups >= 256 ? kFusedBlocks : 448)) return 0;
@@ -637,12 +638,14 @@ size_t fused_lds(int B, int n, int G, int Hkv, int D, int max_blocks) {
   return bytes <= kFusedLds ? bytes : 0;
 }
 
-// Blocks of a workgroup of a call in two launches: two rounds of 256 where that still makes a workgroup for every CU
-// (16 sequences x 5 positions at 32768-65536: 28.4 us; with one round 30.1, three 30.6, four 33.4)
+// Blocks of a workgroup of a call in two launches: as many rounds of 256 as leave workgroups enough (x 5 positions, 4 kv
+// heads; 1, 2, 3, 4 rounds: 16 sequences at 32768-65536 26.5 us, 24.9, 26.9, 29.7; 2, 4, 8: 32, 4000 blocks 41.5, 38.9, 39.7;
+// 128, 4000 blocks 164, 157, 157; 32, 2200 blocks 31.9, 32.4, 35.4)
 int score_chunk(int B, int n, int G, int Hkv, int max_blocks) {
   const long groups = long(B) * Hkv * ((long(n) + score_positions(G) - 1) / score_positions(G));
   constexpr int round = 32 * kWaves;
-  return groups * ((max_blocks + 2 * round - 1) / (2 * round)) >= 256 ? 2 * round : round;
+  auto made = [&](int rounds) { return groups * ((long(max_blocks) + rounds * round - 1) / (rounds * round)); };
+  return made(4) >= 512 ? 4 * round : made(2) >= 256 ? 2 * round : round;
 }
 
 }  // namespace
@@ -703,8 +706,8 @@ hipError_t launch_select_blocks(const void* q, const void* bounds, const int32_t
     pick_kernel<M, W><<<lists, W * kWave, 0, s>>>(p);
   };
   // many lists: few wavefronts each, which wait less for each other; few: as many as shorten the list's own time
-  // (x 5 positions x 4 kv heads, 2200 blocks: 128 sequences 104.7 us, with 8 wavefronts 112.4, 16 sequences 24.5 and
-  // 24.8; 2 x 4 x 4, 2000 blocks 13.8 and 12.1)
+  // (x 5 positions x 4 kv heads, 2200 blocks: 128 sequences 99.9 us, with 8 wavefronts 105, 16 sequences 23.1 and 22.8,
+  // 8 sequences 15.6 and 14.3)
   if (lists >= kManyLists && max_blocks <= 16 * 2 * kWave) pick(std::integral_constant<int, 16>{}, std::integral_constant<int, 2>{});
   else if (lists >= kManyLists && max_blocks <= 16 * 4 * kWave) pick(std::integral_constant<int, 16>{}, std::integral_constant<int, 4>{});
   else if (max_blocks <= 4 * 8 * kWave) pick(std::integral_constant<int, 4>{}, std::integral_constant<int, 8>{});
