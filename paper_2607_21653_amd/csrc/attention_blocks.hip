@@ -265,6 +265,11 @@ MOLT_DEV void store4(float* p, floatx4_t x) { *reinterpret_cast<floatx4_t*>(p) =
 
 // Workgroup = one list (or a part of it) and 16 query rows; wavefronts take its units (pairs of blocks, or blocks) in
 // turn, a unit ahead in registers, with running softmaxes of their own, and join them in LDS.
+// What bounds it goes by how much the lists share. 128 sequences x 1 position, 64 blocks of 4 kv heads x 128 (268 MB, none
+// shared): 47 us, memory at 5.8 TB/s. 16 x 5, 128 blocks: 38 us, 335 MB through the L2 caches of which 176 come from memory
+// (4.6 TB/s). 2 x 257, 64 blocks: 58 us, 1.08 GB from L2 at 18 TB/s, its compute (VALU 35%, MFMA 16%, LDS 39% of the time
+// busy) partly beside it. Positions in pairs over the union of their lists, 1.4 times a list's length, took longer: the
+// union cost 4 us a workgroup.
 template <int D, typename T, int W, bool ONCE>
 __global__ __launch_bounds__(W* kWave, W == 8 || sizeof(T) == 4 ? 2 : 3) void blocks_attention_kernel(BlocksArgs p) {
   typedef std::conditional_t<sizeof(T) == 2, PairBf16<D>, BlockF32<D>> Unit;
@@ -387,7 +392,7 @@ __global__ __launch_bounds__(W* kWave, W == 8 || sizeof(T) == 4 ? 2 : 3) void bl
   }
 }
 
-// Joins the parts of split lists: thread = 4 dims of a query row
+// Joins the parts of split lists: thread = 4 dims of a query row (16 x 5 positions, 32 heads x 128, two parts: 4.8 us)
 template <int D, typename T>
 __global__ __launch_bounds__(256) void blocks_join_kernel(BlocksArgs p) {
   const long at = (long(blockIdx.x) * 256 + threadIdx.x) / (D / 4);
@@ -414,7 +419,8 @@ __global__ __launch_bounds__(256) void blocks_join_kernel(BlocksArgs p) {
 // wavefronts each, and parts, joined by a second launch, up to one workgroup a CU (1 x 1 position, 4 kv heads: 128 blocks
 // 12.2 us, uncut 18.1; with 4 wavefronts and up to 3 parts a CU 12.5). More lists get 4 wavefronts, three workgroups to a
 // CU, and parts where these leave 8 units to a wavefront (16 x 5: 256 blocks 46.8 us, uncut 55.4; 64 blocks 22.5 and
-// 19.4). 64 x 1, 64 blocks: 8 wavefronts 24.7 us, 4 and parts 29.4.
+// 19.4). 64 x 1, 64 blocks: 8 wavefronts 24.7 us, 4 and parts 29.4. ONCE, loads that leave the caches alone, where no other
+// workgroup reads a list's blocks: 256 x 1, 64 blocks 87 us, with ordinary loads 99; but 2 x 257 77 and 68.
 struct BlocksPlan { int row_groups, splits, per_split, waves; };
 BlocksPlan blocks_plan(int B, int n, int Hq, int Hkv, int N) {
   BlocksPlan pl{};
@@ -459,7 +465,8 @@ hipError_t launch_blocks_attention(const void* q, const void* kc, const void* vc
     p.part_o = c.take<float>(rows * 16 * D);
     p.part_ml = c.take<float>(rows * 16 * 2);
   }
-  const unsigned grid = unsigned((by_xcd ? (bh + 7) / 8 * 8 : bh) * n * pl.row_groups * pl.splits), joins = unsigned((long(B) * n * Hq * (D / 4) + 255) / 256);
+  const unsigned grid = unsigned((by_xcd ? (bh + 7) / 8 * 8 : bh) * n * pl.row_groups * pl.splits);
+  const unsigned joins = unsigned((long(B) * n * Hq * (D / 4) + 255) / 256);
   auto go = [&](auto d, auto* t) {
     constexpr int DD = decltype(d)::value;
     typedef std::remove_pointer_t<decltype(t)> T;

@@ -3,6 +3,10 @@
 // with the row's codes c (8 bits) and the block's bounds hi, lo (bounds_format.h). With c+ = max(c, 0) and c- = min(c, 0)
 // the sum is c+ . hi + c- . lo, one product over 2 D whole numbers: 8-bit MFMAs, exact, and so is its scaling. Which
 // blocks are the largest then depends on no order of summation.
+//
+// Bound by the records' bytes (2 D + 1 a block and kv head, read once for all of a position group's rows) and by the chain of
+// id, record, product, search: 128 sequences x 5 positions at 8192, 4 kv heads x 128 (74 MB) 23.4 us, 3.1 TB/s; 16 x 5 at
+// 32768-65536 (51 MB) 16.4 us for the scores and 8.6 for the lists; one position 7.1 us.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
