@@ -268,8 +268,8 @@ MOLT_DEV void store4(float* p, floatx4_t x) { *reinterpret_cast<floatx4_t*>(p) =
 // What bounds it goes by how much the lists share. 128 sequences x 1 position, 64 blocks of 4 kv heads x 128 (268 MB, none
 // shared): 47 us, memory at 5.8 TB/s. 16 x 5, 128 blocks: 38 us, 335 MB through the L2 caches of which 176 come from memory
 // (4.6 TB/s). 2 x 257, 64 blocks: 58 us, 1.08 GB from L2 at 18 TB/s, its compute (VALU 35%, MFMA 16%, LDS 39% of the time
-// busy) partly beside it. Positions in pairs over the union of their lists, 1.4 times a list's length, took longer: the
-// union cost 4 us a workgroup.
+// busy) partly beside it. Positions in pairs over the union of their lists, 1.4 times a list's length, took 55 us there, but
+// 7.5 in place of 5.2 for 4 x 3 positions and 130 or more in place of 122 for 128 x 5 whose lists share less.
 template <int D, typename T, int W, bool ONCE>
 __global__ __launch_bounds__(W* kWave, W == 8 || sizeof(T) == 4 ? 2 : 3) void blocks_attention_kernel(BlocksArgs p) {
   typedef std::conditional_t<sizeof(T) == 2, PairBf16<D>, BlockF32<D>> Unit;
