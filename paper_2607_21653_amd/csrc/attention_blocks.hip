@@ -419,7 +419,8 @@ __global__ __launch_bounds__(256) void blocks_join_kernel(BlocksArgs p) {
 // wavefronts each, and parts, joined by a second launch, up to one workgroup a CU (1 x 1 position, 4 kv heads: 128 blocks
 // 12.2 us, uncut 18.1; with 4 wavefronts and up to 3 parts a CU 12.5). More lists get 4 wavefronts, three workgroups to a
 // CU, and parts where these leave 8 units to a wavefront (16 x 5: 256 blocks 46.8 us, uncut 55.4; 64 blocks 22.5 and
-// 19.4). 64 x 1, 64 blocks: 8 wavefronts 24.7 us, 4 and parts 29.4. ONCE, loads that leave the caches alone, where no other
+// 19.4). 64 x 1, 64 blocks: 8 wavefronts 24.7 us, 4 and parts 29.4. With 2 and 1 wavefronts: 2 x 257 61 and 64 us in place
+// of 58, 16 x 5, 256 blocks 55 and 82 in place of 47. ONCE, loads that leave the caches alone, where no other
 // workgroup reads a list's blocks: 256 x 1, 64 blocks 87 us, with ordinary loads 99; but 2 x 257 77 and 68.
 struct BlocksPlan { int row_groups, splits, per_split, waves; };
 BlocksPlan blocks_plan(int B, int n, int Hq, int Hkv, int N) {
