@@ -279,22 +279,22 @@ __global__ __launch_bounds__(W* kWave, W == 8 || sizeof(T) == 4 ? 2 : 3) void bl
   __shared__ float ml[W][2][16];
   const int lane = threadIdx.x % kWave, g = lane / 16, col = lane % 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  // all of a sequence's and kv head's lists on one XCD where that leaves none idle for long: neighbouring positions list
-  // much the same blocks (x 5 positions x 4 kv heads: 5 sequences 16.0 us, in the grid's order 21.5; 16 sequences 30.5
-  // and 50.6; 120 sequences 117 and 182; but 3 sequences 15.0 and 11.0). They read them at about the same time: lists
-  // begun at different places found less in the L2 cache (16 sequences 43)
-  uint32_t item = blockIdx.x, bh;
-  const uint32_t inner = uint32_t(p.n) * p.row_groups * p.splits;
+  // by XCD: a part of all lists of a sequence and kv head on one of them, since neighbouring positions list much the same
+  // blocks. They read them at about the same time: lists begun at different places found less in the L2 cache (16
+  // sequences x 5 positions, 128 blocks: 43 us in place of 31)
+  uint32_t item = blockIdx.x, group;
+  const uint32_t inner = uint32_t(p.n) * p.row_groups;
   if (p.by_xcd) {
-    bh = item / 8 / inner * 8 + item % 8;
+    group = item / 8 / inner * 8 + item % 8;
     item = item / 8 % inner;
-    if (bh >= uint32_t(p.B) * p.Hkv) return;
+    if (group >= uint32_t(p.B) * p.Hkv * p.splits) return;
   } else {
-    bh = item / inner;
+    group = item / inner;
     item %= inner;
   }
-  const int split = int(item % p.splits), rg = int(item / p.splits % p.row_groups);
-  const int j = int(item / p.splits / p.row_groups), h = int(bh % p.Hkv), b = int(bh / p.Hkv), t = b * p.n + j;
+  const uint32_t bh = group / p.splits;
+  const int split = int(group % p.splits), rg = int(item % p.row_groups);
+  const int j = int(item / p.row_groups), h = int(bh % p.Hkv), b = int(bh / p.Hkv), t = b * p.n + j;
   const long pos = long(p.ctx[b]) + j;
   const int32_t* list = p.blocks + (long(t) * p.Hkv + h) * p.N;
   const int head = h * p.G + rg * 16 + col;
@@ -435,6 +435,16 @@ BlocksPlan blocks_plan(int B, int n, int Hq, int Hkv, int N) {
   return pl;
 }
 
+// Whether workgroups by XCD, `inner` of each group on one, take about as many rounds of the CUs as in the grid's order: then
+// what they share in L2 pays (x 5 positions x 4 kv heads: 16 sequences, 128 blocks 30.6 us, in the grid's order 51.0; 128,
+// 64 blocks 123 and 191; 3, 256 blocks 17.1 and 19.1), else the fullest XCD's second round costs more (17 x 5 x 1, 64 blocks 16.6
+// and 15.0; 1 x 257 x 4 56 and 35)
+bool fits_by_xcd(long groups, long inner, int waves, molt_dtype dt) {
+  const long places = 32 * (waves == 8 ? 1 : dt == MOLT_F32 ? 2 : 3);    // of an XCD
+  const long fullest = ((groups + 7) / 8 * inner + places - 1) / places, even = (groups * inner + 8 * places - 1) / (8 * places);
+  return 4 * fullest <= 5 * even;
+}
+
 }  // namespace
 
 double blocks_attention_groups(int B, int n, int Hq, int Hkv, int N) {
@@ -454,8 +464,9 @@ hipError_t launch_blocks_attention(const void* q, const void* kc, const void* vc
                                    int num_blocks, int N, molt_dtype dt, void* out, void* ws, size_t ws_bytes,
                                    hipStream_t s) {
   const BlocksPlan pl = blocks_plan(B, n, Hq, Hkv, N);
-  const long bh = long(B) * Hkv;
-  const int by_xcd = n > 1 && (bh % 8 == 0 || bh >= 20);
+  const long groups = long(B) * Hkv * pl.splits;
+  const long inner = long(n) * pl.row_groups;
+  const int by_xcd = inner > 1 && fits_by_xcd(groups, inner, pl.waves, dt);
   const bool once = n == 1 && pl.row_groups == 1;
   BlocksArgs p{q, kc, vc, bt, ctx, blocks, out, nullptr, nullptr, B, n, Hq, Hkv, Hq / Hkv, N, max_blocks, num_blocks,
                pl.row_groups, pl.splits, dt == MOLT_F32 ? 2 * pl.per_split : pl.per_split, by_xcd,
@@ -466,7 +477,7 @@ hipError_t launch_blocks_attention(const void* q, const void* kc, const void* vc
     p.part_o = c.take<float>(rows * 16 * D);
     p.part_ml = c.take<float>(rows * 16 * 2);
   }
-  const unsigned grid = unsigned((by_xcd ? (bh + 7) / 8 * 8 : bh) * n * pl.row_groups * pl.splits);
+  const unsigned grid = unsigned((by_xcd ? (groups + 7) / 8 * 8 : groups) * inner);
   const unsigned joins = unsigned((long(B) * n * Hq * (D / 4) + 255) / 256);
   auto go = [&](auto d, auto* t) {
     constexpr int DD = decltype(d)::value;
