@@ -422,26 +422,36 @@ __global__ __launch_bounds__(256) void blocks_join_kernel(BlocksArgs p) {
 // 19.4). 64 x 1, 64 blocks: 8 wavefronts 24.7 us, 4 and parts 29.4. With 2 and 1 wavefronts: 2 x 257 61 and 64 us in place
 // of 58, 16 x 5, 256 blocks 55 and 82 in place of 47. ONCE, loads that leave the caches alone, where no other
 // workgroup reads a list's blocks: 256 x 1, 64 blocks 87 us, with ordinary loads 99; but 2 x 257 77 and 68.
+// Of several positions there are no more parts than let each XCD hold all workgroups of its own, by XCD below (17 x 5 x 1
+// head: 64 blocks 12.0 us, with one part more 15.0, 128 blocks 15.6 and 21.9; 10 x 5 x 1 in f32, 228 blocks 29.6 and 38.1).
 struct BlocksPlan { int row_groups, splits, per_split, waves; };
+// Workgroups on the fullest XCD, where `inner` of each group are on one
+long fullest_xcd(long groups, long inner) { return (groups + 7) / 8 * inner; }
 BlocksPlan blocks_plan(int B, int n, int Hq, int Hkv, int N) {
   BlocksPlan pl{};
   const int units = (N + 1) / 2;
   pl.row_groups = (Hq / Hkv + 15) / 16;
-  const long lists = long(B) * n * Hkv * pl.row_groups;
+  const long inner = long(n) * pl.row_groups, lists = long(B) * Hkv * inner;
   pl.waves = lists <= 256 ? 8 : 4;
-  const long parts = pl.waves == 8 ? std::min(256 / lists, long(units) / 8) : std::min(768 / lists, long(units) / 32);
-  pl.per_split = int((units + std::max(1l, parts) - 1) / std::max(1l, parts));
+  const long most = std::max(1l, pl.waves == 8 ? std::min(256 / lists, long(units) / 8) : std::min(768 / lists, long(units) / 32));
+  long parts = most;
+  if (pl.waves == 8 && inner > 1) {
+    while (parts > 1 && fullest_xcd(B * long(Hkv) * parts, inner) > 32) --parts;
+    if (fullest_xcd(B * long(Hkv) * parts, inner) > 32) parts = most;
+  }
+  pl.per_split = int((units + parts - 1) / parts);
   pl.splits = (units + pl.per_split - 1) / pl.per_split;
   return pl;
 }
 
 // Whether workgroups by XCD, `inner` of each group on one, take about as many rounds of the CUs as in the grid's order: then
 // what they share in L2 pays (x 5 positions x 4 kv heads: 16 sequences, 128 blocks 30.6 us, in the grid's order 51.0; 128,
-// 64 blocks 123 and 191; 3, 256 blocks 17.1 and 19.1), else the fullest XCD's second round costs more (17 x 5 x 1, 64 blocks 16.6
-// and 15.0; 1 x 257 x 4 56 and 35)
+// 64 blocks 123 and 191; 3, 256 blocks 17.1 and 19.1), else the fullest XCD's further round costs more (1 x 257 x 4 heads 56
+// and 35)
 bool fits_by_xcd(long groups, long inner, int waves, molt_dtype dt) {
   const long places = 32 * (waves == 8 ? 1 : dt == MOLT_F32 ? 2 : 3);    // of an XCD
-  const long fullest = ((groups + 7) / 8 * inner + places - 1) / places, even = (groups * inner + 8 * places - 1) / (8 * places);
+  const long fullest = (fullest_xcd(groups, inner) + places - 1) / places;
+  const long even = (groups * inner + 8 * places - 1) / (8 * places);
   return 4 * fullest <= 5 * even;
 }
 
