@@ -433,8 +433,8 @@ MOLT_DEV void emit(int m, Key key, const Border& b, int32_t* out, int first, int
 }
 
 // A workgroup's place: sequence, kv head, position group and chunk of blocks. A sequence's heads, whose records lie side
-// by side, run on one XCD where that leaves none idle for long (x 5 positions: 17 sequences, 2000 blocks 24.1 us, in the
-// grid's order 25.9; 47, 600 blocks 25.8 and 30.4; but 4, 2000 blocks 13.4 and 12.8; x 1: 9, 1500 blocks 14.0 and 12.2).
+// by side, run on one XCD where that leaves none idle for long (x 5 positions: 12 sequences, 2000 blocks 14.8 us, in the
+// grid's order 15.5; 47, 600 blocks 21.2 and 25.9; but 4, 2000 blocks 11.7 and 11.2; x 1: 9, 1500 blocks 12.4 and 10.8).
 struct Item { int b, h, group, chunk; };
 MOLT_DEV Item item_of(const SelectArgs& p) {
   uint32_t at = blockIdx.x;
@@ -680,7 +680,7 @@ hipError_t launch_select_blocks(const void* q, const void* bounds, const int32_t
   p.pos_groups = int((long(n) + positions - 1) / positions);
   p.chunks = 1;
   p.block_bytes = uint32_t(Hkv) * (2 * D + 16);
-  p.by_xcd = B % 8 == 0 || B >= 16;
+  p.by_xcd = B % 8 == 0 || B >= 12;
   if (!fused) {
     p.chunk = score_chunk(B, n, p.G, Hkv, max_blocks);
     p.chunks = (max_blocks + p.chunk - 1) / p.chunk;
