@@ -65,7 +65,7 @@ bool whole(const at::Tensor& t, at::ScalarType type, int dev) {
 }
 bool ints(const at::Tensor& t, int64_t n, int dev) { return whole(t, at::kInt, dev) && t.dim() == 1 && t.size(0) == n; }
 bool table(const at::Tensor& t, int dev) {
-  return whole(t, at::kInt, dev) && t.dim() == 2 && t.size(0) > 0 && t.size(0) < (1l << 31) && t.size(1) < (1l << 31);
+  return whole(t, at::kInt, dev) && t.dim() == 2 && t.size(0) < (1l << 31) && t.size(1) < (1l << 31);
 }
 bool floats(at::ScalarType t) { return t == at::kBFloat16 || t == at::kFloat; }
 molt_dtype code(at::ScalarType t) { return t == at::kFloat ? MOLT_F32 : MOLT_BF16; }

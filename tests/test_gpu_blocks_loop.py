@@ -133,6 +133,44 @@ def test_on_another_stream(molt_lib):
         assert torch.equal(got, again) and torch.equal(lists, lists_b)
 
 
+def test_two_loops_at_once(molt_lib):
+    """Two streams side by side, each with its own tables, caches and workspace: scores and lists in two launches and lists
+    in parts, whose workspaces hold what one launch leaves the next. As one after the other."""
+    def run(loops, streams):
+        out = [[], []]
+        for i in range(12):
+            for x, (lo, s) in enumerate(zip(loops, streams)):
+                with torch.cuda.stream(s):
+                    got, lists, placed = lo.step(lo.rows(), _i32([3, 3]))
+                    lo.ctx = lo.ctx + placed
+                    out[x] += [got, lists]
+        torch.cuda.synchronize()
+        return out
+
+    def make():
+        loops = [Loop(molt_lib, 2, 3, 16, 2, 128, 600, 1300, 40, "bf16", seed=x) for x in (5, 6)]
+        for lo in loops:                                              # 300 blocks of context each, the pool's last ids
+            keys = torch.from_numpy(lo.rng.standard_normal((1300, 2, 16, 128)).astype(np.float32)).cuda()
+            lo.kc.copy_(keys)
+            lo.vc.copy_(keys.flip(0).transpose(2, 3))
+            lo.tables[:, :300] = torch.arange(700, 1300, device="cuda").view(2, 300)
+            lo.n_blocks.fill_(300)
+            lo.ctx.fill_(4790)
+            lo.pool[1] = 700
+            molt_lib.key_bounds_update(lo.kc, lo.bounds, lo.tables, torch.zeros_like(lo.ctx), 4790)
+        assert molt_lib.select_blocks_workspace_size(2, 2, 16, 2, 128, 600) > 0
+        assert molt_lib.paged_attention_blocks_workspace_size(2, 2, 16, 2, 128, 40) > 0
+        return loops
+
+    one, two = torch.cuda.Stream(), torch.cuda.Stream()
+    here = torch.cuda.current_stream()
+    want, pair = run(make(), (here, here)), make()
+    torch.cuda.synchronize()
+    got = run(pair, (one, two))
+    assert all(torch.equal(a, b) for x in (0, 1) for a, b in zip(want[x], got[x]))
+    assert not torch.equal(want[0][0], want[1][0])
+
+
 def test_graphs_that_share_a_workspace(molt_lib):
     """Two captured steps (a verify step, and plain decode) on one state and workspace, replayed in turn with the
     program's own work between, against the same steps made eagerly on a second state."""
@@ -219,6 +257,13 @@ def test_python_refusals(molt_lib):
         lambda: m.paged_attention_blocks(q, lo.kc, lo.vc, lo.tables.cpu(), lo.ctx, 2, lists),
         lambda: m.paged_attention_blocks(q, lo.kc, lo.vc, lo.tables, lo.ctx, 2, lists, workspace=lo.ws[::2]),
     ]
+    no = lo.ctx[:0]
+    for call in (lambda: m.plan_blocks(lo.tables[:0], no, no, no, lo.pool, 3),
+                 lambda: m.key_bounds_update(lo.kc, lo.bounds, lo.tables[:0], no, 3),
+                 lambda: m.select_blocks(q[:0], lo.bounds, lo.tables[:0], no, 2, 3),
+                 lambda: m.paged_attention_blocks(q[:0], lo.kc, lo.vc, lo.tables[:0], no, 2, lists[:0])):
+        with pytest.raises(m.MoltError, match="B = 0"):
+            call()
     lo.ws = torch.empty(64, dtype=torch.uint8, device="cuda")
     for i, call in enumerate(bad):
         with pytest.raises(m.MoltError):
