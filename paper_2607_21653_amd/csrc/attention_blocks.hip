@@ -351,35 +351,28 @@ __global__ __launch_bounds__(W* kWave, W == 8 || sizeof(T) == 4 ? 2 : 3) void bl
   }
 
   r.l = rows_sum4(r.l);
-  if (W > 1) {
-    if (g == 0) { ml[wave][0][col] = r.m; ml[wave][1][col] = r.l; }
-    __syncthreads();
-    float m = ml[0][0][col];
+  if (g == 0) { ml[wave][0][col] = r.m; ml[wave][1][col] = r.l; }
+  __syncthreads();
+  float m = ml[0][0][col];
 #pragma unroll
-    for (int w = 1; w < W; ++w) m = fmaxf(m, ml[w][0][col]);
-    const float base = m == -__builtin_inff() ? 0.f : m, f = __builtin_amdgcn_exp2f(r.m - base);
-    float l = 0.f;
+  for (int w = 1; w < W; ++w) m = fmaxf(m, ml[w][0][col]);
+  const float base = m == -__builtin_inff() ? 0.f : m, f = __builtin_amdgcn_exp2f(r.m - base);
+  float l = 0.f;
 #pragma unroll
-    for (int w = 0; w < W; ++w) l += __builtin_amdgcn_exp2f(ml[w][0][col] - base) * ml[w][1][col];
+  for (int w = 0; w < W; ++w) l += __builtin_amdgcn_exp2f(ml[w][0][col] - base) * ml[w][1][col];
 #pragma unroll
-    for (int d = 0; d < D / 16; ++d) reinterpret_cast<floatx4_t*>(lds[wave])[d * kWave + lane] = r.o[d] * f;
-    __syncthreads();
-    r.m = m;
-    r.l = l;
-  }
+  for (int d = 0; d < D / 16; ++d) reinterpret_cast<floatx4_t*>(lds[wave])[d * kWave + lane] = r.o[d] * f;
+  __syncthreads();
+  r.m = m;
+  r.l = l;
   // wavefront w stores dims 16 d .. + 15 for d = w, w + W, ..
 #pragma unroll
   for (int d0 = 0; d0 < D / 16; d0 += W) {
     const int d = d0 + wave;
     if (d >= D / 16) break;
-    floatx4_t o;
-    if (W > 1) {
-      o = reinterpret_cast<const floatx4_t*>(lds[0])[d * kWave + lane];
+    floatx4_t o = reinterpret_cast<const floatx4_t*>(lds[0])[d * kWave + lane];
 #pragma unroll
-      for (int w = 1; w < W; ++w) o += reinterpret_cast<const floatx4_t*>(lds[w])[d * kWave + lane];
-    } else {
-      o = r.o[d0];
-    }
+    for (int w = 1; w < W; ++w) o += reinterpret_cast<const floatx4_t*>(lds[w])[d * kWave + lane];
     if (p.splits > 1) {
       const long at = (((long(t) * p.Hkv + h) * p.row_groups + rg) * p.splits + split) * 16 + col;
       if (there) *reinterpret_cast<floatx4_t*>(p.part_o + at * D + 16 * d + 4 * g) = o;
