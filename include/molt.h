@@ -334,7 +334,8 @@ int molt_paged_attention_kvq(const void* q, const void* k_cache, const void* v_c
  *   bounds  uint8 [num_blocks, n_kv_heads, 2 D + 16]: codes of M, codes of m, e (signed bytes),
  *           15 bytes of 0; starts at a multiple of 16 bytes. All-zero records score 0.
  * molt_key_bounds_read -- codes of blocks ids[i], i < M, as the values that they stand for:
- * out_hi, out_lo [M, n_kv_heads, D] f32 (e = 127: +inf and -inf; ids outside [0, num_blocks): NaN).
+ * out_hi, out_lo [M, n_kv_heads, D] f32 (infinite where code * 2^e passes f32, from code 64 on at the largest e, 122;
+ * e = 127: +inf and -inf; ids outside [0, num_blocks): NaN).
  *
  * molt_select_blocks -- for each query position t = b (1+k) + j and kv head the n_select blocks of
  * largest score of those that hold positions 0 .. context_lens[b] + j: out [T, n_kv_heads, n_select]

@@ -467,7 +467,7 @@ __global__ __launch_bounds__(kThreads) void bounds_read_kernel(const uint8_t* __
     const uint8_t* rec = bounds + (long(id) * Hkv + at % Hkv) * Rec::kBytes;
     const int e = int(int8_t(rec[Rec::kExponent]));
     const uint32_t x = *reinterpret_cast<const uint32_t*>(rec + d), y = *reinterpret_cast<const uint32_t*>(rec + D + d);
-    const float unit = pow2(min(max(e, kBoundsMinExponent), 121));
+    const float unit = pow2(min(max(e, kBoundsMinExponent), kBoundsMaxExponent));   // (codes from 64 on pass f32 at 2^122)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       a[i] = e == kBoundsNotFinite ? inf : float(int8_t(x >> 8 * i)) * unit;

@@ -8,6 +8,7 @@ struct BoundsRecord {
   static constexpr int kBytes = 2 * D + 16;
 };
 constexpr int kBoundsMinExponent = -100;
+constexpr int kBoundsMaxExponent = 122;          // of finite values past 127 * 2^121, the largest of f32 and bf16 among them
 constexpr int kBoundsNotFinite = 127;            // exponent of a block that holds an infinity or NaN
 
 // The smallest e >= -100 with a <= 127 * 2^e, for the bits of a finite a >= 0: a = 2^(E - 127) (1 + m / 2^23), and

@@ -1,0 +1,58 @@
+"""Sparse attention over listed blocks and the cache's upkeep at the ends of what their types hold."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import blocks as ob
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def _i32(a):
+    return torch.as_tensor(np.asarray(a, np.int32), device="cuda")
+
+
+def _val(t):
+    return t.double().cpu().numpy()
+
+
+# ---------------------------------------------------------------- bounds
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,D", [(2, 64), (1, 128)])
+def test_bounds_of_the_largest_keys_and_back(molt_lib, dtype, H, D):
+    """Keys above 127 * 2^121 have e = 122: the bounds are the codes times 2^122 in f32, infinite from code 64 on, and lie
+    around the keys. 127 * 2^121 itself, and less, have e = 121."""
+    rng = np.random.default_rng(D)
+    big, border = torch.finfo(DT[dtype]).max, 127.0 * 2.0 ** 121
+    kc = torch.from_numpy(rng.standard_normal((9, H, 16, D)).astype(np.float32)).to(DT[dtype])
+    kc[0, 0, 3, 5], kc[0, 0, 9, 6] = big, 2.0 ** 125 + 2.0 ** 119
+    kc[1, 0, 15, 0] = -big
+    kc[2] = big
+    kc[3] = -big
+    kc[4, -1, 7, D - 1] = border                                     # e = 121
+    kc[5, -1, 0, 1], kc[5, -1, 1, 1] = border * (1 + 2.0 ** (-7 if dtype == "bf16" else -23)), -border   # (bf16: infinite)
+    kc[6, 0, :, ::2], kc[6, 0, 2, 1] = 2.0 ** 127, -(2.0 ** 127)     # e = 121
+    kc[7] *= 2.0 ** 124
+    kc[8, 0, 4, 3] = border + 2.0 ** (120 if dtype == "bf16" else 104)   # the next one
+    bounds = molt_lib.key_bounds(9, H, D)
+    molt_lib.key_bounds_update(kc.cuda(), bounds, _i32(np.arange(9)[None]), _i32([0]), 9 * 16)
+    exponents = bounds.view(torch.int8)[..., 2 * D].tolist()
+    assert exponents[0][0] == exponents[1][0] == exponents[2][0] == exponents[3][0] == exponents[8][0] == 122
+    assert exponents[5][-1] == (127 if dtype == "bf16" else 122)
+    assert exponents[4][-1] == exponents[6][0] == 121
+    hi, lo = molt_lib.key_bounds_read(bounds, _i32(np.arange(9)))
+    for i in range(9):
+        for h in range(H):
+            keys = _val(kc[i, h])
+            a, b, e = ob.bounds_of(keys)
+            with np.errstate(over="ignore"):
+                want = np.ldexp(a, e).astype(np.float32), np.ldexp(b, e).astype(np.float32)
+            if e == ob.NOT_FINITE:
+                want = np.full(D, np.inf, np.float32), np.full(D, -np.inf, np.float32)
+            got = hi[i, h].cpu().numpy(), lo[i, h].cpu().numpy()
+            assert np.array_equal(got[0], want[0]) and np.array_equal(got[1], want[1]), (i, h)
+            assert (got[0] >= keys.max(0)).all() and (got[1] <= keys.min(0)).all(), (i, h)
+    assert hi[0, 0, 5].item() == float("inf") and hi[0, 0, 6].item() == 9 * 2.0 ** 122 and lo[1, 0, 0].item() == -float("inf")
