@@ -56,3 +56,36 @@ def test_bounds_of_the_largest_keys_and_back(molt_lib, dtype, H, D):
             assert np.array_equal(got[0], want[0]) and np.array_equal(got[1], want[1]), (i, h)
             assert (got[0] >= keys.max(0)).all() and (got[1] <= keys.min(0)).all(), (i, h)
     assert hi[0, 0, 5].item() == float("inf") and hi[0, 0, 6].item() == 9 * 2.0 ** 122 and lo[1, 0, 0].item() == -float("inf")
+
+
+# ---------------------------------------------------------------- attention
+
+def _attend(molt, q, kc, vc, ctx, n, lists):
+    table = np.arange(len(kc), dtype=np.int32)[None]
+    got = molt.paged_attention_blocks(q.cuda(), kc.cuda(), vc.cuda(), _i32(table), _i32(ctx), n - 1, _i32(lists))
+    want, mag = ob.attend(_val(q), _val(kc), _val(vc), table, ctx, n, lists)
+    return _val(got).reshape(want.shape), want, mag
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("N", [3, 200])
+@pytest.mark.parametrize("scale", [2.0 ** 16, 2.0 ** 24, 2.0 ** 34, 2.0 ** 54])
+def test_attention_of_far_scores(molt_lib, dtype, D, N, scale):
+    """Scores up to 2^112: the largest has all the weight, 1, however coarse the steps of f32 are at its size. Queries and
+    keys are whole numbers in -2 .. 2 times a power of two, so that every score is exact and two that differ do so by scale^2
+    at least: the output is the mean of the values of the keys with the largest score, up to N * 16 of them, whose
+    weights are 1 and whose sum is exact. A value is rounded half a step, and f32 sums of at most 2^12 values of |v| < 8 and
+    their product with the reciprocal are off by 2^12 * 2^-24 of sum w |v| at most."""
+    rng = np.random.default_rng(N)
+    H, G, n, maxb = 2, 5, 3, 220
+    kc = torch.from_numpy(rng.integers(-2, 3, (maxb, H, 16, D)) * np.float32(scale)).to(DT[dtype])
+    vc = torch.from_numpy(rng.standard_normal((maxb, H, D, 16)).astype(np.float32)).to(DT[dtype])
+    q = torch.from_numpy(rng.integers(-2, 3, (n, H * G, D)) * np.float32(scale)).to(DT[dtype])
+    q[1] = -q[1].abs() - q[1, :, :1].abs()
+    kc[:, 1] = kc[:, 1].abs() + kc[:, 1, :, :1].abs()                # position 1, head 1: no score above 0
+    lists = np.tile(np.arange(10, 10 + N, dtype=np.int32), (n, H, 1))
+    lists[2, :, 1] = -1
+    got, want, mag = _attend(molt_lib, q, kc, vc, [16 * maxb - n], n, lists)
+    tol = (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * np.abs(want) + 2.0 ** -12 * mag
+    assert np.isfinite(got).all() and (np.abs(got - want) <= tol).all(), np.abs(got - want).max()
