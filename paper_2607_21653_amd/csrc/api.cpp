@@ -68,6 +68,15 @@ struct ProfScope {
     if (!(cond)) return fail(MOLT_ERR_INVALID_ARG, __VA_ARGS__); \
   } while (0)
 
+// A check's answer without its message: a size function leaves the last one as it is
+template <typename Check>
+bool fits(Check check) {
+  const std::string said = g_err;
+  const bool fine = check() == MOLT_OK;
+  g_err = said;
+  return fine;
+}
+
 int check_ws(void* ws, size_t have, size_t need) {
   if (need > 0 && (ws == nullptr || have < need))
     return fail(MOLT_ERR_WORKSPACE, "workspace of %zu bytes at %p is smaller than the %zu required",
@@ -616,29 +625,45 @@ static bool aligned16(const void* a, const void* b = nullptr, const void* c = nu
           reinterpret_cast<uintptr_t>(d)) % 16 == 0;
 }
 
-static int blocks_sizes_ok(int Hkv, int D, int num_blocks) {
+static int blocks_row_ok(int Hkv, int D) {
   REQUIRE(D == 64 || D == 128, "head_dim = %d must be 64 or 128", D);
   REQUIRE(Hkv >= 1 && double(Hkv) * D < 1.0e6, "n_kv_heads = %d must be >= 1, n_kv_heads * head_dim < 10^6", Hkv);
+  return MOLT_OK;
+}
+static int blocks_sizes_ok(int Hkv, int D, int num_blocks) {
+  if (int r = blocks_row_ok(Hkv, D)) return r;
   REQUIRE(num_blocks >= 1 && num_blocks <= kMaxPoolBlocks, "num_blocks = %d must be in [1, 2^27)", num_blocks);
   return MOLT_OK;
 }
-static int blocks_table_ok(int B, int n, int max_blocks) {
+static int blocks_rows_ok(int B, int n) {
   REQUIRE(B >= 1, "B = %d must be >= 1", B);
   REQUIRE(n >= 1, "n = %d rows of a sequence must be >= 1", n);
   REQUIRE(double(B) * n < 2.0e9, "B = %d times n = %d rows is too large", B, n);
+  return MOLT_OK;
+}
+static int blocks_table_ok(int B, int n, int max_blocks) {
+  if (int r = blocks_rows_ok(B, n)) return r;
   REQUIRE(max_blocks >= 1 && max_blocks <= kMaxTableBlocks, "max_blocks_per_seq = %d must be in [1, 2^26]", max_blocks);
   return MOLT_OK;
 }
 
-size_t molt_plan_blocks_workspace_size(int B, int n) { return B < 1 || n < 1 ? 0 : molt::plan_ws_bytes(B, n); }
+static int plan_sizes_ok(int B, int n) {
+  if (int r = blocks_rows_ok(B, n)) return r;
+  REQUIRE(double(B) * n / 256 + B < kMaxGroups, "B = %d sequences of n = %d rows are too many", B, n);
+  return MOLT_OK;
+}
+
+size_t molt_plan_blocks_workspace_size(int B, int n) {
+  return fits([&] { return plan_sizes_ok(B, n); }) ? molt::plan_ws_bytes(B, n) : 0;
+}
 
 int molt_plan_blocks(int32_t* block_tables, int32_t* n_blocks, const int32_t* context_lens, const int32_t* n_new,
                      int32_t* pool, const int32_t* n_shared, int B, int n, int max_blocks, int num_blocks,
                      int32_t* out_slots, int32_t* out_placed, void* workspace, size_t workspace_bytes,
                      molt_stream_t stream) {
+  if (int r = plan_sizes_ok(B, n)) return r;
   if (int r = blocks_table_ok(B, n, max_blocks)) return r;
   REQUIRE(num_blocks >= 1 && num_blocks <= kMaxPoolBlocks, "num_blocks = %d must be in [1, 2^27)", num_blocks);
-  REQUIRE(double(B) * n / 256 + B < kMaxGroups, "B = %d sequences of n = %d rows are too many", B, n);
   REQUIRE(block_tables && n_blocks && context_lens && n_new && pool && out_slots && out_placed,
           "a required pointer is NULL");
   if (int r = check_ws(workspace, workspace_bytes, molt::plan_ws_bytes(B, n))) return r;
@@ -697,8 +722,8 @@ int molt_key_bounds_read(const void* bounds, const int32_t* ids, int M, int Hkv,
 static int blocks_heads_ok(int B, int k, int Hq, int Hkv, int D) {
   REQUIRE(B >= 1, "B = %d must be >= 1", B);
   REQUIRE(k >= 0 && k < 0x7fffffff, "k = %d must be >= 0", k);
-  REQUIRE(D == 64 || D == 128, "head_dim = %d must be 64 or 128", D);
-  REQUIRE(Hkv >= 1 && Hq >= Hkv && Hq % Hkv == 0, "n_q_heads %d must be a multiple of n_kv_heads %d", Hq, Hkv);
+  if (int r = blocks_row_ok(Hkv, D)) return r;
+  REQUIRE(Hq >= Hkv && Hq % Hkv == 0, "n_q_heads %d must be a multiple of n_kv_heads %d", Hq, Hkv);
   REQUIRE(double(B) * (double(k) + 1) * Hq < 2.0e9, "B * (1+k) * n_q_heads too large");
   return MOLT_OK;
 }
@@ -717,10 +742,8 @@ static int attend_sizes_ok(int B, int k, int Hq, int Hkv, int D, int n_list) {
 }
 
 size_t molt_select_blocks_workspace_size(int B, int k, int Hq, int Hkv, int D, int max_blocks) {
-  const std::string said = g_err;
-  const bool fits = select_sizes_ok(B, k, Hq, Hkv, D, max_blocks) == MOLT_OK;
-  g_err = said;                                  // (a size function fails without a message)
-  return fits ? molt::select_ws_bytes(B, k + 1, Hq, Hkv, D, max_blocks) : 0;
+  return fits([&] { return select_sizes_ok(B, k, Hq, Hkv, D, max_blocks); })
+             ? molt::select_ws_bytes(B, k + 1, Hq, Hkv, D, max_blocks) : 0;
 }
 
 int molt_select_blocks(const void* q, const void* bounds, const int32_t* block_tables, const int32_t* context_lens,
@@ -747,10 +770,8 @@ int molt_select_blocks(const void* q, const void* bounds, const int32_t* block_t
 }
 
 size_t molt_paged_attention_blocks_workspace_size(int B, int k, int Hq, int Hkv, int D, int n_list) {
-  const std::string said = g_err;
-  const bool fits = attend_sizes_ok(B, k, Hq, Hkv, D, n_list) == MOLT_OK;
-  g_err = said;
-  return fits ? molt::blocks_attention_ws_bytes(B, k + 1, Hq, Hkv, D, n_list) : 0;
+  return fits([&] { return attend_sizes_ok(B, k, Hq, Hkv, D, n_list); })
+             ? molt::blocks_attention_ws_bytes(B, k + 1, Hq, Hkv, D, n_list) : 0;
 }
 
 int molt_paged_attention_blocks(const void* q, const void* k_cache, const void* v_cache, const int32_t* block_tables,
