@@ -140,7 +140,8 @@ def load(path=LIB_PATH):
     from . import _calls as calls
     calls.set_entries(MoltError, *(ctypes.cast(getattr(lib, "molt_" + name), c_vp).value for name in (
         "last_error", "plan_blocks", "plan_blocks_workspace_size", "kv_write", "key_bounds_update", "key_bounds_read",
-        "select_blocks", "select_blocks_workspace_size", "paged_attention_blocks", "paged_attention_blocks_workspace_size")))
+        "select_blocks", "select_blocks_workspace_size", "paged_attention_blocks", "paged_attention_blocks_workspace_size",
+        "plan_blocks_takes", "key_bounds_read_takes", "select_blocks_takes", "paged_attention_blocks_takes")))
     _lib, _calls = lib, calls
     return lib
 

@@ -9,6 +9,7 @@
 #include <mutex>
 #include <string>
 
+#include "binding/sizes.h"
 #include "internal.h"
 
 namespace {
@@ -657,13 +658,18 @@ size_t molt_plan_blocks_workspace_size(int B, int n) {
   return fits([&] { return plan_sizes_ok(B, n); }) ? molt::plan_ws_bytes(B, n) : 0;
 }
 
+int molt_plan_blocks_takes(int B, int n, int max_blocks, int num_blocks) {
+  if (int r = plan_sizes_ok(B, n)) return r;
+  if (int r = blocks_table_ok(B, n, max_blocks)) return r;
+  REQUIRE(num_blocks >= 1 && num_blocks <= kMaxPoolBlocks, "num_blocks = %d must be in [1, 2^27)", num_blocks);
+  return MOLT_OK;
+}
+
 int molt_plan_blocks(int32_t* block_tables, int32_t* n_blocks, const int32_t* context_lens, const int32_t* n_new,
                      int32_t* pool, const int32_t* n_shared, int B, int n, int max_blocks, int num_blocks,
                      int32_t* out_slots, int32_t* out_placed, void* workspace, size_t workspace_bytes,
                      molt_stream_t stream) {
-  if (int r = plan_sizes_ok(B, n)) return r;
-  if (int r = blocks_table_ok(B, n, max_blocks)) return r;
-  REQUIRE(num_blocks >= 1 && num_blocks <= kMaxPoolBlocks, "num_blocks = %d must be in [1, 2^27)", num_blocks);
+  if (int r = molt_plan_blocks_takes(B, n, max_blocks, num_blocks)) return r;
   REQUIRE(block_tables && n_blocks && context_lens && n_new && pool && out_slots && out_placed,
           "a required pointer is NULL");
   if (int r = check_ws(workspace, workspace_bytes, molt::plan_ws_bytes(B, n))) return r;
@@ -706,11 +712,16 @@ int molt_key_bounds_update(const void* k_cache, void* bounds, const int32_t* blo
                     "molt_key_bounds_update");
 }
 
-int molt_key_bounds_read(const void* bounds, const int32_t* ids, int M, int Hkv, int D, int num_blocks, float* out_hi,
-                         float* out_lo, molt_stream_t stream) {
+int molt_key_bounds_read_takes(int M, int Hkv, int D, int num_blocks) {
   if (int r = blocks_sizes_ok(Hkv, D, num_blocks)) return r;
   REQUIRE(M >= 1, "M = %d must be >= 1", M);
   REQUIRE(double(M) * Hkv * D / 1024 < kMaxGroups, "M * n_kv_heads * head_dim too large");
+  return MOLT_OK;
+}
+
+int molt_key_bounds_read(const void* bounds, const int32_t* ids, int M, int Hkv, int D, int num_blocks, float* out_hi,
+                         float* out_lo, molt_stream_t stream) {
+  if (int r = molt_key_bounds_read_takes(M, Hkv, D, num_blocks)) return r;
   REQUIRE(bounds && ids && out_hi && out_lo, "a required pointer is NULL");
   REQUIRE(aligned16(bounds, out_hi, out_lo), "bounds and outputs must start at a multiple of 16 bytes");
   return hip_status(molt::launch_bounds_read(bounds, ids, M, Hkv, D, num_blocks, out_hi, out_lo,
@@ -746,16 +757,22 @@ size_t molt_select_blocks_workspace_size(int B, int k, int Hq, int Hkv, int D, i
              ? molt::select_ws_bytes(B, k + 1, Hq, Hkv, D, max_blocks) : 0;
 }
 
+int molt_select_blocks_takes(int B, int k, int Hq, int Hkv, int D, int max_blocks, int num_blocks, int n_select, int n_first,
+                             int n_last) {
+  if (int r = select_sizes_ok(B, k, Hq, Hkv, D, max_blocks)) return r;
+  if (int r = blocks_sizes_ok(Hkv, D, num_blocks)) return r;
+  REQUIRE(n_select >= 1 && n_select <= kMaxTableBlocks, "n_select = %d must be in [1, 2^26]", n_select);
+  REQUIRE(n_first >= 0 && n_last >= 1 && n_first <= n_select && n_last <= n_select - n_first,
+          "n_first = %d >= 0 and n_last = %d >= 1 must fit n_select = %d", n_first, n_last, n_select);
+  return MOLT_OK;
+}
+
 int molt_select_blocks(const void* q, const void* bounds, const int32_t* block_tables, const int32_t* context_lens,
                        const int32_t* lens, int B, int k, int Hq, int Hkv, int D, int max_blocks, int num_blocks,
                        int n_select, int n_first, int n_last, molt_dtype dtype, int32_t* out, void* workspace,
                        size_t workspace_bytes, molt_stream_t stream) {
-  if (int r = select_sizes_ok(B, k, Hq, Hkv, D, max_blocks)) return r;
-  if (int r = blocks_sizes_ok(Hkv, D, num_blocks)) return r;
+  if (int r = molt_select_blocks_takes(B, k, Hq, Hkv, D, max_blocks, num_blocks, n_select, n_first, n_last)) return r;
   REQUIRE(act_ok(dtype), "dtype must be F32 or BF16");
-  REQUIRE(n_select >= 1 && n_select <= kMaxTableBlocks, "n_select = %d must be in [1, 2^26]", n_select);
-  REQUIRE(n_first >= 0 && n_last >= 1 && n_first <= n_select && n_last <= n_select - n_first,
-          "n_first = %d >= 0 and n_last = %d >= 1 must fit n_select = %d", n_first, n_last, n_select);
   REQUIRE(q && bounds && block_tables && context_lens && out, "a required pointer is NULL");
   REQUIRE(aligned16(q, bounds), "q and bounds must start at a multiple of 16 bytes");
   if (int r = check_ws(workspace, workspace_bytes, molt::select_ws_bytes(B, k + 1, Hq, Hkv, D, max_blocks))) return r;
@@ -774,13 +791,17 @@ size_t molt_paged_attention_blocks_workspace_size(int B, int k, int Hq, int Hkv,
              ? molt::blocks_attention_ws_bytes(B, k + 1, Hq, Hkv, D, n_list) : 0;
 }
 
+int molt_paged_attention_blocks_takes(int B, int k, int Hq, int Hkv, int D, int max_blocks, int num_blocks, int n_list) {
+  if (int r = attend_sizes_ok(B, k, Hq, Hkv, D, n_list)) return r;
+  if (int r = blocks_sizes_ok(Hkv, D, num_blocks)) return r;
+  return blocks_table_ok(B, k + 1, max_blocks);
+}
+
 int molt_paged_attention_blocks(const void* q, const void* k_cache, const void* v_cache, const int32_t* block_tables,
                                 const int32_t* context_lens, const int32_t* blocks, int B, int k, int Hq, int Hkv,
                                 int D, int max_blocks, int num_blocks, int n_list, molt_dtype dtype, void* out,
                                 void* workspace, size_t workspace_bytes, molt_stream_t stream) {
-  if (int r = attend_sizes_ok(B, k, Hq, Hkv, D, n_list)) return r;
-  if (int r = blocks_sizes_ok(Hkv, D, num_blocks)) return r;
-  if (int r = blocks_table_ok(B, k + 1, max_blocks)) return r;
+  if (int r = molt_paged_attention_blocks_takes(B, k, Hq, Hkv, D, max_blocks, num_blocks, n_list)) return r;
   REQUIRE(act_ok(dtype), "dtype must be F32 or BF16");
   REQUIRE(q && k_cache && v_cache && block_tables && context_lens && blocks && out, "a required pointer is NULL");
   REQUIRE(aligned16(q, k_cache, v_cache, out), "q, out and the caches must start at a multiple of 16 bytes");

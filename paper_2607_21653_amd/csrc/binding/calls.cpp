@@ -3,7 +3,8 @@
 //
 // Every call returns None where it does not take the arguments (a wrong type, shape, device or stride), having enqueued
 // nothing: the Python function then finds the words for it. What a C entry refuses is raised as a MoltError. A workspace
-// that the caller did not give, or a smaller one, is made here. The entries come from the loaded library (set_entries).
+// that the caller did not give, or a smaller one, is made here, and the outputs are, once the entry's checks of the sizes
+// let them pass. The entries come from the loaded library (set_entries).
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
@@ -12,6 +13,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../../include/molt.h"
+#include "sizes.h"
 
 namespace {
 
@@ -26,6 +28,10 @@ decltype(&molt_select_blocks) select_entry;
 decltype(&molt_select_blocks_workspace_size) select_size;
 decltype(&molt_paged_attention_blocks) attend_entry;
 decltype(&molt_paged_attention_blocks_workspace_size) attend_size;
+decltype(&molt_plan_blocks_takes) plan_takes;
+decltype(&molt_key_bounds_read_takes) read_takes;
+decltype(&molt_select_blocks_takes) select_takes;
+decltype(&molt_paged_attention_blocks_takes) attend_takes;
 
 // Arguments in turn; `fine` ends false where one is not what a call takes
 struct Args {
@@ -126,6 +132,7 @@ CALL(plan, 9)  // block_tables, n_blocks, context_lens, n_new, pool, n, n_shared
   const int64_t B = bt->size(0), cap = pool->numel() - 2;
   TAKE(ints(*have, B, dev) && ints(*ctx, B, dev) && ints(*fresh, B, dev) && cap > 0 && cap < (1l << 31) &&
        ints(*pool, cap + 2, dev) && (!shared || ints(*shared, B, dev)));
+  RUN("molt_plan_blocks", plan_takes(int(B), n, int(bt->size(1)), int(cap)));
   at::Tensor slots = at::empty({B * n}, fresh->options()), placed = at::empty({B}, fresh->options());
   const size_t need = plan_size(int(B), n);
   at::Tensor ws;
@@ -180,6 +187,7 @@ CALL(read, 4)  // bounds, ids, device, stream
   TAKE(in.fine && bounds_of(*bounds, dev));
   const int64_t M = ids->numel(), nb = bounds->size(0), H = bounds->size(1), D = (bounds->size(2) - 16) / 2;
   TAKE(nb < (1l << 31) && H < (1l << 20) && M > 0 && M < (1l << 31) && ints(*ids, M, dev));
+  RUN("molt_key_bounds_read", read_takes(int(M), int(H), int(D), int(nb)));
   const auto as = bounds->options().dtype(at::kFloat);
   at::Tensor hi = at::empty({M, H, D}, as), lo = at::empty({M, H, D}, as);
   RUN("molt_key_bounds_read",
@@ -206,6 +214,8 @@ CALL(select, 12)  // q, bounds, block_tables, context_lens, k, n_select, n_first
   const int64_t D = (bounds->size(2) - 16) / 2;
   TAKE(nb < (1l << 31) && H < (1l << 20) && Hq < (1l << 31) && q->size(0) == T && q->size(2) == D && ints(*ctx, B, dev) &&
        (!lens || ints(*lens, B, dev)));
+  RUN("molt_select_blocks",
+      select_takes(int(B), k, int(Hq), int(H), int(D), int(bt->size(1)), int(nb), N, first, last));
   at::Tensor out = at::empty({T, H, N}, bt->options());
   auto call = [&](void* at, size_t bytes) {
     return select_entry(q->const_data_ptr(), bounds->const_data_ptr(), i32(bt), i32(ctx), i32(lens), int(B), k, int(Hq),
@@ -235,6 +245,8 @@ CALL(attend, 10)  // q, k_cache, v_cache, block_tables, context_lens, k, blocks,
   const int64_t Hq = q->size(1), N = blocks->size(2);
   TAKE(nb < (1l << 31) && H < (1l << 20) && Hq < (1l << 31) && N < (1l << 31) && q->size(0) == T && q->size(2) == D &&
        blocks->size(0) == T && blocks->size(1) == H && ints(*ctx, B, dev));
+  RUN("molt_paged_attention_blocks",
+      attend_takes(int(B), k, int(Hq), int(H), int(D), int(bt->size(1)), int(nb), int(N)));
   at::Tensor out = at::empty({T, Hq * D}, q->options());
   auto call = [&](void* at, size_t bytes) {
     return attend_entry(q->const_data_ptr(), kc->const_data_ptr(), vc->const_data_ptr(), i32(bt), i32(ctx), i32(blocks),
@@ -253,8 +265,9 @@ END_CALL
 // MoltError, then the addresses of the entries
 PyObject* set_entries(PyObject*, PyObject* args) {
   PyObject* error;
-  unsigned long long a[10];
-  if (!PyArg_ParseTuple(args, "OKKKKKKKKKK", &error, a, a + 1, a + 2, a + 3, a + 4, a + 5, a + 6, a + 7, a + 8, a + 9))
+  unsigned long long a[14];
+  if (!PyArg_ParseTuple(args, "OKKKKKKKKKKKKKK", &error, a, a + 1, a + 2, a + 3, a + 4, a + 5, a + 6, a + 7, a + 8, a + 9,
+                        a + 10, a + 11, a + 12, a + 13))
     return nullptr;
   Py_INCREF(error);
   Py_XDECREF(error_class);
@@ -269,6 +282,10 @@ PyObject* set_entries(PyObject*, PyObject* args) {
   select_size = reinterpret_cast<decltype(select_size)>(a[7]);
   attend_entry = reinterpret_cast<decltype(attend_entry)>(a[8]);
   attend_size = reinterpret_cast<decltype(attend_size)>(a[9]);
+  plan_takes = reinterpret_cast<decltype(plan_takes)>(a[10]);
+  read_takes = reinterpret_cast<decltype(read_takes)>(a[11]);
+  select_takes = reinterpret_cast<decltype(select_takes)>(a[12]);
+  attend_takes = reinterpret_cast<decltype(attend_takes)>(a[13]);
   Py_RETURN_NONE;
 }
 

@@ -89,3 +89,30 @@ def test_attention_of_far_scores(molt_lib, dtype, D, N, scale):
     got, want, mag = _attend(molt_lib, q, kc, vc, [16 * maxb - n], n, lists)
     tol = (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * np.abs(want) + 2.0 ** -12 * mag
     assert np.isfinite(got).all() and (np.abs(got - want) <= tol).all(), np.abs(got - want).max()
+
+
+# ---------------------------------------------------------------- refusals
+
+SELECT = dict(n_select=4, n_first=1, n_last=2)
+
+
+@pytest.mark.parametrize("call,words", [("plan", "too many|too large"), ("read", "head_dim = 96"), ("attend", "head_dim = 96"),
+                                        (dict(n_select=2 ** 26 + 1), "n_select = 67108865"),
+                                        (dict(n_select=2 ** 31 - 1), "n_select = 2147483647"), (dict(n_first=3), "n_first = 3")])
+def test_refused_sizes_make_no_outputs(molt_lib, call, words):
+    """Sizes that a call refuses are refused in its own words, before it asks for memory for outputs of such sizes."""
+    z = lambda *s, dt=torch.int32: torch.zeros(s, dtype=dt, device="cuda")  # noqa: E731
+    bf16, table, ctx, new, have, pool = torch.bfloat16, z(4, 8), z(4), z(4), z(4), molt_lib.block_pool(50)
+    q, bounds, odd, ids = z(8, 4, 64, dt=bf16), molt_lib.key_bounds(50, 2, 64), molt_lib.key_bounds(50, 2, 96), z(5)
+    q96, kc, vc, lists = z(8, 4, 96, dt=bf16), z(50, 2, 16, 96, dt=bf16), z(50, 2, 96, 16, dt=bf16), z(8, 2, 3)
+    before = torch.cuda.memory_stats()["allocation.all.allocated"]
+    with pytest.raises(molt_lib.MoltError, match=words):
+        if call == "plan":
+            molt_lib.plan_blocks(table, have, ctx, new, pool, 2 ** 30)
+        elif call == "read":
+            molt_lib.key_bounds_read(odd, ids)
+        elif call == "attend":
+            molt_lib.paged_attention_blocks(q96, kc, vc, table, ctx, 1, lists)
+        else:
+            molt_lib.select_blocks(q, bounds, table, ctx, 1, **{**SELECT, **call})
+    assert torch.cuda.memory_stats()["allocation.all.allocated"] == before
