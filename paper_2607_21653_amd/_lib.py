@@ -22,7 +22,7 @@ DTYPE_CODE = {torch.float32: MOLT_F32, torch.bfloat16: MOLT_BF16, torch.uint8: M
 NAME_CODE = {"f32": MOLT_F32, "bf16": MOLT_BF16, "fp8": MOLT_FP8_E4M3}
 
 _lib = None
-_calls = None                     # the module of csrc/binding/calls.cpp
+_calls = None                     # the module of csrc/binding/calls.cpp, from its first call on
 
 c_int, c_size, c_vp, c_float = ctypes.c_int, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_float
 
@@ -126,24 +126,38 @@ class MoltError(RuntimeError):
 
 def load(path=LIB_PATH):
     """Loads the library (once). Raises if it has not been built."""
-    global _lib, _calls
+    global _lib
     if _lib is not None:
         return _lib
-    for need in (path, CALLS_PATH):
-        if not os.path.exists(need):
-            raise MoltError(f"{need} is missing: build it with `python -m paper_2607_21653_amd.build`")
+    if not os.path.exists(path):
+        raise MoltError(f"{path} is missing: build it with `python -m paper_2607_21653_amd.build`")
     lib = ctypes.CDLL(path)
     for name, (res, args) in _SIGS.items():
         fn = getattr(lib, name)
         fn.restype = res
         fn.argtypes = args
-    from . import _calls as calls
-    calls.set_entries(MoltError, *(ctypes.cast(getattr(lib, "molt_" + name), c_vp).value for name in (
-        "last_error", "plan_blocks", "plan_blocks_workspace_size", "kv_write", "key_bounds_update", "key_bounds_read",
-        "select_blocks", "select_blocks_workspace_size", "paged_attention_blocks", "paged_attention_blocks_workspace_size",
-        "plan_blocks_takes", "key_bounds_read_takes", "select_blocks_takes", "paged_attention_blocks_takes")))
-    _lib, _calls = lib, calls
+    _lib = lib
     return lib
+
+
+def _load_calls():
+    """The module of csrc/binding/calls.cpp, which the calls of sparse attention go through and no others need."""
+    global _calls
+    if _calls is None:
+        lib = load()
+        if not os.path.exists(CALLS_PATH):
+            raise MoltError(f"{CALLS_PATH} is missing: build it with `python -m paper_2607_21653_amd.build`")
+        try:
+            from . import _calls as calls
+        except ImportError as e:
+            raise MoltError(f"{CALLS_PATH} cannot be loaded, build it for this torch with "
+                            f"`python -m paper_2607_21653_amd.build`: {e}") from e
+        calls.set_entries(MoltError, *(ctypes.cast(getattr(lib, "molt_" + name), c_vp).value for name in (
+            "last_error", "plan_blocks", "plan_blocks_workspace_size", "kv_write", "key_bounds_update", "key_bounds_read",
+            "select_blocks", "select_blocks_workspace_size", "paged_attention_blocks", "paged_attention_blocks_workspace_size",
+            "plan_blocks_takes", "key_bounds_read_takes", "select_blocks_takes", "paged_attention_blocks_takes")))
+        _calls = calls
+    return _calls
 
 
 def exported_symbols():
@@ -554,9 +568,9 @@ def plan_blocks(block_tables, n_blocks, context_lens, n_new, pool, n, n_shared=N
     """Lets the block tables follow the lengths (molt_plan_blocks), all on the GPU and in place: sequence b gets the
     blocks that rows context_lens[b] .. + n_new[b] - 1 need from pool, or gives its own back where n_new[b] < 0.
     Returns (slots [B*n] i32 for kv_write, -1 where there is no row; placed [B] i32, rows that have slots)."""
-    _lib or load()
+    calls = _calls or _load_calls()
     dev = _here(block_tables, "block_tables")
-    done = _calls.plan(block_tables, n_blocks, context_lens, n_new, pool, n, n_shared, dev, _raw_stream(dev))
+    done = calls.plan(block_tables, n_blocks, context_lens, n_new, pool, n, n_shared, dev, _raw_stream(dev))
     if done is None:
         i32, rows = torch.int32, block_tables.shape[:1]
         if n < 1:
@@ -572,9 +586,9 @@ def plan_blocks(block_tables, n_blocks, context_lens, n_new, pool, n, n_shared=N
 def kv_write(k, v, k_cache, v_cache, slots):
     """Writes rows k, v [T, Hkv, D] (row-strided views will do) into a bf16 or f32 cache at slots [T] i32 (block * 16 +
     token, as plan_blocks gives them); rows whose slot is outside the cache are left out."""
-    _lib or load()
+    calls = _calls or _load_calls()
     dev = _here(k_cache, "k_cache")
-    if _calls.write(k, v, k_cache, v_cache, slots, dev, _raw_stream(dev)) is None:
+    if calls.write(k, v, k_cache, v_cache, slots, dev, _raw_stream(dev)) is None:
         dt, shape = k_cache.dtype, k_cache.shape
         values = (shape[0], shape[1], shape[3], 16) if len(shape) == 4 else (None,) * 4
         named = [("k_cache", k_cache, float, (None, None, 16, None)), ("v_cache", v_cache, dt, values),
@@ -597,9 +611,9 @@ def key_bounds(num_blocks, n_kv_heads, head_dim, device="cuda"):
 def key_bounds_update(k_cache, bounds, block_tables, starts, n, lens=None):
     """Bounds of the keys of the blocks that hold positions starts[b] + j, j < n (j < lens[b] if given), after
     kv_write of these rows."""
-    _lib or load()
+    calls = _calls or _load_calls()
     dev = _here(k_cache, "k_cache")
-    if _calls.update(k_cache, bounds, block_tables, starts, n, lens, dev, _raw_stream(dev)) is None:
+    if calls.update(k_cache, bounds, block_tables, starts, n, lens, dev, _raw_stream(dev)) is None:
         i32, shape, rows = torch.int32, k_cache.shape, block_tables.shape[:1]
         records = (shape[0], shape[1], 2 * shape[3] + 16) if len(shape) == 4 else (None,) * 3
         _why("molt_key_bounds_update", dev, ("k_cache", k_cache, float, (None, None, 16, None)),
@@ -609,9 +623,9 @@ def key_bounds_update(k_cache, bounds, block_tables, starts, n, lens=None):
 
 def key_bounds_read(bounds, ids):
     """The bounds of blocks ids [M] i32 of the cache as values: (largest, smallest) f32 [M, Hkv, D]."""
-    _lib or load()
+    calls = _calls or _load_calls()
     dev = _here(bounds, "bounds")
-    done = _calls.read(bounds, ids, dev, _raw_stream(dev))
+    done = calls.read(bounds, ids, dev, _raw_stream(dev))
     if done is None:
         if ids.numel() < 1:
             raise MoltError("ids is empty")
@@ -627,9 +641,9 @@ def select_blocks(q, bounds, block_tables, context_lens, k, n_select, n_first=1,
     """For each query position (q [B*(1+k), Hq, D], f32|bf16, at context_lens[b] + j) and kv head the n_select blocks
     of largest score by the keys' bounds (molt_select_blocks), the first n_first and last n_last among them: i32
     [B*(1+k), Hkv, n_select], ascending, then -1. Rows j >= lens[b] have empty lists."""
-    _lib or load()
+    calls = _calls or _load_calls()
     dev = _here(bounds, "bounds")
-    done = _calls.select(q, bounds, block_tables, context_lens, k, n_select, n_first, n_last, lens, workspace, dev,
+    done = calls.select(q, bounds, block_tables, context_lens, k, n_select, n_first, n_last, lens, workspace, dev,
                          _raw_stream(dev))
     if done is None:
         i32, rows = torch.int32, block_tables.shape[:1]
@@ -650,9 +664,9 @@ def paged_attention_blocks_workspace_size(B, k, n_q_heads, n_kv_heads, head_dim,
 def paged_attention_blocks(q, k_cache, v_cache, block_tables, context_lens, k, blocks, workspace=None):
     """paged_attention over the blocks that blocks [B*(1+k), Hkv, N] i32 lists for each position and kv head
     (select_blocks; -1: none): returns [B*(1+k), Hq*D] of q's dtype."""
-    _lib or load()
+    calls = _calls or _load_calls()
     dev = _here(k_cache, "k_cache")
-    done = _calls.attend(q, k_cache, v_cache, block_tables, context_lens, k, blocks, workspace, dev, _raw_stream(dev))
+    done = calls.attend(q, k_cache, v_cache, block_tables, context_lens, k, blocks, workspace, dev, _raw_stream(dev))
     if done is None:
         i32, shape, rows, dt = torch.int32, k_cache.shape, block_tables.shape[:1], k_cache.dtype
         nb, Hkv, _, D = shape if len(shape) == 4 else (None,) * 4

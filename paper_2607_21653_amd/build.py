@@ -70,13 +70,13 @@ def build(jobs=None, verbose=True):
     with cf.ThreadPoolExecutor(jobs) as ex:
         module = ex.submit(_module)
         objs = list(ex.map(_compile, srcs))
-        module.result()
     tmp = LIB + ".tmp"
     cmd = [hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"link failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, LIB)
+    module.result()                                # (where it failed the library is there)
     if verbose:
         print(f"built {LIB} from {len(srcs)} sources")
     return LIB

@@ -1,0 +1,73 @@
+"""The C++ module of sparse attention's Python calls is theirs alone: without it, or with one that does not load, the
+library loads and its other calls run; these say what is wrong. The build leaves the library where the module fails."""
+import os
+import shutil
+import subprocess
+import sys
+
+import pytest
+
+import paper_2607_21653_amd as molt
+from paper_2607_21653_amd import build
+
+HERE = os.path.dirname(os.path.abspath(molt.__file__))
+
+PROGRAM = """
+import torch
+import paper_2607_21653_amd as molt
+molt.load()
+assert molt.select_blocks_workspace_size(2, 4, 32, 4, 128, 6000) > 0
+cache = molt.PrefixCache(4)
+try:
+    molt.kvq_read(torch.zeros(1), torch.zeros(1), torch.zeros(1, 1), torch.zeros(1), 1)
+except molt.MoltError as e:
+    print("kvq:", e)
+i = torch.zeros(2, 2, dtype=torch.int32)
+for name, call in (("plan", lambda: molt.plan_blocks(i, i[0], i[0], i[0], i[0], 1)),
+                   ("write", lambda: molt.kv_write(i, i, i, i, i)),
+                   ("update", lambda: molt.key_bounds_update(i, i, i, i, 1)),
+                   ("read", lambda: molt.key_bounds_read(i, i)),
+                   ("select", lambda: molt.select_blocks(i, i, i, i, 0, 1)),
+                   ("attend", lambda: molt.paged_attention_blocks(i, i, i, i, i, 0, i))):
+    try:
+        call()
+    except molt.MoltError as e:
+        print(name + ":", e)
+"""
+
+
+@pytest.mark.parametrize("module,words", [(None, "is missing: build it"), (b"no shared object", "cannot be loaded")])
+def test_library_without_the_module(tmp_path, module, words):
+    there = tmp_path / "paper_2607_21653_amd"
+    there.mkdir()
+    for name in ("__init__.py", "_lib.py", "build.py"):
+        shutil.copy(os.path.join(HERE, name), there / name)
+    os.symlink(os.path.join(HERE, "libmolt.so"), there / "libmolt.so")
+    if module is not None:
+        (there / "_calls.so").write_bytes(module)
+    r = subprocess.run([sys.executable, "-c", PROGRAM], cwd=tmp_path, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr
+    lines = dict(line.split(":", 1) for line in r.stdout.splitlines())
+    assert set(lines) == {"kvq", "plan", "write", "update", "read", "select", "attend"}
+    assert "GPU" in lines.pop("kvq")
+    for name, said in lines.items():
+        assert "_calls.so" in said and words in said, (name, said)
+
+
+def test_build_leaves_the_library_where_the_module_fails(tmp_path, monkeypatch):
+    def module():
+        raise RuntimeError("no compiler for the module")
+
+    def run(cmd, **kw):
+        with open(cmd[cmd.index("-o") + 1], "w") as f:
+            f.write("linked")
+        return subprocess.CompletedProcess(cmd, 0, "", "")
+
+    monkeypatch.setattr(build, "_module", module)
+    monkeypatch.setattr(build, "_compile", lambda src: src)
+    monkeypatch.setattr(build, "BUILD", str(tmp_path))
+    monkeypatch.setattr(build, "LIB", str(tmp_path / "libmolt.so"))
+    monkeypatch.setattr(build.subprocess, "run", run)
+    with pytest.raises(RuntimeError, match="no compiler for the module"):
+        build.build(verbose=False)
+    assert (tmp_path / "libmolt.so").read_text() == "linked"
