@@ -525,10 +525,12 @@ def paged_attention_kvq(q, k_cache, v_cache, block_tables, context_lens, k, work
 # ------------------------------------------------------------------ sparse attention over listed blocks
 
 # The calls below take 3 to 8 us on the GPU where they are small. They go through _calls, which looks their arguments over
-# in C++ and returns None where it does not take them: then `_why` finds the reason, tensor by tensor.
+# in C++ and returns None where it does not take them: then the reason is found here, argument by argument.
 
 def _here(t, name):
     """Index of a tensor's device, which must be the current one."""
+    if not isinstance(t, torch.Tensor):
+        raise MoltError(f"{name} must be a GPU tensor, is {type(t).__name__}")
     dev = t.get_device()
     if dev < 0:
         raise MoltError(f"{name} must be a GPU tensor")
@@ -537,24 +539,65 @@ def _here(t, name):
     return dev
 
 
-def _why(call, dev, *named):
-    """Raises the reason why a call of _calls did not take its arguments: the first of named (name, tensor, dtype, shape)
-    that is not so (a shape's None stands for any size), else its numbers."""
-    for name, t, dtype, shape in named:
-        if t is None:
-            continue
+def _kinds(tensors, optional=None, **numbers):
+    """Refuses the first of a call's arguments (by name) that is no tensor, or no whole number from its least value,
+    (value, least), to 2^31 - 1. Optional tensors may be None."""
+    for name, t in tensors.items():
         if not isinstance(t, torch.Tensor):
             raise MoltError(f"{name} must be a GPU tensor, is {type(t).__name__}")
-        want = tuple(shape) if shape is not None else t.shape
-        if len(want) != t.dim() or any(w is not None and w != s for w, s in zip(want, t.shape)):
-            raise MoltError(f"{name} has shape {tuple(t.shape)}, expected {want}")
-        if dtype is float:
-            dtype = t.dtype
-            if dtype is not torch.bfloat16 and dtype is not torch.float32:
-                raise MoltError(f"{name} has dtype {dtype}, expected float32 or bfloat16")
-        _dev(t, dtype, None, name)
-        _same_device(t, dev, name)
-    raise MoltError(f"{call}: a number among its arguments is not whole, or not in 0 .. 2^31 - 1")
+    for name, t in (optional or {}).items():
+        if t is not None and not isinstance(t, torch.Tensor):
+            raise MoltError(f"{name} must be a GPU tensor or None, is {type(t).__name__}")
+    for name, (value, least) in numbers.items():
+        if isinstance(value, torch.Tensor) or not hasattr(value, "__index__"):
+            raise MoltError(f"{name} = {value!r} must be a whole number")
+        if not least <= value:
+            raise MoltError(f"{name} = {value} must be >= {least}")
+        if value > 0x7fffffff:
+            raise MoltError(f"{name} = {value} must be < 2^31")
+
+
+def _fits(name, t, dtype, shape, dev):
+    """Refuses a tensor that is not of dtype (float: bf16 or f32; None: any) and shape (None: any, also of one of its
+    sizes), contiguous and on device dev; returns its shape. None is passed over."""
+    if t is None:
+        return None
+    if shape is not None and (len(shape) != t.dim() or any(w is not None and w != n for w, n in zip(shape, t.shape))):
+        raise MoltError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if dtype is float:
+        dtype = t.dtype
+        if dtype is not torch.bfloat16 and dtype is not torch.float32:
+            raise MoltError(f"{name} has dtype {dtype}, expected float32 or bfloat16")
+    _dev(t, dtype, None, name)
+    _same_device(t, dev, name)
+    return t.shape
+
+
+def _fits_caches(k_cache, v_cache, dev):
+    """(num_blocks, n_kv_heads, head_dim) of a cache"""
+    nb, H, _, D = _fits("k_cache", k_cache, float, (None, None, 16, None), dev)
+    _fits("v_cache", v_cache, k_cache.dtype, (nb, H, D, 16), dev)
+    return nb, H, D
+
+
+def _fits_bounds(bounds, dev):
+    """(num_blocks, n_kv_heads, head_dim) of the bounds of a cache's keys"""
+    nb, H, size = _fits("bounds", bounds, torch.uint8, (None, None, None), dev)
+    if size <= 16 or size % 2:
+        raise MoltError(f"bounds has shape {tuple(bounds.shape)}, expected (num_blocks, n_kv_heads, 2 * head_dim + 16)")
+    return nb, H, (size - 16) // 2
+
+
+def _fits_table(block_tables, dev, **rows):
+    """The number of sequences, of a table and int32 tensors of one number each"""
+    B, _ = _fits("block_tables", block_tables, torch.int32, (None, None), dev)
+    for name, t in rows.items():
+        _fits(name, t, torch.int32, (B,), dev)
+    return B
+
+
+def _not_taken(call):
+    raise MoltError(f"{call}: a size among its tensors' is too large")
 
 
 def block_pool(num_blocks, device="cuda"):
@@ -572,14 +615,12 @@ def plan_blocks(block_tables, n_blocks, context_lens, n_new, pool, n, n_shared=N
     dev = _here(block_tables, "block_tables")
     done = calls.plan(block_tables, n_blocks, context_lens, n_new, pool, n, n_shared, dev, _raw_stream(dev))
     if done is None:
-        i32, rows = torch.int32, block_tables.shape[:1]
-        if n < 1:
-            raise MoltError(f"n = {n} must be >= 1")
-        if pool.numel() < 3:
+        _kinds(dict(block_tables=block_tables, n_blocks=n_blocks, context_lens=context_lens, n_new=n_new, pool=pool),
+               dict(n_shared=n_shared), n=(n, 1))
+        _fits_table(block_tables, dev, n_blocks=n_blocks, context_lens=context_lens, n_new=n_new, n_shared=n_shared)
+        if _fits("pool", pool, torch.int32, (None,), dev)[0] < 3:
             raise MoltError(f"pool has shape {tuple(pool.shape)}, expected (2 + num_blocks,)")
-        _why("molt_plan_blocks", dev, ("block_tables", block_tables, i32, (None, None)), ("n_blocks", n_blocks, i32, rows),
-             ("context_lens", context_lens, i32, rows), ("n_new", n_new, i32, rows), ("pool", pool, i32, (None,)),
-             ("n_shared", n_shared, i32, rows))
+        _not_taken("molt_plan_blocks")
     return done
 
 
@@ -589,18 +630,14 @@ def kv_write(k, v, k_cache, v_cache, slots):
     calls = _calls or _load_calls()
     dev = _here(k_cache, "k_cache")
     if calls.write(k, v, k_cache, v_cache, slots, dev, _raw_stream(dev)) is None:
-        dt, shape = k_cache.dtype, k_cache.shape
-        values = (shape[0], shape[1], shape[3], 16) if len(shape) == 4 else (None,) * 4
-        named = [("k_cache", k_cache, float, (None, None, 16, None)), ("v_cache", v_cache, dt, values),
-                 ("slots", slots, torch.int32, (None,))]
-        if len(shape) == 4 and dt in DTYPE_CODE and k.dim() == v.dim() == 3:
-            for name, t in (("k", k), ("v", v)):
-                if t.get_device() < 0:
-                    raise MoltError(f"{name} must be a GPU tensor")
-                _rows_stride(t, dt, slots.numel(), shape[1], shape[3], dev, name)
-        else:
-            named += [("k", k, dt, (None,) * 3), ("v", v, dt, (None,) * 3)]
-        _why("molt_kv_write", dev, *named)
+        _kinds(dict(k=k, v=v, k_cache=k_cache, v_cache=v_cache, slots=slots))
+        _, H, D = _fits_caches(k_cache, v_cache, dev)
+        T, = _fits("slots", slots, torch.int32, (None,), dev)
+        for name, t in (("k", k), ("v", v)):
+            if t.get_device() < 0:
+                raise MoltError(f"{name} must be a GPU tensor")
+            _rows_stride(t, k_cache.dtype, T, H, D, dev, name)
+        _not_taken("molt_kv_write")
 
 
 def key_bounds(num_blocks, n_kv_heads, head_dim, device="cuda"):
@@ -614,11 +651,11 @@ def key_bounds_update(k_cache, bounds, block_tables, starts, n, lens=None):
     calls = _calls or _load_calls()
     dev = _here(k_cache, "k_cache")
     if calls.update(k_cache, bounds, block_tables, starts, n, lens, dev, _raw_stream(dev)) is None:
-        i32, shape, rows = torch.int32, k_cache.shape, block_tables.shape[:1]
-        records = (shape[0], shape[1], 2 * shape[3] + 16) if len(shape) == 4 else (None,) * 3
-        _why("molt_key_bounds_update", dev, ("k_cache", k_cache, float, (None, None, 16, None)),
-             ("bounds", bounds, torch.uint8, records), ("block_tables", block_tables, i32, (None, None)),
-             ("starts", starts, i32, rows), ("lens", lens, i32, rows))
+        _kinds(dict(k_cache=k_cache, bounds=bounds, block_tables=block_tables, starts=starts), dict(lens=lens), n=(n, 1))
+        nb, H, _, D = _fits("k_cache", k_cache, float, (None, None, 16, None), dev)
+        _fits("bounds", bounds, torch.uint8, (nb, H, 2 * D + 16), dev)
+        _fits_table(block_tables, dev, starts=starts, lens=lens)
+        _not_taken("molt_key_bounds_update")
 
 
 def key_bounds_read(bounds, ids):
@@ -627,9 +664,11 @@ def key_bounds_read(bounds, ids):
     dev = _here(bounds, "bounds")
     done = calls.read(bounds, ids, dev, _raw_stream(dev))
     if done is None:
-        if ids.numel() < 1:
+        _kinds(dict(bounds=bounds, ids=ids))
+        _fits_bounds(bounds, dev)
+        if _fits("ids", ids, torch.int32, (None,), dev)[0] < 1:
             raise MoltError("ids is empty")
-        _why("molt_key_bounds_read", dev, ("bounds", bounds, torch.uint8, (None,) * 3), ("ids", ids, torch.int32, (None,)))
+        _not_taken("molt_key_bounds_read")
     return done
 
 
@@ -644,16 +683,16 @@ def select_blocks(q, bounds, block_tables, context_lens, k, n_select, n_first=1,
     calls = _calls or _load_calls()
     dev = _here(bounds, "bounds")
     done = calls.select(q, bounds, block_tables, context_lens, k, n_select, n_first, n_last, lens, workspace, dev,
-                         _raw_stream(dev))
+                        _raw_stream(dev))
     if done is None:
-        i32, rows = torch.int32, block_tables.shape[:1]
-        if n_select < 1:
-            raise MoltError(f"n_select = {n_select} must be >= 1")
-        D = (bounds.shape[2] - 16) // 2 if bounds.dim() == 3 else None
-        _why("molt_select_blocks", dev, ("bounds", bounds, torch.uint8, (None,) * 3),
-             ("block_tables", block_tables, i32, (None, None)), ("context_lens", context_lens, i32, rows),
-             ("q", q, float, (block_tables.shape[0] * (k + 1), None, D)), ("lens", lens, i32, rows),
-             ("workspace", workspace, None, None))
+        _kinds(dict(q=q, bounds=bounds, block_tables=block_tables, context_lens=context_lens),
+               dict(lens=lens, workspace=workspace), k=(k, 0), n_select=(n_select, 1), n_first=(n_first, 0),
+               n_last=(n_last, 1))
+        _, _, D = _fits_bounds(bounds, dev)
+        B = _fits_table(block_tables, dev, context_lens=context_lens, lens=lens)
+        _fits("q", q, float, (B * (int(k) + 1), None, D), dev)
+        _fits("workspace", workspace, None, None, dev)
+        _not_taken("molt_select_blocks")
     return done
 
 
@@ -668,13 +707,14 @@ def paged_attention_blocks(q, k_cache, v_cache, block_tables, context_lens, k, b
     dev = _here(k_cache, "k_cache")
     done = calls.attend(q, k_cache, v_cache, block_tables, context_lens, k, blocks, workspace, dev, _raw_stream(dev))
     if done is None:
-        i32, shape, rows, dt = torch.int32, k_cache.shape, block_tables.shape[:1], k_cache.dtype
-        nb, Hkv, _, D = shape if len(shape) == 4 else (None,) * 4
-        T = block_tables.shape[0] * (k + 1)
-        _why("molt_paged_attention_blocks", dev, ("k_cache", k_cache, float, (None, None, 16, None)),
-             ("v_cache", v_cache, dt, (nb, Hkv, D, 16)), ("block_tables", block_tables, i32, (None, None)),
-             ("context_lens", context_lens, i32, rows), ("q", q, dt, (T, None, D)), ("blocks", blocks, i32, (T, Hkv, None)),
-             ("workspace", workspace, None, None))
+        _kinds(dict(q=q, k_cache=k_cache, v_cache=v_cache, block_tables=block_tables, context_lens=context_lens,
+                    blocks=blocks), dict(workspace=workspace), k=(k, 0))
+        _, H, D = _fits_caches(k_cache, v_cache, dev)
+        B = _fits_table(block_tables, dev, context_lens=context_lens)
+        _fits("q", q, k_cache.dtype, (B * (int(k) + 1), None, D), dev)
+        _fits("blocks", blocks, torch.int32, (B * (int(k) + 1), H, None), dev)
+        _fits("workspace", workspace, None, None, dev)
+        _not_taken("molt_paged_attention_blocks")
     return done
 
 

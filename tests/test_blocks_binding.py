@@ -71,3 +71,15 @@ def test_build_leaves_the_library_where_the_module_fails(tmp_path, monkeypatch):
     with pytest.raises(RuntimeError, match="no compiler for the module"):
         build.build(verbose=False)
     assert (tmp_path / "libmolt.so").read_text() == "linked"
+
+
+def test_first_arguments_that_are_no_tensors():
+    for bad in (None, 3, [[1, 2]], "cuda"):
+        for name, call in (("block_tables", lambda: molt.plan_blocks(bad, None, None, None, None, 1)),
+                           ("k_cache", lambda: molt.kv_write(None, None, bad, None, None)),
+                           ("k_cache", lambda: molt.key_bounds_update(bad, None, None, None, 1)),
+                           ("bounds", lambda: molt.key_bounds_read(bad, None)),
+                           ("bounds", lambda: molt.select_blocks(None, bad, None, None, 0, 1)),
+                           ("k_cache", lambda: molt.paged_attention_blocks(None, bad, None, None, None, 0, None))):
+            with pytest.raises(molt.MoltError, match=f"^{name} must be a GPU tensor, is {type(bad).__name__}$"):
+                call()

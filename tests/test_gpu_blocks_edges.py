@@ -116,3 +116,51 @@ def test_refused_sizes_make_no_outputs(molt_lib, call, words):
         else:
             molt_lib.select_blocks(q, bounds, table, ctx, 1, **{**SELECT, **call})
     assert torch.cuda.memory_stats()["allocation.all.allocated"] == before
+
+
+def _calls_in_full(molt):
+    """Every call with arguments that it takes: name -> (function, tensors, numbers, optional tensors), in the order of the
+    function's own."""
+    z = lambda *s, dt=torch.int32: torch.zeros(s, dtype=dt, device="cuda")  # noqa: E731
+    f32 = torch.float32
+    kc, vc, rows, q = z(9, 2, 16, 64, dt=f32), z(9, 2, 64, 16, dt=f32), z(6, 2, 64, dt=f32), z(6, 8, 64, dt=f32)
+    bounds, table, pool = molt.key_bounds(9, 2, 64), z(2, 4), molt.block_pool(9)
+    return {
+        "plan": (molt.plan_blocks, dict(block_tables=table, n_blocks=z(2), context_lens=z(2), n_new=z(2), pool=pool), dict(n=3),
+                 dict(n_shared=z(2))),
+        "write": (molt.kv_write, dict(k=rows, v=rows, k_cache=kc, v_cache=vc, slots=z(6) - 1), {}, {}),
+        "update": (molt.key_bounds_update, dict(k_cache=kc, bounds=bounds, block_tables=table, starts=z(2)), dict(n=3),
+                   dict(lens=z(2))),
+        "read": (molt.key_bounds_read, dict(bounds=bounds, ids=z(5)), {}, {}),
+        "select": (molt.select_blocks, dict(q=q, bounds=bounds, block_tables=table, context_lens=z(2)),
+                   dict(k=2, n_select=4, n_first=1, n_last=2), dict(lens=z(2), workspace=z(1 << 20))),
+        "attend": (molt.paged_attention_blocks, dict(q=q, k_cache=kc, v_cache=vc, block_tables=table, context_lens=z(2),
+                                                     blocks=z(6, 2, 3)), dict(k=2), dict(workspace=z(1 << 20))),
+    }
+
+
+@pytest.mark.parametrize("name", ["plan", "write", "update", "read", "select", "attend"])
+def test_arguments_of_other_kinds_are_refused_by_name(molt_lib, name):
+    """What is no tensor, or no whole number, is a MoltError that names the argument, and so are tensors of other sizes."""
+    call, tensors, numbers, optional = _calls_in_full(molt_lib)[name]
+    call(**tensors, **numbers, **optional)
+    call(**tensors, **numbers)
+
+    def refused(**bad):
+        key, value = *bad, *bad.values()
+        with pytest.raises(molt_lib.MoltError) as e:
+            call(**{**tensors, **numbers, **optional, **bad})
+            pytest.fail(f"{key} = {value!r} was taken")
+        return str(e.value)
+
+    for key, t in {**tensors, **optional}.items():
+        for bad in ([1, 2], 3, "cuda", t.cpu().numpy()) + ((None,) if key in tensors else ()):
+            assert key in refused(**{key: bad}), (key, bad)
+        assert "must be a GPU tensor" in refused(**{key: t.cpu()})
+        assert key in refused(**{key: t[..., None].transpose(0, -1).expand(2, *t.shape[1:], t.shape[0])})
+        if key != "workspace":
+            for bad in (t.sum(), t[:0].flatten(), t.to(torch.int64), t[None]):
+                refused(**{key: bad})
+    for key, n in numbers.items():
+        for bad in ("3", 1.5, None, [3], torch.tensor(n), -1, 2 ** 31, 10 ** 30):
+            assert key in refused(**{key: bad}), (key, bad)
