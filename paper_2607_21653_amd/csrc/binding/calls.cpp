@@ -48,9 +48,18 @@ struct Args {
     ++at;
     return nullptr;
   }
+  // of any type of whole numbers; a tensor is none, which would have to be waited for
   int number() {
-    const long v = PyLong_Check(*at) ? PyLong_AsLong(*at) : -1;
-    ++at;
+    PyObject* o = *at++;
+    long v = -1;
+    if (PyLong_Check(o)) {
+      v = PyLong_AsLong(o);
+    } else if (PyIndex_Check(o) && !THPVariable_Check(o)) {
+      if (PyObject* whole = PyNumber_Index(o)) {
+        v = PyLong_AsLong(whole);
+        Py_DECREF(whole);
+      }
+    }
     if (v < 0 || v > 0x7fffffff) {
       PyErr_Clear();
       fine = false;

@@ -164,3 +164,14 @@ def test_arguments_of_other_kinds_are_refused_by_name(molt_lib, name):
     for key, n in numbers.items():
         for bad in ("3", 1.5, None, [3], torch.tensor(n), -1, 2 ** 31, 10 ** 30):
             assert key in refused(**{key: bad}), (key, bad)
+
+
+@pytest.mark.parametrize("name", ["plan", "update", "select", "attend"])
+def test_whole_numbers_of_other_types(molt_lib, name):
+    """numpy's integers are whole numbers, as for the other calls."""
+    call, tensors, numbers, _ = _calls_in_full(molt_lib)[name]
+    want = call(**{k: t.clone() for k, t in tensors.items()}, **numbers)
+    for of in (np.int64, np.int32, np.uint8):
+        got = call(**{k: t.clone() for k, t in tensors.items()}, **{k: of(n) for k, n in numbers.items()})
+        for a, b in zip(*(x if isinstance(x, tuple) else (x,) for x in (got, want))):
+            assert a is b is None or torch.equal(a, b)
