@@ -343,10 +343,11 @@ int molt_paged_attention_kvq(const void* q, const void* k_cache, const void* v_c
  * query row q (one head's D elements of dtype) has codes c_d = q_d / 2^f to the nearest integer, ties to even,
  * f by the rule for e above (c = 0 where the row has an infinity or NaN); its score of a block is
  *     2^min(max(e + f, -100), 100) * sum_d max(c_d * M-code_d, c_d * m-code_d),
- * exact, +inf where e = 127; the kv head's is the largest of its Hq/Hkv rows'. So no key of a
- * block that is left out has a larger product with a (rounded) query row than the least score of the list.
- * Blocks 0 .. n_first - 1 and the last n_last that the position sees come before all others; equal
- * scores go to the lower block. Rows j >= lens[b] ([B] i32, or NULL: all count) and rows that
+ * exact, +inf where e = 127; the kv head's is the largest of its Hq/Hkv rows'.
+ * Blocks 0 .. n_first - 1 and the last n_last that the position sees come before all others, whatever
+ * their scores; equal scores go to the lower block. So no block that is left out has a larger score than one
+ * that is in the list for its score, and where its e + f is in -100 .. 100 no key of it has a larger product with a
+ * (rounded) query row. Rows j >= lens[b] ([B] i32, or NULL: all count) and rows that
  * see no position have empty lists; a block whose id is outside [0, num_blocks) is in none.
  * n_first >= 0, n_last >= 1, n_first + n_last <= n_select.
  *
@@ -354,7 +355,7 @@ int molt_paged_attention_kvq(const void* q, const void* k_cache, const void* v_c
  * the blocks blocks[t, h, :] ([T, n_kv_heads, n_list] i32, in any order): positions up to
  * context_lens[b] + j of these. Entries outside [0, max_blocks_per_seq), blocks past the position
  * and blocks whose id is outside [0, num_blocks) are passed over; a block listed twice counts
- * twice; a row without a key is zeros. Keys and values that a row does not see may hold anything.
+ * twice; a row without a key, or all of whose keys score -inf, is zeros. Keys and values that a row does not see may hold anything.
  * Softmax weights are held in 16 bits (BF16, as two bf16 parts) or 24 (F32), sums in f32; an infinite
  * value that a row sees gives an infinity or NaN in its dim, a NaN gives NaN. The same call gives the
  * same bits.

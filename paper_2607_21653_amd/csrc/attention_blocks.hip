@@ -44,7 +44,7 @@ MOLT_DEV Entries entries_of(const BlocksArgs& p, const int32_t* list, int e, boo
 // Running softmax of a lane's query row (lane % 16): maximum of the scores q . k, this lane's share of the sum, and O^T:
 // dims 16 d + 4 (lane / 16) + i. A weight is exp2((s - m) c), of a difference of scores, so that the largest is 1 whatever
 // the scores' size: s c less a rounded m c would be off by half a step of m c, 2^7 where that is past 2^31. (No slower:
-// 16 sequences x 5 positions, 128 blocks 39.5 us both ways, 2 x 257, 64 blocks 57.7 and 57.6.)
+// 16 sequences x 5 positions, 128 of 3000 blocks 39.5 us both ways, 2 x 257, 64 of 512 blocks 57.7 and 57.6.)
 template <int D>
 struct Running {
   float m = -__builtin_inff(), l = 0.f;
@@ -271,7 +271,8 @@ MOLT_DEV void store4(float* p, floatx4_t x) { *reinterpret_cast<floatx4_t*>(p) =
 // Workgroup = one list (or a part of it) and 16 query rows; wavefronts take its units (pairs of blocks, or blocks) in
 // turn, a unit ahead in registers, with running softmaxes of their own, and join them in LDS.
 // What bounds it goes by how much the lists share. 128 sequences x 1 position, 64 blocks of 4 kv heads x 128 (268 MB, none
-// shared): 47 us, memory at 5.8 TB/s. 16 x 5, 128 blocks: 38 us, 335 MB through the L2 caches of which 176 come from memory
+// shared): 47 us, memory at 5.8 TB/s. 16 x 5 at 32768-65536, lists of 128 blocks that selections of similar rows share, 1.46
+// lists' blocks in all: 38 us, 335 MB through the L2 caches of which 176 come from memory
 // (4.6 TB/s). 2 x 257, 64 blocks: 58 us, 1.08 GB from L2 at 18 TB/s, its compute (VALU 35%, MFMA 16%, LDS 39% of the time
 // busy) partly beside it. Positions in pairs over the union of their lists, 1.4 times a list's length, took 55 us there, but
 // 7.5 in place of 5.2 for 4 x 3 positions and 130 or more in place of 122 for 128 x 5 whose lists share less.
@@ -286,7 +287,7 @@ __global__ __launch_bounds__(W* kWave, W == 8 || sizeof(T) == 4 ? 2 : 3) void bl
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   // by XCD: a part of all lists of a sequence and kv head on one of them, since neighbouring positions list much the same
   // blocks. They read them at about the same time: lists begun at different places found less in the L2 cache (16
-  // sequences x 5 positions, 128 blocks: 43 us in place of 31)
+  // sequences x 5 positions, 128 of 1000 blocks: 43 us in place of 31)
   uint32_t item = blockIdx.x, group;
   const uint32_t inner = uint32_t(p.n) * p.row_groups;
   if (p.by_xcd) {
@@ -443,9 +444,9 @@ BlocksPlan blocks_plan(int B, int n, int Hq, int Hkv, int N) {
 }
 
 // Whether workgroups by XCD, `inner` of each group on one, take about as many rounds of the CUs as in the grid's order: then
-// what they share in L2 pays (x 5 positions x 4 kv heads: 16 sequences, 128 blocks 30.6 us, in the grid's order 51.0; 128,
-// 64 blocks 123 and 191; 3, 256 blocks 17.1 and 19.1), else the fullest XCD's further round costs more (1 x 257 x 4 heads 56
-// and 35)
+// what they share in L2 pays (x 5 positions x 4 kv heads, lists out of tables of 1000 blocks: 16 sequences, 128 blocks, 1.65
+// lists' blocks in all, 33.7 us, in the grid's order 56.1; 128, 64 blocks, 2.15 lists', 124 and 196; 3, 256 blocks 17.1 and
+// 19.1), else the fullest XCD's further round costs more (1 x 257 x 4 heads 56 and 35)
 bool fits_by_xcd(long groups, long inner, int waves, molt_dtype dt) {
   const long places = 32 * (waves == 8 ? 1 : dt == MOLT_F32 ? 2 : 3);    // of an XCD
   const long fullest = (fullest_xcd(groups, inner) + places - 1) / places;

@@ -180,8 +180,10 @@ bool plan_whole(int B, int n) { return B <= kPlanThreads && long(B) * n <= 4 * k
 constexpr int kWriteRows = 16, kFewRows = 4;
 // Runs of a tile from which its rows go one by one (8000 rows in runs of 1 33.8 us, run by run 54.7)
 constexpr int kManyRuns = 5;
-// Rows x 128 dims up to which rows count as few. 4 kv heads x 128, bf16: 640 rows in runs of 5 4.7 us, by runs 9.7; 2048 rows
-// in runs of 5 8.9 and 11.4, of 1000 8.4 and 6.0; 4000 rows 14.4 and 13.6, 13.9 and 6.9
+// Rows x 128 dims up to which rows count as few: 1024 rows of 4 kv heads x 128. Calls back to back, bf16: 640 rows in
+// runs of 5 4.7 us, by runs 9.7; 2048 rows in runs of 5 8.9 and 11.4, of 1000 8.4 and 6.0; 4000 rows 14.4 and 13.6, 13.9
+// and 6.9. The host does not know the runs. From 2048 rows on, one kernel for all would cost prompts as much as it saves
+// runs of 5, or more, and calls of so many rows are prompts': a verify step of 5 positions would be of 400 sequences.
 constexpr long kFewUnits = 4096;
 
 // two elements of a row at any element alignment, as the bits that the cache holds
@@ -328,7 +330,8 @@ __global__ __launch_bounds__(kThreads) void kv_write_kernel(const T* __restrict_
 }
 
 // The same for few rows, where the time is that of the loads in a row: wavefront = 4 rows, read before it is known where
-// they go; V's tokens are stored one by one. 640 rows of 4 heads x 128 in bf16: 5.2 us, the loads' and the launch's latency.
+// they go; V's tokens are stored one by one. 640 rows of 4 heads x 128 in bf16, runs of 5: 5.2 us in a kernel trace, 4.7 a call
+// back to back, the loads' and the launch's latency.
 template <int D, typename T>
 __global__ __launch_bounds__(kThreads) void kv_write_few_kernel(const T* __restrict__ k, long k_stride,
                                                                 const T* __restrict__ v, long v_stride,

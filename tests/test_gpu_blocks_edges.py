@@ -91,6 +91,32 @@ def test_attention_of_far_scores(molt_lib, dtype, D, N, scale):
     assert np.isfinite(got).all() and (np.abs(got - want) <= tol).all(), np.abs(got - want).max()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N", [3, 200])
+def test_attention_of_keys_that_score_minus_infinity(molt_lib, dtype, N):
+    """Such keys have no weight beside others; a row that sees no others is zeros."""
+    rng = np.random.default_rng(7)
+    H, G, D, maxb, n = 2, 4, 64, 220, 2
+    kc, vc, q = (torch.from_numpy(rng.standard_normal(s).astype(np.float32)).to(DT[dtype])
+                 for s in ((maxb, H, 16, D), (maxb, H, D, 16), (n, H * G, D)))
+    q[:, :, 5] = q[:, :, 5].abs() + 0.5
+    lists = np.tile(np.arange(10, 10 + N, dtype=np.int32), (n, H, 1))
+    lists[1, 1, 0] = 4
+    kc[10:10 + N, 1, :, 5] = float("-inf")                           # head 1: all but block 4
+    kc[10, 0, :, 5], kc[4, 1, :7, 5] = float("-inf"), float("-inf")
+    got, _, _ = _attend(molt_lib, q, kc, vc, [16 * maxb - n], n, lists)
+    assert (got[0, G:] == 0).all()
+    far = kc.clone()
+    far[far == float("-inf")] = -(2.0 ** 20)                         # no weight either: scores 2^15 below the others
+    far[10:10 + N, 1] = 0                                            # (position 0, head 1 is not compared)
+    few = lists.copy()
+    few[1, 1, 1:] = -1
+    _, want, mag = _attend(molt_lib, q, far, vc, [16 * maxb - n], n, few)
+    tol = (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * np.abs(want) + 2.0 ** -12 * mag + 1e-30   # as in test_gpu_blocks.py
+    for t, heads in ((0, slice(0, G)), (1, slice(0, G)), (1, slice(G, None))):
+        assert (np.abs(got - want)[t, heads] <= tol[t, heads]).all(), (t, heads)
+
+
 # ---------------------------------------------------------------- refusals
 
 SELECT = dict(n_select=4, n_first=1, n_last=2)
